@@ -64,9 +64,16 @@ typedef enum {
 #define SDSAT_DEV_POSITION 0x10u   /* a RoPE position outside [0, max_position); clamped */
 #define SDSAT_DEV_TREE 0x20u       /* a tree parent that is not an earlier row; read as the root */
 
+#define SDSAT_DEV_PAGE 0x40u       /* a page outside the pool, or a sequence to fork from outside the batch; skipped */
+
 #define SDSAT_MAX_Q 16           /* block rows per sequence (k <= 15 adaptive tokens) */
 #define SDSAT_MAX_ROWS 64        /* batch * q rows per block forward */
 #define SDSAT_MAX_ADAPTIVE 16
+#define SDSAT_PAGE 64            /* slots of a page of a paged cache */
+
+/* element types of the kernels that take more than one */
+#define SDSAT_FP32 0
+#define SDSAT_BF16 1
 
 typedef struct sdsat_ctx sdsat_ctx;
 typedef struct sdsat_kv sdsat_kv;
@@ -137,6 +144,48 @@ SDSAT_API sdsat_status sdsat_set_stream(sdsat_ctx* ctx, void* stream);
  * Errors: EINVAL, ENOMEM, ECAPACITY (max_len > max_position or > 32768). */
 SDSAT_API sdsat_status sdsat_kv_create(sdsat_ctx* ctx, int batch, int max_len, sdsat_kv** out);
 SDSAT_API void sdsat_kv_destroy(sdsat_kv* kv);
+
+/* A paged KV cache, for many samples of one prompt: `n_pages` pages of SDSAT_PAGE slots
+ * (every layer and head of them), K and V bf16
+ * [n_layers][n_pages][n_heads][SDSAT_PAGE][head_dim], handed out to `batch` sequences of up
+ * to `max_len` slots each, which may share pages.  Every call that takes a cache takes a
+ * paged one, with two differences: the slots that a call writes (block rows, a prompt,
+ * sdsat_kv_write) need pages that their sequence alone holds (sdsat_kv_reserve), and a row
+ * without one is not written and sets device bit CAPACITY; and block forwards read the
+ * leading pages that all their sequences share once for all of them.
+ * Synchronous.  Errors: EINVAL (batch > 256), ENOMEM, ECAPACITY (as sdsat_kv_create),
+ * EUNSUPPORTED (n_layers * n_pages * n_heads * SDSAT_PAGE >= 2^31). */
+SDSAT_API sdsat_status sdsat_kv_create_paged(sdsat_ctx* ctx, int batch, int max_len, int n_pages, sdsat_kv** out);
+
+/* Device addresses and geometry of a paged cache: table int32 [batch][table_ld], entry j of
+ * a sequence the page of its slots 64 j .. 64 j + 63 (-1: none), and refs int32 [n_pages],
+ * the sequences that hold each page (0: free).  Any output pointer may be NULL.
+ * Errors: EINVAL (a contiguous cache). */
+SDSAT_API sdsat_status sdsat_kv_pages(const sdsat_kv* kv, int32_t** table_dev, int32_t** refs_dev, int* n_pages,
+                                      int* table_ld);
+
+/* Sequence s < b takes the pages and the length that sequence src_dev[s] (any sequence of the
+ * cache, its own included) had before the call; -1 leaves it empty.  Pages are shared, not
+ * copied; a page that no sequence holds any more is free.  src_dev int32 [b].  The emitted
+ * counters stay.  Errors: EINVAL; device bit PAGE where src_dev[s] is not in the batch (s keeps
+ * its pages). */
+SDSAT_API sdsat_status sdsat_kv_fork(sdsat_ctx* ctx, sdsat_kv* kv, const int32_t* src_dev, int b);
+
+/* Sequence seq gives its pages up (length 0).  Errors: EINVAL. */
+SDSAT_API sdsat_status sdsat_kv_free(sdsat_ctx* ctx, sdsat_kv* kv, int seq);
+
+/* Give sequences seq .. seq+b-1 pages of their own for the slots len .. len + n - 1, the next
+ * rows they write: a missing page is the lowest free one, sequences and then slots in order; a
+ * page that other sequences hold too is replaced by the lowest free one, into which its
+ * committed slots are copied (of several sequences that hold it the last one keeps it).
+ * Errors: EINVAL; device bit CAPACITY where a sequence would pass max_len (it gets the pages up
+ * to it) or the pool has too few free pages (nothing changes). */
+SDSAT_API sdsat_status sdsat_kv_reserve(sdsat_ctx* ctx, sdsat_kv* kv, int seq, int b, int n);
+
+/* Move the pages in use to the ids 0 .. u-1 of the pool: the i-th used page with an id >= u
+ * goes to the i-th free one below u, with the slots that any sequence has committed in it.
+ * *used_dev = u (int32, may be NULL).  Errors: EINVAL. */
+SDSAT_API sdsat_status sdsat_kv_compact(sdsat_ctx* ctx, sdsat_kv* kv, int32_t* used_dev);
 
 /* Device addresses and geometry of a KV cache (for tests and benches that fill
  * or inspect it).  Any output pointer may be NULL. */
@@ -381,6 +430,44 @@ SDSAT_API sdsat_status sdsat_op_gemm(sdsat_ctx* ctx, const float* x_dev, int M, 
 SDSAT_API sdsat_status sdsat_op_attention(sdsat_ctx* ctx, const float* q_dev, const void* k_dev, const void* v_dev,
                                 const int32_t* len_dev, int b, int q, int H, int hd, int cap,
                                 float* out_dev);
+
+/* Block-causal attention over pages, for sequences that share their leading ones:
+ * out[s*q+j][h*hd+d] = sum_t softmax_t(q_j . k_t / sqrt(hd)) v_t[d] over slots t < len[s] + j + 1,
+ * or, with anc_dev, over the committed slots t < len[s] and the slots len[s] + i with bit i of
+ * anc_dev[s*q+j] set (a row that sees no slot is 0).
+ *   q_dev      [b*q] rows of H*hd values, q_ld values apart; out_dev the same with out_ld; both of
+ *              `type` SDSAT_FP32 or SDSAT_BF16, sums fp32
+ *   k_dev, v_dev  bf16 [n_pages][Hk][SDSAT_PAGE][hd]; query head h reads cache head h / (H/Hk)
+ *   table_dev  int32 [b][table_ld]: the page of slots 64 j .. of each sequence
+ *   shared_dev int32 [b]: the leading table columns in which the sequence's pages are sequence
+ *              0's; NULL: none.  The whole pages of committed slots among those that all
+ *              sequences share are read once for all of them, through sequence 0's row
+ *   len_dev    int32 [b] committed lengths
+ * A slot on a page outside [0, n_pages) is not attended to and sets device bit PAGE.  hd 64 or
+ * 128, H a multiple of Hk, b*q <= SDSAT_MAX_ROWS, b*q*H*hd <= SDSAT_MAX_ROWS rows of the
+ * context's heads; pointers 16-byte aligned, rows a multiple of 16 bytes apart.  Errors: EINVAL. */
+SDSAT_API sdsat_status sdsat_op_prefix_attention(sdsat_ctx* ctx, const void* q_dev, int64_t q_ld, const void* k_dev,
+                                                 const void* v_dev, int n_pages, const int32_t* table_dev,
+                                                 int table_ld, const int32_t* shared_dev, const int32_t* len_dev,
+                                                 const uint32_t* anc_dev, int b, int q, int H, int Hk, int hd,
+                                                 void* out_dev, int64_t out_ld, int type);
+
+/* Log probabilities of rows of logits at a temperature T: with m the row's maximum,
+ * d_i = (l_i - m) / T and S = sum_i exp(d_i),
+ *   logp[r]    = d_t - log S of the row's token t = tokens_dev[r]
+ *   rank[r]    = 1 + the ids of larger logit, or of the same and lower id (1: the argmax)
+ *   entropy[r] = log S - sum_i exp(d_i) d_i / S
+ *   top_ids, top_logp [rows][n_top]: the n_top largest logits, the lower id first on ties
+ * logits_dev: rows of `vocab` values of `type`, ld values apart (any alignment).  tokens_dev
+ * int32 [rows]; -1: no token (logp 0, rank 0); NULL: none in any row, logp_dev and rank_dev
+ * NULL.  Any output but the two of n_top > 0 may be NULL.  A NaN logit counts as -inf (device
+ * bit NAN_LOGITS), a token outside the vocabulary as id 0 (TOKEN); a logit of +inf shares the
+ * mass with the others of +inf; a row of -inf alone has probabilities 0 and entropy 0.
+ * Errors: EINVAL (temperature <= 0, n_top > 32 or > vocab), EUNSUPPORTED (vocab > 262144). */
+SDSAT_API sdsat_status sdsat_op_logprobs(sdsat_ctx* ctx, const void* logits_dev, int64_t ld, int type, int rows,
+                                         int vocab, const int32_t* tokens_dev, float temperature, int n_top,
+                                         float* logp_dev, float* entropy_dev, int32_t* rank_dev,
+                                         int32_t* top_ids_dev, float* top_logp_dev);
 
 /* Copy a context workspace of the last block forward into dst_dev (fp32,
  * rows x cols row-major, rows = b*q of that forward): which = 0 the residual

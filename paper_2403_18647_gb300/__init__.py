@@ -29,6 +29,11 @@ DEV_TIMEOUT = 0x2
 DEV_CAPACITY = 0x4
 DEV_TOKEN = 0x8
 DEV_POSITION = 0x10
+DEV_TREE = 0x20
+DEV_PAGE = 0x40
+
+PAGE = 64              # slots of a page of a paged cache
+FP32, BF16 = 0, 1      # element types of the kernels that take more than one
 
 
 class SdsatError(RuntimeError):
@@ -68,7 +73,7 @@ def _lib():
         if _build.is_stale():
             _build.build()
         lib = ctypes.CDLL(_build.LIB)
-        P, I, F, U64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint64
+        P, I, F, U64, I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint64, ctypes.c_int64
         sig = {
             "sdsat_create": [ctypes.POINTER(Config), ctypes.POINTER(Weights), P, ctypes.POINTER(P)],
             "sdsat_set_stream": [P, P],
@@ -98,6 +103,14 @@ def _lib():
             "sdsat_op_gemm": [P, P, I, I, P, I, P],
             "sdsat_op_attention": [P, P, P, P, P, I, I, I, I, I, P],
             "sdsat_op_exp": [P, P, P, I],
+            "sdsat_kv_create_paged": [P, I, I, I, ctypes.POINTER(P)],
+            "sdsat_kv_pages": [P, ctypes.POINTER(P), ctypes.POINTER(P), ctypes.POINTER(I), ctypes.POINTER(I)],
+            "sdsat_kv_fork": [P, P, P, I],
+            "sdsat_kv_free": [P, P, I],
+            "sdsat_kv_reserve": [P, P, I, I, I],
+            "sdsat_kv_compact": [P, P, P],
+            "sdsat_op_prefix_attention": [P, P, I64, P, P, I, P, I, P, P, P, I, I, I, I, I, P, I64, I],
+            "sdsat_op_logprobs": [P, P, I64, I, I, I, P, F, I, P, P, P, P, P],
             "sdsat_debug_workspace": [P, I, I, P],
             "sdsat_debug_wait_timeout": [P],
             "sdsat_attention_grid": [I, P, I, I, ctypes.POINTER(I), ctypes.POINTER(I)],
@@ -133,6 +146,16 @@ def _ptr(t) -> Optional[int]:
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
     return t.data_ptr()
+
+
+def _rows(t):
+    """(address, values from one row to the next, element type) of a CUDA matrix whose rows are contiguous."""
+    import torch
+    if not t.is_cuda or t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("expected a float32 or bfloat16 CUDA matrix")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("expected contiguous rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1], BF16 if t.dtype == torch.bfloat16 else FP32
 
 
 def _check(status: int, what: str):
@@ -207,6 +230,68 @@ class KV:
             pass
 
 
+class _Memory:
+    """Device memory of a cache as a CUDA array; the cache lives as long as its views."""
+
+    def __init__(self, owner, address: int, shape, typestr: str):
+        self.owner = owner
+        self.__cuda_array_interface__ = dict(data=(address, False), shape=tuple(shape), typestr=typestr, version=3)
+
+
+class PagedKV(KV):
+    """A library-owned cache of `n_pages` pages of PAGE slots, which sequences may share."""
+
+    def __init__(self, ctx: "Context", batch: int, max_len: int, n_pages: int):
+        self.ctx = ctx
+        h = ctypes.c_void_p()
+        _check(_lib().sdsat_kv_create_paged(ctx.handle, batch, max_len, n_pages, ctypes.byref(h)),
+               "sdsat_kv_create_paged")
+        self.handle = h
+        self.batch, self.max_len, self.n_pages = batch, max_len, n_pages
+        self.table_ld = -(-max_len // PAGE)
+
+    def pages(self):
+        t, r, n, ld = ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_int(), ctypes.c_int()
+        _check(_lib().sdsat_kv_pages(self.handle, ctypes.byref(t), ctypes.byref(r), ctypes.byref(n), ctypes.byref(ld)),
+               "sdsat_kv_pages")
+        return t.value, r.value, n.value, ld.value
+
+    # the cache's own memory as tensors (what it holds is read on the stream of the calls before)
+    def _view(self, address, shape, typestr="<i4"):
+        import torch
+        return torch.as_tensor(_Memory(self, address, shape, typestr), device="cuda")
+
+    @property
+    def table(self):
+        """int32 [batch][table_ld]: the page of slots PAGE*j .. of each sequence, -1 where it has none."""
+        return self._view(self.pages()[0], (self.batch, self.table_ld))
+
+    @property
+    def refs(self):
+        """int32 [n_pages]: the sequences that hold each page."""
+        return self._view(self.pages()[1], (self.n_pages,))
+
+    @property
+    def lens(self):
+        """int32 [batch]: the committed lengths."""
+        return self._view(self.info()[2], (self.batch,))
+
+    def _pool(self, which):
+        import torch
+        s = self.ctx.shape
+        shape = (s.n_layers, self.n_pages, s.n_heads, PAGE, s.head_dim)
+        return self._view(self.info()[which], shape, "<i2").view(torch.bfloat16)
+
+    @property
+    def k(self):
+        """bf16 [n_layers][n_pages][n_heads][PAGE][head_dim]."""
+        return self._pool(0)
+
+    @property
+    def v(self):
+        return self._pool(1)
+
+
 class Context:
     """Borrowed weights + TMA descriptors + workspaces for one model shape."""
 
@@ -237,6 +322,29 @@ class Context:
 
     def kv(self, batch: int, max_len: int) -> KV:
         return KV(self, batch, max_len)
+
+    # ---- paged caches: many samples of one prompt ----
+    def kv_paged(self, batch: int, max_len: int, n_pages: int) -> PagedKV:
+        return PagedKV(self, batch, max_len, n_pages)
+
+    def kv_fork(self, kv: PagedKV, src, b: int = None):
+        """Sequence s takes the pages and the length of sequence src[s] (int32 CUDA tensor [b]; -1: none)."""
+        self._bind_stream()
+        _check(_lib().sdsat_kv_fork(self.handle, kv.handle, _ptr(src), src.numel() if b is None else b), "sdsat_kv_fork")
+
+    def kv_free(self, kv: PagedKV, seq: int):
+        self._bind_stream()
+        _check(_lib().sdsat_kv_free(self.handle, kv.handle, seq), "sdsat_kv_free")
+
+    def kv_reserve(self, kv: PagedKV, b: int, n: int, seq: int = 0):
+        """Pages of their own for the next n slots of sequences seq .. seq+b-1."""
+        self._bind_stream()
+        _check(_lib().sdsat_kv_reserve(self.handle, kv.handle, seq, b, n), "sdsat_kv_reserve")
+
+    def kv_compact(self, kv: PagedKV, used=None):
+        """Pages in use move to the front of the pool; used: int32 CUDA tensor [1] for their number."""
+        self._bind_stream()
+        _check(_lib().sdsat_kv_compact(self.handle, kv.handle, _ptr(used)), "sdsat_kv_compact")
 
     def kv_write(self, kv: KV, layer: int, seq: int, slot0: int, k, v):
         """k, v: bf16 CUDA tensors [n_heads, n, head_dim] written to slots slot0 .. slot0+n-1."""
@@ -392,6 +500,31 @@ class Context:
         self._bind_stream()
         _check(_lib().sdsat_op_attention(self.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(lens), b, qn, H, hd, cap,
                                          _ptr(out)), "sdsat_op_attention")
+
+    def op_prefix_attention(self, q, k, v, table, shared, lens, b: int, qn: int, H: int, Hk: int, hd: int, out, anc=None):
+        """q, out [b*qn][H*hd] fp32 or bf16 (rows any distance apart); k, v bf16 [pages][Hk][PAGE][hd]; table int32
+        [b][columns]; shared (leading columns equal to sequence 0's, may be None) and lens int32 [b]; anc int32 [b*qn]
+        block-row masks of a tree block."""
+        self._bind_stream()
+        (qp, q_ld, kind), (op, out_ld, kind_out) = _rows(q), _rows(out)
+        if kind != kind_out:
+            raise ValueError("q and out are of different types")
+        if table.shape[0] < b or q.shape[0] < b * qn or out.shape[0] < b * qn:
+            raise ValueError("fewer rows than b or b * qn")
+        _check(_lib().sdsat_op_prefix_attention(self.handle, qp, q_ld, _ptr(k), _ptr(v), k.shape[0], _ptr(table),
+                                                table.shape[1], _ptr(shared), _ptr(lens), _ptr(anc), b, qn, H, Hk, hd, op,
+                                                out_ld, kind), "sdsat_op_prefix_attention")
+
+    def op_logprobs(self, logits, tokens=None, logp=None, entropy=None, rank=None, top_ids=None, top_logp=None,
+                    temperature: float = 1.0):
+        """logits [rows][vocab] fp32 or bf16 (rows any distance apart); tokens, rank int32 and logp, entropy fp32 [rows];
+        top_ids int32 and top_logp fp32 [rows][n]."""
+        self._bind_stream()
+        lp, ld, kind = _rows(logits)
+        n = 0 if top_ids is None else top_ids.shape[1]
+        _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, logits.shape[0], logits.shape[1], _ptr(tokens),
+                                        temperature, n, _ptr(logp), _ptr(entropy), _ptr(rank), _ptr(top_ids),
+                                        _ptr(top_logp)), "sdsat_op_logprobs")
 
     def debug_workspace(self, which: int, rows: int):
         """Last-layer workspace of the last forward: 0 h, 1 q, 2 attention out, 3 SwiGLU act."""

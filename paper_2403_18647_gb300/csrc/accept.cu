@@ -822,7 +822,7 @@ cudaError_t launch_tree_prep(const int* parent, const int* len, int nb, int q, i
 // Slot len0 + i receives the K and V rows of slot len0 + n_i (i = 1..m; n_i >= i, so no
 // source is overwritten before it is read).  One CTA per (layer, head) and sequence, 16-byte
 // chunks.
-__global__ void tree_compact_kernel(const int* ws, int H, int hd, int cap, int batch, __nv_bfloat16* kc,
+__global__ void tree_compact_kernel(const int* ws, int H, int hd, int cap, int batch, PageMap pages, __nv_bfloat16* kc,
                                     __nv_bfloat16* vc) {
   pdl_wait();
   pdl_trigger();
@@ -830,23 +830,26 @@ __global__ void tree_compact_kernel(const int* ws, int H, int hd, int cap, int b
   const int* w = ws + s * TREE_WS_STRIDE;
   const int len0 = __ldcg(w), m = __ldcg(w + 1);
   const int chunks = hd / 8;   // 16-byte chunks per row
-  const size_t off = (((size_t)l * batch + s) * H + h) * cap * hd;
+  // this head's rows of the layer (a paged cache's rows are on pages of this sequence alone)
+  const size_t off = pages.table ? ((size_t)l * pages.n * H + h) * KV_PAGE * hd : ((size_t)l * batch * H + h) * cap * hd;
   for (int x = threadIdx.x; x < 2 * m * chunks; x += blockDim.x) {
     const int which = x / (m * chunks), rem = x % (m * chunks);
     const int i = 1 + rem / chunks, ch = rem % chunks;
     const int n = __ldcg(w + 2 + i);
     if (n == i || len0 + n >= cap) continue;
+    const long long from = cache_row(pages, s, len0 + n, H, cap, hd), to = cache_row(pages, s, len0 + i, H, cap, hd);
+    if (from < 0 || to < 0) continue;   // (the row was not written)
     __nv_bfloat16* base = (which ? vc : kc) + off;
-    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(base + (size_t)(len0 + n) * hd) + ch);
-    __stcg(reinterpret_cast<uint4*>(base + (size_t)(len0 + i) * hd) + ch, v);
+    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(base + from) + ch);
+    __stcg(reinterpret_cast<uint4*>(base + to) + ch, v);
   }
 }
 
-cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int cap, int batch,
+cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int cap, int batch, const PageMap& pages,
                                 __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t st, bool pdl) {
   cudaLaunchAttribute attr[1];
   cudaLaunchConfig_t cfg = make_cfg(dim3(L * H, nb), dim3(64), st, pdl, attr);
-  return cudaLaunchKernelEx(&cfg, tree_compact_kernel, ws, H, hd, cap, batch, k, v);
+  return cudaLaunchKernelEx(&cfg, tree_compact_kernel, ws, H, hd, cap, batch, pages, k, v);
 }
 
 // ---- the bounded wait, run out on purpose (a test hook) ----------------------------------

@@ -231,7 +231,7 @@ __device__ __forceinline__ void epilogue_final(const GemmParams& p, int tile, in
     const int partner = (i < half) ? r + half : r - half;
     const float* other = staging + partner * (MPAD + 1);
     const float sgn = (i < half) ? -1.f : 1.f;   // rotate-half RoPE: x cos -+ partner sin
-    __nv_bfloat16* cache = ((which == 1) ? p.k_layer : p.v_layer) + ((long long)head * p.cap * hd + i);
+    __nv_bfloat16* cache = ((which == 1) ? p.k_layer : p.v_layer) + ((long long)head * p.head_rows * hd + i);
     float* qout = p.out + f;
 #pragma unroll 2   // two rows in flight (4 made the cold loop slower)
     for (int m = 0; m < M; ++m, qout += p.out_ld) {
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(192, SDSAT_GEMM_MINB) gemm_kernel(const __grid
   float* sinv = staging + C::STAGING;   // [64] RMSNorm row factors of the operand
   int* s_pos = reinterpret_cast<int*>(sinv + 64);    // [64] EPI_QKV: RoPE position of each row
   // [64] EPI_QKV: offset of each row's cache element (sequence, head 0, slot, dimension 0),
-  // -1 past the capacity (8-byte aligned: the area before is a multiple of 8 bytes)
+  // -1 where it must not be written (8-byte aligned: the area before is a multiple of 8 bytes)
   long long* s_rowbase = reinterpret_cast<long long*>(s_pos + 64);
   float2* s_cs = reinterpret_cast<float2*>(s_rowbase + 64);   // [MPAD][64] EPI_QKV: RoPE factors
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_cs + C::CS);
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(192, SDSAT_GEMM_MINB) gemm_kernel(const __grid
           pos = pos < 0 ? 0 : p.rope_len - 1;
         }
         s_pos[r] = pos;
-        s_rowbase[r] = slot < p.cap ? ((long long)seq * p.H * p.cap + slot) * p.hd : -1;
+        s_rowbase[r] = cache_row(p.pages, seq, slot, p.H, p.cap, p.hd);
       }
       named_bar_sync(1, 128);
       // the RoPE factors of every row, in shared memory long before any accumulator is ready
@@ -693,12 +693,15 @@ __global__ void __launch_bounds__(256) gemm_finish_kernel(const __grid_constant_
     float* dst = p.out + (size_t)m * p.out_ld + f;
     *reinterpret_cast<float2*>(dst) = a;
     *reinterpret_cast<float2*>(dst + half) = b;
-  } else if (slot < p.cap) {
-    __nv_bfloat16* dst = (which == 1 ? p.k_layer : p.v_layer) + (((size_t)seq * p.H + (f - i) / p.hd) * p.cap + slot) * p.hd + i;
-    *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(a.x, a.y);
-    *reinterpret_cast<__nv_bfloat162*>(dst + half) = __floats2bfloat162_rn(b.x, b.y);
-  } else if (lane == 0 && which == 1) {
-    set_error(p.err, ERR_CAPACITY);
+  } else {
+    const long long base = cache_row(p.pages, seq, slot, p.H, p.cap, p.hd);
+    if (base >= 0) {
+      __nv_bfloat16* dst = (which == 1 ? p.k_layer : p.v_layer) + base + (long long)((f - i) / p.hd) * p.head_rows * p.hd + i;
+      *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(a.x, a.y);
+      *reinterpret_cast<__nv_bfloat162*>(dst + half) = __floats2bfloat162_rn(b.x, b.y);
+    } else if (lane == 0 && which == 1) {
+      set_error(p.err, ERR_CAPACITY);
+    }
   }
 }
 

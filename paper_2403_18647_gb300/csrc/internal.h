@@ -50,6 +50,25 @@ cudaError_t prefer_shared(K* kernel) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
+// ---- where a cache row is ----------------------------------------------------
+constexpr int KV_PAGE = 64;           // slots of a page of a paged cache (one attention unit)
+// The page table of a paged cache; table == nullptr: the cache is contiguous.
+struct PageMap {
+  const int* table;   // [batch][ld] page of slots KV_PAGE j .. of a sequence, or -1
+  const int* refs;    // [n] sequences that hold the page
+  int ld, n;
+};
+// Element offset within a layer of (sequence, head 0, slot, dimension 0), -1 where the slot must not
+// be written: past the capacity, without a page, or on a page that other sequences hold too.
+// (Heads are KV_PAGE rows apart in a paged cache, cap rows in a contiguous one.)
+__device__ __forceinline__ long long cache_row(const PageMap& pg, int seq, int slot, int H, int cap, int hd) {
+  if (slot >= cap) return -1;
+  if (!pg.table) return ((long long)seq * H * cap + slot) * hd;
+  const int page = __ldcg(pg.table + (size_t)seq * pg.ld + slot / KV_PAGE);
+  if (page < 0 || page >= pg.n || __ldcg(pg.refs + page) != 1) return -1;
+  return ((long long)page * H * KV_PAGE + slot % KV_PAGE) * hd;
+}
+
 // ---- skinny weight-streaming GEMM --------------------------------------------
 // CTAs per SM of the skinny GEMM's grid (compile-time tuning).
 // Every user of the grid size (the split-K partials, the fixed scratch of the
@@ -109,6 +128,8 @@ struct GemmParams {
   __nv_bfloat16* k_layer;   // KV cache of this layer: [B][H][cap][hd]
   __nv_bfloat16* v_layer;
   int H, hd, cap, q, seq0;
+  int head_rows;            // cache rows from one head to the next: cap, or KV_PAGE
+  PageMap pages;            // of a paged cache (k_layer: [pages][H][KV_PAGE][hd])
   const int* len;           // committed lengths [B] (device)
   const int* positions;     // [M] or null
   const float2* rope;       // [rope_len][hd/2] (cos, sin)
@@ -173,6 +194,7 @@ struct PfAttnParams {
   int row0;                 // first cache row of this layer
   const int* len;
   int seq, M, H, hd, cap;
+  PageMap pages;            // of a paged cache: row0 + (page * H + h) * KV_PAGE
   int tiles;                // set by launch_prefill_attention: tiles of 128 positions per CTA (1 or 2)
   int out_ld;
   __nv_bfloat16* out_hi;    // [M][out_ld] the O projection's operand
@@ -222,6 +244,8 @@ struct PfGemmParams {
   const int* positions;     // [M], or null: each row's cache slot
   int seq0, q;              // row m belongs to sequence seq0 + m / q, slot len[that] + m % q
   int H, hd, cap;
+  int head_rows;            // as GemmParams
+  PageMap pages;
   const float2* rope;
   int rope_len;
   uint32_t* err;
@@ -291,7 +315,7 @@ cudaError_t launch_build_block(const BuildParams& b, cudaStream_t st, bool pdl);
 cudaError_t launch_tree_prep(const int* parent, const int* len, int nb, int q, int* pos, uint32_t* anc,
                              uint32_t* err, cudaStream_t st, bool pdl);
 // move the accepted path's K / V rows to contiguous slots (input: AcceptParams::tree_ws)
-cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int cap, int batch,
+cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int cap, int batch, const PageMap& pages,
                                 __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t st, bool pdl);
 cudaError_t launch_commit(int* len, const int* new_len, int nb, int cap, uint32_t* err, cudaStream_t st,
                           bool pdl);
@@ -299,5 +323,72 @@ cudaError_t launch_add_len(int* len, int seq, int n, int cap, uint32_t* err, cud
 cudaError_t launch_exp(const float* in, float* out, int n, cudaStream_t st);
 // a bounded wait that nothing satisfies: sets ERR_TIMEOUT after WAIT_LIMIT_NS (test hook)
 cudaError_t launch_wait_timeout(uint32_t* err, cudaStream_t st);
+
+// ---- paged cache -------------------------------------------------------------
+constexpr int PAGES_MAX_BATCH = 256;
+struct PagesParams {
+  int *table, *refs, *len;  // as PageMap; committed lengths [batch]
+  int* common;              // [batch] leading pages held together with sequence 0
+  int *ids, *kinds;         // scratch: [n_pages], [max(n_pages, batch * ld)]
+  int* copies;              // scratch: [0] pages to copy, from [4]: source, destination, slots of each
+  int batch, ld, cap, n_pages;
+  const int* src;           // fork: [nb] where each sequence's pages come from (-1: none); null: seq0 is freed
+  int seq0, nb, n;
+  int* used;                // compact: the pages in use, or null
+  int L, H, hd;
+  __nv_bfloat16 *k, *v;     // [L][n_pages][H][KV_PAGE][hd]
+  uint32_t* err;
+};
+cudaError_t pages_prepare();
+cudaError_t launch_pages_fork(const PagesParams& p, cudaStream_t st, bool pdl);
+cudaError_t launch_pages_reserve(const PagesParams& p, cudaStream_t st, bool pdl);
+cudaError_t launch_pages_compact(const PagesParams& p, cudaStream_t st, bool pdl);
+cudaError_t launch_pages_copy(const PagesParams& p, int num_sms, cudaStream_t st, bool pdl);   // the listed pages
+// n slots of sequence seq0 from slot0 on, one layer, to or from k and v [H][n][hd]
+cudaError_t launch_pages_rows(const PagesParams& p, int layer, int slot0, void* k, void* v, bool write, cudaStream_t st,
+                              bool pdl);
+
+// Block-causal attention of sequences that share their leading pages (prefix_attention.cu)
+struct PrefixAttnParams {
+  CUtensorMap kmap, vmap;   // pages as a 2-D tensor [rows][hd] bf16, boxes of 64 dims x KV_PAGE rows
+  const void *k, *v;        // the same
+  int row0;                 // row of (page, head, slot) = row0 + (page * Hk + head) * KV_PAGE + slot
+  const void* q;            // [b*q][q_ld] fp32 or bf16
+  long long q_ld, out_ld;
+  bool bf16;                // of q and out
+  const int* table;         // [b][ld]
+  int ld, n_pages;
+  const int* common;        // [b] leading table columns that equal sequence 0's, or null
+  const int* len;           // [b]
+  const uint32_t* anc;      // as AttnParams
+  int b, nq, H, Hk, hd;
+  void* out;                // [b*q][out_ld], the type of q
+  __nv_bfloat16 *out_hi, *out_lo;   // [b*q][H*hd], or null: the O projection's operand
+  float* part;              // scratch: prefix_attention_scratch() floats
+  uint32_t* err;
+};
+size_t prefix_attention_scratch(int row_heads, int hd, int num_sms);
+cudaError_t prefix_attention_prepare();
+cudaError_t launch_prefix_attention(const PrefixAttnParams& p, int num_sms, cudaStream_t st, bool pdl);
+
+// Log probabilities (logprobs.cu)
+constexpr int LP_MAX_TOP = 32;
+constexpr int LP_MAX_VOCAB = 1 << 18;
+struct LogprobParams {
+  const void* logits;       // [rows][ld] fp32 or bf16
+  bool bf16;
+  long long ld;
+  int rows, V;
+  const int* tokens;        // [rows], -1: none; null: no token's figures
+  float inv_t;              // 1 / temperature
+  float *logp, *entropy;    // [rows] each, any of them null
+  int* rank;
+  int n_top;
+  int* top_ids;             // [rows][n_top]
+  float* top_logp;
+  uint32_t* err;
+};
+cudaError_t logprobs_prepare();
+cudaError_t launch_logprobs(const LogprobParams& p, int num_sms, cudaStream_t st, bool pdl);
 
 }  // namespace sdsat

@@ -141,8 +141,9 @@ struct PfRow {
     slot = (p.q >= p.M ? len0 : __ldcg(p.len + seq)) + m - s * p.q;
     pos = p.positions ? __ldcg(p.positions + m) : slot;
   }
+  __device__ long long cache(const PfGemmParams& p) const { return cache_row(p.pages, seq, slot, p.H, p.cap, p.hd); }
   __device__ void report(const PfGemmParams& p) const {   // (by one thread of a row)
-    if (slot >= p.cap) set_error(p.err, ERR_CAPACITY);
+    if (cache(p) < 0) set_error(p.err, ERR_CAPACITY);
     if (pos < 0 || pos >= p.rope_len) set_error(p.err, ERR_POSITION);
   }
 };
@@ -169,9 +170,9 @@ __device__ __forceinline__ void pf_qkv_store(const PfGemmParams& p, int which, i
       pf_store4(p.out_hi, p.out_lo, o, a.x, a.y, a.z, a.w);
       pf_store4(p.out_hi, p.out_lo, o + half, b.x, b.y, b.z, b.w);
     }
-  } else if (r.slot < p.cap) {
-    __nv_bfloat16* dst = (which == 1 ? p.k_layer : p.v_layer) +
-                         ((size_t)(r.seq * p.H + (f - i) / p.hd) * p.cap + r.slot) * p.hd + i;
+  } else if (const long long base = r.cache(p); base >= 0) {
+    __nv_bfloat16* dst =
+        (which == 1 ? p.k_layer : p.v_layer) + base + (long long)((f - i) / p.hd) * p.head_rows * p.hd + i;
     *reinterpret_cast<uint2*>(dst) = make_uint2(pf_pack(a.x, a.y), pf_pack(a.z, a.w));
     *reinterpret_cast<uint2*>(dst + half) = make_uint2(pf_pack(b.x, b.y), pf_pack(b.z, b.w));
   }

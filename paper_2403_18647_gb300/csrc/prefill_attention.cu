@@ -31,6 +31,7 @@
 
 namespace sdsat {
 
+static_assert(KV_PAGE == 64, "a page is one box of keys");
 constexpr int PA_ROWS = 128;      // chunk positions per tile, and keys per block
 constexpr int PA_SLOTS = 3;
 constexpr int PA_THREADS = 384;
@@ -175,11 +176,16 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         if (!mbar_wait_bounded(&empty[s], ((it / PA_SLOTS) & 1) ^ 1, abort_flag, p.err)) break;
         mbar_arrive_expect_tx(&full[s], C::TILE);
         const CUtensorMap* map = (it & 1) ? &p.vmap : &p.kmap;
-        const int row = rowbase + (it >> 1) * PA_ROWS;
+        int row[2] = {rowbase + (it >> 1) * PA_ROWS, rowbase + (it >> 1) * PA_ROWS + 64};
+        if (p.pages.table) {   // (a box past the sequence's pages holds no visible key: any page does)
+          for (int b = 0; b < 2; ++b) {
+            const int j = (it & ~1) + b, page = j < p.pages.ld ? __ldcg(p.pages.table + (size_t)p.seq * p.pages.ld + j) : 0;
+            row[b] = p.row0 + (min(max(page, 0), p.pages.n - 1) * p.H + h) * KV_PAGE;
+          }
+        }
         for (int hh = 0; hh < C::HALVES; ++hh)
           for (int b = 0; b < 2; ++b)
-            tma_load_2d(ring + (size_t)s * C::TILE + hh * C::HALF + b * C::BOX, map, &full[s], hh * 64, row + b * 64,
-                        pol);
+            tma_load_2d(ring + (size_t)s * C::TILE + hh * C::HALF + b * C::BOX, map, &full[s], hh * 64, row[b], pol);
       }
       if (*abort_flag) {   // let the copies in flight land before the CTA exits
         auto land = [&](uint64_t* bar, uint32_t parity) {

@@ -90,12 +90,12 @@ struct LayerMaps {
 enum KClass : int {
   K_RMSNORM = 0, K_GEMM_QKV, K_ATTENTION, K_GEMM_O, K_GEMM_GATEUP, K_GEMM_DOWN, K_GEMM_LM_HEAD, K_ACCEPT,
   K_BUILD_BLOCK, K_KV_COMMIT, K_PREFILL_COMMIT, K_GEMM_OP, K_ATTENTION_OP, K_TREE_PREP, K_TREE_COMPACT,
-  K_PF_GEMM, K_PF_ATTENTION, K_COUNT
+  K_PF_GEMM, K_PF_ATTENTION, K_PAGES, K_PREFIX_ATTENTION, K_LOGPROBS, K_COUNT
 };
 const char* const KCLASS_NAME[K_COUNT] = {"rmsnorm", "gemm_qkv", "attention", "gemm_o", "gemm_gateup", "gemm_down",
                                           "gemm_lm_head", "accept", "build_block", "kv_commit", "prefill_commit",
                                           "gemm_op", "attention_op", "tree_prep", "tree_compact", "prefill_gemm",
-                                          "prefill_attention"};
+                                          "prefill_attention", "pages", "prefix_attention", "logprobs"};
 
 static_assert(SDSAT_MAX_ROWS == 64, "block rows fill one 64-row tile of the prefill GEMM");
 constexpr int MAX_GEMM_TILES = 1 << 16;
@@ -133,6 +133,7 @@ struct sdsat_ctx {
   uint32_t* tree_anc = nullptr;   // [SDSAT_MAX_ROWS] tree block attention masks
   int* tree_ws = nullptr;      // [SDSAT_MAX_ROWS][TREE_WS_STRIDE] tree commit: len, m, path
   int* adaptive = nullptr;
+  float* prefix_part = nullptr;   // partial results of the prefix attention
   uint32_t* err = nullptr;
   // prefill workspaces (chunks of up to pf_rows positions; allocated with the weights)
   int pf_rows = 0;
@@ -170,6 +171,15 @@ struct sdsat_kv {
   int* len = nullptr;
   long long* emitted = nullptr;
   CUtensorMap kmap, vmap;   // the caches as 2-D tensors for the attention kernel
+  // a paged cache: k and v are [n_layers][pages][n_heads][KV_PAGE][head_dim]
+  int pages = 0, page_ld = 0;   // pages of the pool (0: contiguous), entries of a sequence's table row
+  int* page_mem = nullptr;      // one allocation: table, refs, common, ids, kinds, copies
+  int *table = nullptr, *refs = nullptr, *common = nullptr, *ids = nullptr, *kinds = nullptr, *copies = nullptr;
+
+  PageMap map() const { return PageMap{table, refs, page_ld, pages}; }
+  int head_rows() const { return pages ? KV_PAGE : cap; }
+  // rows of one layer in the caches' 2-D view
+  long long layer_rows(int H) const { return pages ? (long long)pages * H * KV_PAGE : (long long)batch * H * cap; }
 };
 
 namespace {
@@ -273,7 +283,7 @@ sdsat_status tiled_layers(sdsat_ctx* c, sdsat_kv* kv, const Tiled& t, const int3
   const sdsat_config& cf = c->cfg;
   const int M = t.M, d = cf.d_model, H = cf.n_heads, hd = cf.head_dim, F = cf.ffn_dim, R = H * hd, L = cf.n_layers;
   cudaStream_t st = c->stream;
-  const size_t layer_elems = (size_t)kv->batch * H * kv->cap * hd;
+  const size_t layer_elems = (size_t)kv->layer_rows(H) * hd;
   // RMSNorm folded into the GEMMs as in forward(): O and down emit the next operand and the
   // sums of squares, gate/up and the next QKV scale by the factor (unless O or down ended in a
   // kernel of its own, which normalises)
@@ -342,6 +352,8 @@ sdsat_status tiled_layers(sdsat_ctx* c, sdsat_kv* kv, const Tiled& t, const int3
     gq.H = H;
     gq.hd = hd;
     gq.cap = kv->cap;
+    gq.head_rows = kv->head_rows();
+    gq.pages = kv->map();
     gq.rope = c->rope;
     gq.rope_len = cf.max_position;
     if (!normed) fold_in(gq);
@@ -401,9 +413,36 @@ sdsat_status forward(sdsat_ctx* c, sdsat_kv* kv, int seq0, int nb, int q, const 
   const sdsat_config& cf = c->cfg;
   const int M = nb * q, d = cf.d_model, H = cf.n_heads, hd = cf.head_dim, F = cf.ffn_dim, R = H * hd, L = cf.n_layers;
   cudaStream_t st = c->stream;
-  const size_t layer_elems = (size_t)kv->batch * H * kv->cap * hd;
+  const size_t layer_elems = (size_t)kv->layer_rows(H) * hd;
   auto attention = [&](int l) {
     // block-causal attention; its merge emits the O projection's operand
+    if (kv->pages) {
+      PrefixAttnParams a;
+      std::memset(&a, 0, sizeof(a));
+      a.kmap = kv->kmap;
+      a.vmap = kv->vmap;
+      a.k = kv->k;
+      a.v = kv->v;
+      a.row0 = (int)(l * kv->layer_rows(H));
+      a.q = c->qbuf;
+      a.q_ld = a.out_ld = R;
+      a.table = kv->table + (size_t)seq0 * kv->page_ld;
+      a.ld = kv->page_ld;
+      a.n_pages = kv->pages;
+      a.common = seq0 == 0 ? kv->common : nullptr;   // (counted against sequence 0)
+      a.len = kv->len + seq0;
+      a.anc = anc;
+      a.b = nb;
+      a.nq = q;
+      a.H = a.Hk = H;
+      a.hd = hd;
+      a.out = c->attn;
+      a.out_hi = c->x_hi[X_ATTN];
+      a.out_lo = c->x_lo[X_ATTN];
+      a.part = c->prefix_part;
+      a.err = c->err;
+      return timed(c, K_PREFIX_ATTENTION, [&] { return launch_prefix_attention(a, c->num_sms, st, c->pdl); });
+    }
     AttnParams a;
     std::memset(&a, 0, sizeof(a));
     a.kmap = kv->kmap;
@@ -488,6 +527,8 @@ sdsat_status forward(sdsat_ctx* c, sdsat_kv* kv, int seq0, int nb, int q, const 
     g.H = H;
     g.hd = hd;
     g.cap = kv->cap;
+    g.head_rows = kv->head_rows();
+    g.pages = kv->map();
     g.q = q;
     g.seq0 = seq0;
     g.len = kv->len;
@@ -590,13 +631,14 @@ sdsat_status prefill_chunk(sdsat_ctx* c, sdsat_kv* kv, int seq, const int32_t* t
     a.vmap = kv->vmap;
     a.qmap[0] = c->pf_qmap[0];
     a.qmap[1] = c->pf_qmap[1];
-    a.row0 = l * kv->batch * H * kv->cap;
+    a.row0 = (int)(l * kv->layer_rows(H));
     a.len = kv->len;
     a.seq = seq;
     a.M = M;
     a.H = H;
     a.hd = hd;
     a.cap = kv->cap;
+    a.pages = kv->map();
     a.out_ld = R;
     a.out_hi = c->pf_hi[X_ATTN];
     a.out_lo = c->pf_lo[X_ATTN];
@@ -651,8 +693,8 @@ sdsat_status accept_common(sdsat_ctx* c, sdsat_kv* kv, const float* logits, cons
   if (!parent) return SDSAT_OK;
   const sdsat_config& cf = c->cfg;
   return timed(c, K_TREE_COMPACT, [&] {
-           return launch_tree_compact(c->tree_ws, b, cf.n_layers, cf.n_heads, cf.head_dim, kv->cap, kv->batch, kv->k,
-                                      kv->v, c->stream, c->pdl);
+           return launch_tree_compact(c->tree_ws, b, cf.n_layers, cf.n_heads, cf.head_dim, kv->cap, kv->batch, kv->map(),
+                                      kv->k, kv->v, c->stream, c->pdl);
          }) == cudaSuccess
              ? SDSAT_OK
              : SDSAT_ECUDA;
@@ -701,7 +743,8 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
   if (cudaGetDevice(&c->device) != cudaSuccess ||
       cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
       gemm_prepare() != cudaSuccess || attention_prepare() != cudaSuccess || prefill_prepare() != cudaSuccess ||
-      prefill_attention_prepare() != cudaSuccess || accept_prepare() != cudaSuccess) {
+      prefill_attention_prepare() != cudaSuccess || accept_prepare() != cudaSuccess || pages_prepare() != cudaSuccess ||
+      prefix_attention_prepare() != cudaSuccess || logprobs_prepare() != cudaSuccess) {
     delete c;
     return SDSAT_ECUDA;
   }
@@ -756,6 +799,7 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
             dalloc(c, &c->acc_counters, rows) && dalloc(c, &c->adaptive, SDSAT_MAX_ADAPTIVE) &&
             dalloc(c, &c->tree_pos, rows) && dalloc(c, &c->tree_anc, rows) &&
             dalloc(c, &c->tree_ws, (size_t)rows * TREE_WS_STRIDE) &&
+            dalloc(c, &c->prefix_part, prefix_attention_scratch(rows * cfg->n_heads, cfg->head_dim, c->num_sms)) &&
             dalloc(c, &c->err, 1) && dalloc(c, &c->xop_hi, (size_t)OP_MAX_M * OP_MAX_K) &&
             dalloc(c, &c->ssq, (size_t)rows * ((d + 127) / 128)) &&
             dalloc(c, &c->xop_lo, (size_t)OP_MAX_M * OP_MAX_K);
@@ -820,8 +864,8 @@ sdsat_status sdsat_set_stream(sdsat_ctx* c, void* stream) {
   return SDSAT_OK;
 }
 
-sdsat_status sdsat_kv_create(sdsat_ctx* c, int batch, int max_len, sdsat_kv** out) {
-  if (!c || !out || batch < 1 || max_len < 1) return SDSAT_EINVAL;
+// pages > 0: a paged cache
+static sdsat_status kv_create(sdsat_ctx* c, int batch, int max_len, int pages, sdsat_kv** out) {
   *out = nullptr;
   if (max_len > c->cfg.max_position || max_len > ATT_MAX_CAP) return SDSAT_ECAPACITY;
   sdsat_kv* kv = new (std::nothrow) sdsat_kv();
@@ -829,44 +873,62 @@ sdsat_status sdsat_kv_create(sdsat_ctx* c, int batch, int max_len, sdsat_kv** ou
   kv->ctx = c;
   kv->batch = batch;
   kv->cap = max_len;
-  const size_t n = (size_t)c->cfg.n_layers * batch * c->cfg.n_heads * max_len * c->cfg.head_dim;
-  void *k = nullptr, *v = nullptr, *len = nullptr, *em = nullptr;
-  if (cudaMalloc(&k, n * 2) != cudaSuccess || cudaMalloc(&v, n * 2) != cudaSuccess ||
-      cudaMalloc(&len, batch * sizeof(int)) != cudaSuccess || cudaMalloc(&em, batch * sizeof(long long)) != cudaSuccess) {
-    cudaGetLastError();   // clear the runtime's record of the failed allocation (not sticky)
+  kv->pages = pages;
+  kv->page_ld = (max_len + KV_PAGE - 1) / KV_PAGE;
+  const long long rows = c->cfg.n_layers * kv->layer_rows(c->cfg.n_heads);
+  const size_t n = (size_t)rows * c->cfg.head_dim;
+  const size_t entries = (size_t)batch * kv->page_ld, list = 4 + 3 * (size_t)std::max(pages, batch);
+  const size_t page_ints = pages ? entries + 2 * (size_t)pages + batch + std::max<size_t>(pages, entries) + list : 0;
+  void *k = nullptr, *v = nullptr, *len = nullptr, *em = nullptr, *pm = nullptr;
+  auto fail = [&](sdsat_status s) {
     cudaFree(k);
     cudaFree(v);
     cudaFree(len);
     cudaFree(em);
+    cudaFree(pm);
     delete kv;
-    return SDSAT_ENOMEM;
+    return s;
+  };
+  if (cudaMalloc(&k, n * 2) != cudaSuccess || cudaMalloc(&v, n * 2) != cudaSuccess ||
+      cudaMalloc(&len, batch * sizeof(int)) != cudaSuccess || cudaMalloc(&em, batch * sizeof(long long)) != cudaSuccess ||
+      (pages && cudaMalloc(&pm, page_ints * sizeof(int)) != cudaSuccess)) {
+    cudaGetLastError();   // clear the runtime's record of the failed allocation (not sticky)
+    return fail(SDSAT_ENOMEM);
   }
   if (cudaMemset(k, 0, n * 2) != cudaSuccess || cudaMemset(v, 0, n * 2) != cudaSuccess ||
       cudaMemset(len, 0, batch * sizeof(int)) != cudaSuccess ||
-      cudaMemset(em, 0, batch * sizeof(long long)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
-    cudaFree(k);
-    cudaFree(v);
-    cudaFree(len);
-    cudaFree(em);
-    delete kv;
-    return SDSAT_ECUDA;
-  }
-  kv->emitted = static_cast<long long*>(em);
-  const long long rows = (long long)c->cfg.n_layers * batch * c->cfg.n_heads * max_len;
+      cudaMemset(em, 0, batch * sizeof(long long)) != cudaSuccess ||
+      (pages && (cudaMemset(pm, 0, page_ints * sizeof(int)) != cudaSuccess ||
+                 cudaMemset(pm, 0xFF, entries * sizeof(int)) != cudaSuccess)) ||   // the table: -1
+      cudaDeviceSynchronize() != cudaSuccess)
+    return fail(SDSAT_ECUDA);
   if (rows > 0x7FFFFFFFll || !make_kvmap(&kv->kmap, k, rows, c->cfg.head_dim) ||
-      !make_kvmap(&kv->vmap, v, rows, c->cfg.head_dim)) {
-    cudaFree(k);
-    cudaFree(v);
-    cudaFree(len);
-    cudaFree(em);
-    delete kv;
-    return SDSAT_EUNSUPPORTED;
-  }
+      !make_kvmap(&kv->vmap, v, rows, c->cfg.head_dim))
+    return fail(SDSAT_EUNSUPPORTED);
+  kv->emitted = static_cast<long long*>(em);
   kv->k = static_cast<__nv_bfloat16*>(k);
   kv->v = static_cast<__nv_bfloat16*>(v);
   kv->len = static_cast<int*>(len);
+  if (pages) {
+    kv->page_mem = kv->table = static_cast<int*>(pm);
+    kv->refs = kv->table + entries;
+    kv->ids = kv->refs + pages;
+    kv->common = kv->ids + pages;
+    kv->copies = kv->common + batch;
+    kv->kinds = kv->copies + list;
+  }
   *out = kv;
   return SDSAT_OK;
+}
+
+sdsat_status sdsat_kv_create(sdsat_ctx* c, int batch, int max_len, sdsat_kv** out) {
+  if (!c || !out || batch < 1 || max_len < 1) return SDSAT_EINVAL;
+  return kv_create(c, batch, max_len, 0, out);
+}
+
+sdsat_status sdsat_kv_create_paged(sdsat_ctx* c, int batch, int max_len, int n_pages, sdsat_kv** out) {
+  if (!c || !out || batch < 1 || batch > PAGES_MAX_BATCH || max_len < 1 || n_pages < 1) return SDSAT_EINVAL;
+  return kv_create(c, batch, max_len, n_pages, out);
 }
 
 void sdsat_kv_destroy(sdsat_kv* kv) {
@@ -876,6 +938,7 @@ void sdsat_kv_destroy(sdsat_kv* kv) {
   cudaFree(kv->v);
   cudaFree(kv->len);
   cudaFree(kv->emitted);
+  cudaFree(kv->page_mem);
   delete kv;
 }
 
@@ -890,6 +953,75 @@ sdsat_status sdsat_kv_info(const sdsat_kv* kv, void** k_dev, void** v_dev, int32
   return SDSAT_OK;
 }
 
+static PagesParams pages_params(sdsat_ctx* c, sdsat_kv* kv) {
+  PagesParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.table = kv->table;
+  p.refs = kv->refs;
+  p.len = kv->len;
+  p.common = kv->common;
+  p.ids = kv->ids;
+  p.kinds = kv->kinds;
+  p.copies = kv->copies;
+  p.batch = kv->batch;
+  p.ld = kv->page_ld;
+  p.cap = kv->cap;
+  p.n_pages = kv->pages;
+  p.L = c->cfg.n_layers;
+  p.H = c->cfg.n_heads;
+  p.hd = c->cfg.head_dim;
+  p.k = kv->k;
+  p.v = kv->v;
+  p.err = c->err;
+  return p;
+}
+
+sdsat_status sdsat_kv_pages(const sdsat_kv* kv, int32_t** table_dev, int32_t** refs_dev, int* n_pages, int* table_ld) {
+  if (!kv || !kv->pages) return SDSAT_EINVAL;
+  if (table_dev) *table_dev = kv->table;
+  if (refs_dev) *refs_dev = kv->refs;
+  if (n_pages) *n_pages = kv->pages;
+  if (table_ld) *table_ld = kv->page_ld;
+  return SDSAT_OK;
+}
+
+sdsat_status sdsat_kv_fork(sdsat_ctx* c, sdsat_kv* kv, const int32_t* src_dev, int b) {
+  if (!c || !kv || kv->ctx != c || !kv->pages || !src_dev || b < 1 || b > kv->batch) return SDSAT_EINVAL;
+  PagesParams p = pages_params(c, kv);
+  p.src = src_dev;
+  p.nb = b;
+  return timed(c, K_PAGES, [&] { return launch_pages_fork(p, c->stream, c->pdl); }) == cudaSuccess ? SDSAT_OK : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_kv_free(sdsat_ctx* c, sdsat_kv* kv, int seq) {
+  if (!c || !kv || kv->ctx != c || !kv->pages || seq < 0 || seq >= kv->batch) return SDSAT_EINVAL;
+  PagesParams p = pages_params(c, kv);
+  p.seq0 = seq;
+  p.nb = 1;
+  return timed(c, K_PAGES, [&] { return launch_pages_fork(p, c->stream, c->pdl); }) == cudaSuccess ? SDSAT_OK : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_kv_reserve(sdsat_ctx* c, sdsat_kv* kv, int seq, int b, int n) {
+  if (!c || !kv || kv->ctx != c || !kv->pages || seq < 0 || b < 1 || b > kv->batch - seq || n < 0) return SDSAT_EINVAL;
+  if (n == 0) return SDSAT_OK;
+  PagesParams p = pages_params(c, kv);
+  p.seq0 = seq;
+  p.nb = b;
+  p.n = n;
+  if (timed(c, K_PAGES, [&] { return launch_pages_reserve(p, c->stream, c->pdl); }) != cudaSuccess) return SDSAT_ECUDA;
+  return timed(c, K_PAGES, [&] { return launch_pages_copy(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess ? SDSAT_OK
+                                                                                                   : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_kv_compact(sdsat_ctx* c, sdsat_kv* kv, int32_t* used_dev) {
+  if (!c || !kv || kv->ctx != c || !kv->pages) return SDSAT_EINVAL;
+  PagesParams p = pages_params(c, kv);
+  p.used = used_dev;
+  if (timed(c, K_PAGES, [&] { return launch_pages_compact(p, c->stream, c->pdl); }) != cudaSuccess) return SDSAT_ECUDA;
+  return timed(c, K_PAGES, [&] { return launch_pages_copy(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess ? SDSAT_OK
+                                                                                                   : SDSAT_ECUDA;
+}
+
 static sdsat_status kv_copy(sdsat_ctx* c, const sdsat_kv* kv, int layer, int seq, int slot0, int n, const void* ks,
                             const void* vs, void* kd, void* vd) {
   if (!c || !kv || kv->ctx != c || layer < 0 || layer >= c->cfg.n_layers || seq < 0 || seq >= kv->batch ||
@@ -897,7 +1029,20 @@ static sdsat_status kv_copy(sdsat_ctx* c, const sdsat_kv* kv, int layer, int seq
     return SDSAT_EINVAL;
   if (n == 0) return SDSAT_OK;
   const int H = c->cfg.n_heads, hd = c->cfg.head_dim;
-  const size_t layer_elems = (size_t)kv->batch * H * kv->cap * hd;
+  if (kv->pages) {
+    const bool write = ks || vs;
+    if (!aligned16(write ? ks : kd) || !aligned16(write ? vs : vd)) return SDSAT_EINVAL;
+    PagesParams p = pages_params(c, const_cast<sdsat_kv*>(kv));
+    p.seq0 = seq;
+    p.n = n;
+    return timed(c, K_PAGES, [&] {
+             return launch_pages_rows(p, layer, slot0, const_cast<void*>(write ? ks : kd),
+                                      const_cast<void*>(write ? vs : vd), write, c->stream, c->pdl);
+           }) == cudaSuccess
+               ? SDSAT_OK
+               : SDSAT_ECUDA;
+  }
+  const size_t layer_elems = (size_t)kv->layer_rows(H) * hd;
   const size_t off = layer * layer_elems + ((size_t)seq * H * kv->cap + slot0) * hd;
   const size_t cache_pitch = (size_t)kv->cap * hd * 2, buf_pitch = (size_t)n * hd * 2, width = buf_pitch;
   for (int which = 0; which < 2; ++which) {
@@ -1271,6 +1416,80 @@ sdsat_status sdsat_op_attention(sdsat_ctx* c, const float* q_dev, const void* k_
   return timed(c, K_ATTENTION_OP, [&] { return launch_attention(a, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
              ? SDSAT_OK
                                                                                                    : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_op_prefix_attention(sdsat_ctx* c, const void* q_dev, int64_t q_ld, const void* k_dev,
+                                       const void* v_dev, int n_pages, const int32_t* table_dev, int table_ld,
+                                       const int32_t* shared_dev, const int32_t* len_dev, const uint32_t* anc_dev,
+                                       int b, int q, int H, int Hk, int hd, void* out_dev, int64_t out_ld, int type) {
+  if (!c || !table_dev || !len_dev || !aligned16(q_dev) || !aligned16(k_dev) || !aligned16(v_dev) || !aligned16(out_dev))
+    return SDSAT_EINVAL;
+  if (b < 1 || q < 1 || q > SDSAT_MAX_Q || b > SDSAT_MAX_ROWS / q || (hd != 64 && hd != 128) || H < 1 || Hk < 1 ||
+      H % Hk || n_pages < 1 || table_ld < 1 || (type != SDSAT_FP32 && type != SDSAT_BF16))
+    return SDSAT_EINVAL;
+  const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
+  if (q_ld < (long long)H * hd || out_ld < (long long)H * hd || q_ld % per16 || out_ld % per16) return SDSAT_EINVAL;
+  if ((size_t)b * q * H * hd > (size_t)SDSAT_MAX_ROWS * c->cfg.n_heads * c->cfg.head_dim) return SDSAT_EINVAL;
+  const long long rows = (long long)n_pages * Hk * KV_PAGE;
+  if (rows > 0x7FFFFFFFll) return SDSAT_EINVAL;
+  PrefixAttnParams a;
+  std::memset(&a, 0, sizeof(a));
+  if (!make_kvmap(&a.kmap, k_dev, rows, hd) || !make_kvmap(&a.vmap, v_dev, rows, hd)) return SDSAT_ECUDA;
+  a.k = k_dev;
+  a.v = v_dev;
+  a.q = q_dev;
+  a.q_ld = q_ld;
+  a.out = out_dev;
+  a.out_ld = out_ld;
+  a.bf16 = type == SDSAT_BF16;
+  a.table = table_dev;
+  a.ld = table_ld;
+  a.n_pages = n_pages;
+  a.common = shared_dev;
+  a.len = len_dev;
+  a.anc = anc_dev;
+  a.b = b;
+  a.nq = q;
+  a.H = H;
+  a.Hk = Hk;
+  a.hd = hd;
+  a.part = c->prefix_part;
+  a.err = c->err;
+  return timed(c, K_PREFIX_ATTENTION, [&] { return launch_prefix_attention(a, c->num_sms, c->stream, c->pdl); }) ==
+                 cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_op_logprobs(sdsat_ctx* c, const void* logits_dev, int64_t ld, int type, int rows, int vocab,
+                               const int32_t* tokens_dev, float temperature, int n_top, float* logp_dev,
+                               float* entropy_dev, int32_t* rank_dev, int32_t* top_ids_dev, float* top_logp_dev) {
+  if (!c || rows < 0 || vocab < 1 || ld < vocab || (type != SDSAT_FP32 && type != SDSAT_BF16)) return SDSAT_EINVAL;
+  if (!(temperature > 0.f) || std::isinf(temperature) || n_top < 0 || n_top > LP_MAX_TOP || n_top > vocab) return SDSAT_EINVAL;
+  if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
+  if (!logits_dev || reinterpret_cast<uintptr_t>(logits_dev) % (type == SDSAT_BF16 ? 2 : 4)) return SDSAT_EINVAL;
+  if (!tokens_dev && (logp_dev || rank_dev)) return SDSAT_EINVAL;
+  if (n_top && (!top_ids_dev || !top_logp_dev)) return SDSAT_EINVAL;
+  if (vocab > LP_MAX_VOCAB) return SDSAT_EUNSUPPORTED;
+  LogprobParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.logits = logits_dev;
+  p.bf16 = type == SDSAT_BF16;
+  p.ld = ld;
+  p.rows = rows;
+  p.V = vocab;
+  p.tokens = tokens_dev;
+  p.inv_t = 1.0f / temperature;
+  p.logp = logp_dev;
+  p.entropy = entropy_dev;
+  p.rank = rank_dev;
+  p.n_top = n_top;
+  p.top_ids = top_ids_dev;
+  p.top_logp = top_logp_dev;
+  p.err = c->err;
+  return timed(c, K_LOGPROBS, [&] { return launch_logprobs(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
 }
 
 sdsat_status sdsat_debug_workspace(sdsat_ctx* c, int which, int rows, float* dst_dev) {
