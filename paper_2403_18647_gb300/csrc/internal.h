@@ -374,6 +374,7 @@ cudaError_t launch_prefix_attention(const PrefixAttnParams& p, int num_sms, cuda
 // Log probabilities (logprobs.cu)
 constexpr int LP_MAX_TOP = 32;
 constexpr int LP_MAX_VOCAB = 1 << 18;
+constexpr int LP_MAX_ROWS = 1 << 27;
 struct LogprobParams {
   const void* logits;       // [rows][ld] fp32 or bf16
   bool bf16;
@@ -386,6 +387,7 @@ struct LogprobParams {
   int n_top;
   int* top_ids;             // [rows][n_top]
   float* top_logp;
+  int cs;                   // CTAs of a row (set by launch_logprobs)
   uint32_t* err;
 };
 cudaError_t logprobs_prepare();

@@ -1464,7 +1464,7 @@ sdsat_status sdsat_op_prefix_attention(sdsat_ctx* c, const void* q_dev, int64_t 
 sdsat_status sdsat_op_logprobs(sdsat_ctx* c, const void* logits_dev, int64_t ld, int type, int rows, int vocab,
                                const int32_t* tokens_dev, float temperature, int n_top, float* logp_dev,
                                float* entropy_dev, int32_t* rank_dev, int32_t* top_ids_dev, float* top_logp_dev) {
-  if (!c || rows < 0 || vocab < 1 || ld < vocab || (type != SDSAT_FP32 && type != SDSAT_BF16)) return SDSAT_EINVAL;
+  if (!c || rows < 0 || rows > LP_MAX_ROWS || vocab < 1 || ld < vocab || (type != SDSAT_FP32 && type != SDSAT_BF16)) return SDSAT_EINVAL;
   if (!(temperature > 0.f) || std::isinf(temperature) || n_top < 0 || n_top > LP_MAX_TOP || n_top > vocab) return SDSAT_EINVAL;
   if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
   if (!logits_dev || reinterpret_cast<uintptr_t>(logits_dev) % (type == SDSAT_BF16 ? 2 : 4)) return SDSAT_EINVAL;
