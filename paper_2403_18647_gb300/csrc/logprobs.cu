@@ -38,6 +38,8 @@ constexpr int LP_UNROLL = 4;      // vectors of a thread and round
 constexpr int LP_STAGES = 4;      // rounds in the ring
 constexpr int LP_GROUPS = 64;     // groups of 4 threads whose maxima bound the alternatives
 constexpr int LP_NOTED = 512;     // logits noted by a CTA
+constexpr int LP_FEW = 64;        // noted logits that are ranked as they are
+static_assert(LP_NOTED <= 2 * LP_THREADS, "two noted logits a thread");
 constexpr int LP_CS = 8;          // CTAs of a row
 constexpr int LP_PER_SM = 3;
 constexpr int LP_ROUND = LP_UNROLL * LP_THREADS;   // vectors of a round
@@ -311,11 +313,20 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
           if (lane == 0) mbar_arrive(&sm.empty[it % LP_STAGES]);
           ++it;
         }
-        float top = -INFINITY;
+        float vtop[LP_UNROLL];   // the largest of each vector (a NaN is passed over)
 #pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u)
-#pragma unroll
-          for (int k = 0; k < E; k += 2) top = fmaxf(fmaxf(top, value(r[u], k)), value(r[u], k + 1));   // (a NaN is passed over)
+        for (int u = 0; u < LP_UNROLL; ++u) {
+          if constexpr (BF16) {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r[u]);
+            const __nv_bfloat162 x = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+            vtop[u] = fmaxf(__low2float(x), __high2float(x));
+          } else {
+            vtop[u] = fmaxf(fmaxf(value(r[u], 0), value(r[u], 1)), fmaxf(value(r[u], 2), value(r[u], 3)));
+          }
+          vtop[u] = fmaxf(vtop[u], -INFINITY);
+        }
+        const float top = fmaxf(fmaxf(vtop[0], vtop[1]), fmaxf(vtop[2], vtop[3]));
+        static_assert(LP_UNROLL == 4, "the round's maximum");
         // (the same for every thread)
         if (round == 0 || (n && (bound == -INFINITY || round == 2 || round == 8 || round == 32))) {
           const float old = s.S > 0.f ? s.m : -INFINITY;
@@ -352,22 +363,34 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
           lp_unpack(E2, s.E, b);
           s.E += b;
         }
-        // the logits before the token, and those to note: rounds without either are passed over
-        if (top >= fminf(lt, bound) || (CLEAN && given)) {
+        // the logits before the token, and those to note: most vectors have neither
+        if (top >= lt) {
 #pragma unroll
           for (int u = 0; u < LP_UNROLL; ++u) {
             const int at = v + u * LP_THREADS, id0 = run.head + at * E;
-            if (at >= run.v1) continue;
+            if (vtop[u] < lt || at >= run.v1) continue;
             const float lo = id0 + E <= t ? lt : above;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
               float x = value(r[u], k);
               if (CLEAN && isnan(x)) x = -INFINITY;
               s.before += x >= lo;
-              if (x >= bound) note(x, id0 + k);
             }
             if (id0 <= t && t < id0 + E)   // equal logits before the token in its own vector
               for (int k = 0; id0 + k < t; ++k) s.before += logit(id0 + k) == lt;
+          }
+        }
+        if (top >= bound) {
+#pragma unroll
+          for (int u = 0; u < LP_UNROLL; ++u) {
+            const int at = v + u * LP_THREADS, id0 = run.head + at * E;
+            if (vtop[u] < bound || at >= run.v1) continue;
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+              float x = value(r[u], k);
+              if (CLEAN && isnan(x)) x = -INFINITY;
+              if (x >= bound) note(x, id0 + k);
+            }
           }
         }
       }
@@ -454,6 +477,19 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
       }
     } else {
       lp_bar();   // the warps' sums
+    }
+    // Many noted ones (those of the early rounds, from lower bounds on): the whole run's bound keeps
+    // about n of them.  2000 rows of 32016, 32 alternatives: XX us, XX without.
+    if (count > LP_FEW) {
+      const unsigned long long low = lp_key(nth_group(mine, false), INT_MAX);
+      const unsigned long long k0 = tid < count ? sm.noted[tid] : 0, k1 = tid + LP_THREADS < count ? sm.noted[tid + LP_THREADS] : 0;
+      lp_bar();
+      if (tid == 0) sm.count = 0;
+      lp_bar();
+      if (k0 >= low) sm.noted[atomicAdd(&sm.count, 1)] = k0;
+      if (k1 >= low) sm.noted[atomicAdd(&sm.count, 1)] = k1;
+      lp_bar();
+      count = sm.count;
     }
     // a noted logit's place is the number of larger keys (the keys differ)
     auto ranked = [&](const unsigned long long* keys, int total, auto&& put) {
