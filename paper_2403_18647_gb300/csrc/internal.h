@@ -351,7 +351,6 @@ cudaError_t launch_pages_rows(const PagesParams& p, int layer, int slot0, void* 
 // Block-causal attention of sequences that share their leading pages (prefix_attention.cu)
 struct PrefixAttnParams {
   CUtensorMap kmap, vmap;   // pages as a 2-D tensor [rows][hd] bf16, boxes of 64 dims x KV_PAGE rows
-  const void *k, *v;        // the same
   int row0;                 // row of (page, head, slot) = row0 + (page * Hk + head) * KV_PAGE + slot
   const void* q;            // [b*q][q_ld] fp32 or bf16
   long long q_ld, out_ld;
@@ -364,7 +363,8 @@ struct PrefixAttnParams {
   int b, nq, H, Hk, hd;
   void* out;                // [b*q][out_ld], the type of q
   __nv_bfloat16 *out_hi, *out_lo;   // [b*q][H*hd], or null: the O projection's operand
-  float* part;              // scratch: prefix_attention_scratch() floats
+  float* part;              // scratch: prefix_attention_scratch() floats, 1024-byte aligned
+  int ctas;                 // set by launch_prefix_attention
   uint32_t* err;
 };
 size_t prefix_attention_scratch(int row_heads, int hd, int num_sms);

@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
       lp_bar();   // the warps' sums
     }
     // Many noted ones (those of the early rounds, from lower bounds on): the whole run's bound keeps
-    // about n of them.  2000 rows of 32016, 32 alternatives: XX us, XX without.
+    // about n of them.  2000 rows of 32016, 32 alternatives: 79 us, 87 without.
     if (count > LP_FEW) {
       const unsigned long long low = lp_key(nth_group(mine, false), INT_MAX);
       const unsigned long long k0 = tid < count ? sm.noted[tid] : 0, k1 = tid + LP_THREADS < count ? sm.noted[tid + LP_THREADS] : 0;

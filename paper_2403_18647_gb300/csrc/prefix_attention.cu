@@ -2,10 +2,36 @@
 //
 // Row j of sequence s attends to the committed slots [0, len[s]) and to block rows 0..j (or its
 // ancestors in a tree block), slots len[s] .. len[s] + j, all on pages of KV_PAGE slots named by the
-// page table.  G = H / Hk query heads read the same cache head.
+// page table.  G = H / Hk query heads read the same cache head, so a sequence has q G rows for each
+// cache head, and the batch R = b q G.
 //
-// A CTA per (row, head): a warp takes every fourth key with the head's dimensions over its lanes, a
-// running maximum and sum, and the four warps' results are merged at the end.
+// Softmax is associative: with partial results (m, l, o) of disjoint sets of slots -- row maximum,
+// sum of exponentials and weighted sum of values relative to it -- a row's output is
+// sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  The whole committed pages that all sequences share are
+// one set, read once with all R rows against them; the rest of a sequence's slots is another, read
+// with its q G rows.  What bounds it are those bytes (K and V once each).
+//
+// Work: items are (cache head, tile of up to PX_ROWS rows) of the shared pages and (sequence, cache
+// head, tile) of the others; units are 128 slots of an item.  The units, items in order, are divided
+// evenly among the CTAs (one on an SM), so that every CTA streams the same bytes; an item's partial
+// results from the CTAs that share it are merged by a second kernel, a warp for each row and head.
+//
+// Per unit, on tcgen05 in the form that puts the slots on the 128 lanes (the rows, often few, are
+// the N of the products, so they do not pad to 128):
+//   S^T = K Q^T     A = the K tile, B = Q (shared memory, K-major)            128 slots x N rows
+//   P^T = exp2(c S^T - m)  one thread for a slot (two groups of 128 threads share the rows)
+//   O^T += V^T P^T  A = the V tile read MN-major, B = P (shared memory, MN-major)   hd x N rows
+// K and V are the cache's bf16 values.  fp32 queries and the probabilities enter as three bf16 parts
+// (24 bits: nothing is lost against fp32 products; one part for bf16 queries, whose probabilities
+// have two), one product each into the same fp32 accumulator.
+//
+// The reference m of a row is its maximum over the segment's first unit; later units only check that
+// no score passes it by more than 2^PX_LAZY, which is rare, and then rescale: a maximum over lanes for
+// each row and unit would cost more than the exponentials.  Sums of exponentials stay in each
+// thread (a slot's) until the segment's end.
+//
+// Warp 0: TMA (pages by the table), warp 1: MMA issue and TMEM, warps 4-11: queries, softmax, results.
+// Shared memory: a ring of K and V tiles, P and Q in three parts.
 #include <algorithm>
 
 #include "common.cuh"
@@ -14,90 +40,742 @@
 namespace sdsat {
 namespace {
 
+constexpr int PX_UNIT = 128;      // slots of a unit: two pages
+constexpr int PX_ROWS = 64;       // rows of a tile
+constexpr int PX_PARTS = 3;       // bf16 parts of fp32 queries and of their probabilities
+constexpr int PX_THREADS = 384;
+constexpr int PX_SOFTMAX = 256;   // softmax threads, two groups of 128
+constexpr int PX_MAX_B = 64;
+constexpr float PX_LAZY = 8.0f;   // log2 of the growth of a row maximum that is left unscaled
+constexpr float PX_UNSET = -1e30f;   // reference of a row that has seen no slot
+static_assert(PX_UNIT == 2 * KV_PAGE, "a unit is two pages");
+
 template <int HD>
-__global__ void __launch_bounds__(128) prefix_attention_kernel(const __grid_constant__ PrefixAttnParams p,
-                                                               const __nv_bfloat16* kc, const __nv_bfloat16* vc) {
-  constexpr int E = HD / 32;
-  __shared__ float o_s[4][HD], m_s[4], l_s[4];
-  pdl_wait();
-  pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = blockIdx.x / p.H, h = blockIdx.x % p.H, s = r / p.nq, j = r % p.nq, hk = h / (p.H / p.Hk);
-  const int len = __ldcg(p.len + s), end = min(len + p.nq, p.ld * KV_PAGE);
-  const uint32_t own = p.anc ? __ldcg(p.anc + r) : (2u << j) - 1u;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const long long at = r * p.q_ld + (long long)h * HD + lane + 32 * e;
-    q[e] = (p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.q)[at]) : static_cast<const float*>(p.q)[at]) *
-           rsqrtf((float)HD);
-    o[e] = 0.f;
+struct PxCfg {
+  static constexpr int HALVES = HD / 64;
+  static constexpr int BOX = KV_PAGE * 128;                 // one TMA box: a page's slots x 64 dims
+  static constexpr int HALF = PX_UNIT * 128;                // 128 slots x 64 dims, 128-byte swizzle
+  static constexpr int TILE = HALVES * HALF;                // K or V of a unit
+  static constexpr int SLOTS = HD == 128 ? 4 : 8;           // of the ring
+  static constexpr int P_PART = PX_UNIT * 128;              // 128 slots x 64 rows
+  static constexpr int Q_HALF = PX_ROWS * 128;              // 64 rows x 64 dims
+  static constexpr int Q_PART = HALVES * Q_HALF;
+  static constexpr size_t OFF_P = (size_t)SLOTS * TILE;     // (MN-major reads of 64-dim tiles run into it)
+  static constexpr size_t OFF_Q = OFF_P + PX_PARTS * P_PART;
+  static constexpr size_t OFF_MISC = OFF_Q + PX_PARTS * Q_PART;
+};
+
+// what the CTAs agree on; the first one leaves it for the merge
+struct PxSched {
+  int shared;              // pages that all sequences share, whole and committed
+  int up;                  // units of an item of the shared pages
+  int tp;                  // units of all of them
+  int total;
+  int cum[PX_MAX_B + 1];   // units of the items of the sequences before
+};
+struct PxMisc {
+  PxSched sched;
+  int len[PX_MAX_B];
+  float red[2][4][32];     // per group and warp: a row's maximum, or sum
+  __align__(16) float m[2][32];   // per group: the rows' references
+  float f[2][32];          // their rescaling
+  uint16_t seen[2][PX_ROWS];   // by segment parity: the block rows that a row sees
+  uint64_t full[8], empty[8];
+  uint64_t q_full, q_empty, s_full[2], s_empty[2], p_full, p_empty, o_full[2], o_empty[2], drain;
+  uint32_t tmem;
+  volatile int abort;
+  uint32_t pages_ok[8];    // by unit: its pages are in the pool (bits 0, 1)
+};
+
+// rows of a tile of `rows` in all: tiles of nearly the same number of rows, a multiple of 16
+struct PxTiles {
+  int n, rows;
+  __host__ __device__ explicit PxTiles(int all) {
+    n = (all + PX_ROWS - 1) / PX_ROWS;
+    rows = ((all + n - 1) / n + 15) / 16 * 16;
+    n = (all + rows - 1) / rows;
   }
-  for (int t = warp; t < end; t += 4) {
-    if (t >= len && !((own >> (t - len)) & 1u)) continue;
-    const int page = __ldcg(p.table + (size_t)s * p.ld + t / KV_PAGE);
-    if (page < 0 || page >= p.n_pages) {
-      if (lane == 0) set_error(p.err, ERR_PAGE);
-      continue;
+};
+
+// a run of units of one item
+struct PxSeg {
+  int s;                   // sequence, or -1: the shared pages
+  int hk, row0, rows;      // cache head, rows [row0, row0 + rows) of its R
+  int u0, u1;              // units
+  int slot0, end, len;     // unit u: slots slot0 + 128 u .., those below `end`; committed below len
+};
+
+// first unit of CTA c's share; with fewer units than CTAs the first `total` of them take one each
+__device__ __forceinline__ int px_begin(int c, int total, int ctas) {
+  const int n = min(total, ctas);
+  return c >= n ? total : (int)((long long)c * total / n);
+}
+
+// the segment that starts at unit g and ends at the item's end or at gend
+__device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int g, int gend) {
+  const int G = p.H / p.Hk;
+  PxSeg e;
+  int U, rt;
+  if (g < sc.tp) {
+    const PxTiles t(p.b * p.nq * G);
+    U = sc.up;
+    const int item = g / U;
+    e.u0 = g - item * U;
+    e.hk = item / t.n;
+    rt = item - e.hk * t.n;
+    e.s = -1;
+    e.row0 = rt * t.rows;
+    e.rows = min(t.rows, p.b * p.nq * G - e.row0);
+    e.slot0 = 0;
+    e.end = e.len = sc.shared * KV_PAGE;
+  } else {
+    const PxTiles t(p.nq * G);
+    int x = g - sc.tp, s = 0;
+    while (sc.cum[s + 1] <= x) ++s;
+    x -= sc.cum[s];
+    U = (sc.cum[s + 1] - sc.cum[s]) / (p.Hk * t.n);
+    const int item = x / U;
+    e.u0 = x - item * U;
+    e.hk = item / t.n;
+    rt = item - e.hk * t.n;
+    e.s = s;
+    e.row0 = s * p.nq * G + rt * t.rows;
+    e.rows = min(t.rows, p.nq * G - rt * t.rows);
+    e.slot0 = sc.shared * KV_PAGE;
+    e.len = len[s];
+    e.end = min(e.len + p.nq, p.ld * KV_PAGE);
+  }
+  e.u1 = min(U, e.u0 + gend - g);
+  return e;
+}
+
+__device__ __forceinline__ void px_ld8(uint32_t taddr, float* v) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void px_st8(uint32_t taddr, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+               "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+               "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
+}
+// MN-major operand in the 128-byte swizzle layout: atoms of 64 elements (128 bytes) x 8 lines of K;
+// `lead` bytes to the next 64 elements, 1024 to the next 8 lines
+__device__ __forceinline__ uint64_t px_desc_mn(uint32_t saddr, uint32_t lead) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(lead >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+__device__ __forceinline__ float px_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two values as packed bf16 (a in the low half); what is left of them stays in a and b
+__device__ __forceinline__ uint32_t px_part(float& a, float& b) {
+  uint32_t h;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
+  a -= __uint_as_float(h << 16);
+  b -= __uint_as_float(h & 0xFFFF0000u);
+  return h;
+}
+__device__ __forceinline__ bool px_bar_or(int id, bool pred) {   // over a group's 128 threads
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %1, 0;\n\t"
+      "barrier.cta.red.or.pred p, %2, 128, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)pred), "r"(id)
+      : "memory");
+  return r != 0;
+}
+// Eight columns of a value a lane each -> in every lane, column (lane & 7) over the warp's 32 lanes
+template <typename F>
+__device__ __forceinline__ float px_across(const float* v, int lane, F&& f) {
+  float a[4], b[2], c;
+  const bool h4 = lane & 4, h2 = lane & 2, h1 = lane & 1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float keep = h4 ? v[i + 4] : v[i], give = h4 ? v[i] : v[i + 4];
+    a[i] = f(keep, __shfl_xor_sync(0xffffffffu, give, 4));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float keep = h2 ? a[i + 2] : a[i], give = h2 ? a[i] : a[i + 2];
+    b[i] = f(keep, __shfl_xor_sync(0xffffffffu, give, 2));
+  }
+  c = f(h1 ? b[1] : b[0], __shfl_xor_sync(0xffffffffu, h1 ? b[0] : b[1], 1));
+  c = f(c, __shfl_xor_sync(0xffffffffu, c, 8));
+  return f(c, __shfl_xor_sync(0xffffffffu, c, 16));
+}
+
+// where partial results are: of an item's rows from the CTA that holds its first unit, and, for each
+// CTA, from the item that it continues
+struct PxScratch {
+  float* o;        // [2 * row heads + PX_ROWS * CTAs][hd]
+  float2* ml;      // the same rows' reference and sum
+  PxSched* sched;
+  __host__ __device__ PxScratch(const PrefixAttnParams& p) {
+    const size_t rows = (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * p.ctas;
+    sched = reinterpret_cast<PxSched*>(p.part);
+    ml = reinterpret_cast<float2*>(p.part + 256);
+    o = p.part + 256 + (2 * rows + 31) / 32 * 32;
+  }
+};
+static_assert(sizeof(PxSched) <= 1024, "the schedule's place");
+
+template <int HD>
+__global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const __grid_constant__ PrefixAttnParams p) {
+  using C = PxCfg<HD>;
+  constexpr int NS = C::SLOTS;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t* Ps = smem + C::OFF_P;
+  uint8_t* Qs = smem + C::OFF_Q;
+  PxMisc& sm = *reinterpret_cast<PxMisc*>(smem + C::OFF_MISC);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = p.H / p.Hk, R = p.b * p.nq * G;
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], 1);
     }
-    const long long row = (p.row0 + ((long long)page * p.Hk + hk) * KV_PAGE + t % KV_PAGE) * HD;
-    float x = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x += q[e] * __bfloat162float(kc[row + lane + 32 * e]);
-#pragma unroll
-    for (int a = 16; a > 0; a >>= 1) x += __shfl_xor_sync(0xffffffffu, x, a);
-    const float mn = fmaxf(m, x), f = m == -INFINITY ? 0.f : expf(m - mn), w = expf(x - mn);
-    l = l * f + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * __bfloat162float(vc[row + lane + 32 * e]);
-    m = mn;
+    mbar_init(&sm.q_full, PX_SOFTMAX);
+    mbar_init(&sm.q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.s_full[i], 1);
+      mbar_init(&sm.s_empty[i], PX_SOFTMAX);
+      mbar_init(&sm.o_full[i], 1);
+      mbar_init(&sm.o_empty[i], PX_SOFTMAX);
+    }
+    mbar_init(&sm.p_full, PX_SOFTMAX);
+    mbar_init(&sm.p_empty, 1);
+    mbar_init(&sm.drain, 1);
+    sm.abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&p.kmap);
+    tma_prefetch_desc(&p.vmap);
   }
+  if (warp == 1) tmem_alloc(&sm.tmem, 256);
+  pdl_wait();   // q, lengths, tables and rows come from the kernels before
+  pdl_trigger();
+  if (warp == 2) {   // the schedule: two sequences a lane
+    const int s0 = 2 * lane, s1 = s0 + 1;
+    const int n0 = s0 < p.b ? max(0, __ldcg(p.len + s0)) : 0, n1 = s1 < p.b ? max(0, __ldcg(p.len + s1)) : 0;
+    int shared = 0;
+    if (p.common && p.b > 1) {
+      shared = p.ld;
+      if (s0 < p.b) shared = min(shared, min(__ldcg(p.common + s0), n0 / KV_PAGE));
+      if (s1 < p.b) shared = min(shared, min(__ldcg(p.common + s1), n1 / KV_PAGE));
+      shared = max(0, __reduce_min_sync(0xffffffffu, shared));
+    }
+    const int per = p.Hk * PxTiles(p.nq * G).n;
+    auto units = [&](int n) { return per * ((min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
+    const int u0 = s0 < p.b ? units(n0) : 0, u1 = s1 < p.b ? units(n1) : 0;
+    int x = u0 + u1;
 #pragma unroll
-  for (int e = 0; e < E; ++e) o_s[warp][lane + 32 * e] = o[e];
-  if (lane == 0) m_s[warp] = m, l_s[warp] = l;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    sm.len[s0] = n0;
+    sm.len[s1] = n1;
+    sm.sched.cum[s0 + 1] = x - u1;
+    sm.sched.cum[s1 + 1] = x;
+    if (lane == 31) {
+      sm.sched.cum[0] = 0;
+      sm.sched.shared = shared;
+      sm.sched.up = (shared + 1) / 2;
+      sm.sched.tp = p.Hk * PxTiles(R).n * sm.sched.up;
+      sm.sched.total = sm.sched.tp + x;
+    }
+  }
+  tc_fence_before();
   __syncthreads();
-  if (threadIdx.x >= HD) return;
-  float M = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3])), L = 0.f, a = 0.f;
-  for (int w = 0; w < 4; ++w) {
-    const float f = m_s[w] == -INFINITY ? 0.f : expf(m_s[w] - M);
-    L += f * l_s[w];
-    a += f * o_s[w][threadIdx.x];
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;   // S at columns 0 and 64, O at 128 and 192
+  const PxScratch scratch(p);
+  if (blockIdx.x == 0 && tid < (int)(sizeof(PxSched) / 4)) reinterpret_cast<int*>(scratch.sched)[tid] = reinterpret_cast<int*>(&sm.sched)[tid];
+  const int g0 = px_begin(blockIdx.x, sm.sched.total, gridDim.x), g1 = px_begin(blockIdx.x + 1, sm.sched.total, gridDim.x);
+  const int q_parts = p.bf16 ? 1 : PX_PARTS, p_parts = p.bf16 ? 2 : PX_PARTS;
+
+  if (warp == 0) {
+    // ---- K and V tiles: K of unit 0, V of unit 0, K of unit 1, ...
+    const uint64_t pol = l2_policy_evict_normal();
+    int it = 0;
+    for (int g = g0; g < g1 && !sm.abort;) {
+      const PxSeg e = px_segment(p, sm.sched, sm.len, g, g1);
+      g += e.u1 - e.u0;
+      const int* row = p.table + (size_t)max(e.s, 0) * p.ld;
+      const int j0 = e.slot0 / KV_PAGE + 2 * e.u0, j1 = min((e.end + KV_PAGE - 1) / KV_PAGE, e.slot0 / KV_PAGE + 2 * e.u1);
+      int entry = 0;
+      for (int u = e.u0; u < e.u1; ++u) {
+        const int at = 2 * (u - e.u0), j = j0 + at;
+        if ((at & 31) == 0) entry = j + lane < j1 ? __ldcg(row + j + lane) : 0;
+        const int page[2] = {__shfl_sync(0xffffffffu, entry, at & 31), __shfl_sync(0xffffffffu, entry, (at & 31) + 1)};
+        uint32_t ok = 0;
+        for (int i = 0; i < 2; ++i)
+          if (j + i < j1) {
+            if (page[i] >= 0 && page[i] < p.n_pages) ok |= 1u << i;
+            else if (lane == 0) set_error(p.err, ERR_PAGE);
+          }
+        if (lane == 0) {
+          for (int kv = 0; kv < 2; ++kv, ++it) {
+            const int s = it % NS;
+            if (!mbar_wait_bounded(&sm.empty[s], ((it / NS) & 1) ^ 1, &sm.abort, p.err)) break;
+            // (read until the unit's V slot is free again, 2 or 4 units on)
+            sm.pages_ok[(it >> 1) & 7] = ok;
+            mbar_arrive_expect_tx(&sm.full[s], __popc(ok) * C::HALVES * C::BOX);
+            for (int i = 0; i < 2; ++i) {
+              if (!((ok >> i) & 1)) continue;
+              const int r = p.row0 + (page[i] * p.Hk + e.hk) * KV_PAGE;
+              for (int hh = 0; hh < C::HALVES; ++hh)
+                tma_load_2d(smem + (size_t)s * C::TILE + hh * C::HALF + i * C::BOX, kv ? &p.vmap : &p.kmap, &sm.full[s], hh * 64,
+                            r, pol);
+            }
+          }
+        }
+        __syncwarp();
+      }
+    }
+    if (lane == 0 && sm.abort) {   // let the copies in flight land before the CTA exits
+      for (int i = max(0, it - NS); i < it; ++i) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(&sm.full[i % NS], (i / NS) & 1))
+          if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && mbar_wait_bounded(bar, parity, &sm.abort, p.err);
+        if (ok) tc_fence_after();
+        return ok;
+      };
+      int k = 0;   // units issued
+      auto scores = [&](int cols) {
+        const int slot = (2 * k) % NS;
+        if (!wait(&sm.full[slot], ((2 * k) / NS) & 1) || !wait(&sm.s_empty[k & 1], ((k >> 1) & 1) ^ 1)) return;
+        const uint32_t a = smem_u32(smem + (size_t)slot * C::TILE), b = smem_u32(Qs), idesc = idesc_bf16_f32(128, cols);
+        for (int part = 0; part < q_parts; ++part)
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk)
+            umma_bf16(tmem + 64 * (k & 1), sdesc_sw128(a + (kk >> 2) * C::HALF + (kk & 3) * 32),
+                      sdesc_sw128(b + part * C::Q_PART + (kk >> 2) * C::Q_HALF + (kk & 3) * 32), idesc, part | kk ? 1u : 0u);
+        umma_commit(&sm.s_full[k & 1]);
+        umma_commit(&sm.empty[slot]);
+      };
+      // unit x: the seg'th segment's; keys: its slots
+      auto values = [&](int x, int seg, int cols, int keys, bool first, bool last) {
+        const int slot = (2 * x + 1) % NS;
+        if (first && !wait(&sm.o_empty[seg & 1], ((seg >> 1) & 1) ^ 1)) return;
+        if (!wait(&sm.p_full, x & 1) || !wait(&sm.full[slot], ((2 * x + 1) / NS) & 1)) return;
+        const uint32_t a = smem_u32(smem + (size_t)slot * C::TILE), b = smem_u32(Ps);
+        const uint32_t idesc = idesc_bf16_f32(128, cols) | (1u << 15) | (1u << 16);   // A and B MN-major
+        const int steps = (keys + 15) / 16;
+        for (int part = 0; part < p_parts; ++part)
+          for (int kk = 0; kk < steps; ++kk)
+            umma_bf16(tmem + 128 + 64 * (seg & 1), px_desc_mn(a + kk * 2048, C::HALF), px_desc_mn(b + part * C::P_PART + kk * 2048, C::P_PART),
+                      idesc, first && !(part | kk) ? 0u : 1u);
+        umma_commit(&sm.empty[slot]);
+        umma_commit(&sm.p_empty);
+        if (last) umma_commit(&sm.o_full[seg & 1]);
+      };
+      int seg = 0;
+      for (int g = g0; g < g1 && ok; ++seg) {
+        const PxSeg e = px_segment(p, sm.sched, sm.len, g, g1);
+        g += e.u1 - e.u0;
+        const int cols = (e.rows + 15) / 16 * 16;
+        auto keys = [&](int u) { return min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT); };
+        if (!wait(&sm.q_full, seg & 1)) break;
+        for (int u = e.u0; u < e.u1 && ok; ++u, ++k) {
+          scores(cols);
+          if (u + 1 == e.u1 && ok) umma_commit(&sm.q_empty);
+          if (u > e.u0 && ok) values(k - 1, seg, cols, keys(u - 1), u - 1 == e.u0, false);
+        }
+        if (ok) values(k - 1, seg, cols, keys(e.u1 - 1), e.u1 - 1 == e.u0, true);
+      }
+      if (sm.abort) {   // wait for issued MMAs before shared memory goes away
+        umma_commit(&sm.drain);
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(&sm.drain, 0))
+          if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
+      }
+    }
+  } else if (warp >= 4) {
+    // Every thread goes through every wait and barrier of the share, whatever the waits return: a
+    // wait that ran out has set the error bit, and the results are invalid.
+    const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = rsqrtf((float)HD) * 1.4426950408889634f;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      mbar_wait_bounded(bar, parity, &sm.abort, p.err);
+      __syncwarp();
+      tc_fence_after();
+    };
+    // the queries of a segment into shared memory, rows past its own as zeros
+    auto load_q = [&](const PxSeg& x, int seg) {
+      const int cols = (x.rows + 15) / 16 * 16;
+      if (seg > 0) wait(&sm.q_empty, (seg - 1) & 1);
+      if (st < cols && x.s >= 0) {
+        const int tr = (x.row0 + st) / G;   // token row
+        sm.seen[seg & 1][st] = (uint16_t)(st >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
+      }
+      for (int i = st; i < cols * (HD / 8); i += PX_SOFTMAX) {
+        const int r = i / (HD / 8), d = i % (HD / 8), hh = d >> 3;
+        uint8_t* dst = Qs + hh * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
+        uint4 w = make_uint4(0, 0, 0, 0), w1 = w;
+        if (r < x.rows) {
+          const int rr = x.row0 + r;
+          const long long at = (long long)(rr / G) * p.q_ld + (long long)(x.hk * G + rr % G) * HD + d * 8;
+          if (p.bf16) {
+            w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
+          } else {
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(p.q) + at);
+            w = __ldcg(src);
+            w1 = __ldcg(src + 1);
+          }
+        }
+        if (p.bf16) {
+          *reinterpret_cast<uint4*>(dst) = w;
+        } else {
+          float v[8] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w),
+                        __uint_as_float(w1.x), __uint_as_float(w1.y), __uint_as_float(w1.z), __uint_as_float(w1.w)};
+#pragma unroll
+          for (int part = 0; part < PX_PARTS; ++part) {
+            uint4 o;
+            o.x = px_part(v[0], v[1]);
+            o.y = px_part(v[2], v[3]);
+            o.z = px_part(v[4], v[5]);
+            o.w = px_part(v[6], v[7]);
+            *reinterpret_cast<uint4*>(dst + part * C::Q_PART) = o;
+          }
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&sm.q_full);
+    };
+    PxSeg x{};
+    if (g0 < g1) {
+      x = px_segment(p, sm.sched, sm.len, g0, g1);
+      load_q(x, 0);
+    }
+    int k = 0, seg = 0;
+    for (int g = g0; g < g1; ++seg) {
+      g += x.u1 - x.u0;
+      const int chunks = (x.rows + 15) / 16;   // of eight rows for each group
+      const int c0 = wg * 8 * chunks;          // this group's first row (of the tile)
+      float l[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) l[i] = 0.f;
+      named_bar_sync(3, PX_SOFTMAX);   // what the rows see is written
+      for (int u = x.u0; u < x.u1; ++u, ++k) {
+        const int slot = x.slot0 + u * PX_UNIT + e;
+        wait(&sm.s_full[k & 1], (k >> 1) & 1);
+        float s[32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i < chunks) px_ld8(tmem + lanes + 64 * (k & 1) + c0 + 8 * i, s + 8 * i);
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(&sm.s_empty[k & 1]);
+        // the slot is seen by every row (committed), by some (a block row's) or by none
+        const uint32_t ok = sm.pages_ok[k & 7];
+        const bool here = slot < x.end && ((ok >> (e >> 6)) & 1);
+        if (x.slot0 + (u + 1) * PX_UNIT > x.len || ok != 3u) {
+          const int i0 = slot - x.len;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (i < 8 * chunks) {
+              const bool sees = here && (i0 < 0 || ((sm.seen[seg & 1][c0 + i] >> i0) & 1u));
+              if (!sees) s[i] = -INFINITY;
+            }
+          }
+        }
+        // the largest score of each row over the group's 128 slots, into m (and the rescaling into f)
+        auto reference = [&](bool first) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < chunks) {
+              const float mx = px_across(s + 8 * i, lane, [](float a, float b) { return fmaxf(a, b); });
+              if (lane < 8) sm.red[wg][warp & 3][8 * i + lane] = mx;
+            }
+          named_bar_sync(1 + wg, 128);
+          if (e < 8 * chunks) {
+            const float top = fmaxf(fmaxf(sm.red[wg][0][e], sm.red[wg][1][e]), fmaxf(sm.red[wg][2][e], sm.red[wg][3][e])) * c;
+            const float old = first ? PX_UNSET : sm.m[wg][e], now = top == -INFINITY ? old : fmaxf(old, top);
+            sm.m[wg][e] = now;
+            sm.f[wg][e] = px_ex2(old - now);
+          }
+          named_bar_sync(1 + wg, 128);
+        };
+        if (u == x.u0) {
+          reference(true);
+        } else {
+          bool grown = false;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            if (i < 8 * chunks) {
+              const float4 m = *reinterpret_cast<const float4*>(&sm.m[wg][i]);
+              grown |= fmaf(s[i], c, -m.x) > PX_LAZY || fmaf(s[i + 1], c, -m.y) > PX_LAZY || fmaf(s[i + 2], c, -m.z) > PX_LAZY ||
+                       fmaf(s[i + 3], c, -m.w) > PX_LAZY;
+            }
+          if (px_bar_or(1 + wg, grown)) {
+            reference(false);
+            wait(&sm.p_empty, (k - 1) & 1);   // O holds the units before
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (i < chunks) {
+                const uint32_t at = tmem + lanes + 128 + 64 * (seg & 1) + c0 + 8 * i;
+                float o[8];
+                px_ld8(at, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int z = 0; z < 8; ++z) {
+                  const float f = sm.f[wg][8 * i + z];
+                  o[z] *= f;
+                  l[8 * i + z] *= f;
+                }
+                px_st8(at, o);
+              }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          }
+        }
+        if (k > 0) wait(&sm.p_empty, (k - 1) & 1);   // P of the unit before has been read
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i < chunks) {
+            float v[8];
+#pragma unroll
+            for (int z = 0; z < 8; z += 4) {
+              const float4 m = *reinterpret_cast<const float4*>(&sm.m[wg][8 * i + z]);
+              v[z] = px_ex2(fmaf(s[8 * i + z], c, -m.x));
+              v[z + 1] = px_ex2(fmaf(s[8 * i + z + 1], c, -m.y));
+              v[z + 2] = px_ex2(fmaf(s[8 * i + z + 2], c, -m.z));
+              v[z + 3] = px_ex2(fmaf(s[8 * i + z + 3], c, -m.w));
+            }
+#pragma unroll
+            for (int z = 0; z < 8; ++z) l[8 * i + z] += v[z];
+            uint8_t* dst = Ps + e * 128 + (((c0 / 8 + i) ^ (e & 7)) << 4);
+#pragma unroll
+            for (int part = 0; part < PX_PARTS; ++part) {
+              if (part < p_parts) {
+                uint4 o;
+                o.x = px_part(v[0], v[1]);
+                o.y = px_part(v[2], v[3]);
+                o.z = px_part(v[4], v[5]);
+                o.w = px_part(v[6], v[7]);
+                *reinterpret_cast<uint4*>(dst + part * C::P_PART) = o;
+              }
+            }
+          }
+        // a slot that no row sees may hold anything: its values as zeros (0 times anything finite)
+        if (wg == 0 && !here) {
+          const int vs = (2 * k + 1) % NS;
+          mbar_wait_bounded(&sm.full[vs], ((2 * k + 1) / NS) & 1, &sm.abort, p.err);
+          uint8_t* v = smem + (size_t)vs * C::TILE + e * 128;
+          for (int hh = 0; hh < C::HALVES; ++hh)
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(v + hh * C::HALF + i * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(&sm.p_full);
+      }
+      // ---- the segment's end: the next one's queries first, then this one's results
+      const PxSeg done = x;
+      if (g < g1) {
+        x = px_segment(p, sm.sched, sm.len, g, g1);
+        load_q(x, seg + 1);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < chunks) {
+          const float sum = px_across(l + 8 * i, lane, [](float a, float b) { return a + b; });
+          if (lane < 8) sm.red[wg][warp & 3][8 * i + lane] = sum;
+        }
+      named_bar_sync(1 + wg, 128);
+      // rows of an item from its first unit on, or the CTA's first segment, which continues one
+      const size_t row = done.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
+                                     : (size_t)(done.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)done.hk * R + done.row0;
+      if (e < 8 * chunks && c0 + e < done.rows)
+        scratch.ml[row + c0 + e] = make_float2(sm.m[wg][e], sm.red[wg][0][e] + sm.red[wg][1][e] + sm.red[wg][2][e] + sm.red[wg][3][e]);
+      wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < chunks) {
+          float o[8];
+          px_ld8(tmem + lanes + 128 + 64 * (seg & 1) + c0 + 8 * i, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int z = 0; z < 8; ++z)
+            if (c0 + 8 * i + z < done.rows && e < HD) scratch.o[(row + c0 + 8 * i + z) * HD + e] = o[z];
+        }
+      tc_fence_before();
+      mbar_arrive(&sm.o_empty[seg & 1]);
+      named_bar_sync(1 + wg, 128);   // (red and m have been read)
+    }
   }
-  a = L == 0.f ? 0.f : a / L;   // (a row that sees no slot: 0)
-  const long long at = r * p.out_ld + (long long)h * HD + threadIdx.x;
-  if (p.bf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(a);
-  else static_cast<float*>(p.out)[at] = a;
-  if (p.out_hi) {
-    const size_t x = (size_t)r * p.H * HD + h * HD + threadIdx.x;
-    const __nv_bfloat16 hi = __float2bfloat16_rn(a);
-    p.out_hi[x] = hi;
-    p.out_lo[x] = __float2bfloat16_rn(a - __bfloat162float(hi));
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 256);
   }
+}
+
+// A warp for each row and head: its partial results by weight.
+template <int HD>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant__ PrefixAttnParams p) {
+  constexpr int E = HD / 32;
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, w = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (w >= p.b * p.nq * p.H) return;
+  const int r = w / p.H, h = w - r * p.H;
+  const int G = p.H / p.Hk, R = p.b * p.nq * G, hk = h / G, rr = r * G + h % G, s = r / p.nq;
+  const PxScratch scratch(p);
+  const int shared = __ldcg(&scratch.sched->shared), up = __ldcg(&scratch.sched->up), tp = __ldcg(&scratch.sched->tp),
+            total = __ldcg(&scratch.sched->total), c_s = __ldcg(&scratch.sched->cum[s]), c_e = __ldcg(&scratch.sched->cum[s + 1]);
+  // the CTA that holds a unit
+  auto owner = [&](int g) {
+    int c = (int)((long long)g * min(total, p.ctas) / total);
+    while (px_begin(c + 1, total, p.ctas) <= g) ++c;
+    return c;
+  };
+  const size_t all = (size_t)p.b * p.nq * p.H, mine = (size_t)hk * R + rr;
+  int lo[2] = {0, 0}, n[2] = {0, 0}, at[2];   // of the shared pages, of the others: first CTA, CTAs, row of the tile
+  if (shared > 0) {
+    const PxTiles t(R);
+    const int first = (hk * t.n + rr / t.rows) * up;
+    lo[0] = owner(first);
+    n[0] = owner(first + up - 1) - lo[0] + 1;
+    at[0] = rr % t.rows;
+  }
+  {
+    const PxTiles t(p.nq * G);
+    const int x = rr - s * p.nq * G, U = (c_e - c_s) / (p.Hk * t.n), first = tp + c_s + (hk * t.n + x / t.rows) * U;
+    at[1] = x % t.rows;
+    if (U > 0) {
+      lo[1] = owner(first);
+      n[1] = owner(first + U - 1) - lo[1] + 1;
+    }
+  }
+  const int parts = n[0] + n[1];
+  auto row_of = [&](int i) {   // part i's row of the scratch
+    const int k = i >= n[0], c = i - (k ? n[0] : 0);
+    return c == 0 ? k * all + mine : 2 * all + (size_t)PX_ROWS * (lo[k] + c) + at[k];
+  };
+  float M = PX_UNSET, L = 0.f, o[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) o[i] = 0.f;
+  for (int i0 = 0; i0 < parts; i0 += 32) {
+    const float2 ml = i0 + lane < parts ? __ldcg(scratch.ml + row_of(i0 + lane)) : make_float2(PX_UNSET, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int a = 16; a > 0; a >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, a));
+    const float now = fmaxf(M, top), f = px_ex2(M - now), wt = ml.y == 0.f ? 0.f : px_ex2(ml.x - now);
+    float sum = wt * ml.y;
+#pragma unroll
+    for (int a = 16; a > 0; a >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, a);
+    M = now;
+    L = L * f + sum;
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] *= f;
+    const int m = min(32, parts - i0);
+#pragma unroll 4
+    for (int i = 0; i < m; ++i) {
+      const float* src = scratch.o + row_of(i0 + i) * HD + E * lane;
+      const float x = __shfl_sync(0xffffffffu, wt, i);
+      if (x == 0.f) continue;
+      if constexpr (E == 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+        o[0] += x * v.x, o[1] += x * v.y, o[2] += x * v.z, o[3] += x * v.w;
+      } else {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+        o[0] += x * v.x, o[1] += x * v.y;
+      }
+    }
+  }
+  const float inv = L == 0.f ? 0.f : 1.0f / L;   // (a row that sees no slot: 0)
+#pragma unroll
+  for (int i = 0; i < E; ++i) o[i] *= inv;
+  const long long out = r * p.out_ld + (long long)h * HD + E * lane;
+  const size_t op = (size_t)r * p.H * HD + (size_t)h * HD + E * lane;
+#pragma unroll
+  for (int i = 0; i < E; i += 2) {
+    float a = o[i], b = o[i + 1];
+    const uint32_t hi = px_part(a, b);
+    if (p.bf16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + out + i) = hi;
+    else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + out + i) = make_float2(o[i], o[i + 1]);
+    if (p.out_hi) {
+      *reinterpret_cast<uint32_t*>(p.out_hi + op + i) = hi;
+      *reinterpret_cast<uint32_t*>(p.out_lo + op + i) = px_part(a, b);
+    }
+  }
+}
+
+template <int HD>
+constexpr size_t px_smem() {
+  static_assert(PxCfg<HD>::OFF_MISC + sizeof(PxMisc) <= 232448, "shared memory of one CTA");
+  return PxCfg<HD>::OFF_MISC + sizeof(PxMisc);
+}
+
+template <int HD>
+cudaError_t px_launch(const PrefixAttnParams& p, cudaStream_t st, bool pdl) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.ctas);
+  cfg.blockDim = dim3(PX_THREADS);
+  cfg.dynamicSmemBytes = px_smem<HD>();
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_attention_kernel<HD>, p);
+  if (e != cudaSuccess) return e;
+  cfg.gridDim = dim3((p.b * p.nq * p.H + 7) / 8);
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<HD>, p);
 }
 
 }  // namespace
 
-size_t prefix_attention_scratch(int, int, int) { return 1; }
+// floats for row_heads rows of hd (twice as many of half the size)
+size_t prefix_attention_scratch(int row_heads, int hd, int num_sms) {
+  const size_t rows = (size_t)2 * row_heads + (size_t)PX_ROWS * num_sms;
+  return 256 + 2 * (2 * rows + 64) + rows * std::max(hd, 128);
+}
 
 cudaError_t prefix_attention_prepare() {
-  cudaError_t e = prefer_shared(prefix_attention_kernel<64>);
+  const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(prefix_attention_kernel<64>, a, (int)px_smem<64>());
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefix_attention_kernel<128>, a, (int)px_smem<128>());
+  if (e == cudaSuccess) e = prefer_shared(prefix_attention_kernel<64>);
   if (e == cudaSuccess) e = prefer_shared(prefix_attention_kernel<128>);
+  if (e == cudaSuccess) e = prefer_shared(prefix_merge_kernel<64>);
+  if (e == cudaSuccess) e = prefer_shared(prefix_merge_kernel<128>);
   return e;
 }
 
-cudaError_t launch_prefix_attention(const PrefixAttnParams& p, int, cudaStream_t st, bool pdl) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.b * p.nq * p.H);
-  cfg.blockDim = dim3(128);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = pdl ? 1 : 0;
-  const __nv_bfloat16 *k = static_cast<const __nv_bfloat16*>(p.k), *v = static_cast<const __nv_bfloat16*>(p.v);
-  return p.hd == 64 ? cudaLaunchKernelEx(&cfg, prefix_attention_kernel<64>, p, k, v)
-                    : cudaLaunchKernelEx(&cfg, prefix_attention_kernel<128>, p, k, v);
+cudaError_t launch_prefix_attention(const PrefixAttnParams& p0, int num_sms, cudaStream_t st, bool pdl) {
+  PrefixAttnParams p = p0;
+  p.ctas = num_sms;
+  return p.hd == 64 ? px_launch<64>(p, st, pdl) : px_launch<128>(p, st, pdl);
 }
 
 }  // namespace sdsat

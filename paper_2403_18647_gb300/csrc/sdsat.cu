@@ -421,8 +421,6 @@ sdsat_status forward(sdsat_ctx* c, sdsat_kv* kv, int seq0, int nb, int q, const 
       std::memset(&a, 0, sizeof(a));
       a.kmap = kv->kmap;
       a.vmap = kv->vmap;
-      a.k = kv->k;
-      a.v = kv->v;
       a.row0 = (int)(l * kv->layer_rows(H));
       a.q = c->qbuf;
       a.q_ld = a.out_ld = R;
@@ -1431,12 +1429,10 @@ sdsat_status sdsat_op_prefix_attention(sdsat_ctx* c, const void* q_dev, int64_t 
   if (q_ld < (long long)H * hd || out_ld < (long long)H * hd || q_ld % per16 || out_ld % per16) return SDSAT_EINVAL;
   if ((size_t)b * q * H * hd > (size_t)SDSAT_MAX_ROWS * c->cfg.n_heads * c->cfg.head_dim) return SDSAT_EINVAL;
   const long long rows = (long long)n_pages * Hk * KV_PAGE;
-  if (rows > 0x7FFFFFFFll) return SDSAT_EINVAL;
+  if (rows > 0x7FFFFFFFll || (long long)b * q * H * table_ld > 1ll << 30) return SDSAT_EINVAL;   // (units are counted in 32 bits)
   PrefixAttnParams a;
   std::memset(&a, 0, sizeof(a));
   if (!make_kvmap(&a.kmap, k_dev, rows, hd) || !make_kvmap(&a.vmap, v_dev, rows, hd)) return SDSAT_ECUDA;
-  a.k = k_dev;
-  a.v = v_dev;
   a.q = q_dev;
   a.q_ld = q_ld;
   a.out = out_dev;
