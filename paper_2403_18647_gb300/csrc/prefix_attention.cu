@@ -30,8 +30,15 @@
 // each row and unit would cost more than the exponentials.  Sums of exponentials stay in each
 // thread (a slot's) until the segment's end.
 //
-// Warp 0: TMA (pages by the table), warp 1: MMA issue and TMEM, warps 4-11: queries, softmax, results.
-// Shared memory: a ring of K and V tiles, P and Q in three parts.
+// The products of S take their three parts one after the other (N rows); those of O side by side in B
+// (N = three times the rows), so that the V tile is read once: an MMA of 128 x N x 16 costs 48 cycles
+// of shared-memory reads up to N = 64 and N / 2 cycles above, and 40 to issue.
+//
+// Warps: 0 TMA (pages by the table), 1 MMA issue (the whole warp, one lane's instructions: descriptors
+// stay in uniform registers; 100 cycles an MMA when a single thread ran the loop), 2 the segments,
+// ahead of their use, 4-11 softmax, 12-15 queries and results, so that a segment's queries are in place
+// before the one ahead of it ends and its results leave while the next one runs.
+// Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: two S and two O.
 #include <algorithm>
 
 #include "common.cuh"
@@ -43,8 +50,13 @@ namespace {
 constexpr int PX_UNIT = 128;      // slots of a unit: two pages
 constexpr int PX_ROWS = 64;       // rows of a tile
 constexpr int PX_PARTS = 3;       // bf16 parts of fp32 queries and of their probabilities
-constexpr int PX_THREADS = 384;
+constexpr int PX_THREADS = 512;
 constexpr int PX_SOFTMAX = 256;   // softmax threads, two groups of 128
+constexpr int PX_SEGS = 4;        // segments described ahead
+constexpr int PX_O = 128;         // TMEM column of O (S at 0 and 64)
+constexpr int PX_O_STEP = 160;    // to the second O, for segments of at most PX_O_ROWS rows
+constexpr int PX_O_ROWS = 48;
+constexpr int PX_Q_ROWS = 32;     // rows of segments whose queries fit twice
 constexpr int PX_MAX_B = 64;
 constexpr float PX_LAZY = 8.0f;   // log2 of the growth of a row maximum that is left unscaled
 constexpr float PX_UNSET = -1e30f;   // reference of a row that has seen no slot
@@ -60,6 +72,7 @@ struct PxCfg {
   static constexpr int P_PART = PX_UNIT * 128;              // 128 slots x 64 rows
   static constexpr int Q_HALF = PX_ROWS * 128;              // 64 rows x 64 dims
   static constexpr int Q_PART = HALVES * Q_HALF;
+  static constexpr int Q_HALF_SPACE = PX_Q_ROWS * 128;      // a second segment's queries: the other rows
   static constexpr size_t OFF_P = (size_t)SLOTS * TILE;     // (MN-major reads of 64-dim tiles run into it)
   static constexpr size_t OFF_Q = OFF_P + PX_PARTS * P_PART;
   static constexpr size_t OFF_MISC = OFF_Q + PX_PARTS * Q_PART;
@@ -71,17 +84,37 @@ struct PxSched {
   int up;                  // units of an item of the shared pages
   int tp;                  // units of all of them
   int total;
+  int q, r;                // units of a CTA's share; the first r CTAs have one more
   int cum[PX_MAX_B + 1];   // units of the items of the sequences before
+  __device__ int begin(int c) const { return c * q + min(c, r); }
+};
+__device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has unit g
+  const int x = g - (q + 1) * r;
+  return x < 0 ? g / (q + 1) : r + x / q;
+}
+
+// a run of units of one item
+struct PxSeg {
+  int s;                   // sequence, or -1: the shared pages
+  int hk, row0, rows;      // cache head, rows [row0, row0 + rows) of its R
+  int u0, u1;              // units; none: the share has ended
+  int slot0, end, len;     // unit u: slots slot0 + 128 u .., those below `end`; committed below len
+  int q_at, o_at;          // 0 or 1: which half of the queries' space, which O
+  int q_whole, o_whole;    // it takes the whole space, or the segment before does
+  __device__ int cols() const { return (rows + 15) / 16 * 16; }
 };
 struct PxMisc {
   PxSched sched;
   int len[PX_MAX_B];
-  float red[2][4][32];     // per group and warp: a row's maximum, or sum
-  __align__(16) float m[2][32];   // per group: the rows' references
-  float f[2][32];          // their rescaling
-  uint16_t seen[2][PX_ROWS];   // by segment parity: the block rows that a row sees
+  __align__(16) float red[2][4][32];   // per group and warp: a row's maximum, or sum
+  float m[2][32];          // per group: the rows' references
+  uint16_t seen[PX_SEGS][PX_ROWS];     // the block rows that a row sees
+  PxSeg seg[PX_SEGS];
   uint64_t full[8], empty[8];
-  uint64_t q_full, q_empty, s_full[2], s_empty[2], p_full, p_empty, o_full[2], o_empty[2], drain;
+  uint64_t seg_full[PX_SEGS], seg_empty[PX_SEGS];
+  // [2]: by segment or unit parity.  A phase of a barrier is waited for before the one after it can
+  // end: with one barrier for every segment the queries of two segments ahead would end two phases.
+  uint64_t q_full[2], q_empty[2], o_full[2], o_empty[2], s_full[2], s_empty[2], p_full, p_empty, drain;
   uint32_t tmem;
   volatile int abort;
   uint32_t pages_ok[8];    // by unit: its pages are in the pool (bits 0, 1)
@@ -97,22 +130,9 @@ struct PxTiles {
   }
 };
 
-// a run of units of one item
-struct PxSeg {
-  int s;                   // sequence, or -1: the shared pages
-  int hk, row0, rows;      // cache head, rows [row0, row0 + rows) of its R
-  int u0, u1;              // units
-  int slot0, end, len;     // unit u: slots slot0 + 128 u .., those below `end`; committed below len
-};
-
-// first unit of CTA c's share; with fewer units than CTAs the first `total` of them take one each
-__device__ __forceinline__ int px_begin(int c, int total, int ctas) {
-  const int n = min(total, ctas);
-  return c >= n ? total : (int)((long long)c * total / n);
-}
-
-// the segment that starts at unit g and ends at the item's end or at gend
-__device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int g, int gend) {
+// the segment that starts at unit g and ends at the item's end or at gend; `near`: no later sequence
+// than its own
+__device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int g, int gend, int& near) {
   const int G = p.H / p.Hk;
   PxSeg e;
   int U, rt;
@@ -130,19 +150,19 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
     e.end = e.len = sc.shared * KV_PAGE;
   } else {
     const PxTiles t(p.nq * G);
-    int x = g - sc.tp, s = 0;
-    while (sc.cum[s + 1] <= x) ++s;
-    x -= sc.cum[s];
-    U = (sc.cum[s + 1] - sc.cum[s]) / (p.Hk * t.n);
+    int x = g - sc.tp;
+    while (sc.cum[near + 1] <= x) ++near;
+    x -= sc.cum[near];
+    U = (sc.cum[near + 1] - sc.cum[near]) / (p.Hk * t.n);
     const int item = x / U;
     e.u0 = x - item * U;
     e.hk = item / t.n;
     rt = item - e.hk * t.n;
-    e.s = s;
-    e.row0 = s * p.nq * G + rt * t.rows;
+    e.s = near;
+    e.row0 = near * p.nq * G + rt * t.rows;
     e.rows = min(t.rows, p.nq * G - rt * t.rows);
     e.slot0 = sc.shared * KV_PAGE;
-    e.len = len[s];
+    e.len = len[near];
     e.end = min(e.len + p.nq, p.ld * KV_PAGE);
   }
   e.u1 = min(U, e.u0 + gend - g);
@@ -175,6 +195,25 @@ __device__ __forceinline__ uint64_t px_desc_mn(uint32_t saddr, uint32_t lead) {
   d |= static_cast<uint64_t>(1) << 46;
   d |= static_cast<uint64_t>(2) << 61;
   return d;
+}
+// one lane's MMA in a converged warp (mine: 1 in that lane)
+__device__ __forceinline__ void px_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t mine) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine)
+      : "memory");
+}
+__device__ __forceinline__ uint32_t px_elect() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r;
 }
 __device__ __forceinline__ float px_ex2(float x) {
   float y;
@@ -251,13 +290,17 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], 1);
     }
-    mbar_init(&sm.q_full, PX_SOFTMAX);
-    mbar_init(&sm.q_empty, 1);
+    for (int i = 0; i < PX_SEGS; ++i) {
+      mbar_init(&sm.seg_full[i], 1);
+      mbar_init(&sm.seg_empty[i], 2 + PX_SOFTMAX + 128);   // TMA, MMA, softmax, queries and results
+    }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.q_full[i], 128);
+      mbar_init(&sm.q_empty[i], 1);
+      mbar_init(&sm.o_full[i], 1);
+      mbar_init(&sm.o_empty[i], 128);
       mbar_init(&sm.s_full[i], 1);
       mbar_init(&sm.s_empty[i], PX_SOFTMAX);
-      mbar_init(&sm.o_full[i], 1);
-      mbar_init(&sm.o_empty[i], PX_SOFTMAX);
     }
     mbar_init(&sm.p_full, PX_SOFTMAX);
     mbar_init(&sm.p_empty, 1);
@@ -267,7 +310,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     tma_prefetch_desc(&p.kmap);
     tma_prefetch_desc(&p.vmap);
   }
-  if (warp == 1) tmem_alloc(&sm.tmem, 256);
+  if (warp == 1) tmem_alloc(&sm.tmem, 512);
   pdl_wait();   // q, lengths, tables and rows come from the kernels before
   pdl_trigger();
   if (warp == 2) {   // the schedule: two sequences a lane
@@ -298,25 +341,64 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       sm.sched.shared = shared;
       sm.sched.up = (shared + 1) / 2;
       sm.sched.tp = p.Hk * PxTiles(R).n * sm.sched.up;
-      sm.sched.total = sm.sched.tp + x;
+      const int total = sm.sched.tp + x;
+      sm.sched.total = total;
+      sm.sched.q = total / (int)gridDim.x;
+      sm.sched.r = total % (int)gridDim.x;
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sm.tmem;   // S at columns 0 and 64, O at 128 and 192
+  const uint32_t tmem = sm.tmem;
   const PxScratch scratch(p);
   if (blockIdx.x == 0 && tid < (int)(sizeof(PxSched) / 4)) reinterpret_cast<int*>(scratch.sched)[tid] = reinterpret_cast<int*>(&sm.sched)[tid];
-  const int g0 = px_begin(blockIdx.x, sm.sched.total, gridDim.x), g1 = px_begin(blockIdx.x + 1, sm.sched.total, gridDim.x);
   const int q_parts = p.bf16 ? 1 : PX_PARTS, p_parts = p.bf16 ? 2 : PX_PARTS;
+  // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
+  // return: one that ran out has set the error bit, and the results are invalid.
+  auto wait = [&](uint64_t* bar, uint32_t parity) { mbar_wait_bounded(bar, parity, &sm.abort, p.err); };
+  // the i-th segment's description (by all threads of a warp)
+  auto segment = [&](int i) {
+    wait(&sm.seg_full[i % PX_SEGS], (i / PX_SEGS) & 1);
+    return sm.seg[i % PX_SEGS];
+  };
 
-  if (warp == 0) {
+  // where a segment's results go: the rows of an item from its first unit on, or those of the CTA's
+  // first segment, which continues one
+  auto scratch_row = [&](const PxSeg& x) {
+    return x.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
+                    : (size_t)(x.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)x.hk * R + x.row0;
+  };
+
+  if (warp == 2) {
+    // ---- the segments
+    if (lane == 0) {
+      const int g1 = sm.sched.begin(blockIdx.x + 1);
+      int near = 0, rows = 0;
+      for (int i = 0, g = sm.sched.begin(blockIdx.x);; ++i) {
+        PxSeg e{};
+        if (g < g1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
+        g += e.u1 - e.u0;
+        e.q_at = e.rows <= PX_Q_ROWS ? i & 1 : 0;
+        e.o_at = e.rows <= PX_O_ROWS ? i & 1 : 0;
+        e.q_whole = max(rows, e.rows) > PX_Q_ROWS;
+        e.o_whole = max(rows, e.rows) > PX_O_ROWS;
+        rows = e.rows;
+        wait(&sm.seg_empty[i % PX_SEGS], ((i / PX_SEGS) & 1) ^ 1);
+        sm.seg[i % PX_SEGS] = e;
+        mbar_arrive(&sm.seg_full[i % PX_SEGS]);
+        if (e.u0 == e.u1) break;
+      }
+    }
+  } else if (warp == 0) {
     // ---- K and V tiles: K of unit 0, V of unit 0, K of unit 1, ...
     const uint64_t pol = l2_policy_evict_normal();
     int it = 0;
-    for (int g = g0; g < g1 && !sm.abort;) {
-      const PxSeg e = px_segment(p, sm.sched, sm.len, g, g1);
-      g += e.u1 - e.u0;
+    for (int seg = 0;; ++seg) {
+      const PxSeg e = segment(seg);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      if (e.u0 == e.u1) break;
       const int* row = p.table + (size_t)max(e.s, 0) * p.ld;
       const int j0 = e.slot0 / KV_PAGE + 2 * e.u0, j1 = min((e.end + KV_PAGE - 1) / KV_PAGE, e.slot0 / KV_PAGE + 2 * e.u1);
       int entry = 0;
@@ -330,7 +412,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             if (page[i] >= 0 && page[i] < p.n_pages) ok |= 1u << i;
             else if (lane == 0) set_error(p.err, ERR_PAGE);
           }
-        if (lane == 0) {
+        if (lane == 0 && !sm.abort) {
           for (int kv = 0; kv < 2; ++kv, ++it) {
             const int s = it % NS;
             if (!mbar_wait_bounded(&sm.empty[s], ((it / NS) & 1) ^ 1, &sm.abort, p.err)) break;
@@ -357,89 +439,100 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      bool ok = true;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && mbar_wait_bounded(bar, parity, &sm.abort, p.err);
-        if (ok) tc_fence_after();
-        return ok;
-      };
-      int k = 0;   // units issued
-      auto scores = [&](int cols) {
-        const int slot = (2 * k) % NS;
-        if (!wait(&sm.full[slot], ((2 * k) / NS) & 1) || !wait(&sm.s_empty[k & 1], ((k >> 1) & 1) ^ 1)) return;
-        const uint32_t a = smem_u32(smem + (size_t)slot * C::TILE), b = smem_u32(Qs), idesc = idesc_bf16_f32(128, cols);
-        for (int part = 0; part < q_parts; ++part)
+    // ---- products; nothing is issued any more once a wait has run out
+    const uint32_t mine = px_elect();
+    auto ready = [&](uint64_t* bar, uint32_t parity) {
+      wait(bar, parity);
+      __syncwarp();
+      tc_fence_after();
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (mine) umma_commit(bar);
+      __syncwarp();
+    };
+    const uint64_t kd = sdesc_sw128(smem_u32(smem)), qd = sdesc_sw128(smem_u32(Qs));
+    const uint64_t vd = px_desc_mn(smem_u32(smem), C::HALF), pd = px_desc_mn(smem_u32(Ps), C::P_PART);
+    int k = 0;   // units whose scores were issued
+    auto scores = [&](const PxSeg& e) {
+      const int slot = (2 * k) % NS;
+      ready(&sm.full[slot], ((2 * k) / NS) & 1);
+      ready(&sm.s_empty[k & 1], ((k >> 1) & 1) ^ 1);
+      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, e.cols());
+      const uint64_t a = kd + (uint64_t)(slot * (C::TILE >> 4)), b = qd + (uint64_t)(e.q_at * (C::Q_HALF_SPACE >> 4));
+      for (int part = 0; part < q_parts; ++part)
 #pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk)
-            umma_bf16(tmem + 64 * (k & 1), sdesc_sw128(a + (kk >> 2) * C::HALF + (kk & 3) * 32),
-                      sdesc_sw128(b + part * C::Q_PART + (kk >> 2) * C::Q_HALF + (kk & 3) * 32), idesc, part | kk ? 1u : 0u);
-        umma_commit(&sm.s_full[k & 1]);
-        umma_commit(&sm.empty[slot]);
-      };
-      // unit x: the seg'th segment's; keys: its slots
-      auto values = [&](int x, int seg, int cols, int keys, bool first, bool last) {
-        const int slot = (2 * x + 1) % NS;
-        if (first && !wait(&sm.o_empty[seg & 1], ((seg >> 1) & 1) ^ 1)) return;
-        if (!wait(&sm.p_full, x & 1) || !wait(&sm.full[slot], ((2 * x + 1) / NS) & 1)) return;
-        const uint32_t a = smem_u32(smem + (size_t)slot * C::TILE), b = smem_u32(Ps);
-        const uint32_t idesc = idesc_bf16_f32(128, cols) | (1u << 15) | (1u << 16);   // A and B MN-major
-        const int steps = (keys + 15) / 16;
-        for (int part = 0; part < p_parts; ++part)
-          for (int kk = 0; kk < steps; ++kk)
-            umma_bf16(tmem + 128 + 64 * (seg & 1), px_desc_mn(a + kk * 2048, C::HALF), px_desc_mn(b + part * C::P_PART + kk * 2048, C::P_PART),
-                      idesc, first && !(part | kk) ? 0u : 1u);
-        umma_commit(&sm.empty[slot]);
-        umma_commit(&sm.p_empty);
-        if (last) umma_commit(&sm.o_full[seg & 1]);
-      };
-      int seg = 0;
-      for (int g = g0; g < g1 && ok; ++seg) {
-        const PxSeg e = px_segment(p, sm.sched, sm.len, g, g1);
-        g += e.u1 - e.u0;
-        const int cols = (e.rows + 15) / 16 * 16;
-        auto keys = [&](int u) { return min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT); };
-        if (!wait(&sm.q_full, seg & 1)) break;
-        for (int u = e.u0; u < e.u1 && ok; ++u, ++k) {
-          scores(cols);
-          if (u + 1 == e.u1 && ok) umma_commit(&sm.q_empty);
-          if (u > e.u0 && ok) values(k - 1, seg, cols, keys(u - 1), u - 1 == e.u0, false);
-        }
-        if (ok) values(k - 1, seg, cols, keys(e.u1 - 1), e.u1 - 1 == e.u0, true);
+        for (int kk = 0; kk < HD / 16; ++kk)
+          px_mma(tmem + 64 * (k & 1), a + ((kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2),
+                 b + (uint64_t)(part * (C::Q_PART >> 4)) + ((kk >> 2) * (C::Q_HALF >> 4) + (kk & 3) * 2), idesc,
+                 part | kk ? 1u : 0u, on);
+      commit(&sm.s_full[k & 1]);
+      commit(&sm.empty[slot]);
+      ++k;
+    };
+    // unit x, the u-th of the seg'th segment
+    auto values = [&](int x, const PxSeg& e, int seg, int u) {
+      const int slot = (2 * x + 1) % NS;
+      if (u == e.u0) {   // O: the last or the last but one segment's results have left
+        const int before = seg - (e.o_whole ? 1 : 2);
+        if (before >= 0) ready(&sm.o_empty[before & 1], (before >> 1) & 1);
       }
-      if (sm.abort) {   // wait for issued MMAs before shared memory goes away
-        umma_commit(&sm.drain);
+      ready(&sm.p_full, x & 1);
+      ready(&sm.full[slot], ((2 * x + 1) / NS) & 1);
+      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, p_parts * e.cols()) | (1u << 15) | (1u << 16);   // both MN-major
+      const uint64_t a = vd + (uint64_t)(slot * (C::TILE >> 4));
+      const int steps = (min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT) + 15) / 16;   // 16 slots each
+#pragma unroll
+      for (int kk = 0; kk < PX_UNIT / 16; ++kk)
+        if (kk < steps) px_mma(tmem + PX_O + PX_O_STEP * e.o_at, a + kk * 128, pd + kk * 128, idesc, u > e.u0 || kk ? 1u : 0u, on);
+      commit(&sm.empty[slot]);
+      commit(&sm.p_empty);
+      if (u + 1 == e.u1) commit(&sm.o_full[seg & 1]);
+    };
+    for (int seg = 0;; ++seg) {
+      const PxSeg e = segment(seg);
+      if (e.u0 == e.u1) break;
+      ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
+      for (int u = e.u0; u < e.u1; ++u) {
+        scores(e);
+        if (u + 1 == e.u1) commit(&sm.q_empty[seg & 1]);
+        if (u > e.u0) values(k - 2, e, seg, u - 1);
+      }
+      values(k - 1, e, seg, e.u1 - 1);
+      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+    }
+    if (sm.abort) {   // wait for issued MMAs before shared memory goes away
+      commit(&sm.drain);
+      if (lane == 0) {
         const uint64_t t0 = globaltimer_ns();
         while (!mbar_try_wait(&sm.drain, 0))
           if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
       }
     }
-  } else if (warp >= 4) {
-    // Every thread goes through every wait and barrier of the share, whatever the waits return: a
-    // wait that ran out has set the error bit, and the results are invalid.
-    const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
+  } else if (warp >= 12) {
+    // ---- queries in and results out: queries of segments 0 and 1, results of 0, queries of 2, ...
+    const int st = tid - 384;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const float c = rsqrtf((float)HD) * 1.4426950408889634f;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      mbar_wait_bounded(bar, parity, &sm.abort, p.err);
-      __syncwarp();
-      tc_fence_after();
-    };
-    // the queries of a segment into shared memory, rows past its own as zeros
-    auto load_q = [&](const PxSeg& x, int seg) {
-      const int cols = (x.rows + 15) / 16 * 16;
-      if (seg > 0) wait(&sm.q_empty, (seg - 1) & 1);
+    auto load_q = [&](int seg) {
+      const PxSeg x = segment(seg);
+      if (x.u0 == x.u1) return;
+      const int cols = x.cols();
+      // its space is free once the scores of the segment before (or of the one before that) are done
+      const int before = seg - (x.q_whole ? 1 : 2);
+      if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
       if (st < cols && x.s >= 0) {
         const int tr = (x.row0 + st) / G;   // token row
-        sm.seen[seg & 1][st] = (uint16_t)(st >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
+        sm.seen[seg % PX_SEGS][st] =
+            (uint16_t)(st >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
       }
-      for (int i = st; i < cols * (HD / 8); i += PX_SOFTMAX) {
+      uint8_t* base = Qs + x.q_at * C::Q_HALF_SPACE;
+#pragma unroll 2
+      for (int i = st; i < cols * (HD / 8); i += 128) {
         const int r = i / (HD / 8), d = i % (HD / 8), hh = d >> 3;
-        uint8_t* dst = Qs + hh * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
+        uint8_t* dst = base + hh * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
         uint4 w = make_uint4(0, 0, 0, 0), w1 = w;
         if (r < x.rows) {
-          const int rr = x.row0 + r;
-          const long long at = (long long)(rr / G) * p.q_ld + (long long)(x.hk * G + rr % G) * HD + d * 8;
+          const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
+          const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
           if (p.bf16) {
             w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
           } else {
@@ -465,25 +558,63 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         }
       }
       fence_proxy_async_smem();
-      mbar_arrive(&sm.q_full);
+      mbar_arrive(&sm.q_full[seg & 1]);
     };
-    PxSeg x{};
-    if (g0 < g1) {
-      x = px_segment(p, sm.sched, sm.len, g0, g1);
-      load_q(x, 0);
+    load_q(0);
+    bool more = sm.seg[0].u0 < sm.seg[0].u1;   // (described: load_q has waited for it)
+    if (more) load_q(1);
+    for (int seg = 0; more; ++seg) {
+      const PxSeg x = segment(seg);
+      const int cols = x.cols();
+      const size_t row = scratch_row(x);
+      wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
+      __syncwarp();
+      tc_fence_after();
+      for (int r = 0; r < x.rows; r += 8) {
+        float o[8], o1[8], o2[8];
+        const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + r;
+        px_ld8(at, o);
+        px_ld8(at + cols, o1);
+        if (p_parts > 2) px_ld8(at + 2 * cols, o2);
+        tmem_wait_ld();
+        float* dst = scratch.o + (row + r) * HD + st;
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+          o[z] += o1[z];
+          if (p_parts > 2) o[z] += o2[z];
+          if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(&sm.o_empty[seg & 1]);
+      mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      const PxSeg next = segment(seg + 1);
+      more = next.u0 < next.u1;
+      if (more) load_q(seg + 2);
     }
-    int k = 0, seg = 0;
-    for (int g = g0; g < g1; ++seg) {
-      g += x.u1 - x.u0;
-      const int chunks = (x.rows + 15) / 16;   // of eight rows for each group
-      const int c0 = wg * 8 * chunks;          // this group's first row (of the tile)
+  } else if (warp >= 4) {
+    const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = rsqrtf((float)HD) * 1.4426950408889634f;
+    auto ready = [&](uint64_t* bar, uint32_t parity) {
+      wait(bar, parity);
+      __syncwarp();
+      tc_fence_after();
+    };
+    int k = 0;
+    for (int seg = 0;; ++seg) {
+      const PxSeg x = segment(seg);
+      if (x.u0 == x.u1) break;
+      const int cols = x.cols(), chunks = cols / 16;   // of eight rows for each group
+      const int c0 = wg * 8 * chunks;                  // this group's first row (of the tile)
+      const uint16_t* seen = sm.seen[seg % PX_SEGS] + c0;
       float l[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) l[i] = 0.f;
-      named_bar_sync(3, PX_SOFTMAX);   // what the rows see is written
+      wait(&sm.q_full[seg & 1], (seg >> 1) & 1);   // (what the rows see is written)
       for (int u = x.u0; u < x.u1; ++u, ++k) {
         const int slot = x.slot0 + u * PX_UNIT + e;
-        wait(&sm.s_full[k & 1], (k >> 1) & 1);
+        ready(&sm.s_full[k & 1], (k >> 1) & 1);
         float s[32];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -499,12 +630,12 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             if (i < 8 * chunks) {
-              const bool sees = here && (i0 < 0 || ((sm.seen[seg & 1][c0 + i] >> i0) & 1u));
+              const bool sees = here && (i0 < 0 || ((seen[i] >> i0) & 1u));
               if (!sees) s[i] = -INFINITY;
             }
           }
         }
-        // the largest score of each row over the group's 128 slots, into m (and the rescaling into f)
+        // the largest score of each row over the group's 128 slots, into m (and the rescaling into red[.][0])
         auto reference = [&](bool first) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -517,43 +648,44 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             const float top = fmaxf(fmaxf(sm.red[wg][0][e], sm.red[wg][1][e]), fmaxf(sm.red[wg][2][e], sm.red[wg][3][e])) * c;
             const float old = first ? PX_UNSET : sm.m[wg][e], now = top == -INFINITY ? old : fmaxf(old, top);
             sm.m[wg][e] = now;
-            sm.f[wg][e] = px_ex2(old - now);
+            sm.red[wg][0][e] = px_ex2(old - now);
           }
           named_bar_sync(1 + wg, 128);
         };
         if (u == x.u0) {
           reference(true);
         } else {
-          bool grown = false;
+          float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
             if (i < 8 * chunks) {
               const float4 m = *reinterpret_cast<const float4*>(&sm.m[wg][i]);
-              grown |= fmaf(s[i], c, -m.x) > PX_LAZY || fmaf(s[i + 1], c, -m.y) > PX_LAZY || fmaf(s[i + 2], c, -m.z) > PX_LAZY ||
-                       fmaf(s[i + 3], c, -m.w) > PX_LAZY;
+              top = fmaxf(fmaxf(top, fmaf(s[i], c, -m.x)), fmaf(s[i + 1], c, -m.y));
+              top = fmaxf(fmaxf(top, fmaf(s[i + 2], c, -m.z)), fmaf(s[i + 3], c, -m.w));
             }
-          if (px_bar_or(1 + wg, grown)) {
+          if (px_bar_or(1 + wg, top > PX_LAZY)) {
             reference(false);
-            wait(&sm.p_empty, (k - 1) & 1);   // O holds the units before
+            ready(&sm.p_empty, (k - 1) & 1);   // O holds the units before
+            for (int part = 0; part < p_parts; ++part)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (i < chunks) {
-                const uint32_t at = tmem + lanes + 128 + 64 * (seg & 1) + c0 + 8 * i;
-                float o[8];
-                px_ld8(at, o);
-                tmem_wait_ld();
+              for (int i = 0; i < 4; ++i)
+                if (i < chunks) {
+                  const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + part * cols + c0 + 8 * i;
+                  float o[8];
+                  px_ld8(at, o);
+                  tmem_wait_ld();
 #pragma unroll
-                for (int z = 0; z < 8; ++z) {
-                  const float f = sm.f[wg][8 * i + z];
-                  o[z] *= f;
-                  l[8 * i + z] *= f;
+                  for (int z = 0; z < 8; ++z) o[z] *= sm.red[wg][0][8 * i + z];
+                  px_st8(at, o);
                 }
-                px_st8(at, o);
-              }
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i < 8 * chunks) l[i] *= sm.red[wg][0][i];
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            named_bar_sync(1 + wg, 128);   // (red has been read)
           }
         }
-        if (k > 0) wait(&sm.p_empty, (k - 1) & 1);   // P of the unit before has been read
+        if (k > 0) ready(&sm.p_empty, (k - 1) & 1);   // P of the unit before has been read
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (i < chunks) {
@@ -568,23 +700,23 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             }
 #pragma unroll
             for (int z = 0; z < 8; ++z) l[8 * i + z] += v[z];
-            uint8_t* dst = Ps + e * 128 + (((c0 / 8 + i) ^ (e & 7)) << 4);
 #pragma unroll
             for (int part = 0; part < PX_PARTS; ++part) {
-              if (part < p_parts) {
+              if (part < p_parts) {   // B's columns: the parts side by side
+                const int ch = (part * cols + c0) / 8 + i;
                 uint4 o;
                 o.x = px_part(v[0], v[1]);
                 o.y = px_part(v[2], v[3]);
                 o.z = px_part(v[4], v[5]);
                 o.w = px_part(v[6], v[7]);
-                *reinterpret_cast<uint4*>(dst + part * C::P_PART) = o;
+                *reinterpret_cast<uint4*>(Ps + (ch >> 3) * C::P_PART + e * 128 + (((ch & 7) ^ (e & 7)) << 4)) = o;
               }
             }
           }
         // a slot that no row sees may hold anything: its values as zeros (0 times anything finite)
         if (wg == 0 && !here) {
           const int vs = (2 * k + 1) % NS;
-          mbar_wait_bounded(&sm.full[vs], ((2 * k + 1) / NS) & 1, &sm.abort, p.err);
+          wait(&sm.full[vs], ((2 * k + 1) / NS) & 1);
           uint8_t* v = smem + (size_t)vs * C::TILE + e * 128;
           for (int hh = 0; hh < C::HALVES; ++hh)
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(v + hh * C::HALF + i * 16) = make_uint4(0, 0, 0, 0);
@@ -594,12 +726,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         tc_fence_before();
         mbar_arrive(&sm.p_full);
       }
-      // ---- the segment's end: the next one's queries first, then this one's results
-      const PxSeg done = x;
-      if (g < g1) {
-        x = px_segment(p, sm.sched, sm.len, g, g1);
-        load_q(x, seg + 1);
-      }
+      // ---- the rows' references and sums for the results
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (i < chunks) {
@@ -607,24 +734,10 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           if (lane < 8) sm.red[wg][warp & 3][8 * i + lane] = sum;
         }
       named_bar_sync(1 + wg, 128);
-      // rows of an item from its first unit on, or the CTA's first segment, which continues one
-      const size_t row = done.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
-                                     : (size_t)(done.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)done.hk * R + done.row0;
-      if (e < 8 * chunks && c0 + e < done.rows)
-        scratch.ml[row + c0 + e] = make_float2(sm.m[wg][e], sm.red[wg][0][e] + sm.red[wg][1][e] + sm.red[wg][2][e] + sm.red[wg][3][e]);
-      wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < chunks) {
-          float o[8];
-          px_ld8(tmem + lanes + 128 + 64 * (seg & 1) + c0 + 8 * i, o);
-          tmem_wait_ld();
-#pragma unroll
-          for (int z = 0; z < 8; ++z)
-            if (c0 + 8 * i + z < done.rows && e < HD) scratch.o[(row + c0 + 8 * i + z) * HD + e] = o[z];
-        }
-      tc_fence_before();
-      mbar_arrive(&sm.o_empty[seg & 1]);
+      if (e < 8 * chunks && c0 + e < x.rows)
+        scratch.ml[scratch_row(x) + c0 + e] =
+            make_float2(sm.m[wg][e], (sm.red[wg][0][e] + sm.red[wg][1][e]) + (sm.red[wg][2][e] + sm.red[wg][3][e]));
+      mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
       named_bar_sync(1 + wg, 128);   // (red and m have been read)
     }
   }
@@ -632,7 +745,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, 256);
+    tmem_dealloc(tmem, 512);
   }
 }
 
@@ -648,13 +761,9 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
   const int G = p.H / p.Hk, R = p.b * p.nq * G, hk = h / G, rr = r * G + h % G, s = r / p.nq;
   const PxScratch scratch(p);
   const int shared = __ldcg(&scratch.sched->shared), up = __ldcg(&scratch.sched->up), tp = __ldcg(&scratch.sched->tp),
-            total = __ldcg(&scratch.sched->total), c_s = __ldcg(&scratch.sched->cum[s]), c_e = __ldcg(&scratch.sched->cum[s + 1]);
-  // the CTA that holds a unit
-  auto owner = [&](int g) {
-    int c = (int)((long long)g * min(total, p.ctas) / total);
-    while (px_begin(c + 1, total, p.ctas) <= g) ++c;
-    return c;
-  };
+            q = __ldcg(&scratch.sched->q), rest = __ldcg(&scratch.sched->r), c_s = __ldcg(&scratch.sched->cum[s]),
+            c_e = __ldcg(&scratch.sched->cum[s + 1]);
+  auto owner = [&](int g) { return px_owner(g, q, rest); };
   const size_t all = (size_t)p.b * p.nq * p.H, mine = (size_t)hk * R + rr;
   int lo[2] = {0, 0}, n[2] = {0, 0}, at[2];   // of the shared pages, of the others: first CTA, CTAs, row of the tile
   if (shared > 0) {
