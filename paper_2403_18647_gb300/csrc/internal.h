@@ -349,6 +349,9 @@ cudaError_t launch_pages_rows(const PagesParams& p, int layer, int slot0, void* 
                               bool pdl);
 
 // Block-causal attention of sequences that share their leading pages (prefix_attention.cu)
+struct PxTiles {
+  int n, rows;              // tiles of `rows` rows (the last one may have fewer)
+};
 struct PrefixAttnParams {
   CUtensorMap kmap, vmap;   // pages as a 2-D tensor [rows][hd] bf16, boxes of 64 dims x KV_PAGE rows
   int row0;                 // row of (page, head, slot) = row0 + (page * Hk + head) * KV_PAGE + slot
@@ -364,7 +367,8 @@ struct PrefixAttnParams {
   void* out;                // [b*q][out_ld], the type of q
   __nv_bfloat16 *out_hi, *out_lo;   // [b*q][H*hd], or null: the O projection's operand
   float* part;              // scratch: prefix_attention_scratch() floats, 1024-byte aligned
-  int ctas;                 // set by launch_prefix_attention
+  int ctas;                 // set by launch_prefix_attention, as the next two
+  PxTiles tiles[2];         // of a cache head's rows: of the batch, of a sequence
   uint32_t* err;
 };
 size_t prefix_attention_scratch(int row_heads, int hd, int num_sms);

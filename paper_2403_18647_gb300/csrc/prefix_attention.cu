@@ -19,7 +19,7 @@
 // Per unit, on tcgen05 in the form that puts the slots on the 128 lanes (the rows, often few, are
 // the N of the products, so they do not pad to 128):
 //   S^T = K Q^T     A = the K tile, B = Q (shared memory, K-major)            128 slots x N rows
-//   P^T = exp2(c S^T - m)  one thread for a slot (two groups of 128 threads share the rows)
+//   P^T = exp2(c S^T - m)  one thread for a slot (four groups of 128 threads share the rows)
 //   O^T += V^T P^T  A = the V tile read MN-major, B = P (shared memory, MN-major)   hd x N rows
 // K and V are the cache's bf16 values.  fp32 queries and the probabilities enter as three bf16 parts
 // (24 bits: nothing is lost against fp32 products; one part for bf16 queries, whose probabilities
@@ -30,15 +30,17 @@
 // each row and unit would cost more than the exponentials.  Sums of exponentials stay in each
 // thread (a slot's) until the segment's end.
 //
-// The products of S take their three parts one after the other (N rows); those of O side by side in B
-// (N = three times the rows), so that the V tile is read once: an MMA of 128 x N x 16 costs 48 cycles
-// of shared-memory reads up to N = 64 and N / 2 cycles above, and 40 to issue.
+// The three parts are side by side in B (N = three times the rows) and their products in columns of
+// their own, added up when they are read: 8 MMAs a tile of K or V instead of 24.  An MMA takes N / 2
+// cycles from N = 96 on and 50 below, and 40 to issue from a warp by itself, 100 from one that shares
+// its scheduler with the softmax (64 rows: 2300 cycles for 24 of N = 64, 4000 a unit in all).
 //
 // Warps: 0 TMA (pages by the table), 1 MMA issue (the whole warp, one lane's instructions: descriptors
 // stay in uniform registers; 100 cycles an MMA when a single thread ran the loop), 2 the segments,
-// ahead of their use, 4-11 softmax, 12-15 queries and results, so that a segment's queries are in place
+// ahead of their use, 4-19 softmax (the code of a row is unrolled: with 32 rows a thread on 8 warps
+// the instructions no longer came in time, 5000 cycles a unit), 20-23 queries and results, so that a segment's queries are in place
 // before the one ahead of it ends and its results leave while the next one runs.
-// Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: two S and two O.
+// Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: S and two O.
 #include <algorithm>
 
 #include "common.cuh"
@@ -50,10 +52,13 @@ namespace {
 constexpr int PX_UNIT = 128;      // slots of a unit: two pages
 constexpr int PX_ROWS = 64;       // rows of a tile
 constexpr int PX_PARTS = 3;       // bf16 parts of fp32 queries and of their probabilities
-constexpr int PX_THREADS = 512;
-constexpr int PX_SOFTMAX = 256;   // softmax threads, two groups of 128
+constexpr int PX_GROUPS = 4;      // softmax groups of 128 threads
+constexpr int PX_SOFTMAX = 128 * PX_GROUPS;
+constexpr int PX_SOFTMAX_WARPS = PX_SOFTMAX / 32;
+constexpr int PX_THREADS = 128 + PX_SOFTMAX + 128;
+constexpr int PX_MINE = PX_ROWS / 8 / PX_GROUPS;   // pieces of eight rows of a thread
 constexpr int PX_SEGS = 4;        // segments described ahead
-constexpr int PX_O = 128;         // TMEM column of O (S at 0 and 64)
+constexpr int PX_O = PX_PARTS * PX_ROWS;   // TMEM column of O (S from 0 on)
 constexpr int PX_O_STEP = 160;    // to the second O, for segments of at most PX_O_ROWS rows
 constexpr int PX_O_ROWS = 48;
 constexpr int PX_Q_ROWS = 32;     // rows of segments whose queries fit twice
@@ -70,12 +75,11 @@ struct PxCfg {
   static constexpr int TILE = HALVES * HALF;                // K or V of a unit
   static constexpr int SLOTS = HD == 128 ? 4 : 8;           // of the ring
   static constexpr int P_PART = PX_UNIT * 128;              // 128 slots x 64 rows
-  static constexpr int Q_HALF = PX_ROWS * 128;              // 64 rows x 64 dims
-  static constexpr int Q_PART = HALVES * Q_HALF;
-  static constexpr int Q_HALF_SPACE = PX_Q_ROWS * 128;      // a second segment's queries: the other rows
+  static constexpr int Q_HALF = PX_PARTS * PX_ROWS * 128;   // 3 x 64 rows x 64 dims
+  static constexpr int Q_SECOND = PX_PARTS * PX_Q_ROWS * 128;   // where a second segment's queries start
   static constexpr size_t OFF_P = (size_t)SLOTS * TILE;     // (MN-major reads of 64-dim tiles run into it)
   static constexpr size_t OFF_Q = OFF_P + PX_PARTS * P_PART;
-  static constexpr size_t OFF_MISC = OFF_Q + PX_PARTS * Q_PART;
+  static constexpr size_t OFF_MISC = OFF_Q + HALVES * Q_HALF;
 };
 
 // what the CTAs agree on; the first one leaves it for the merge
@@ -106,28 +110,18 @@ struct PxSeg {
 struct PxMisc {
   PxSched sched;
   int len[PX_MAX_B];
-  __align__(16) float red[2][4][32];   // per group and warp: a row's maximum, or sum
-  float m[2][32];          // per group: the rows' references
-  uint16_t seen[PX_SEGS][PX_ROWS];     // the block rows that a row sees
+  __align__(16) float red[4][PX_ROWS];   // per warp of a group: a row's maximum, or sum
+  float m[PX_ROWS];        // the rows' references
+  __align__(16) uint16_t seen[PX_SEGS][PX_ROWS];     // the block rows that a row sees
   PxSeg seg[PX_SEGS];
   uint64_t full[8], empty[8];
   uint64_t seg_full[PX_SEGS], seg_empty[PX_SEGS];
-  // [2]: by segment or unit parity.  A phase of a barrier is waited for before the one after it can
+  // [2]: by segment parity.  A phase of a barrier is waited for before the one after it can
   // end: with one barrier for every segment the queries of two segments ahead would end two phases.
-  uint64_t q_full[2], q_empty[2], o_full[2], o_empty[2], s_full[2], s_empty[2], p_full, p_empty, drain;
+  uint64_t q_full[2], q_empty[2], o_full[2], o_empty[2], s_full, s_empty, p_full, p_empty, drain;
   uint32_t tmem;
   volatile int abort;
   uint32_t pages_ok[8];    // by unit: its pages are in the pool (bits 0, 1)
-};
-
-// rows of a tile of `rows` in all: tiles of nearly the same number of rows, a multiple of 16
-struct PxTiles {
-  int n, rows;
-  __host__ __device__ explicit PxTiles(int all) {
-    n = (all + PX_ROWS - 1) / PX_ROWS;
-    rows = ((all + n - 1) / n + 15) / 16 * 16;
-    n = (all + rows - 1) / rows;
-  }
 };
 
 // the segment that starts at unit g and ends at the item's end or at gend; `near`: no later sequence
@@ -137,7 +131,7 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
   PxSeg e;
   int U, rt;
   if (g < sc.tp) {
-    const PxTiles t(p.b * p.nq * G);
+    const PxTiles& t = p.tiles[0];
     U = sc.up;
     const int item = g / U;
     e.u0 = g - item * U;
@@ -149,7 +143,7 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
     e.slot0 = 0;
     e.end = e.len = sc.shared * KV_PAGE;
   } else {
-    const PxTiles t(p.nq * G);
+    const PxTiles& t = p.tiles[1];
     int x = g - sc.tp;
     while (sc.cum[near + 1] <= x) ++near;
     x -= sc.cum[near];
@@ -292,17 +286,17 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     }
     for (int i = 0; i < PX_SEGS; ++i) {
       mbar_init(&sm.seg_full[i], 1);
-      mbar_init(&sm.seg_empty[i], 2 + PX_SOFTMAX + 128);   // TMA, MMA, softmax, queries and results
+      mbar_init(&sm.seg_empty[i], 2 + PX_SOFTMAX_WARPS + 4);   // TMA, MMA, softmax, queries and results
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.q_full[i], 128);
+      mbar_init(&sm.q_full[i], 4);
       mbar_init(&sm.q_empty[i], 1);
       mbar_init(&sm.o_full[i], 1);
-      mbar_init(&sm.o_empty[i], 128);
-      mbar_init(&sm.s_full[i], 1);
-      mbar_init(&sm.s_empty[i], PX_SOFTMAX);
+      mbar_init(&sm.o_empty[i], 4);
     }
-    mbar_init(&sm.p_full, PX_SOFTMAX);
+    mbar_init(&sm.s_full, 1);
+    mbar_init(&sm.s_empty, PX_SOFTMAX_WARPS);
+    mbar_init(&sm.p_full, PX_SOFTMAX_WARPS);
     mbar_init(&sm.p_empty, 1);
     mbar_init(&sm.drain, 1);
     sm.abort = 0;
@@ -323,7 +317,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       if (s1 < p.b) shared = min(shared, min(__ldcg(p.common + s1), n1 / KV_PAGE));
       shared = max(0, __reduce_min_sync(0xffffffffu, shared));
     }
-    const int per = p.Hk * PxTiles(p.nq * G).n;
+    const int per = p.Hk * p.tiles[1].n;
     auto units = [&](int n) { return per * ((min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
     const int u0 = s0 < p.b ? units(n0) : 0, u1 = s1 < p.b ? units(n1) : 0;
     int x = u0 + u1;
@@ -340,7 +334,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       sm.sched.cum[0] = 0;
       sm.sched.shared = shared;
       sm.sched.up = (shared + 1) / 2;
-      sm.sched.tp = p.Hk * PxTiles(R).n * sm.sched.up;
+      sm.sched.tp = p.Hk * p.tiles[0].n * sm.sched.up;
       const int total = sm.sched.tp + x;
       sm.sched.total = total;
       sm.sched.q = total / (int)gridDim.x;
@@ -357,8 +351,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
   // return: one that ran out has set the error bit, and the results are invalid.
   auto wait = [&](uint64_t* bar, uint32_t parity) { mbar_wait_bounded(bar, parity, &sm.abort, p.err); };
-  // the i-th segment's description (by all threads of a warp)
-  auto segment = [&](int i) {
+  // the i-th segment's description (in place until each role has arrived at seg_empty)
+  auto segment = [&](int i) -> const PxSeg& {
     wait(&sm.seg_full[i % PX_SEGS], (i / PX_SEGS) & 1);
     return sm.seg[i % PX_SEGS];
   };
@@ -368,6 +362,71 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   auto scratch_row = [&](const PxSeg& x) {
     return x.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
                     : (size_t)(x.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)x.hk * R + x.row0;
+  };
+
+  // a segment's queries (thread i of n) into shared memory, rows past its own as zeros; the loads of
+  // two pieces of eight dimensions are in flight together
+  auto queries = [&](const PxSeg& x, int seg, int i0, int n) {
+    const int cols = x.cols(), total = cols * (HD / 8);
+    if (i0 < cols && x.s >= 0) {
+      const int tr = (x.row0 + i0) / G;   // token row
+      sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
+    }
+    uint8_t* base = Qs + x.q_at * C::Q_SECOND;
+    for (int i = i0; i < total; i += 2 * n) {
+      uint4 w[2], w1[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
+        w[z] = w1[z] = make_uint4(0, 0, 0, 0);
+        if (r < x.rows) {
+          const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
+          const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
+          if (p.bf16) {
+            w[z] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
+          } else {
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(p.q) + at);
+            w[z] = __ldcg(src);
+            w1[z] = __ldcg(src + 1);
+          }
+        }
+      }
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
+        if (i + z * n >= total) break;
+        uint8_t* dst = base + (d >> 3) * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
+        if (p.bf16) {
+          *reinterpret_cast<uint4*>(dst) = w[z];
+          continue;
+        }
+        float v[8] = {__uint_as_float(w[z].x),  __uint_as_float(w[z].y),  __uint_as_float(w[z].z),  __uint_as_float(w[z].w),
+                      __uint_as_float(w1[z].x), __uint_as_float(w1[z].y), __uint_as_float(w1[z].z), __uint_as_float(w1[z].w)};
+#pragma unroll
+        for (int part = 0; part < PX_PARTS; ++part) {
+          uint4 o;
+          o.x = px_part(v[0], v[1]);
+          o.y = px_part(v[2], v[3]);
+          o.z = px_part(v[4], v[5]);
+          o.w = px_part(v[6], v[7]);
+          *reinterpret_cast<uint4*>(dst + part * cols * 128) = o;
+        }
+      }
+    }
+  };
+  // a warp's arrival, after what its lanes did before
+  auto arrive = [&](uint64_t* bar) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+  };
+  // the first segment's, which everything waits for: by warps 4 to 23; whether there is one
+  auto first_queries = [&](int i) {
+    const PxSeg& x = segment(0);
+    if (x.u0 == x.u1) return false;
+    queries(x, 0, i, PX_SOFTMAX + 128);
+    fence_proxy_async_smem();
+    named_bar_sync(1 + PX_GROUPS, PX_SOFTMAX + 128);
+    return true;
   };
 
   if (warp == 2) {
@@ -456,16 +515,14 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     auto scores = [&](const PxSeg& e) {
       const int slot = (2 * k) % NS;
       ready(&sm.full[slot], ((2 * k) / NS) & 1);
-      ready(&sm.s_empty[k & 1], ((k >> 1) & 1) ^ 1);
-      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, e.cols());
-      const uint64_t a = kd + (uint64_t)(slot * (C::TILE >> 4)), b = qd + (uint64_t)(e.q_at * (C::Q_HALF_SPACE >> 4));
-      for (int part = 0; part < q_parts; ++part)
+      if (k > 0) ready(&sm.s_empty, (k - 1) & 1);
+      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, q_parts * e.cols());
+      const uint64_t a = kd + (uint64_t)(slot * (C::TILE >> 4)), b = qd + (uint64_t)(e.q_at * (C::Q_SECOND >> 4));
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
-          px_mma(tmem + 64 * (k & 1), a + ((kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2),
-                 b + (uint64_t)(part * (C::Q_PART >> 4)) + ((kk >> 2) * (C::Q_HALF >> 4) + (kk & 3) * 2), idesc,
-                 part | kk ? 1u : 0u, on);
-      commit(&sm.s_full[k & 1]);
+      for (int kk = 0; kk < HD / 16; ++kk)
+        px_mma(tmem, a + ((kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2), b + ((kk >> 2) * (C::Q_HALF >> 4) + (kk & 3) * 2), idesc,
+               kk ? 1u : 0u, on);
+      commit(&sm.s_full);
       commit(&sm.empty[slot]);
       ++k;
     };
@@ -488,17 +545,21 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       commit(&sm.p_empty);
       if (u + 1 == e.u1) commit(&sm.o_full[seg & 1]);
     };
+    // scores of a unit, then values of the one before it, over the ends of segments too
     for (int seg = 0;; ++seg) {
-      const PxSeg e = segment(seg);
-      if (e.u0 == e.u1) break;
-      ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
+      const PxSeg& e = segment(seg);
+      const PxSeg& was = sm.seg[(seg + PX_SEGS - 1) % PX_SEGS];
+      const bool more = e.u0 < e.u1;
+      if (more) ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
       for (int u = e.u0; u < e.u1; ++u) {
         scores(e);
         if (u + 1 == e.u1) commit(&sm.q_empty[seg & 1]);
         if (u > e.u0) values(k - 2, e, seg, u - 1);
+        else if (seg > 0) values(k - 2, was, seg - 1, was.u1 - 1);
       }
-      values(k - 1, e, seg, e.u1 - 1);
-      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      if (!more && seg > 0) values(k - 1, was, seg - 1, was.u1 - 1);
+      if (seg > 0 && lane == 0) mbar_arrive(&sm.seg_empty[(seg - 1) % PX_SEGS]);
+      if (!more) break;
     }
     if (sm.abort) {   // wait for issued MMAs before shared memory goes away
       commit(&sm.drain);
@@ -508,63 +569,25 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
       }
     }
-  } else if (warp >= 12) {
+  } else if (warp >= 4 + PX_SOFTMAX_WARPS) {
     // ---- queries in and results out: queries of segments 0 and 1, results of 0, queries of 2, ...
-    const int st = tid - 384;
+    const int st = tid - 128 - PX_SOFTMAX;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     auto load_q = [&](int seg) {
-      const PxSeg x = segment(seg);
+      const PxSeg& x = segment(seg);
       if (x.u0 == x.u1) return;
-      const int cols = x.cols();
       // its space is free once the scores of the segment before (or of the one before that) are done
       const int before = seg - (x.q_whole ? 1 : 2);
       if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
-      if (st < cols && x.s >= 0) {
-        const int tr = (x.row0 + st) / G;   // token row
-        sm.seen[seg % PX_SEGS][st] =
-            (uint16_t)(st >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
-      }
-      uint8_t* base = Qs + x.q_at * C::Q_HALF_SPACE;
-#pragma unroll 2
-      for (int i = st; i < cols * (HD / 8); i += 128) {
-        const int r = i / (HD / 8), d = i % (HD / 8), hh = d >> 3;
-        uint8_t* dst = base + hh * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
-        uint4 w = make_uint4(0, 0, 0, 0), w1 = w;
-        if (r < x.rows) {
-          const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
-          const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
-          if (p.bf16) {
-            w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
-          } else {
-            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(p.q) + at);
-            w = __ldcg(src);
-            w1 = __ldcg(src + 1);
-          }
-        }
-        if (p.bf16) {
-          *reinterpret_cast<uint4*>(dst) = w;
-        } else {
-          float v[8] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w),
-                        __uint_as_float(w1.x), __uint_as_float(w1.y), __uint_as_float(w1.z), __uint_as_float(w1.w)};
-#pragma unroll
-          for (int part = 0; part < PX_PARTS; ++part) {
-            uint4 o;
-            o.x = px_part(v[0], v[1]);
-            o.y = px_part(v[2], v[3]);
-            o.z = px_part(v[4], v[5]);
-            o.w = px_part(v[6], v[7]);
-            *reinterpret_cast<uint4*>(dst + part * C::Q_PART) = o;
-          }
-        }
-      }
+      queries(x, seg, st, 128);
       fence_proxy_async_smem();
-      mbar_arrive(&sm.q_full[seg & 1]);
+      arrive(&sm.q_full[seg & 1]);
     };
-    load_q(0);
-    bool more = sm.seg[0].u0 < sm.seg[0].u1;   // (described: load_q has waited for it)
+    bool more = first_queries(st);
+    if (more) arrive(&sm.q_full[0]);
     if (more) load_q(1);
     for (int seg = 0; more; ++seg) {
-      const PxSeg x = segment(seg);
+      const PxSeg& x = segment(seg);
       const int cols = x.cols();
       const size_t row = scratch_row(x);
       wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
@@ -586,9 +609,9 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         }
       }
       tc_fence_before();
-      mbar_arrive(&sm.o_empty[seg & 1]);
-      mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
-      const PxSeg next = segment(seg + 1);
+      arrive(&sm.o_empty[seg & 1]);
+      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      const PxSeg& next = segment(seg + 1);
       more = next.u0 < next.u1;
       if (more) load_q(seg + 2);
     }
@@ -601,98 +624,122 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       __syncwarp();
       tc_fence_after();
     };
+    first_queries(128 + st);
     int k = 0;
     for (int seg = 0;; ++seg) {
-      const PxSeg x = segment(seg);
+      const PxSeg& x = segment(seg);
       if (x.u0 == x.u1) break;
-      const int cols = x.cols(), chunks = cols / 16;   // of eight rows for each group
-      const int c0 = wg * 8 * chunks;                  // this group's first row (of the tile)
-      const uint16_t* seen = sm.seen[seg % PX_SEGS] + c0;
-      float l[32];
+      // this group's pieces of eight rows: wg and wg + 4 of them, as far as there are rows
+      const int cols = x.cols(), mine = (cols / 8 - wg + PX_GROUPS - 1) / PX_GROUPS;
+      auto first_row = [&](int i) { return 8 * (wg + PX_GROUPS * i); };
+      const uint16_t* seen = sm.seen[seg % PX_SEGS];
+      float l[8 * PX_MINE];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) l[i] = 0.f;
+      for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
+      // f over the group's 128 slots of every row that the thread has, into red[0 .. 3]
+      auto across = [&](const float* v, auto&& f) {
+#pragma unroll
+        for (int i = 0; i < PX_MINE; ++i)
+          if (i < mine) {
+            const float r = px_across(v + 8 * i, lane, f);
+            if (lane < 8) sm.red[warp & 3][first_row(i) + lane] = r;
+          }
+        named_bar_sync(1 + wg, 128);
+      };
+      // the row whose result thread e puts together: 8 of the first piece, 8 of the second
+      const int my_row = e < 8 * mine ? first_row(e >> 3) + (e & 7) : 0;
       wait(&sm.q_full[seg & 1], (seg >> 1) & 1);   // (what the rows see is written)
       for (int u = x.u0; u < x.u1; ++u, ++k) {
         const int slot = x.slot0 + u * PX_UNIT + e;
-        ready(&sm.s_full[k & 1], (k >> 1) & 1);
-        float s[32];
+        ready(&sm.s_full, k & 1);
+        float s[8 * PX_MINE];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < chunks) px_ld8(tmem + lanes + 64 * (k & 1) + c0 + 8 * i, s + 8 * i);
-        tmem_wait_ld();
+        for (int i = 0; i < PX_MINE; ++i)
+          if (i < mine) {
+            const uint32_t at = tmem + lanes + first_row(i);
+            float a[8], b[8];   // the second and third parts' products
+            px_ld8(at, s + 8 * i);
+            if (q_parts > 1) {
+              px_ld8(at + cols, a);
+              px_ld8(at + 2 * cols, b);
+            }
+            tmem_wait_ld();
+            if (q_parts > 1) {
+#pragma unroll
+              for (int z = 0; z < 8; ++z) s[8 * i + z] += a[z] + b[z];
+            }
+          }
         tc_fence_before();
-        mbar_arrive(&sm.s_empty[k & 1]);
+        arrive(&sm.s_empty);
         // the slot is seen by every row (committed), by some (a block row's) or by none
         const uint32_t ok = sm.pages_ok[k & 7];
         const bool here = slot < x.end && ((ok >> (e >> 6)) & 1);
         if (x.slot0 + (u + 1) * PX_UNIT > x.len || ok != 3u) {
           const int i0 = slot - x.len;
+          const uint32_t all = here && i0 < 0 ? 0xFFFFu : 0u, bit = here && i0 >= 0 ? 1u << i0 : 0u;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            if (i < 8 * chunks) {
-              const bool sees = here && (i0 < 0 || ((seen[i] >> i0) & 1u));
-              if (!sees) s[i] = -INFINITY;
+          for (int i = 0; i < PX_MINE; ++i)
+            if (i < mine) {
+              const uint4 w = *reinterpret_cast<const uint4*>(seen + first_row(i));   // eight rows'
+#pragma unroll
+              for (int z = 0; z < 8; ++z) {
+                const uint32_t bits = ((&w.x)[z >> 1] >> (16 * (z & 1))) & bit;
+                if (!(bits | all)) s[8 * i + z] = -INFINITY;
+              }
             }
-          }
         }
-        // the largest score of each row over the group's 128 slots, into m (and the rescaling into red[.][0])
-        auto reference = [&](bool first) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < chunks) {
-              const float mx = px_across(s + 8 * i, lane, [](float a, float b) { return fmaxf(a, b); });
-              if (lane < 8) sm.red[wg][warp & 3][8 * i + lane] = mx;
-            }
-          named_bar_sync(1 + wg, 128);
-          if (e < 8 * chunks) {
-            const float top = fmaxf(fmaxf(sm.red[wg][0][e], sm.red[wg][1][e]), fmaxf(sm.red[wg][2][e], sm.red[wg][3][e])) * c;
-            const float old = first ? PX_UNSET : sm.m[wg][e], now = top == -INFINITY ? old : fmaxf(old, top);
-            sm.m[wg][e] = now;
-            sm.red[wg][0][e] = px_ex2(old - now);
-          }
-          named_bar_sync(1 + wg, 128);
-        };
-        if (u == x.u0) {
-          reference(true);
-        } else {
+        // the rows' references: the first unit's maxima, and new ones where a score passes them by far
+        const bool first = u == x.u0;
+        bool move = first;
+        if (!first) {
           float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            if (i < 8 * chunks) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.m[wg][i]);
+          for (int i = 0; i < 8 * PX_MINE; i += 4)
+            if (i < 8 * mine) {
+              const float4 m = *reinterpret_cast<const float4*>(&sm.m[first_row(i >> 3) + (i & 4)]);
               top = fmaxf(fmaxf(top, fmaf(s[i], c, -m.x)), fmaf(s[i + 1], c, -m.y));
               top = fmaxf(fmaxf(top, fmaf(s[i + 2], c, -m.z)), fmaf(s[i + 3], c, -m.w));
             }
-          if (px_bar_or(1 + wg, top > PX_LAZY)) {
-            reference(false);
+          move = px_bar_or(1 + wg, top > PX_LAZY);
+        }
+        if (move) {
+          across(s, [](float a, float b) { return fmaxf(a, b); });
+          if (e < 8 * mine) {
+            const float top = fmaxf(fmaxf(sm.red[0][my_row], sm.red[1][my_row]), fmaxf(sm.red[2][my_row], sm.red[3][my_row])) * c;
+            const float old = first ? PX_UNSET : sm.m[my_row], now = top == -INFINITY ? old : fmaxf(old, top);
+            sm.m[my_row] = now;
+            sm.red[0][my_row] = px_ex2(old - now);   // the rescaling of what is there
+          }
+          named_bar_sync(1 + wg, 128);
+          if (!first) {
             ready(&sm.p_empty, (k - 1) & 1);   // O holds the units before
+#pragma unroll 1
             for (int part = 0; part < p_parts; ++part)
+#pragma unroll 1
+              for (int i = 0; i < mine; ++i) {
+                const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + part * cols + first_row(i);
+                float o[8];
+                px_ld8(at, o);
+                tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (i < chunks) {
-                  const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + part * cols + c0 + 8 * i;
-                  float o[8];
-                  px_ld8(at, o);
-                  tmem_wait_ld();
+                for (int z = 0; z < 8; ++z) o[z] *= sm.red[0][first_row(i) + z];
+                px_st8(at, o);
+              }
 #pragma unroll
-                  for (int z = 0; z < 8; ++z) o[z] *= sm.red[wg][0][8 * i + z];
-                  px_st8(at, o);
-                }
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i < 8 * chunks) l[i] *= sm.red[wg][0][i];
+            for (int i = 0; i < 8 * PX_MINE; ++i)
+              if (i < 8 * mine) l[i] *= sm.red[0][first_row(i >> 3) + (i & 7)];
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             named_bar_sync(1 + wg, 128);   // (red has been read)
           }
         }
         if (k > 0) ready(&sm.p_empty, (k - 1) & 1);   // P of the unit before has been read
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < chunks) {
+        for (int i = 0; i < PX_MINE; ++i)
+          if (i < mine) {
             float v[8];
 #pragma unroll
             for (int z = 0; z < 8; z += 4) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.m[wg][8 * i + z]);
+              const float4 m = *reinterpret_cast<const float4*>(&sm.m[first_row(i) + z]);
               v[z] = px_ex2(fmaf(s[8 * i + z], c, -m.x));
               v[z + 1] = px_ex2(fmaf(s[8 * i + z + 1], c, -m.y));
               v[z + 2] = px_ex2(fmaf(s[8 * i + z + 2], c, -m.z));
@@ -703,7 +750,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll
             for (int part = 0; part < PX_PARTS; ++part) {
               if (part < p_parts) {   // B's columns: the parts side by side
-                const int ch = (part * cols + c0) / 8 + i;
+                const int ch = part * cols / 8 + wg + PX_GROUPS * i;
                 uint4 o;
                 o.x = px_part(v[0], v[1]);
                 o.y = px_part(v[2], v[3]);
@@ -713,31 +760,26 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
               }
             }
           }
-        // a slot that no row sees may hold anything: its values as zeros (0 times anything finite)
-        if (wg == 0 && !here) {
+        // a slot that no row sees may hold anything: its values as zeros (0 times anything finite), as
+        // far as the product reads (steps of 16 slots)
+        if (wg == 0 && !here && e < (x.end - x.slot0 - u * PX_UNIT + 15) / 16 * 16) {
           const int vs = (2 * k + 1) % NS;
           wait(&sm.full[vs], ((2 * k + 1) / NS) & 1);
           uint8_t* v = smem + (size_t)vs * C::TILE + e * 128;
-          for (int hh = 0; hh < C::HALVES; ++hh)
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(v + hh * C::HALF + i * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+          for (int i = 0; i < 8 * C::HALVES; ++i)
+            *reinterpret_cast<uint4*>(v + (i >> 3) * C::HALF + (((i & 7) ^ (e & 7)) << 4)) = make_uint4(0, 0, 0, 0);
         }
-        __syncwarp();
         fence_proxy_async_smem();
         tc_fence_before();
-        mbar_arrive(&sm.p_full);
+        arrive(&sm.p_full);
       }
       // ---- the rows' references and sums for the results
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < chunks) {
-          const float sum = px_across(l + 8 * i, lane, [](float a, float b) { return a + b; });
-          if (lane < 8) sm.red[wg][warp & 3][8 * i + lane] = sum;
-        }
-      named_bar_sync(1 + wg, 128);
-      if (e < 8 * chunks && c0 + e < x.rows)
-        scratch.ml[scratch_row(x) + c0 + e] =
-            make_float2(sm.m[wg][e], (sm.red[wg][0][e] + sm.red[wg][1][e]) + (sm.red[wg][2][e] + sm.red[wg][3][e]));
-      mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      across(l, [](float a, float b) { return a + b; });
+      if (e < 8 * mine && my_row < x.rows)
+        scratch.ml[scratch_row(x) + my_row] =
+            make_float2(sm.m[my_row], (sm.red[0][my_row] + sm.red[1][my_row]) + (sm.red[2][my_row] + sm.red[3][my_row]));
+      arrive(&sm.seg_empty[seg % PX_SEGS]);
       named_bar_sync(1 + wg, 128);   // (red and m have been read)
     }
   }
@@ -767,14 +809,14 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
   const size_t all = (size_t)p.b * p.nq * p.H, mine = (size_t)hk * R + rr;
   int lo[2] = {0, 0}, n[2] = {0, 0}, at[2];   // of the shared pages, of the others: first CTA, CTAs, row of the tile
   if (shared > 0) {
-    const PxTiles t(R);
+    const PxTiles& t = p.tiles[0];
     const int first = (hk * t.n + rr / t.rows) * up;
     lo[0] = owner(first);
     n[0] = owner(first + up - 1) - lo[0] + 1;
     at[0] = rr % t.rows;
   }
   {
-    const PxTiles t(p.nq * G);
+    const PxTiles& t = p.tiles[1];
     const int x = rr - s * p.nq * G, U = (c_e - c_s) / (p.Hk * t.n), first = tp + c_s + (hk * t.n + x / t.rows) * U;
     at[1] = x % t.rows;
     if (U > 0) {
@@ -864,6 +906,15 @@ cudaError_t px_launch(const PrefixAttnParams& p, cudaStream_t st, bool pdl) {
 
 }  // namespace
 
+// tiles of nearly the same number of rows, a multiple of 16
+static PxTiles px_tiles(int all) {
+  PxTiles t;
+  t.n = (all + PX_ROWS - 1) / PX_ROWS;
+  t.rows = ((all + t.n - 1) / t.n + 15) / 16 * 16;
+  t.n = (all + t.rows - 1) / t.rows;
+  return t;
+}
+
 // floats for row_heads rows of hd (twice as many of half the size)
 size_t prefix_attention_scratch(int row_heads, int hd, int num_sms) {
   const size_t rows = (size_t)2 * row_heads + (size_t)PX_ROWS * num_sms;
@@ -884,6 +935,8 @@ cudaError_t prefix_attention_prepare() {
 cudaError_t launch_prefix_attention(const PrefixAttnParams& p0, int num_sms, cudaStream_t st, bool pdl) {
   PrefixAttnParams p = p0;
   p.ctas = num_sms;
+  p.tiles[0] = px_tiles(p.b * p.nq * (p.H / p.Hk));
+  p.tiles[1] = px_tiles(p.nq * (p.H / p.Hk));
   return p.hd == 64 ? px_launch<64>(p, st, pdl) : px_launch<128>(p, st, pdl);
 }
 
