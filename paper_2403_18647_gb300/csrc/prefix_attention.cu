@@ -234,6 +234,28 @@ __device__ __forceinline__ bool px_bar_or(int id, bool pred) {   // over a group
       : "memory");
   return r != 0;
 }
+// Waits for the phase of `bar` with this parity: at most PX_POLLS times PX_POLL_NS (2 s), after which
+// it raises ERR_TIMEOUT and sets *abort, which ends every other wait of the CTA.  (A few instructions:
+// the kernel has some thirty waits, and its code has to stay near the instruction caches' 32 KB.)
+constexpr uint32_t PX_POLL_NS = 1000, PX_POLLS = 2000000;
+__device__ __forceinline__ void px_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
+  const uint32_t at = smem_u32(bar);
+  uint32_t left = PX_POLLS;
+#pragma unroll 1
+  do {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity), "r"(PX_POLL_NS)
+        : "memory");
+    if (ok) return;
+  } while (--left && !*abort);
+  *abort = 1;
+  set_error(err, ERR_TIMEOUT);
+}
 // Eight columns of a value a lane each -> in every lane, column (lane & 7) over the warp's 32 lanes
 template <typename F>
 __device__ __forceinline__ float px_across(const float* v, int lane, F&& f) {
@@ -350,7 +372,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   const int q_parts = p.bf16 ? 1 : PX_PARTS, p_parts = p.bf16 ? 2 : PX_PARTS;
   // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
   // return: one that ran out has set the error bit, and the results are invalid.
-  auto wait = [&](uint64_t* bar, uint32_t parity) { mbar_wait_bounded(bar, parity, &sm.abort, p.err); };
+  auto wait = [&](uint64_t* bar, uint32_t parity) { px_wait(bar, parity, &sm.abort, p.err); };
   // the i-th segment's description (in place until each role has arrived at seg_empty)
   auto segment = [&](int i) -> const PxSeg& {
     wait(&sm.seg_full[i % PX_SEGS], (i / PX_SEGS) & 1);
@@ -419,15 +441,16 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
   };
-  // the first segment's, which everything waits for: by warps 4 to 23; whether there is one
+  // the first segment's, which everything waits for: by warps 4 to 23
   auto first_queries = [&](int i) {
     const PxSeg& x = segment(0);
-    if (x.u0 == x.u1) return false;
+    if (x.u0 == x.u1) return;
     queries(x, 0, i, PX_SOFTMAX + 128);
     fence_proxy_async_smem();
     named_bar_sync(1 + PX_GROUPS, PX_SOFTMAX + 128);
-    return true;
   };
+
+  if (warp >= 4) first_queries(tid - 128);
 
   if (warp == 2) {
     // ---- the segments
@@ -472,12 +495,15 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             else if (lane == 0) set_error(p.err, ERR_PAGE);
           }
         if (lane == 0 && !sm.abort) {
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv, ++it) {
             const int s = it % NS;
-            if (!mbar_wait_bounded(&sm.empty[s], ((it / NS) & 1) ^ 1, &sm.abort, p.err)) break;
+            wait(&sm.empty[s], ((it / NS) & 1) ^ 1);
+            if (sm.abort) break;
             // (read until the unit's V slot is free again, 2 or 4 units on)
             sm.pages_ok[(it >> 1) & 7] = ok;
             mbar_arrive_expect_tx(&sm.full[s], __popc(ok) * C::HALVES * C::BOX);
+#pragma unroll 1
             for (int i = 0; i < 2; ++i) {
               if (!((ok >> i) & 1)) continue;
               const int r = p.row0 + (page[i] * p.Hk + e.hk) * KV_PAGE;
@@ -546,20 +572,32 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       if (u + 1 == e.u1) commit(&sm.o_full[seg & 1]);
     };
     // scores of a unit, then values of the one before it, over the ends of segments too
-    for (int seg = 0;; ++seg) {
-      const PxSeg& e = segment(seg);
-      const PxSeg& was = sm.seg[(seg + PX_SEGS - 1) % PX_SEGS];
-      const bool more = e.u0 < e.u1;
-      if (more) ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
-      for (int u = e.u0; u < e.u1; ++u) {
+    int seg = 0, u = 0, seg_was = -1, u_was = 0;
+    for (bool open = false;;) {
+      if (!open) {
+        const PxSeg& e = segment(seg);
+        u = e.u0;
+        open = true;
+        if (u < e.u1) ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
+      }
+      const PxSeg& e = sm.seg[seg % PX_SEGS];
+      const bool more = u < e.u1;
+      if (more) {
         scores(e);
         if (u + 1 == e.u1) commit(&sm.q_empty[seg & 1]);
-        if (u > e.u0) values(k - 2, e, seg, u - 1);
-        else if (seg > 0) values(k - 2, was, seg - 1, was.u1 - 1);
       }
-      if (!more && seg > 0) values(k - 1, was, seg - 1, was.u1 - 1);
-      if (seg > 0 && lane == 0) mbar_arrive(&sm.seg_empty[(seg - 1) % PX_SEGS]);
+      if (seg_was >= 0) {
+        const PxSeg& w = sm.seg[seg_was % PX_SEGS];
+        values(k - 1 - (int)more, w, seg_was, u_was);
+        if (u_was + 1 == w.u1 && lane == 0) mbar_arrive(&sm.seg_empty[seg_was % PX_SEGS]);
+      }
       if (!more) break;
+      seg_was = seg;
+      u_was = u;
+      if (++u == e.u1) {
+        ++seg;
+        open = false;
+      }
     }
     if (sm.abort) {   // wait for issued MMAs before shared memory goes away
       commit(&sm.drain);
@@ -570,29 +608,27 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
     }
   } else if (warp >= 4 + PX_SOFTMAX_WARPS) {
-    // ---- queries in and results out: queries of segments 0 and 1, results of 0, queries of 2, ...
+    // ---- queries in and results out: queries of segment 1, results of 0, queries of 2, ...
     const int st = tid - 128 - PX_SOFTMAX;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    auto load_q = [&](int seg) {
-      const PxSeg& x = segment(seg);
-      if (x.u0 == x.u1) return;
-      // its space is free once the scores of the segment before (or of the one before that) are done
-      const int before = seg - (x.q_whole ? 1 : 2);
-      if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
-      queries(x, seg, st, 128);
-      fence_proxy_async_smem();
-      arrive(&sm.q_full[seg & 1]);
-    };
-    bool more = first_queries(st);
-    if (more) arrive(&sm.q_full[0]);
-    if (more) load_q(1);
-    for (int seg = 0; more; ++seg) {
-      const PxSeg& x = segment(seg);
+    if (sm.seg[0].u0 < sm.seg[0].u1) arrive(&sm.q_full[0]);   // (in place: first_queries)
+    for (int seg = 0; segment(seg).u0 < segment(seg).u1; ++seg) {
+      const PxSeg& next = segment(seg + 1);
+      if (next.u0 < next.u1) {
+        // its space is free once the scores of the segment before (or of the one before that) are done
+        const int before = seg + 1 - (next.q_whole ? 1 : 2);
+        if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
+        queries(next, seg + 1, st, 128);
+        fence_proxy_async_smem();
+        arrive(&sm.q_full[(seg + 1) & 1]);
+      }
+      const PxSeg& x = sm.seg[seg % PX_SEGS];
       const int cols = x.cols();
       const size_t row = scratch_row(x);
       wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
       __syncwarp();
       tc_fence_after();
+#pragma unroll 1
       for (int r = 0; r < x.rows; r += 8) {
         float o[8], o1[8], o2[8];
         const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + r;
@@ -611,9 +647,6 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       tc_fence_before();
       arrive(&sm.o_empty[seg & 1]);
       if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
-      const PxSeg& next = segment(seg + 1);
-      more = next.u0 < next.u1;
-      if (more) load_q(seg + 2);
     }
   } else if (warp >= 4) {
     const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
@@ -624,7 +657,6 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       __syncwarp();
       tc_fence_after();
     };
-    first_queries(128 + st);
     int k = 0;
     for (int seg = 0;; ++seg) {
       const PxSeg& x = segment(seg);
