@@ -25,21 +25,26 @@
 // (24 bits: nothing is lost against fp32 products; one part for bf16 queries, whose probabilities
 // have two), one product each into the same fp32 accumulator.
 //
-// The reference m of a row is its maximum over the segment's first unit; later units only check that
-// no score passes it by more than 2^PX_LAZY, which is rare, and then rescale: a maximum over lanes for
-// each row and unit would cost more than the exponentials.  Sums of exponentials stay in each
-// thread (a slot's) until the segment's end.
+// The reference m of a row is its maximum over the first unit; later units only check that no score
+// passes it by more than 2^PX_LAZY, which is rare, and then rescale: a maximum over lanes for each
+// row and unit would cost more than the exponentials.  Sums of exponentials stay in each thread (a
+// slot's) until the end.
+//
+// The tensor cores cut off what an addition to their fp32 accumulator cannot hold, so that an error of
+// half a unit grows with every 16 slots added (2.4 times the error of fp32 products at 40 units).
+// After PX_RUN units O is therefore added, rounded, to a total in TMEM and begun anew.
 //
 // The three parts are side by side in B (N = three times the rows) and their products in columns of
 // their own, added up when they are read: 8 MMAs a tile of K or V instead of 24.  An MMA takes N / 2
-// cycles from N = 96 on and 50 below, and 40 to issue from a warp by itself, 100 from one that shares
-// its scheduler with the softmax (64 rows: 2300 cycles for 24 of N = 64, 4000 a unit in all).
+// cycles from N = 96 on and 50 below.
 //
-// Warps: 0 TMA (pages by the table), 1 MMA issue (the whole warp, one lane's instructions: descriptors
-// stay in uniform registers; 100 cycles an MMA when a single thread ran the loop), 2 the segments,
-// ahead of their use, 4-19 softmax (the code of a row is unrolled: with 32 rows a thread on 8 warps
-// the instructions no longer came in time, 5000 cycles a unit), 20-23 queries and results, so that a segment's queries are in place
-// before the one ahead of it ends and its results leave while the next one runs.
+// Warps: 0 TMA (pages by the table), 1 and 3 MMA issue (a whole warp, one lane's instructions), 2 the
+// segments, ahead of their use, 4-19 softmax, 20-23 queries and results, so that a segment's queries are
+// in place before the one ahead of it ends and its results leave while the next one runs.  What bounds
+// a unit of 64 rows is the softmax' chain of loads, barriers and stores, 3700 cycles, against 1600 of
+// the tensor cores'; on one warp the products' issue, 1500 and 1950 cycles for a unit's scores and
+// values beside busy warps, was as long (8x6 rows after 2048 slots, 7B heads: 36 us, 32 on two warps;
+// 64 rows of 16 bits over 8200 slots: 96 us, 62).
 // Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: S and two O.
 #include <algorithm>
 
@@ -59,9 +64,11 @@ constexpr int PX_THREADS = 128 + PX_SOFTMAX + 128;
 constexpr int PX_MINE = PX_ROWS / 8 / PX_GROUPS;   // pieces of eight rows of a thread
 constexpr int PX_SEGS = 4;        // segments described ahead
 constexpr int PX_O = PX_PARTS * PX_ROWS;   // TMEM column of O (S from 0 on)
-constexpr int PX_O_STEP = 160;    // to the second O, for segments of at most PX_O_ROWS rows
-constexpr int PX_O_ROWS = 48;
-constexpr int PX_Q_ROWS = 32;     // rows of segments whose queries fit twice
+constexpr int PX_O_STEP = 160;    // to the second O, for segments of at most PX_TWICE rows
+constexpr int PX_TWICE = 32;      // rows of segments whose queries, and whose O, fit twice
+constexpr int PX_TOTAL = 448;     // TMEM column of the total that O is added to
+constexpr int PX_RUN = 16;        // units of a segment
+static_assert(PX_O + PX_O_STEP + PX_PARTS * PX_TWICE <= PX_TOTAL && PX_O + PX_PARTS * PX_ROWS <= PX_TOTAL, "columns");
 constexpr int PX_MAX_B = 64;
 constexpr float PX_LAZY = 8.0f;   // log2 of the growth of a row maximum that is left unscaled
 constexpr float PX_UNSET = -1e30f;   // reference of a row that has seen no slot
@@ -76,7 +83,7 @@ struct PxCfg {
   static constexpr int SLOTS = HD == 128 ? 4 : 8;           // of the ring
   static constexpr int P_PART = PX_UNIT * 128;              // 128 slots x 64 rows
   static constexpr int Q_HALF = PX_PARTS * PX_ROWS * 128;   // 3 x 64 rows x 64 dims
-  static constexpr int Q_SECOND = PX_PARTS * PX_Q_ROWS * 128;   // where a second segment's queries start
+  static constexpr int Q_SECOND = PX_PARTS * PX_TWICE * 128;   // where a second segment's queries start
   static constexpr size_t OFF_P = (size_t)SLOTS * TILE;     // (MN-major reads of 64-dim tiles run into it)
   static constexpr size_t OFF_Q = OFF_P + PX_PARTS * P_PART;
   static constexpr size_t OFF_MISC = OFF_Q + HALVES * Q_HALF;
@@ -97,14 +104,16 @@ __device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that
   return x < 0 ? g / (q + 1) : r + x / q;
 }
 
-// a run of units of one item
+// a run of at most PX_RUN units of one item
 struct PxSeg {
   int s;                   // sequence, or -1: the shared pages
   int hk, row0, rows;      // cache head, rows [row0, row0 + rows) of its R
   int u0, u1;              // units; none: the share has ended
+  int from;                // the item's first unit in the CTA's share
   int slot0, end, len;     // unit u: slots slot0 + 128 u .., those below `end`; committed below len
   int q_at, o_at;          // 0 or 1: which half of the queries' space, which O
-  int q_whole, o_whole;    // it takes the whole space, or the segment before does
+  int whole;               // it takes the whole space, or the segment before does
+  int goes_on, more;       // it goes on where the CTA's segment before ended; the next one goes on
   __device__ int cols() const { return (rows + 15) / 16 * 16; }
 };
 struct PxMisc {
@@ -118,7 +127,7 @@ struct PxMisc {
   uint64_t seg_full[PX_SEGS], seg_empty[PX_SEGS];
   // [2]: by segment parity.  A phase of a barrier is waited for before the one after it can
   // end: with one barrier for every segment the queries of two segments ahead would end two phases.
-  uint64_t q_full[2], q_empty[2], o_full[2], o_empty[2], s_full, s_empty, p_full, p_empty, drain;
+  uint64_t q_full[2], q_empty[2], o_full[2], o_empty[2], s_full, s_empty, p_full, p_empty, drain[2];
   uint32_t tmem;
   volatile int abort;
   uint32_t pages_ok[8];    // by unit: its pages are in the pool (bits 0, 1)
@@ -145,6 +154,7 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
   } else {
     const PxTiles& t = p.tiles[1];
     int x = g - sc.tp;
+#pragma unroll 1
     while (sc.cum[near + 1] <= x) ++near;
     x -= sc.cum[near];
     U = (sc.cum[near + 1] - sc.cum[near]) / (p.Hk * t.n);
@@ -159,7 +169,8 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
     e.len = len[near];
     e.end = min(e.len + p.nq, p.ld * KV_PAGE);
   }
-  e.u1 = min(U, e.u0 + gend - g);
+  e.u1 = min(e.u0 + PX_RUN, min(U, e.u0 + gend - g));
+  e.more = e.u1 < min(U, e.u0 + gend - g);
   return e;
 }
 
@@ -234,27 +245,22 @@ __device__ __forceinline__ bool px_bar_or(int id, bool pred) {   // over a group
       : "memory");
   return r != 0;
 }
-// Waits for the phase of `bar` with this parity: at most PX_POLLS times PX_POLL_NS (2 s), after which
-// it raises ERR_TIMEOUT and sets *abort, which ends every other wait of the CTA.  (A few instructions:
-// the kernel has some thirty waits, and its code has to stay near the instruction caches' 32 KB.)
-constexpr uint32_t PX_POLL_NS = 1000, PX_POLLS = 2000000;
-__device__ __forceinline__ void px_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
-  const uint32_t at = smem_u32(bar);
-  uint32_t left = PX_POLLS;
+// Waits for the phase of `bar` with this parity: WAIT_LIMIT_NS at most, after which it raises
+// ERR_TIMEOUT and sets *abort, which ends every other wait of the CTA.  (A few instructions: the kernel
+// has some thirty waits, and its code has to stay near the instruction caches' 32 KB.)
+__device__ __noinline__ void px_wait_on(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
+  const uint64_t t0 = globaltimer_ns();
 #pragma unroll 1
-  do {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(at), "r"(parity), "r"(PX_POLL_NS)
-        : "memory");
-    if (ok) return;
-  } while (--left && !*abort);
-  *abort = 1;
-  set_error(err, ERR_TIMEOUT);
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort || globaltimer_ns() - t0 > WAIT_LIMIT_NS) {
+      *abort = 1;
+      set_error(err, ERR_TIMEOUT);
+      return;
+    }
+  }
+}
+__device__ __forceinline__ void px_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
+  if (!mbar_try_wait(bar, parity)) px_wait_on(bar, parity, abort, err);
 }
 // Eight columns of a value a lane each -> in every lane, column (lane & 7) over the warp's 32 lanes
 template <typename F>
@@ -291,6 +297,61 @@ struct PxScratch {
 };
 static_assert(sizeof(PxSched) <= 1024, "the schedule's place");
 
+// a segment's queries (thread i of n) into shared memory, rows past its own as zeros; the loads of
+// two pieces of eight dimensions are in flight together
+template <int HD>
+__device__ __noinline__ void px_queries(const PrefixAttnParams& p, PxMisc& sm, uint8_t* Qs, const PxSeg& x, int seg, int i0, int n) {
+  using C = PxCfg<HD>;
+  const int G = p.H / p.Hk;
+  const int cols = x.cols(), total = cols * (HD / 8);
+  if (i0 < cols && x.s >= 0) {
+    const int tr = (x.row0 + i0) / G;   // token row
+    sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
+  }
+  if (x.goes_on) return;   // (they are there)
+  uint8_t* base = Qs + x.q_at * C::Q_SECOND;
+#pragma unroll 1
+  for (int i = i0; i < total; i += 2 * n) {
+    uint4 w[2], w1[2];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
+      w[z] = w1[z] = make_uint4(0, 0, 0, 0);
+      if (r < x.rows) {
+        const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
+        const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
+        if (p.bf16) {
+          w[z] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
+        } else {
+          const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(p.q) + at);
+          w[z] = __ldcg(src);
+          w1[z] = __ldcg(src + 1);
+        }
+      }
+    }
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
+      if (i + z * n >= total) break;
+      uint8_t* dst = base + (d >> 3) * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
+      if (p.bf16) {
+        *reinterpret_cast<uint4*>(dst) = w[z];
+        continue;
+      }
+      float v[8] = {__uint_as_float(w[z].x),  __uint_as_float(w[z].y),  __uint_as_float(w[z].z),  __uint_as_float(w[z].w),
+                    __uint_as_float(w1[z].x), __uint_as_float(w1[z].y), __uint_as_float(w1[z].z), __uint_as_float(w1[z].w)};
+#pragma unroll
+      for (int part = 0; part < PX_PARTS; ++part) {
+        uint4 o;
+        o.x = px_part(v[0], v[1]);
+        o.y = px_part(v[2], v[3]);
+        o.z = px_part(v[4], v[5]);
+        o.w = px_part(v[6], v[7]);
+        *reinterpret_cast<uint4*>(dst + part * cols * 128) = o;
+      }
+    }
+  }
+}
 template <int HD>
 __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const __grid_constant__ PrefixAttnParams p) {
   using C = PxCfg<HD>;
@@ -302,14 +363,17 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = p.H / p.Hk, R = p.b * p.nq * G;
   if (tid == 0) {
+#pragma unroll 1
     for (int i = 0; i < NS; ++i) {
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], 1);
     }
+#pragma unroll 1
     for (int i = 0; i < PX_SEGS; ++i) {
       mbar_init(&sm.seg_full[i], 1);
-      mbar_init(&sm.seg_empty[i], 2 + PX_SOFTMAX_WARPS + 4);   // TMA, MMA, softmax, queries and results
+      mbar_init(&sm.seg_empty[i], 3 + PX_SOFTMAX_WARPS + 4);   // TMA, MMA, softmax, queries and results
     }
+#pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.q_full[i], 4);
       mbar_init(&sm.q_empty[i], 1);
@@ -320,7 +384,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     mbar_init(&sm.s_empty, PX_SOFTMAX_WARPS);
     mbar_init(&sm.p_full, PX_SOFTMAX_WARPS);
     mbar_init(&sm.p_empty, 1);
-    mbar_init(&sm.drain, 1);
+    mbar_init(&sm.drain[0], 1);
+    mbar_init(&sm.drain[1], 1);
     sm.abort = 0;
     fence_mbar_init();
     tma_prefetch_desc(&p.kmap);
@@ -382,60 +447,10 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   // where a segment's results go: the rows of an item from its first unit on, or those of the CTA's
   // first segment, which continues one
   auto scratch_row = [&](const PxSeg& x) {
-    return x.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
+    return x.from > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
                     : (size_t)(x.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)x.hk * R + x.row0;
   };
 
-  // a segment's queries (thread i of n) into shared memory, rows past its own as zeros; the loads of
-  // two pieces of eight dimensions are in flight together
-  auto queries = [&](const PxSeg& x, int seg, int i0, int n) {
-    const int cols = x.cols(), total = cols * (HD / 8);
-    if (i0 < cols && x.s >= 0) {
-      const int tr = (x.row0 + i0) / G;   // token row
-      sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
-    }
-    uint8_t* base = Qs + x.q_at * C::Q_SECOND;
-    for (int i = i0; i < total; i += 2 * n) {
-      uint4 w[2], w1[2];
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
-        w[z] = w1[z] = make_uint4(0, 0, 0, 0);
-        if (r < x.rows) {
-          const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
-          const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
-          if (p.bf16) {
-            w[z] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
-          } else {
-            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(p.q) + at);
-            w[z] = __ldcg(src);
-            w1[z] = __ldcg(src + 1);
-          }
-        }
-      }
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
-        if (i + z * n >= total) break;
-        uint8_t* dst = base + (d >> 3) * C::Q_HALF + r * 128 + (((d & 7) ^ (r & 7)) << 4);
-        if (p.bf16) {
-          *reinterpret_cast<uint4*>(dst) = w[z];
-          continue;
-        }
-        float v[8] = {__uint_as_float(w[z].x),  __uint_as_float(w[z].y),  __uint_as_float(w[z].z),  __uint_as_float(w[z].w),
-                      __uint_as_float(w1[z].x), __uint_as_float(w1[z].y), __uint_as_float(w1[z].z), __uint_as_float(w1[z].w)};
-#pragma unroll
-        for (int part = 0; part < PX_PARTS; ++part) {
-          uint4 o;
-          o.x = px_part(v[0], v[1]);
-          o.y = px_part(v[2], v[3]);
-          o.z = px_part(v[4], v[5]);
-          o.w = px_part(v[6], v[7]);
-          *reinterpret_cast<uint4*>(dst + part * cols * 128) = o;
-        }
-      }
-    }
-  };
   // a warp's arrival, after what its lanes did before
   auto arrive = [&](uint64_t* bar) {
     __syncwarp();
@@ -445,7 +460,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   auto first_queries = [&](int i) {
     const PxSeg& x = segment(0);
     if (x.u0 == x.u1) return;
-    queries(x, 0, i, PX_SOFTMAX + 128);
+    px_queries<HD>(p, sm, Qs, x, 0, i, PX_SOFTMAX + 128);
     fence_proxy_async_smem();
     named_bar_sync(1 + PX_GROUPS, PX_SOFTMAX + 128);
   };
@@ -456,16 +471,19 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     // ---- the segments
     if (lane == 0) {
       const int g1 = sm.sched.begin(blockIdx.x + 1);
-      int near = 0, rows = 0;
+      int near = 0, rows = 0, q_at = 1, goes_on = 0, from = 0;
+#pragma unroll 1
       for (int i = 0, g = sm.sched.begin(blockIdx.x);; ++i) {
         PxSeg e{};
         if (g < g1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
         g += e.u1 - e.u0;
-        e.q_at = e.rows <= PX_Q_ROWS ? i & 1 : 0;
-        e.o_at = e.rows <= PX_O_ROWS ? i & 1 : 0;
-        e.q_whole = max(rows, e.rows) > PX_Q_ROWS;
-        e.o_whole = max(rows, e.rows) > PX_O_ROWS;
+        e.goes_on = goes_on;
+        e.from = from = goes_on ? from : e.u0;
+        e.q_at = q_at = goes_on ? q_at : e.rows <= PX_TWICE ? q_at ^ 1 : 0;
+        e.o_at = e.rows <= PX_TWICE ? i & 1 : 0;
+        e.whole = max(rows, e.rows) > PX_TWICE;
         rows = e.rows;
+        goes_on = e.more;
         wait(&sm.seg_empty[i % PX_SEGS], ((i / PX_SEGS) & 1) ^ 1);
         sm.seg[i % PX_SEGS] = e;
         mbar_arrive(&sm.seg_full[i % PX_SEGS]);
@@ -476,6 +494,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     // ---- K and V tiles: K of unit 0, V of unit 0, K of unit 1, ...
     const uint64_t pol = l2_policy_evict_normal();
     int it = 0;
+#pragma unroll 1
     for (int seg = 0;; ++seg) {
       const PxSeg e = segment(seg);
       __syncwarp();
@@ -484,6 +503,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       const int* row = p.table + (size_t)max(e.s, 0) * p.ld;
       const int j0 = e.slot0 / KV_PAGE + 2 * e.u0, j1 = min((e.end + KV_PAGE - 1) / KV_PAGE, e.slot0 / KV_PAGE + 2 * e.u1);
       int entry = 0;
+#pragma unroll 1
       for (int u = e.u0; u < e.u1; ++u) {
         const int at = 2 * (u - e.u0), j = j0 + at;
         if ((at & 31) == 0) entry = j + lane < j1 ? __ldcg(row + j + lane) : 0;
@@ -507,6 +527,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             for (int i = 0; i < 2; ++i) {
               if (!((ok >> i) & 1)) continue;
               const int r = p.row0 + (page[i] * p.Hk + e.hk) * KV_PAGE;
+#pragma unroll 1
               for (int hh = 0; hh < C::HALVES; ++hh)
                 tma_load_2d(smem + (size_t)s * C::TILE + hh * C::HALF + i * C::BOX, kv ? &p.vmap : &p.kmap, &sm.full[s], hh * 64,
                             r, pol);
@@ -517,14 +538,16 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
     }
     if (lane == 0 && sm.abort) {   // let the copies in flight land before the CTA exits
+#pragma unroll 1
       for (int i = max(0, it - NS); i < it; ++i) {
         const uint64_t t0 = globaltimer_ns();
         while (!mbar_try_wait(&sm.full[i % NS], (i / NS) & 1))
           if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
       }
     }
-  } else if (warp == 1) {
-    // ---- products; nothing is issued any more once a wait has run out
+  } else if (warp == 1 || warp == 3) {
+    // ---- products: scores on one warp, values on the other; nothing is issued any more once a wait
+    // has run out
     const uint32_t mine = px_elect();
     auto ready = [&](uint64_t* bar, uint32_t parity) {
       wait(bar, parity);
@@ -535,75 +558,67 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       if (mine) umma_commit(bar);
       __syncwarp();
     };
-    const uint64_t kd = sdesc_sw128(smem_u32(smem)), qd = sdesc_sw128(smem_u32(Qs));
-    const uint64_t vd = px_desc_mn(smem_u32(smem), C::HALF), pd = px_desc_mn(smem_u32(Ps), C::P_PART);
-    int k = 0;   // units whose scores were issued
-    auto scores = [&](const PxSeg& e) {
-      const int slot = (2 * k) % NS;
-      ready(&sm.full[slot], ((2 * k) / NS) & 1);
-      if (k > 0) ready(&sm.s_empty, (k - 1) & 1);
-      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, q_parts * e.cols());
-      const uint64_t a = kd + (uint64_t)(slot * (C::TILE >> 4)), b = qd + (uint64_t)(e.q_at * (C::Q_SECOND >> 4));
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk)
-        px_mma(tmem, a + ((kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2), b + ((kk >> 2) * (C::Q_HALF >> 4) + (kk & 3) * 2), idesc,
-               kk ? 1u : 0u, on);
-      commit(&sm.s_full);
-      commit(&sm.empty[slot]);
-      ++k;
-    };
-    // unit x, the u-th of the seg'th segment
-    auto values = [&](int x, const PxSeg& e, int seg, int u) {
-      const int slot = (2 * x + 1) % NS;
-      if (u == e.u0) {   // O: the last or the last but one segment's results have left
-        const int before = seg - (e.o_whole ? 1 : 2);
-        if (before >= 0) ready(&sm.o_empty[before & 1], (before >> 1) & 1);
-      }
-      ready(&sm.p_full, x & 1);
-      ready(&sm.full[slot], ((2 * x + 1) / NS) & 1);
-      const uint32_t on = sm.abort ? 0u : mine, idesc = idesc_bf16_f32(128, p_parts * e.cols()) | (1u << 15) | (1u << 16);   // both MN-major
-      const uint64_t a = vd + (uint64_t)(slot * (C::TILE >> 4));
-      const int steps = (min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT) + 15) / 16;   // 16 slots each
-#pragma unroll
-      for (int kk = 0; kk < PX_UNIT / 16; ++kk)
-        if (kk < steps) px_mma(tmem + PX_O + PX_O_STEP * e.o_at, a + kk * 128, pd + kk * 128, idesc, u > e.u0 || kk ? 1u : 0u, on);
-      commit(&sm.empty[slot]);
-      commit(&sm.p_empty);
-      if (u + 1 == e.u1) commit(&sm.o_full[seg & 1]);
-    };
-    // scores of a unit, then values of the one before it, over the ends of segments too
-    int seg = 0, u = 0, seg_was = -1, u_was = 0;
-    for (bool open = false;;) {
-      if (!open) {
+    int k = 0;   // unit of the share
+    if (warp == 1) {
+      const uint64_t kd = sdesc_sw128(smem_u32(smem)), qd = sdesc_sw128(smem_u32(Qs));
+#pragma unroll 1
+      for (int seg = 0;; ++seg) {
         const PxSeg& e = segment(seg);
-        u = e.u0;
-        open = true;
-        if (u < e.u1) ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
+        if (e.u0 == e.u1) break;
+        const uint32_t idesc = idesc_bf16_f32(128, q_parts * e.cols());
+        const uint64_t b0 = qd + (uint64_t)(e.q_at * (C::Q_SECOND >> 4));
+        ready(&sm.q_full[seg & 1], (seg >> 1) & 1);
+#pragma unroll 1
+        for (int u = e.u0; u < e.u1; ++u, ++k) {
+          const int slot = (2 * k) % NS;
+          ready(&sm.full[slot], ((2 * k) / NS) & 1);
+          if (k > 0) ready(&sm.s_empty, (k - 1) & 1);
+          const uint64_t a0 = kd + (uint64_t)(slot * (C::TILE >> 4));
+          if (!sm.abort) {
+#pragma unroll 1
+            for (int kk = 0; kk < HD / 16; ++kk)
+              px_mma(tmem, a0 + ((kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2), b0 + ((kk >> 2) * (C::Q_HALF >> 4) + (kk & 3) * 2), idesc,
+                     kk ? 1u : 0u, mine);
+          }
+          commit(&sm.s_full);
+          commit(&sm.empty[slot]);
+        }
+        commit(&sm.q_empty[seg & 1]);
+        if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
       }
-      const PxSeg& e = sm.seg[seg % PX_SEGS];
-      const bool more = u < e.u1;
-      if (more) {
-        scores(e);
-        if (u + 1 == e.u1) commit(&sm.q_empty[seg & 1]);
-      }
-      if (seg_was >= 0) {
-        const PxSeg& w = sm.seg[seg_was % PX_SEGS];
-        values(k - 1 - (int)more, w, seg_was, u_was);
-        if (u_was + 1 == w.u1 && lane == 0) mbar_arrive(&sm.seg_empty[seg_was % PX_SEGS]);
-      }
-      if (!more) break;
-      seg_was = seg;
-      u_was = u;
-      if (++u == e.u1) {
-        ++seg;
-        open = false;
+    } else {
+      const uint64_t vd = px_desc_mn(smem_u32(smem), C::HALF), pd = px_desc_mn(smem_u32(Ps), C::P_PART);
+#pragma unroll 1
+      for (int seg = 0;; ++seg) {
+        const PxSeg& e = segment(seg);
+        if (e.u0 == e.u1) break;
+        const uint32_t idesc = idesc_bf16_f32(128, p_parts * e.cols()) | (1u << 15) | (1u << 16);   // both MN-major
+        const uint32_t o = tmem + PX_O + PX_O_STEP * e.o_at;
+        const int before = seg - (e.whole ? 1 : 2);   // O: its results have left
+        if (before >= 0) ready(&sm.o_empty[before & 1], (before >> 1) & 1);
+#pragma unroll 1
+        for (int u = e.u0; u < e.u1; ++u, ++k) {
+          const int slot = (2 * k + 1) % NS, steps = (min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT) + 15) / 16;   // 16 slots each
+          const uint64_t a0 = vd + (uint64_t)(slot * (C::TILE >> 4));
+          ready(&sm.full[slot], ((2 * k + 1) / NS) & 1);
+          ready(&sm.p_full, k & 1);
+          if (!sm.abort) {
+#pragma unroll 1
+            for (int kk = 0; kk < steps; ++kk) px_mma(o, a0 + kk * 128, pd + kk * 128, idesc, u > e.u0 || kk ? 1u : 0u, mine);
+          }
+          commit(&sm.p_empty);
+          commit(&sm.empty[slot]);
+        }
+        commit(&sm.o_full[seg & 1]);
+        if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
       }
     }
     if (sm.abort) {   // wait for issued MMAs before shared memory goes away
-      commit(&sm.drain);
+      uint64_t* const drain = &sm.drain[warp >> 1];
+      commit(drain);
       if (lane == 0) {
         const uint64_t t0 = globaltimer_ns();
-        while (!mbar_try_wait(&sm.drain, 0))
+        while (!mbar_try_wait(drain, 0))
           if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
       }
     }
@@ -612,13 +627,14 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     const int st = tid - 128 - PX_SOFTMAX;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     if (sm.seg[0].u0 < sm.seg[0].u1) arrive(&sm.q_full[0]);   // (in place: first_queries)
+#pragma unroll 1
     for (int seg = 0; segment(seg).u0 < segment(seg).u1; ++seg) {
       const PxSeg& next = segment(seg + 1);
       if (next.u0 < next.u1) {
         // its space is free once the scores of the segment before (or of the one before that) are done
-        const int before = seg + 1 - (next.q_whole ? 1 : 2);
-        if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
-        queries(next, seg + 1, st, 128);
+        const int before = seg + 1 - (next.whole ? 1 : 2);
+        if (before >= 0 && !next.goes_on) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
+        px_queries<HD>(p, sm, Qs, next, seg + 1, st, 128);
         fence_proxy_async_smem();
         arrive(&sm.q_full[(seg + 1) & 1]);
       }
@@ -631,24 +647,37 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll 1
       for (int r = 0; r < x.rows; r += 8) {
         float o[8], o1[8], o2[8];
-        const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + r;
+        const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + r, total = tmem + lanes + PX_TOTAL + r;
         px_ld8(at, o);
         px_ld8(at + cols, o1);
         if (p_parts > 2) px_ld8(at + 2 * cols, o2);
         tmem_wait_ld();
-        float* dst = scratch.o + (row + r) * HD + st;
 #pragma unroll
         for (int z = 0; z < 8; ++z) {
           o[z] += o1[z];
           if (p_parts > 2) o[z] += o2[z];
-          if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
         }
+        if (x.goes_on) {
+          px_ld8(total, o1);
+          tmem_wait_ld();
+#pragma unroll
+          for (int z = 0; z < 8; ++z) o[z] += o1[z];
+        }
+        if (x.more) {
+          px_st8(total, o);
+          continue;
+        }
+        float* dst = scratch.o + (row + r) * HD + st;
+#pragma unroll
+        for (int z = 0; z < 8; ++z)
+          if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
       }
+      if (x.more) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       tc_fence_before();
       arrive(&sm.o_empty[seg & 1]);
       if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
     }
-  } else if (warp >= 4) {
+  } else {
     const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = rsqrtf((float)HD) * 1.4426950408889634f;
@@ -658,6 +687,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       tc_fence_after();
     };
     int k = 0;
+    float l[8 * PX_MINE];   // the rows' sums of this thread's slots
+#pragma unroll 1
     for (int seg = 0;; ++seg) {
       const PxSeg& x = segment(seg);
       if (x.u0 == x.u1) break;
@@ -665,9 +696,10 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       const int cols = x.cols(), mine = (cols / 8 - wg + PX_GROUPS - 1) / PX_GROUPS;
       auto first_row = [&](int i) { return 8 * (wg + PX_GROUPS * i); };
       const uint16_t* seen = sm.seen[seg % PX_SEGS];
-      float l[8 * PX_MINE];
+      if (!x.goes_on) {
 #pragma unroll
-      for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
+        for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
+      }
       // f over the group's 128 slots of every row that the thread has, into red[0 .. 3]
       auto across = [&](const float* v, auto&& f) {
 #pragma unroll
@@ -681,6 +713,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       // the row whose result thread e puts together: 8 of the first piece, 8 of the second
       const int my_row = e < 8 * mine ? first_row(e >> 3) + (e & 7) : 0;
       wait(&sm.q_full[seg & 1], (seg >> 1) & 1);   // (what the rows see is written)
+#pragma unroll 1
       for (int u = x.u0; u < x.u1; ++u, ++k) {
         const int slot = x.slot0 + u * PX_UNIT + e;
         ready(&sm.s_full, k & 1);
@@ -721,7 +754,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             }
         }
         // the rows' references: the first unit's maxima, and new ones where a score passes them by far
-        const bool first = u == x.u0;
+        const bool first = u == x.u0 && !x.goes_on;
         bool move = first;
         if (!first) {
           float top = -INFINITY;
@@ -744,12 +777,14 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           }
           named_bar_sync(1 + wg, 128);
           if (!first) {
-            ready(&sm.p_empty, (k - 1) & 1);   // O holds the units before
+            if (x.goes_on) ready(&sm.o_empty[(seg - 1) & 1], ((seg - 1) >> 1) & 1);   // the total is complete
+            ready(&sm.p_empty, (k - 1) & 1);   // and O holds the units before
 #pragma unroll 1
-            for (int part = 0; part < p_parts; ++part)
+            for (int part = u > x.u0 ? 0 : p_parts; part < p_parts + x.goes_on; ++part)
 #pragma unroll 1
               for (int i = 0; i < mine; ++i) {
-                const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + part * cols + first_row(i);
+                const uint32_t at =
+                    tmem + lanes + first_row(i) + (part < p_parts ? PX_O + PX_O_STEP * x.o_at + part * cols : PX_TOTAL);
                 float o[8];
                 px_ld8(at, o);
                 tmem_wait_ld();
@@ -794,23 +829,30 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           }
         // a slot that no row sees may hold anything: its values as zeros (0 times anything finite), as
         // far as the product reads (steps of 16 slots)
-        if (wg == 0 && !here && e < (x.end - x.slot0 - u * PX_UNIT + 15) / 16 * 16) {
-          const int vs = (2 * k + 1) % NS;
+        const int there = x.end - x.slot0 - u * PX_UNIT;   // slots of the unit
+        if (wg == PX_GROUPS - 1 && (there < PX_UNIT || ok != 3u)) {
+          constexpr int CHUNKS = 8 * C::HALVES;   // of a slot
+          const int vs = (2 * k + 1) % NS, z1 = min(PX_UNIT, (there + 15) / 16 * 16) * CHUNKS;
           wait(&sm.full[vs], ((2 * k + 1) / NS) & 1);
-          uint8_t* v = smem + (size_t)vs * C::TILE + e * 128;
 #pragma unroll 1
-          for (int i = 0; i < 8 * C::HALVES; ++i)
-            *reinterpret_cast<uint4*>(v + (i >> 3) * C::HALF + (((i & 7) ^ (e & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+          for (int z = (ok == 3u ? there * CHUNKS : 0) + e; z < z1; z += 128) {
+            const int at = z / CHUNKS, i = z % CHUNKS;
+            if (at >= there || !((ok >> (at >> 6)) & 1))
+              *reinterpret_cast<uint4*>(smem + (size_t)vs * C::TILE + at * 128 + (i >> 3) * C::HALF + (((i & 7) ^ (at & 7)) << 4)) =
+                  make_uint4(0, 0, 0, 0);
+          }
         }
         fence_proxy_async_smem();
         tc_fence_before();
         arrive(&sm.p_full);
       }
       // ---- the rows' references and sums for the results
-      across(l, [](float a, float b) { return a + b; });
-      if (e < 8 * mine && my_row < x.rows)
-        scratch.ml[scratch_row(x) + my_row] =
-            make_float2(sm.m[my_row], (sm.red[0][my_row] + sm.red[1][my_row]) + (sm.red[2][my_row] + sm.red[3][my_row]));
+      if (!x.more) {
+        across(l, [](float a, float b) { return a + b; });
+        if (e < 8 * mine && my_row < x.rows)
+          scratch.ml[scratch_row(x) + my_row] =
+              make_float2(sm.m[my_row], (sm.red[0][my_row] + sm.red[1][my_row]) + (sm.red[2][my_row] + sm.red[3][my_row]));
+      }
       arrive(&sm.seg_empty[seg % PX_SEGS]);
       named_bar_sync(1 + wg, 128);   // (red and m have been read)
     }

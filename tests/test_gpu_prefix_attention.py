@@ -180,6 +180,29 @@ def test_large_scores_and_one_key_that_wins(ctx):
     c.check(c.run(ctx))
 
 
+@pytest.mark.parametrize("b,q,H,Hk,hd,lens,shared", [
+    (1, 1, 40, 40, 128, [9000], 0), (2, 16, 40, 40, 128, [9001, 8950], 139), (1, 3, 64, 64, 64, [12345], 0), (2, 4, 40, 40, 64, [7000, 6990], 0),
+])
+@pytest.mark.parametrize("type", [torch.float32, torch.bfloat16])
+def test_long_shares(ctx, b, q, H, Hk, hd, lens, shared, type):
+    """More than 16 units of 128 slots for every SM, so that sums are added up in several runs."""
+    c = Case(16, b, q, H, Hk, hd, lens, shared, type)
+    c.check(c.run(ctx))
+    assert ctx.get_error() == 0
+
+
+def test_maxima_that_move_from_run_to_run(ctx):
+    """Scores that grow along 9000 slots by 30 and more (a probability is off by some 2^-24 of its exponent)."""
+    c = Case(17, 1, 4, 40, 40, 128, [9000], 0, scale=0.0)
+    c.x += torch.linspace(-1, 1, 128, device="cuda").repeat(40)
+    at = torch.zeros(c.k.shape[0], device="cuda")
+    at[c.table[0].long()] = torch.arange(c.table.shape[1], device="cuda", dtype=torch.float32)
+    c.k = (c.k.float() * 0.2 + at[:, None, None, None] * torch.linspace(-0.06, 0.06, 128, device="cuda")).bfloat16()
+    for _ in range(2):
+        c.check(c.run(ctx))
+        c.x.neg_()
+
+
 def test_strides_and_other_streams(ctx):
     """q as a slice of a wider row, out into one; on a stream of its own."""
     c = Case(11, 3, 5, 4, 4, 64, [100, 130, 150], 1)
