@@ -99,6 +99,8 @@ struct PxSched {
   int cum[PX_MAX_B + 1];   // units of the items of the sequences before
   __device__ int begin(int c) const { return c * q + min(c, r); }
 };
+// n / d for n < 2^16, inv = px_inv(d)
+__device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
 __device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has unit g
   const int x = g - (q + 1) * r;
   return x < 0 ? g / (q + 1) : r + x / q;
@@ -119,8 +121,9 @@ struct PxSeg {
 struct PxMisc {
   PxSched sched;
   int len[PX_MAX_B];
-  __align__(16) float red[4][PX_ROWS];   // per warp of a group: a row's maximum, or sum
-  float m[PX_ROWS];        // the rows' references
+  uint32_t top[3][PX_ROWS];   // a row's maximum over the unit, as px_order
+  __align__(16) float m[PX_ROWS];   // the rows' references
+  float by[PX_ROWS];       // the rescaling of what is there
   __align__(16) uint16_t seen[PX_SEGS][PX_ROWS];     // the block rows that a row sees
   PxSeg seg[PX_SEGS];
   uint64_t full[8], empty[8];
@@ -136,7 +139,7 @@ struct PxMisc {
 // the segment that starts at unit g and ends at the item's end or at gend; `near`: no later sequence
 // than its own
 __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int g, int gend, int& near) {
-  const int G = p.H / p.Hk;
+  const int G = p.G;
   PxSeg e;
   int U, rt;
   if (g < sc.tp) {
@@ -262,6 +265,19 @@ __device__ __noinline__ void px_wait_on(uint64_t* bar, uint32_t parity, volatile
 __device__ __forceinline__ void px_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
   if (!mbar_try_wait(bar, parity)) px_wait_on(bar, parity, abort, err);
 }
+// floats as whole numbers of the same order, all of them above 0
+__device__ __forceinline__ uint32_t px_order(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float px_unorder(uint32_t u) {
+  return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ float px_warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 // Eight columns of a value a lane each -> in every lane, column (lane & 7) over the warp's 32 lanes
 template <typename F>
 __device__ __forceinline__ float px_across(const float* v, int lane, F&& f) {
@@ -286,13 +302,16 @@ __device__ __forceinline__ float px_across(const float* v, int lane, F&& f) {
 // CTA, from the item that it continues
 struct PxScratch {
   float* o;        // [2 * row heads + PX_ROWS * CTAs][hd]
-  float2* ml;      // the same rows' reference and sum
+  float* m;        // the same rows' references
+  float4* l;       // and sums, in four parts
   PxSched* sched;
+  static __host__ __device__ size_t rows(size_t row_heads, int ctas) { return (2 * row_heads + (size_t)PX_ROWS * ctas + 31) / 32 * 32; }
   __host__ __device__ PxScratch(const PrefixAttnParams& p) {
-    const size_t rows = (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * p.ctas;
+    const size_t n = rows((size_t)p.b * p.nq * p.H, p.ctas);
     sched = reinterpret_cast<PxSched*>(p.part);
-    ml = reinterpret_cast<float2*>(p.part + 256);
-    o = p.part + 256 + (2 * rows + 31) / 32 * 32;
+    l = reinterpret_cast<float4*>(p.part + 256);
+    m = p.part + 256 + 4 * n;
+    o = m + n;
   }
 };
 static_assert(sizeof(PxSched) <= 1024, "the schedule's place");
@@ -302,11 +321,10 @@ static_assert(sizeof(PxSched) <= 1024, "the schedule's place");
 template <int HD>
 __device__ __noinline__ void px_queries(const PrefixAttnParams& p, PxMisc& sm, uint8_t* Qs, const PxSeg& x, int seg, int i0, int n) {
   using C = PxCfg<HD>;
-  const int G = p.H / p.Hk;
-  const int cols = x.cols(), total = cols * (HD / 8);
+  const int G = p.G, cols = x.cols(), total = cols * (HD / 8);
   if (i0 < cols && x.s >= 0) {
-    const int tr = (x.row0 + i0) / G;   // token row
-    sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr % p.nq)) - 1u);
+    const int tr = px_div(x.row0 + i0, p.inv_g);   // token row
+    sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr - px_div(tr, p.inv_nq) * p.nq)) - 1u);
   }
   if (x.goes_on) return;   // (they are there)
   uint8_t* base = Qs + x.q_at * C::Q_SECOND;
@@ -318,7 +336,7 @@ __device__ __noinline__ void px_queries(const PrefixAttnParams& p, PxMisc& sm, u
       const int r = (i + z * n) / (HD / 8), d = (i + z * n) % (HD / 8);
       w[z] = w1[z] = make_uint4(0, 0, 0, 0);
       if (r < x.rows) {
-        const unsigned rr = x.row0 + r, tr = rr / (unsigned)G;
+        const int rr = x.row0 + r, tr = px_div(rr, p.inv_g);
         const long long at = (long long)tr * p.q_ld + (long long)(x.hk * G + (rr - tr * G)) * HD + d * 8;
         if (p.bf16) {
           w[z] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at));
@@ -361,7 +379,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   uint8_t* Qs = smem + C::OFF_Q;
   PxMisc& sm = *reinterpret_cast<PxMisc*>(smem + C::OFF_MISC);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = p.H / p.Hk, R = p.b * p.nq * G;
+  const int R = p.b * p.nq * p.G;
   if (tid == 0) {
 #pragma unroll 1
     for (int i = 0; i < NS; ++i) {
@@ -392,6 +410,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     tma_prefetch_desc(&p.vmap);
   }
   if (warp == 1) tmem_alloc(&sm.tmem, 512);
+  if (tid < PX_ROWS) sm.top[0][tid] = 0;
   pdl_wait();   // q, lengths, tables and rows come from the kernels before
   pdl_trigger();
   if (warp == 2) {   // the schedule: two sequences a lane
@@ -623,20 +642,26 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
     }
   } else if (warp >= 4 + PX_SOFTMAX_WARPS) {
-    // ---- queries in and results out: queries of segment 1, results of 0, queries of 2, ...
+    // ---- queries in and results out.  A segment's queries come when the scores of the one before the
+    // last are done, which frees their space, or, where they need all of it, of the last one.
     const int st = tid - 128 - PX_SOFTMAX;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    auto queries = [&](int j) {   // of segment j, once those of segment j - (whole ? 1 : 2) are done with
+      const PxSeg& y = sm.seg[j % PX_SEGS];
+      const int before = j - (y.whole ? 1 : 2);
+      if (before >= 0 && !y.goes_on) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
+      px_queries<HD>(p, sm, Qs, y, j, st, 128);
+      fence_proxy_async_smem();
+      arrive(&sm.q_full[j & 1]);
+    };
     if (sm.seg[0].u0 < sm.seg[0].u1) arrive(&sm.q_full[0]);   // (in place: first_queries)
 #pragma unroll 1
-    for (int seg = 0; segment(seg).u0 < segment(seg).u1; ++seg) {
-      const PxSeg& next = segment(seg + 1);
-      if (next.u0 < next.u1) {
-        // its space is free once the scores of the segment before (or of the one before that) are done
-        const int before = seg + 1 - (next.whole ? 1 : 2);
-        if (before >= 0 && !next.goes_on) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
-        px_queries<HD>(p, sm, Qs, next, seg + 1, st, 128);
-        fence_proxy_async_smem();
-        arrive(&sm.q_full[(seg + 1) & 1]);
+    for (int seg = 0, j = 1; segment(seg).u0 < segment(seg).u1; ++seg) {
+#pragma unroll 1
+      for (; j <= seg + 2; ++j) {
+        const PxSeg& y = segment(j);
+        if (y.u0 == y.u1 || (j == seg + 2 && y.whole)) break;
+        queries(j);
       }
       const PxSeg& x = sm.seg[seg % PX_SEGS];
       const int cols = x.cols();
@@ -687,6 +712,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       tc_fence_after();
     };
     int k = 0;
+    int moves = 0;
+    float m_mine = 0.f;     // the reference of the lane's row
     float l[8 * PX_MINE];   // the rows' sums of this thread's slots
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
@@ -700,23 +727,12 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll
         for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
       }
-      // f over the group's 128 slots of every row that the thread has, into red[0 .. 3]
-      auto across = [&](const float* v, auto&& f) {
-#pragma unroll
-        for (int i = 0; i < PX_MINE; ++i)
-          if (i < mine) {
-            const float r = px_across(v + 8 * i, lane, f);
-            if (lane < 8) sm.red[warp & 3][first_row(i) + lane] = r;
-          }
-        named_bar_sync(1 + wg, 128);
-      };
-      // the row whose result thread e puts together: 8 of the first piece, 8 of the second
-      const int my_row = e < 8 * mine ? first_row(e >> 3) + (e & 7) : 0;
-      wait(&sm.q_full[seg & 1], (seg >> 1) & 1);   // (what the rows see is written)
+      // the row that the lane looks after in its warp: 8 of the first piece, 8 of the second
+      const int my_row = lane < 8 * mine ? first_row(lane >> 3) + (lane & 7) : 0;
 #pragma unroll 1
       for (int u = x.u0; u < x.u1; ++u, ++k) {
         const int slot = x.slot0 + u * PX_UNIT + e;
-        ready(&sm.s_full, k & 1);
+        ready(&sm.s_full, k & 1);   // (the queries, and what the rows see, were there before)
         float s[8 * PX_MINE];
 #pragma unroll
         for (int i = 0; i < PX_MINE; ++i)
@@ -768,14 +784,33 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           move = px_bar_or(1 + wg, top > PX_LAZY);
         }
         if (move) {
-          across(s, [](float a, float b) { return fmaxf(a, b); });
-          if (e < 8 * mine) {
-            const float top = fmaxf(fmaxf(sm.red[0][my_row], sm.red[1][my_row]), fmaxf(sm.red[2][my_row], sm.red[3][my_row])) * c;
-            const float old = first ? PX_UNSET : sm.m[my_row], now = top == -INFINITY ? old : fmaxf(old, top);
-            sm.m[my_row] = now;
-            sm.red[0][my_row] = px_ex2(old - now);   // the rescaling of what is there
+          // three places in turn: all have read one before any comes to its next use
+          const int now_at = moves % 3, next_at = (moves + 1) % 3;
+          ++moves;
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < PX_MINE; ++i)
+            if (i < mine) {
+#pragma unroll
+              for (int z = 0; z < 8; ++z) {
+                const float r = px_warp_max(s[8 * i + z]);
+                if (lane == 8 * i + z) top = r;
+              }
+            }
+          if (lane < 8 * mine) {
+            atomicMax(&sm.top[now_at][my_row], px_order(top));
           }
+          if (lane < 8 * PX_MINE) sm.top[next_at][first_row(lane >> 3) + (lane & 7)] = 0;
           named_bar_sync(1 + wg, 128);
+          // (every warp of the group finds, and writes, the same)
+          if (lane < 8 * mine) {
+            top = px_unorder(sm.top[now_at][my_row]) * c;
+            const float old = first ? PX_UNSET : m_mine;
+            m_mine = top == -INFINITY ? old : fmaxf(old, top);
+            sm.m[my_row] = m_mine;
+            sm.by[my_row] = px_ex2(old - m_mine);
+          }
+          __syncwarp();
           if (!first) {
             if (x.goes_on) ready(&sm.o_empty[(seg - 1) & 1], ((seg - 1) >> 1) & 1);   // the total is complete
             ready(&sm.p_empty, (k - 1) & 1);   // and O holds the units before
@@ -789,14 +824,13 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
                 px_ld8(at, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int z = 0; z < 8; ++z) o[z] *= sm.red[0][first_row(i) + z];
+                for (int z = 0; z < 8; ++z) o[z] *= sm.by[first_row(i) + z];
                 px_st8(at, o);
               }
 #pragma unroll
             for (int i = 0; i < 8 * PX_MINE; ++i)
-              if (i < 8 * mine) l[i] *= sm.red[0][first_row(i >> 3) + (i & 7)];
+              if (i < 8 * mine) l[i] *= sm.by[first_row(i >> 3) + (i & 7)];
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            named_bar_sync(1 + wg, 128);   // (red has been read)
           }
         }
         if (k > 0) ready(&sm.p_empty, (k - 1) & 1);   // P of the unit before has been read
@@ -846,15 +880,19 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         tc_fence_before();
         arrive(&sm.p_full);
       }
-      // ---- the rows' references and sums for the results
+      // ---- the rows' references and sums (a warp's part of them) for the results
       if (!x.more) {
-        across(l, [](float a, float b) { return a + b; });
-        if (e < 8 * mine && my_row < x.rows)
-          scratch.ml[scratch_row(x) + my_row] =
-              make_float2(sm.m[my_row], (sm.red[0][my_row] + sm.red[1][my_row]) + (sm.red[2][my_row] + sm.red[3][my_row]));
+        const size_t row = scratch_row(x);
+#pragma unroll
+        for (int i = 0; i < PX_MINE; ++i)
+          if (i < mine) {
+            const float sum = px_across(l + 8 * i, lane, [](float a, float b) { return a + b; });
+            const int r = first_row(i) + lane;
+            if (lane < 8 && r < x.rows) reinterpret_cast<float*>(scratch.l + row + r)[warp & 3] = sum;
+          }
+        if ((warp & 3) == 0 && lane < 8 * mine && my_row < x.rows) scratch.m[row + my_row] = m_mine;
       }
       arrive(&sm.seg_empty[seg % PX_SEGS]);
-      named_bar_sync(1 + wg, 128);   // (red and m have been read)
     }
   }
   tc_fence_before();
@@ -865,7 +903,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   }
 }
 
-// A warp for each row and head: its partial results by weight.
+// A warp for each row and head: its partial results by weight, the loads of PX_JOIN of them in flight.
+constexpr int PX_JOIN = 8;
 template <int HD>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant__ PrefixAttnParams p) {
   constexpr int E = HD / 32;
@@ -873,65 +912,65 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
   pdl_wait();
   const int lane = threadIdx.x & 31, w = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (w >= p.b * p.nq * p.H) return;
-  const int r = w / p.H, h = w - r * p.H;
-  const int G = p.H / p.Hk, R = p.b * p.nq * G, hk = h / G, rr = r * G + h % G, s = r / p.nq;
   const PxScratch scratch(p);
+  const int r = w / p.H, h = w - r * p.H, s = px_div(r, p.inv_nq), hk = px_div(h, p.inv_g);
   const int shared = __ldcg(&scratch.sched->shared), up = __ldcg(&scratch.sched->up), tp = __ldcg(&scratch.sched->tp),
             q = __ldcg(&scratch.sched->q), rest = __ldcg(&scratch.sched->r), c_s = __ldcg(&scratch.sched->cum[s]),
             c_e = __ldcg(&scratch.sched->cum[s + 1]);
-  auto owner = [&](int g) { return px_owner(g, q, rest); };
-  const size_t all = (size_t)p.b * p.nq * p.H, mine = (size_t)hk * R + rr;
-  int lo[2] = {0, 0}, n[2] = {0, 0}, at[2];   // of the shared pages, of the others: first CTA, CTAs, row of the tile
+  const int R = p.b * p.nq * p.G, rr = r * p.G + h - hk * p.G;
+  // of the shared pages, of the others: parts, the first one's row of the scratch (an item's own), and
+  // how far the second one's (a CTA's) is from 0, the later ones PX_ROWS on each
+  const int all = p.b * p.nq * p.H, mine = hk * R + rr;
+  int n[2] = {0, 0}, next[2] = {0, 0};
+  auto item = [&](int k, int first, int U, int at) {   // its first unit, units, and the row of the tile
+    const int c0 = px_owner(first, q, rest);
+    n[k] = px_owner(first + U - 1, q, rest) - c0 + 1;
+    next[k] = 2 * all + PX_ROWS * c0 + at;
+  };
   if (shared > 0) {
-    const PxTiles& t = p.tiles[0];
-    const int first = (hk * t.n + rr / t.rows) * up;
-    lo[0] = owner(first);
-    n[0] = owner(first + up - 1) - lo[0] + 1;
-    at[0] = rr % t.rows;
+    const int t = rr / p.tiles[0].rows;
+    item(0, (hk * p.tiles[0].n + t) * up, up, rr - t * p.tiles[0].rows);
   }
-  {
-    const PxTiles& t = p.tiles[1];
-    const int x = rr - s * p.nq * G, U = (c_e - c_s) / (p.Hk * t.n), first = tp + c_s + (hk * t.n + x / t.rows) * U;
-    at[1] = x % t.rows;
-    if (U > 0) {
-      lo[1] = owner(first);
-      n[1] = owner(first + U - 1) - lo[1] + 1;
-    }
+  if (c_e > c_s) {
+    const int x = rr - s * p.nq * p.G, t = x / p.tiles[1].rows, U = (c_e - c_s) / (p.Hk * p.tiles[1].n);
+    item(1, tp + c_s + (hk * p.tiles[1].n + t) * U, U, x - t * p.tiles[1].rows);
   }
   const int parts = n[0] + n[1];
-  auto row_of = [&](int i) {   // part i's row of the scratch
-    const int k = i >= n[0], c = i - (k ? n[0] : 0);
-    return c == 0 ? k * all + mine : 2 * all + (size_t)PX_ROWS * (lo[k] + c) + at[k];
-  };
   float M = PX_UNSET, L = 0.f, o[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) o[i] = 0.f;
-  for (int i0 = 0; i0 < parts; i0 += 32) {
-    const float2 ml = i0 + lane < parts ? __ldcg(scratch.ml + row_of(i0 + lane)) : make_float2(PX_UNSET, 0.f);
-    float top = ml.x;
+#pragma unroll 1
+  for (int i0 = 0; i0 < parts; i0 += PX_JOIN) {
+    float v[PX_JOIN][E], m[PX_JOIN];
+    float4 l[PX_JOIN];
 #pragma unroll
-    for (int a = 16; a > 0; a >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, a));
-    const float now = fmaxf(M, top), f = px_ex2(M - now), wt = ml.y == 0.f ? 0.f : px_ex2(ml.x - now);
-    float sum = wt * ml.y;
+    for (int i = 0; i < PX_JOIN; ++i) {
+      const int k = i0 + i >= n[0], c = i0 + i - (k ? n[0] : 0), at = c == 0 ? k * all + mine : next[k] + c * PX_ROWS;
+      m[i] = PX_UNSET;
+      l[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i0 + i < parts) {
+        const float* src = scratch.o + (size_t)at * HD + E * lane;
+        m[i] = __ldcg(scratch.m + at);
+        l[i] = __ldcg(scratch.l + at);
+        if constexpr (E == 4) *reinterpret_cast<float4*>(v[i]) = __ldcg(reinterpret_cast<const float4*>(src));
+        else *reinterpret_cast<float2*>(v[i]) = __ldcg(reinterpret_cast<const float2*>(src));
+      }
+    }
+    float now = M;
 #pragma unroll
-    for (int a = 16; a > 0; a >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, a);
+    for (int i = 0; i < PX_JOIN; ++i) now = fmaxf(now, m[i]);
+    const float f = px_ex2(M - now);
     M = now;
-    L = L * f + sum;
+    L *= f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] *= f;
-    const int m = min(32, parts - i0);
-#pragma unroll 4
-    for (int i = 0; i < m; ++i) {
-      const float* src = scratch.o + row_of(i0 + i) * HD + E * lane;
-      const float x = __shfl_sync(0xffffffffu, wt, i);
-      if (x == 0.f) continue;
-      if constexpr (E == 4) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-        o[0] += x * v.x, o[1] += x * v.y, o[2] += x * v.z, o[3] += x * v.w;
-      } else {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-        o[0] += x * v.x, o[1] += x * v.y;
-      }
+#pragma unroll
+    for (int i = 0; i < PX_JOIN; ++i) {
+      const float sum = (l[i].x + l[i].y) + (l[i].z + l[i].w), wt = px_ex2(m[i] - now);
+      if (sum == 0.f) continue;   // (none, or of a row that has seen no slot)
+      L += wt * sum;
+#pragma unroll
+      for (int z = 0; z < E; ++z) o[z] += wt * v[i][z];
     }
   }
   const float inv = L == 0.f ? 0.f : 1.0f / L;   // (a row that sees no slot: 0)
@@ -989,10 +1028,13 @@ static PxTiles px_tiles(int all) {
   return t;
 }
 
+// for px_div: n * (inv d - 2^32) < 2^32
+static uint32_t px_inv(int d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
+
 // floats for row_heads rows of hd (twice as many of half the size)
 size_t prefix_attention_scratch(int row_heads, int hd, int num_sms) {
-  const size_t rows = (size_t)2 * row_heads + (size_t)PX_ROWS * num_sms;
-  return 256 + 2 * (2 * rows + 64) + rows * std::max(hd, 128);
+  const size_t most = hd < 128 ? (size_t)row_heads * 2 : row_heads;
+  return std::max(256 + PxScratch::rows(row_heads, num_sms) * (5 + std::max(hd, 128)), 256 + PxScratch::rows(most, num_sms) * (5 + 64));
 }
 
 cudaError_t prefix_attention_prepare() {
@@ -1009,6 +1051,9 @@ cudaError_t prefix_attention_prepare() {
 cudaError_t launch_prefix_attention(const PrefixAttnParams& p0, int num_sms, cudaStream_t st, bool pdl) {
   PrefixAttnParams p = p0;
   p.ctas = num_sms;
+  p.G = p.H / p.Hk;
+  p.inv_g = px_inv(p.G);
+  p.inv_nq = px_inv(p.nq);
   p.tiles[0] = px_tiles(p.b * p.nq * (p.H / p.Hk));
   p.tiles[1] = px_tiles(p.nq * (p.H / p.Hk));
   return p.hd == 64 ? px_launch<64>(p, st, pdl) : px_launch<128>(p, st, pdl);
