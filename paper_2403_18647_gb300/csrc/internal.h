@@ -330,7 +330,8 @@ struct PagesParams {
   int *table, *refs, *len;  // as PageMap; committed lengths [batch]
   int* common;              // [batch] leading pages held together with sequence 0
   int *ids, *kinds;         // scratch: [n_pages], [max(n_pages, batch * ld)]
-  int* copies;              // scratch: [0] pages to copy, from [4]: source, destination, slots of each
+  int* copies;              // scratch, 16-byte aligned: [0] runs; from [4]: source, slots, first and number of the destinations
+                            // of each; from [4 + 4 n_pages]: destinations
   int batch, ld, cap, n_pages;
   const int* src;           // fork: [nb] where each sequence's pages come from (-1: none); null: seq0 is freed
   int seq0, nb, n;

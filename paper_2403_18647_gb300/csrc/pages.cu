@@ -10,7 +10,8 @@
 //
 // The tables are small (one CTA works on them, a few microseconds of dependent steps); what costs
 // is the copying, a page being 2 L H KV_PAGE hd values (33.5 MB of a 7B-shaped cache).  So the table
-// kernels write a list of (source, destination, slots) and a second kernel on every SM copies.
+// kernels list what to copy, a source page with all of its destinations, and a second kernel on every SM
+// copies: a source is read once.
 #include <algorithm>
 
 #include "common.cuh"
@@ -118,11 +119,13 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const __grid_con
 enum : int { KEEP = 0, FRESH = 1, COPY = 2 };
 
 __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_constant__ PagesParams p) {
-  __shared__ int first_s[PAGES_MAX_BATCH], end_s[PAGES_MAX_BATCH], at_s[PAGES_MAX_BATCH];
-  __shared__ int sums[PG_WARPS], s_copies;
+  __shared__ int first_s[PAGES_MAX_BATCH], end_s[PAGES_MAX_BATCH], at_s[PAGES_MAX_BATCH], part_s[PAGES_MAX_BATCH];
+  __shared__ int sums[PG_WARPS], s_copies, s_runs, s_ids[PG_THREADS];
+  __shared__ int old_s[PAGES_MAX_BATCH], new_s[PAGES_MAX_BATCH], rows_s[PAGES_MAX_BATCH];   // a sequence's copy
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int refs_mine = tid < p.n_pages ? __ldcg(p.refs + tid) : 1;   // (needed later; on its way now)
   for (int s = tid; s < p.nb; s += PG_THREADS) {
     const int len = __ldcg(p.len + p.seq0 + s);
     long long end = (long long)len + p.n;
@@ -131,28 +134,38 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
       end = p.cap;
     }
     first_s[s] = len / KV_PAGE;
+    part_s[s] = len % KV_PAGE;
     end_s[s] = max(len / KV_PAGE, (int)((end + KV_PAGE - 1) / KV_PAGE));
   }
-  if (tid == 0) s_copies = 0;
+  if (tid == 0) s_copies = s_runs = 0;
+  for (int s = tid; s < p.nb; s += PG_THREADS) rows_s[s] = 0;
   __syncthreads();
-  // what each wanted page needs
+  // what each wanted page needs; of a warp's first 32 it is kept, with the page that is there
+  int kind0 = KEEP, page0 = -1;
   for (int s = warp; s < p.nb; s += PG_WARPS) {
     int need = 0;
     for (int j0 = first_s[s]; j0 < end_s[s]; j0 += 32) {
       const int j = j0 + lane;
-      int kind = KEEP;
+      int kind = KEEP, page = -1;
       if (j < end_s[s]) {
-        const int page = __ldcg(p.table + (size_t)(p.seq0 + s) * p.ld + j);
+        page = __ldcg(p.table + (size_t)(p.seq0 + s) * p.ld + j);
         if (page < 0) {
           kind = FRESH;
         } else {
           int others = __ldcg(p.refs + page) - 1;
-          // earlier sequences of this call give their hold on it up
-          for (int t = 0; t < s && others > 0; ++t)
-            if (j >= first_s[t] && j < end_s[t] && __ldcg(p.table + (size_t)(p.seq0 + t) * p.ld + j) == page) --others;
+          if (others > 0) {
+            // earlier sequences of this call give their hold on it up (eight loads in flight)
+#pragma unroll 8
+            for (int t = 0; t < s; ++t)
+              if (j >= first_s[t] && j < end_s[t] && __ldcg(p.table + (size_t)(p.seq0 + t) * p.ld + j) == page) --others;
+          }
           if (others > 0) kind = COPY;
         }
         p.kinds[(size_t)s * p.ld + j] = kind;
+      }
+      if (s == warp && j0 == first_s[s]) {
+        kind0 = kind;
+        page0 = page;
       }
       need += __popc(__ballot_sync(0xffffffffu, kind != KEEP));
     }
@@ -169,10 +182,13 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
   int found = 0;
   for (int c0 = 0; c0 < p.n_pages && found < need; c0 += PG_THREADS) {
     const int page = c0 + tid;
-    const bool idle = page < p.n_pages && __ldcg(p.refs + page) == 0;
+    const bool idle = page < p.n_pages && (c0 == 0 ? refs_mine : __ldcg(p.refs + page)) == 0;
     int got;
     const int at = found + block_scan(idle, sums, &got);
-    if (idle && at < need) p.ids[at] = page;
+    if (idle && at < need) {
+      if (at < PG_THREADS) s_ids[at] = page;
+      else p.ids[at] = page;
+    }
     found += got;
   }
   __syncthreads();
@@ -185,22 +201,21 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
   }
   for (int s = warp; s < p.nb; s += PG_WARPS) {
     int at = at_s[s];
-    const int len = __ldcg(p.len + p.seq0 + s);
     for (int j0 = first_s[s]; j0 < end_s[s]; j0 += 32) {
       const int j = j0 + lane;
-      const int kind = j < end_s[s] ? p.kinds[(size_t)s * p.ld + j] : KEEP;
+      const bool kept = s == warp && j0 == first_s[s];
+      const int kind = kept ? kind0 : j < end_s[s] ? p.kinds[(size_t)s * p.ld + j] : KEEP;
       const unsigned who = __ballot_sync(0xffffffffu, kind != KEEP);
       if (kind != KEEP) {
         int* entry = p.table + (size_t)(p.seq0 + s) * p.ld + j;
-        const int page = __ldcg(p.ids + at + __popc(who & ((1u << lane) - 1u)));
+        const int i = at + __popc(who & ((1u << lane) - 1u)), page = i < PG_THREADS ? s_ids[i] : __ldcg(p.ids + i);
         if (kind == COPY) {
-          const int old = __ldcg(entry), rows = min(KV_PAGE, len - j * KV_PAGE);
+          const int old = kept ? page0 : __ldcg(entry), rows = j == first_s[s] ? part_s[s] : 0;   // committed ones
           atomicSub(p.refs + old, 1);
           if (rows > 0) {
-            int* c = p.copies + 4 + 3 * atomicAdd(&s_copies, 1);
-            c[0] = old;
-            c[1] = page;
-            c[2] = rows;
+            old_s[s] = old;
+            new_s[s] = page;
+            rows_s[s] = rows;
           }
         }
         __stcg(entry, page);
@@ -210,7 +225,27 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
     }
   }
   __syncthreads();
-  if (tid == 0) p.copies[0] = s_copies;
+  // the copies of one source side by side: a run for each first one of them
+  if (tid < p.nb && rows_s[tid] > 0) {
+    int same = 0, earlier = 0;
+    for (int t = 0; t < p.nb; ++t)
+      if (rows_s[t] == rows_s[tid] && old_s[t] == old_s[tid]) {
+        ++same;
+        earlier += t < tid;
+      }
+    if (earlier == 0) {
+      int at = atomicAdd(&s_copies, same);
+      int* run = p.copies + 4 + 4 * atomicAdd(&s_runs, 1);
+      run[0] = old_s[tid];
+      run[1] = rows_s[tid];
+      run[2] = at;
+      run[3] = same;
+      for (int t = tid; t < p.nb; ++t)
+        if (rows_s[t] == rows_s[tid] && old_s[t] == old_s[tid]) p.copies[4 + 4 * p.n_pages + at++] = new_s[t];
+    }
+  }
+  __syncthreads();
+  if (tid == 0) p.copies[0] = s_runs;
   common_pages(p);
 }
 
@@ -264,10 +299,12 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const __grid_
     if (held > 0) {
       const int to = __ldcg(p.ids + at);
       if (rows > 0) {
-        int* e = p.copies + 4 + 3 * c;
-        e[0] = page;
-        e[1] = to;
-        e[2] = rows;
+        int* run = p.copies + 4 + 4 * c;
+        run[0] = page;
+        run[1] = rows;
+        run[2] = c;
+        run[3] = 1;
+        p.copies[4 + 4 * p.n_pages + c] = to;
       }
       __stcg(p.refs + to, held);
       __stcg(p.refs + page, 0);
@@ -285,27 +322,92 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const __grid_
 }
 
 // ---- copying -------------------------------------------------------------------------------------
-// A warp copies the listed slots of one (page, layer, head) of K or of V: hd * 2 bytes a slot, in one
-// piece.
-__global__ void __launch_bounds__(256) pages_copy_kernel(const __grid_constant__ PagesParams p) {
+// Blocks of the committed slots of one (page, layer, head) of K or of V, at most KV_PAGE hd 2 = 16 KB in
+// one piece, go through a ring in shared memory by bulk copies: one in, one out for each destination.
+// One thread on an SM drives them, loads PC_AHEAD blocks ahead; the warp's lanes have the next 32
+// blocks' places.  A branch of a 7B-shaped cache into eight, 288 MB to move at the least: 61 us
+// in all, 103 with warps that copied through registers, 32 on an SM; a round of ten samples on a
+// 13B-shaped one, 693 MB: 111 and 208.
+constexpr int PC_SLOTS = 12, PC_AHEAD = 6;
+__device__ __forceinline__ void bulk_store_s2g(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+__global__ void __launch_bounds__(32) pages_copy_kernel(const __grid_constant__ PagesParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ uint64_t full[PC_SLOTS];
+  __shared__ volatile int abort;
+  const int lane = threadIdx.x;
+  if (lane == 0) {
+    for (int i = 0; i < PC_SLOTS; ++i) mbar_init(&full[i], 1);
+    abort = 0;
+    fence_mbar_init();
+  }
+  __syncwarp();
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const int count = __ldcg(p.copies);
-  const long long blocks = 2ll * p.L * p.H, total = blocks * count;
-  const long long step = (long long)gridDim.x * 8;
-  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += step) {
-    const int e = (int)(w % count);
-    const long long b = w / count;
-    const int h = (int)(b % p.H), l = (int)(b / p.H) >> 1;
-    const bool v = (b / p.H) & 1;
-    const int src = __ldcg(p.copies + 4 + 3 * e), dst = __ldcg(p.copies + 5 + 3 * e), rows = __ldcg(p.copies + 6 + 3 * e);
-    const long long page = (long long)KV_PAGE * p.hd;   // elements of one page and head
-    __nv_bfloat16* base = (v ? p.v : p.k) + ((long long)l * p.n_pages * p.H + h) * page;
-    const uint4* a = reinterpret_cast<const uint4*>(base + (long long)src * p.H * page);
-    uint4* z = reinterpret_cast<uint4*>(base + (long long)dst * p.H * page);
-    const int n = rows * p.hd / 8;
-    for (int i = lane; i < n; i += 32) __stcg(z + i, __ldcg(a + i));
+  const int runs = __ldcg(p.copies);
+  const long long total = 2ll * p.L * p.H * runs;
+  const int mine = (int)((total - blockIdx.x + gridDim.x - 1) / gridDim.x);   // blocks of this CTA
+  const long long page = (long long)KV_PAGE * p.hd;   // elements of one page and head
+  const int* to = p.copies + 4 + 4 * p.n_pages;
+  __nv_bfloat16* my_base = nullptr;   // of block (this group of 32) + lane: page 0 of its layer and head
+  int4 my_run = make_int4(0, 0, 0, 0);
+  int my_to = 0;
+  // block i: its base, run and first destination, from the lane that has them
+  auto places = [&](int group) {
+    const long long u = blockIdx.x + (long long)(32 * group + lane) * gridDim.x;
+    if (u < total) {
+      const long long b = u / runs;
+      const int h = (int)(b % p.H), l = (int)(b / p.H) >> 1;
+      my_base = (((b / p.H) & 1) ? p.v : p.k) + ((long long)l * p.n_pages * p.H + h) * page;
+      my_run = __ldcg(reinterpret_cast<const int4*>(p.copies + 4) + u % runs);
+      my_to = __ldcg(to + my_run.z);
+    }
+  };
+  auto at = [&](const __nv_bfloat16* base, int id) { return const_cast<__nv_bfloat16*>(base) + (long long)id * p.H * page; };
+  int loaded = 0, done = 0;
+  // loads and stores of a group of 32 blocks: the loads run ahead inside of it
+  for (int g = 0; 32 * g < mine; ++g) {
+    places(g);
+    const int end = min(mine, 32 * g + 32);
+    for (; done < end && !abort; ++done) {
+      for (; loaded < min(end, done + PC_AHEAD); ++loaded) {
+        const int from = loaded & 31;
+        const __nv_bfloat16* base = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_base), from));
+        const int src = __shfl_sync(0xffffffffu, my_run.x, from), rows = __shfl_sync(0xffffffffu, my_run.y, from);
+        if (lane == 0) {
+          const int slot = loaded % PC_SLOTS;
+          // what was stored from the slot has been read: at most PC_SLOTS - PC_AHEAD blocks since
+          asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PC_SLOTS - PC_AHEAD) : "memory");
+          const uint32_t bytes = rows * p.hd * 2;
+          mbar_arrive_expect_tx(&full[slot], bytes);
+          bulk_load_g2s(ring + (size_t)slot * page * 2, at(base, src), bytes, &full[slot]);
+        }
+      }
+      const int from = done & 31;
+      const __nv_bfloat16* base = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(my_base), from));
+      const int rows = __shfl_sync(0xffffffffu, my_run.y, from), first = __shfl_sync(0xffffffffu, my_run.z, from),
+                n = __shfl_sync(0xffffffffu, my_run.w, from), dst = __shfl_sync(0xffffffffu, my_to, from);
+      if (lane == 0) {
+        const int slot = done % PC_SLOTS;
+        if (mbar_wait_bounded(&full[slot], (done / PC_SLOTS) & 1, &abort, p.err)) {
+          for (int i = 0; i < n; ++i)
+            bulk_store_s2g(at(base, i == 0 ? dst : __ldcg(to + first + i)), ring + (size_t)slot * page * 2, rows * p.hd * 2);
+        }
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+      __syncwarp();
+    }
+  }
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (abort) {   // let the copies in flight land before the CTA exits
+      for (done = max(0, done - 1); done < loaded; ++done) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(&full[done % PC_SLOTS], (done / PC_SLOTS) & 1))
+          if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
+      }
+    }
   }
 }
 
@@ -338,7 +440,7 @@ __global__ void __launch_bounds__(256) pages_rows_kernel(const __grid_constant__
 }
 
 template <typename... A>
-cudaError_t launch_pages(void (*kernel)(A...), dim3 grid, int threads, cudaStream_t st, bool pdl,
+cudaError_t launch_pages(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool pdl,
                          std::common_type_t<A>... args) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -346,11 +448,13 @@ cudaError_t launch_pages(void (*kernel)(A...), dim3 grid, int threads, cudaStrea
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
+size_t pages_copy_smem(int hd) { return (size_t)PC_SLOTS * KV_PAGE * hd * 2; }
 }  // namespace
 
 cudaError_t pages_prepare() {
@@ -358,26 +462,28 @@ cudaError_t pages_prepare() {
   if (e == cudaSuccess) e = prefer_shared(pages_reserve_kernel);
   if (e == cudaSuccess) e = prefer_shared(pages_compact_kernel);
   if (e == cudaSuccess) e = prefer_shared(pages_copy_kernel);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(pages_copy_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pages_copy_smem(128));
   if (e == cudaSuccess) e = prefer_shared(pages_rows_kernel);
   return e;
 }
 
 cudaError_t launch_pages_fork(const PagesParams& p, cudaStream_t st, bool pdl) {
-  return launch_pages(pages_fork_kernel, dim3(1), PG_THREADS, st, pdl, p);
+  return launch_pages(pages_fork_kernel, dim3(1), PG_THREADS, 0, st, pdl, p);
 }
 cudaError_t launch_pages_reserve(const PagesParams& p, cudaStream_t st, bool pdl) {
-  return launch_pages(pages_reserve_kernel, dim3(1), PG_THREADS, st, pdl, p);
+  return launch_pages(pages_reserve_kernel, dim3(1), PG_THREADS, 0, st, pdl, p);
 }
 cudaError_t launch_pages_compact(const PagesParams& p, cudaStream_t st, bool pdl) {
-  return launch_pages(pages_compact_kernel, dim3(1), PG_THREADS, st, pdl, p);
+  return launch_pages(pages_compact_kernel, dim3(1), PG_THREADS, 0, st, pdl, p);
 }
 cudaError_t launch_pages_copy(const PagesParams& p, int num_sms, cudaStream_t st, bool pdl) {
-  return launch_pages(pages_copy_kernel, dim3(4 * num_sms), 256, st, pdl, p);
+  return launch_pages(pages_copy_kernel, dim3(num_sms), 32, pages_copy_smem(p.hd), st, pdl, p);
 }
 cudaError_t launch_pages_rows(const PagesParams& p, int layer, int slot0, void* k, void* v, bool write, cudaStream_t st,
                               bool pdl) {
   const long long pieces = 2ll * p.H * p.n * (p.hd / 8);
-  return launch_pages(pages_rows_kernel, dim3((unsigned)((pieces + 255) / 256)), 256, st, pdl, p, layer, slot0,
+  return launch_pages(pages_rows_kernel, dim3((unsigned)((pieces + 255) / 256)), 256, 0, st, pdl, p, layer, slot0,
                       static_cast<uint4*>(k), static_cast<uint4*>(v), write ? 1 : 0);
 }
 

@@ -173,7 +173,7 @@ struct sdsat_kv {
   CUtensorMap kmap, vmap;   // the caches as 2-D tensors for the attention kernel
   // a paged cache: k and v are [n_layers][pages][n_heads][KV_PAGE][head_dim]
   int pages = 0, page_ld = 0;   // pages of the pool (0: contiguous), entries of a sequence's table row
-  int* page_mem = nullptr;      // one allocation: table, refs, common, ids, kinds, copies
+  int* page_mem = nullptr;      // one allocation: copies, table, refs, ids, common, kinds
   int *table = nullptr, *refs = nullptr, *common = nullptr, *ids = nullptr, *kinds = nullptr, *copies = nullptr;
 
   PageMap map() const { return PageMap{table, refs, page_ld, pages}; }
@@ -875,8 +875,8 @@ static sdsat_status kv_create(sdsat_ctx* c, int batch, int max_len, int pages, s
   kv->page_ld = (max_len + KV_PAGE - 1) / KV_PAGE;
   const long long rows = c->cfg.n_layers * kv->layer_rows(c->cfg.n_heads);
   const size_t n = (size_t)rows * c->cfg.head_dim;
-  const size_t entries = (size_t)batch * kv->page_ld, list = 4 + 3 * (size_t)std::max(pages, batch);
-  const size_t page_ints = pages ? entries + 2 * (size_t)pages + batch + std::max<size_t>(pages, entries) + list : 0;
+  const size_t entries = (size_t)batch * kv->page_ld, list = 4 + 5 * (size_t)pages;
+  const size_t page_ints = pages ? list + entries + 2 * (size_t)pages + batch + std::max<size_t>(pages, entries) : 0;
   void *k = nullptr, *v = nullptr, *len = nullptr, *em = nullptr, *pm = nullptr;
   auto fail = [&](sdsat_status s) {
     cudaFree(k);
@@ -897,7 +897,7 @@ static sdsat_status kv_create(sdsat_ctx* c, int batch, int max_len, int pages, s
       cudaMemset(len, 0, batch * sizeof(int)) != cudaSuccess ||
       cudaMemset(em, 0, batch * sizeof(long long)) != cudaSuccess ||
       (pages && (cudaMemset(pm, 0, page_ints * sizeof(int)) != cudaSuccess ||
-                 cudaMemset(pm, 0xFF, entries * sizeof(int)) != cudaSuccess)) ||   // the table: -1
+                 cudaMemset(static_cast<int*>(pm) + list, 0xFF, entries * sizeof(int)) != cudaSuccess)) ||   // the table: -1
       cudaDeviceSynchronize() != cudaSuccess)
     return fail(SDSAT_ECUDA);
   if (rows > 0x7FFFFFFFll || !make_kvmap(&kv->kmap, k, rows, c->cfg.head_dim) ||
@@ -908,12 +908,12 @@ static sdsat_status kv_create(sdsat_ctx* c, int batch, int max_len, int pages, s
   kv->v = static_cast<__nv_bfloat16*>(v);
   kv->len = static_cast<int*>(len);
   if (pages) {
-    kv->page_mem = kv->table = static_cast<int*>(pm);
+    kv->page_mem = kv->copies = static_cast<int*>(pm);
+    kv->table = kv->copies + list;
     kv->refs = kv->table + entries;
     kv->ids = kv->refs + pages;
     kv->common = kv->ids + pages;
-    kv->copies = kv->common + batch;
-    kv->kinds = kv->copies + list;
+    kv->kinds = kv->common + batch;
   }
   *out = kv;
   return SDSAT_OK;
