@@ -819,9 +819,9 @@ cudaError_t launch_tree_prep(const int* parent, const int* len, int nb, int q, i
   return cudaLaunchKernelEx(&cfg, tree_prep_kernel, parent, len, nb, q, pos, anc, err);
 }
 
-// Slot len0 + i receives the K and V rows of slot len0 + n_i (i = 1..m; n_i >= i, so no
-// source is overwritten before it is read).  One CTA per (layer, head) and sequence, 16-byte
-// chunks.
+// Slot len0 + i receives the K and V rows of slot len0 + n_i (i = 1..m, n_i >= i).  One CTA per
+// (layer, head) and sequence; a thread moves a 16-byte column of every row, all of them read before
+// the first is written (row n_i may be the place of a later row).
 __global__ void tree_compact_kernel(const int* ws, int H, int hd, int cap, int batch, PageMap pages, __nv_bfloat16* kc,
                                     __nv_bfloat16* vc) {
   pdl_wait();
@@ -832,23 +832,32 @@ __global__ void tree_compact_kernel(const int* ws, int H, int hd, int cap, int b
   const int chunks = hd / 8;   // 16-byte chunks per row
   // this head's rows of the layer (a paged cache's rows are on pages of this sequence alone)
   const size_t off = pages.table ? ((size_t)l * pages.n * H + h) * KV_PAGE * hd : ((size_t)l * batch * H + h) * cap * hd;
-  for (int x = threadIdx.x; x < 2 * m * chunks; x += blockDim.x) {
-    const int which = x / (m * chunks), rem = x % (m * chunks);
-    const int i = 1 + rem / chunks, ch = rem % chunks;
-    const int n = __ldcg(w + 2 + i);
-    if (n == i || len0 + n >= cap) continue;
-    const long long from = cache_row(pages, s, len0 + n, H, cap, hd), to = cache_row(pages, s, len0 + i, H, cap, hd);
-    if (from < 0 || to < 0) continue;   // (the row was not written)
-    __nv_bfloat16* base = (which ? vc : kc) + off;
-    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(base + from) + ch);
-    __stcg(reinterpret_cast<uint4*>(base + to) + ch, v);
+  for (int x = threadIdx.x; x < 2 * chunks; x += blockDim.x) {
+    __nv_bfloat16* base = (x < chunks ? kc : vc) + off;
+    const int ch = x % chunks;
+    long long to[SDSAT_ATT_MAXQ];
+    uint4 v[SDSAT_ATT_MAXQ];
+#pragma unroll
+    for (int i = 1; i < SDSAT_ATT_MAXQ; ++i) {
+      to[i] = -1;
+      if (i > m) continue;
+      const int n = __ldcg(w + 2 + i);
+      if (n == i || len0 + n >= cap) continue;
+      const long long from = cache_row(pages, s, len0 + n, H, cap, hd);
+      if (from < 0) continue;   // (the row was not written)
+      to[i] = cache_row(pages, s, len0 + i, H, cap, hd);
+      v[i] = __ldcg(reinterpret_cast<const uint4*>(base + from) + ch);
+    }
+#pragma unroll
+    for (int i = 1; i < SDSAT_ATT_MAXQ; ++i)
+      if (to[i] >= 0) __stcg(reinterpret_cast<uint4*>(base + to[i]) + ch, v[i]);
   }
 }
 
 cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int cap, int batch, const PageMap& pages,
                                 __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t st, bool pdl) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = make_cfg(dim3(L * H, nb), dim3(64), st, pdl, attr);
+  cudaLaunchConfig_t cfg = make_cfg(dim3(L * H, nb), dim3(32), st, pdl, attr);
   return cudaLaunchKernelEx(&cfg, tree_compact_kernel, ws, H, hd, cap, batch, pages, k, v);
 }
 
