@@ -51,31 +51,6 @@ __device__ __forceinline__ float lp_ex2(float x) {
   return y;
 }
 
-// two fp32 values at a time
-__device__ __forceinline__ uint64_t lp_pack(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void lp_unpack(uint64_t v, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-}
-__device__ __forceinline__ uint64_t lp_add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t lp_mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t lp_fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
 // larger key = earlier alternative: the logit's order in the high half, the id's inverse in the low
 // (every key is above 0)
 __device__ __forceinline__ unsigned long long lp_key(float x, int id) {
@@ -343,24 +318,24 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
               add(isnan(x) ? -INFINITY : x);
             }
         } else {
-          const uint64_t m2 = lp_pack(-s.m, -s.m), c2 = lp_pack(c, c);
-          uint64_t S2 = lp_pack(s.S, 0.f), E2 = lp_pack(s.E, 0.f);
+          const uint64_t m2 = f2_pack(-s.m, -s.m), c2 = f2_pack(c, c);
+          uint64_t S2 = f2_pack(s.S, 0.f), E2 = f2_pack(s.E, 0.f);
 #pragma unroll
           for (int u = 0; u < LP_UNROLL; ++u)
 #pragma unroll
             for (int k = 0; k < E; k += 2) {
-              const uint64_t d2 = lp_add2(lp_pack(value(r[u], k), value(r[u], k + 1)), m2);
+              const uint64_t d2 = f2_add(f2_pack(value(r[u], k), value(r[u], k + 1)), m2);
               float da, db, ea, eb;
-              lp_unpack(lp_mul2(d2, c2), ea, eb);
-              const uint64_t e2 = lp_pack(lp_ex2(ea), lp_ex2(eb));
-              S2 = lp_add2(S2, e2);
-              lp_unpack(d2, da, db);
-              E2 = lp_fma2(e2, lp_pack(fmaxf(da, -FLT_MAX), fmaxf(db, -FLT_MAX)), E2);
+              f2_unpack(f2_mul(d2, c2), ea, eb);
+              const uint64_t e2 = f2_pack(lp_ex2(ea), lp_ex2(eb));
+              S2 = f2_add(S2, e2);
+              f2_unpack(d2, da, db);
+              E2 = f2_fma(e2, f2_pack(fmaxf(da, -FLT_MAX), fmaxf(db, -FLT_MAX)), E2);
             }
           float b;
-          lp_unpack(S2, s.S, b);
+          f2_unpack(S2, s.S, b);
           s.S += b;
-          lp_unpack(E2, s.E, b);
+          f2_unpack(E2, s.E, b);
           s.E += b;
         }
         // the logits before the token, and those to note: most vectors have neither

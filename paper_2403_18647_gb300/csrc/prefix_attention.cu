@@ -31,8 +31,10 @@
 // slot's) until the end.
 //
 // The tensor cores cut off what an addition to their fp32 accumulator cannot hold, so that an error of
-// half a unit grows with every 16 slots added (2.4 times the error of fp32 products at 40 units).
-// After PX_RUN units O is therefore added, rounded, to a total in TMEM and begun anew.
+// half a unit in the last place grows with every 16 slots added.  After PX_RUN units O is therefore
+// added, rounded, to a total in TMEM and begun anew (16x4 rows of 7B heads after 16500 slots: an error of
+// 0.9e-6 and 107 us; 1.4e-6 and 104 with 8 units, 2.4e-6 and 102 with 16, 5.9e-6 without; fp32
+// products in a row 2.5e-6).
 //
 // The three parts are side by side in B (N = three times the rows) and their products in columns of
 // their own, added up when they are read: 8 MMAs a tile of K or V instead of 24.  An MMA takes N / 2
@@ -67,7 +69,7 @@ constexpr int PX_O = PX_PARTS * PX_ROWS;   // TMEM column of O (S from 0 on)
 constexpr int PX_O_STEP = 160;    // to the second O, for segments of at most PX_TWICE rows
 constexpr int PX_TWICE = 32;      // rows of segments whose queries, and whose O, fit twice
 constexpr int PX_TOTAL = 448;     // TMEM column of the total that O is added to
-constexpr int PX_RUN = 16;        // units of a segment
+constexpr int PX_RUN = 4;         // units that O takes before it is added to the total
 static_assert(PX_O + PX_O_STEP + PX_PARTS * PX_TWICE <= PX_TOTAL && PX_O + PX_PARTS * PX_ROWS <= PX_TOTAL, "columns");
 constexpr int PX_MAX_B = 64;
 constexpr float PX_LAZY = 8.0f;   // log2 of the growth of a row maximum that is left unscaled
@@ -106,23 +108,21 @@ __device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that
   return x < 0 ? g / (q + 1) : r + x / q;
 }
 
-// a run of at most PX_RUN units of one item
+// a CTA's units of one item
 struct PxSeg {
   int s;                   // sequence, or -1: the shared pages
   int hk, row0, rows;      // cache head, rows [row0, row0 + rows) of its R
   int u0, u1;              // units; none: the share has ended
-  int from;                // the item's first unit in the CTA's share
   int slot0, end, len;     // unit u: slots slot0 + 128 u .., those below `end`; committed below len
-  int q_at, o_at;          // 0 or 1: which half of the queries' space, which O
-  int whole;               // it takes the whole space, or the segment before does
-  int goes_on, more;       // it goes on where the CTA's segment before ended; the next one goes on
+  int q_at;                // 0 or 1: which half of the queries' space
+  int whole;               // it takes the whole space of queries and O, or the segment before does
   __device__ int cols() const { return (rows + 15) / 16 * 16; }
 };
 struct PxMisc {
   PxSched sched;
   int len[PX_MAX_B];
   uint32_t top[3][PX_ROWS];   // a row's maximum over the unit, as px_order
-  __align__(16) float m[PX_ROWS];   // the rows' references
+  __align__(16) float minus_m[PX_ROWS];   // the rows' references, negative
   float by[PX_ROWS];       // the rescaling of what is there
   __align__(16) uint16_t seen[PX_SEGS][PX_ROWS];     // the block rows that a row sees
   PxSeg seg[PX_SEGS];
@@ -172,8 +172,7 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
     e.len = len[near];
     e.end = min(e.len + p.nq, p.ld * KV_PAGE);
   }
-  e.u1 = min(e.u0 + PX_RUN, min(U, e.u0 + gend - g));
-  e.more = e.u1 < min(U, e.u0 + gend - g);
+  e.u1 = min(U, e.u0 + gend - g);
   return e;
 }
 
@@ -228,12 +227,13 @@ __device__ __forceinline__ float px_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// two values as packed bf16 (a in the low half); what is left of them stays in a and b
-__device__ __forceinline__ uint32_t px_part(float& a, float& b) {
+// two values as packed bf16; what is left of them stays in v
+__device__ __forceinline__ uint32_t px_part(uint64_t& v) {
+  float a, b;
+  f2_unpack(v, a, b);
   uint32_t h;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(b), "f"(a));
-  a -= __uint_as_float(h << 16);
-  b -= __uint_as_float(h & 0xFFFF0000u);
+  v = f2_sub(v, f2_pack(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u)));
   return h;
 }
 __device__ __forceinline__ bool px_bar_or(int id, bool pred) {   // over a group's 128 threads
@@ -326,7 +326,6 @@ __device__ __noinline__ void px_queries(const PrefixAttnParams& p, PxMisc& sm, u
     const int tr = px_div(x.row0 + i0, p.inv_g);   // token row
     sm.seen[seg % PX_SEGS][i0] = (uint16_t)(i0 >= x.rows ? 0u : p.anc ? __ldcg(p.anc + tr) : (2u << (tr - px_div(tr, p.inv_nq) * p.nq)) - 1u);
   }
-  if (x.goes_on) return;   // (they are there)
   uint8_t* base = Qs + x.q_at * C::Q_SECOND;
 #pragma unroll 1
   for (int i = i0; i < total; i += 2 * n) {
@@ -356,15 +355,15 @@ __device__ __noinline__ void px_queries(const PrefixAttnParams& p, PxMisc& sm, u
         *reinterpret_cast<uint4*>(dst) = w[z];
         continue;
       }
-      float v[8] = {__uint_as_float(w[z].x),  __uint_as_float(w[z].y),  __uint_as_float(w[z].z),  __uint_as_float(w[z].w),
-                    __uint_as_float(w1[z].x), __uint_as_float(w1[z].y), __uint_as_float(w1[z].z), __uint_as_float(w1[z].w)};
+      uint64_t v[4] = {(uint64_t)w[z].y << 32 | w[z].x, (uint64_t)w[z].w << 32 | w[z].z, (uint64_t)w1[z].y << 32 | w1[z].x,
+                       (uint64_t)w1[z].w << 32 | w1[z].z};
 #pragma unroll
       for (int part = 0; part < PX_PARTS; ++part) {
         uint4 o;
-        o.x = px_part(v[0], v[1]);
-        o.y = px_part(v[2], v[3]);
-        o.z = px_part(v[4], v[5]);
-        o.w = px_part(v[6], v[7]);
+        o.x = px_part(v[0]);
+        o.y = px_part(v[1]);
+        o.z = px_part(v[2]);
+        o.w = px_part(v[3]);
         *reinterpret_cast<uint4*>(dst + part * cols * 128) = o;
       }
     }
@@ -466,7 +465,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   // where a segment's results go: the rows of an item from its first unit on, or those of the CTA's
   // first segment, which continues one
   auto scratch_row = [&](const PxSeg& x) {
-    return x.from > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
+    return x.u0 > 0 ? (size_t)2 * p.b * p.nq * p.H + (size_t)PX_ROWS * blockIdx.x
                     : (size_t)(x.s < 0 ? 0 : p.b * p.nq * p.H) + (size_t)x.hk * R + x.row0;
   };
 
@@ -490,19 +489,15 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     // ---- the segments
     if (lane == 0) {
       const int g1 = sm.sched.begin(blockIdx.x + 1);
-      int near = 0, rows = 0, q_at = 1, goes_on = 0, from = 0;
+      int near = 0, rows = 0, q_at = 1;
 #pragma unroll 1
       for (int i = 0, g = sm.sched.begin(blockIdx.x);; ++i) {
         PxSeg e{};
         if (g < g1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
         g += e.u1 - e.u0;
-        e.goes_on = goes_on;
-        e.from = from = goes_on ? from : e.u0;
-        e.q_at = q_at = goes_on ? q_at : e.rows <= PX_TWICE ? q_at ^ 1 : 0;
-        e.o_at = e.rows <= PX_TWICE ? i & 1 : 0;
+        e.q_at = q_at = e.rows <= PX_TWICE ? q_at ^ 1 : 0;
         e.whole = max(rows, e.rows) > PX_TWICE;
         rows = e.rows;
-        goes_on = e.more;
         wait(&sm.seg_empty[i % PX_SEGS], ((i / PX_SEGS) & 1) ^ 1);
         sm.seg[i % PX_SEGS] = e;
         mbar_arrive(&sm.seg_full[i % PX_SEGS]);
@@ -607,28 +602,36 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
     } else {
       const uint64_t vd = px_desc_mn(smem_u32(smem), C::HALF), pd = px_desc_mn(smem_u32(Ps), C::P_PART);
+      int run = 0;
 #pragma unroll 1
       for (int seg = 0;; ++seg) {
         const PxSeg& e = segment(seg);
         if (e.u0 == e.u1) break;
         const uint32_t idesc = idesc_bf16_f32(128, p_parts * e.cols()) | (1u << 15) | (1u << 16);   // both MN-major
-        const uint32_t o = tmem + PX_O + PX_O_STEP * e.o_at;
-        const int before = seg - (e.whole ? 1 : 2);   // O: its results have left
-        if (before >= 0) ready(&sm.o_empty[before & 1], (before >> 1) & 1);
+        uint32_t o = 0;
 #pragma unroll 1
         for (int u = e.u0; u < e.u1; ++u, ++k) {
+          const int in_run = (u - e.u0) % PX_RUN;
+          if (in_run == 0) {   // O: the last or the last but one run has been read
+            o = tmem + PX_O + (e.rows <= PX_TWICE ? PX_O_STEP * (run & 1) : 0);
+            const int before = run - (e.rows > PX_TWICE || (u == e.u0 && e.whole) ? 1 : 2);
+            if (before >= 0) ready(&sm.o_empty[before & 1], (before >> 1) & 1);
+          }
           const int slot = (2 * k + 1) % NS, steps = (min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT) + 15) / 16;   // 16 slots each
           const uint64_t a0 = vd + (uint64_t)(slot * (C::TILE >> 4));
           ready(&sm.full[slot], ((2 * k + 1) / NS) & 1);
           ready(&sm.p_full, k & 1);
           if (!sm.abort) {
 #pragma unroll 1
-            for (int kk = 0; kk < steps; ++kk) px_mma(o, a0 + kk * 128, pd + kk * 128, idesc, u > e.u0 || kk ? 1u : 0u, mine);
+            for (int kk = 0; kk < steps; ++kk) px_mma(o, a0 + kk * 128, pd + kk * 128, idesc, in_run || kk ? 1u : 0u, mine);
           }
           commit(&sm.p_empty);
           commit(&sm.empty[slot]);
+          if (in_run == PX_RUN - 1 || u + 1 == e.u1) {
+            commit(&sm.o_full[run & 1]);
+            ++run;
+          }
         }
-        commit(&sm.o_full[seg & 1]);
         if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
       }
     }
@@ -649,70 +652,77 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     auto queries = [&](int j) {   // of segment j, once those of segment j - (whole ? 1 : 2) are done with
       const PxSeg& y = sm.seg[j % PX_SEGS];
       const int before = j - (y.whole ? 1 : 2);
-      if (before >= 0 && !y.goes_on) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
+      if (before >= 0) wait(&sm.q_empty[before & 1], (before >> 1) & 1);
       px_queries<HD>(p, sm, Qs, y, j, st, 128);
       fence_proxy_async_smem();
       arrive(&sm.q_full[j & 1]);
     };
     if (sm.seg[0].u0 < sm.seg[0].u1) arrive(&sm.q_full[0]);   // (in place: first_queries)
+    int run = 0;
 #pragma unroll 1
     for (int seg = 0, j = 1; segment(seg).u0 < segment(seg).u1; ++seg) {
-#pragma unroll 1
-      for (; j <= seg + 2; ++j) {
-        const PxSeg& y = segment(j);
-        if (y.u0 == y.u1 || (j == seg + 2 && y.whole)) break;
-        queries(j);
-      }
       const PxSeg& x = sm.seg[seg % PX_SEGS];
       const int cols = x.cols();
       const size_t row = scratch_row(x);
-      wait(&sm.o_full[seg & 1], (seg >> 1) & 1);
-      __syncwarp();
-      tc_fence_after();
 #pragma unroll 1
-      for (int r = 0; r < x.rows; r += 8) {
-        float o[8], o1[8], o2[8];
-        const uint32_t at = tmem + lanes + PX_O + PX_O_STEP * x.o_at + r, total = tmem + lanes + PX_TOTAL + r;
-        px_ld8(at, o);
-        px_ld8(at + cols, o1);
-        if (p_parts > 2) px_ld8(at + 2 * cols, o2);
-        tmem_wait_ld();
-#pragma unroll
-        for (int z = 0; z < 8; ++z) {
-          o[z] += o1[z];
-          if (p_parts > 2) o[z] += o2[z];
+      for (int u = x.u0; u < x.u1; u += PX_RUN, ++run) {
+        const bool more = u + PX_RUN < x.u1;
+        if (!more) {   // (the scores of the segment's last units need what its runs before have left)
+#pragma unroll 1
+          for (; j <= seg + 2; ++j) {
+            const PxSeg& y = segment(j);
+            if (y.u0 == y.u1 || (j == seg + 2 && y.whole)) break;
+            queries(j);
+          }
         }
-        if (x.goes_on) {
-          px_ld8(total, o1);
+        wait(&sm.o_full[run & 1], (run >> 1) & 1);
+        __syncwarp();
+        tc_fence_after();
+#pragma unroll 1
+        for (int r = 0; r < x.rows; r += 8) {
+          float o[8], o1[8], o2[8];
+          const uint32_t at = tmem + lanes + PX_O + (x.rows <= PX_TWICE ? PX_O_STEP * (run & 1) : 0) + r, total = tmem + lanes + PX_TOTAL + r;
+          px_ld8(at, o);
+          px_ld8(at + cols, o1);
+          if (p_parts > 2) px_ld8(at + 2 * cols, o2);
           tmem_wait_ld();
 #pragma unroll
-          for (int z = 0; z < 8; ++z) o[z] += o1[z];
-        }
-        if (x.more) {
-          px_st8(total, o);
-          continue;
-        }
-        float* dst = scratch.o + (row + r) * HD + st;
+          for (int z = 0; z < 8; ++z) {
+            o[z] += o1[z];
+            if (p_parts > 2) o[z] += o2[z];
+          }
+          if (u > x.u0) {
+            px_ld8(total, o1);
+            tmem_wait_ld();
 #pragma unroll
-        for (int z = 0; z < 8; ++z)
-          if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
+            for (int z = 0; z < 8; ++z) o[z] += o1[z];
+          }
+          if (more) {
+            px_st8(total, o);
+            continue;
+          }
+          float* dst = scratch.o + (row + r) * HD + st;
+#pragma unroll
+          for (int z = 0; z < 8; ++z)
+            if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
+        }
+        if (more) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        arrive(&sm.o_empty[run & 1]);
       }
-      if (x.more) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-      tc_fence_before();
-      arrive(&sm.o_empty[seg & 1]);
       if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
     }
   } else {
     const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float c = rsqrtf((float)HD) * 1.4426950408889634f;
+    const uint64_t c2 = f2_pack(c, c);
     auto ready = [&](uint64_t* bar, uint32_t parity) {
       wait(bar, parity);
       __syncwarp();
       tc_fence_after();
     };
-    int k = 0;
-    int moves = 0;
+    int k = 0, moves = 0, run0 = 0;   // units, new references, runs of the segments before
     float m_mine = 0.f;     // the reference of the lane's row
     float l[8 * PX_MINE];   // the rows' sums of this thread's slots
 #pragma unroll 1
@@ -723,10 +733,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       const int cols = x.cols(), mine = (cols / 8 - wg + PX_GROUPS - 1) / PX_GROUPS;
       auto first_row = [&](int i) { return 8 * (wg + PX_GROUPS * i); };
       const uint16_t* seen = sm.seen[seg % PX_SEGS];
-      if (!x.goes_on) {
 #pragma unroll
-        for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
-      }
+      for (int i = 0; i < 8 * PX_MINE; ++i) l[i] = 0.f;
       // the row that the lane looks after in its warp: 8 of the first piece, 8 of the second
       const int my_row = lane < 8 * mine ? first_row(lane >> 3) + (lane & 7) : 0;
 #pragma unroll 1
@@ -747,7 +755,9 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             tmem_wait_ld();
             if (q_parts > 1) {
 #pragma unroll
-              for (int z = 0; z < 8; ++z) s[8 * i + z] += a[z] + b[z];
+              for (int z = 0; z < 8; z += 2)
+                f2_unpack(f2_add(f2_pack(s[8 * i + z], s[8 * i + z + 1]), f2_add(f2_pack(a[z], a[z + 1]), f2_pack(b[z], b[z + 1]))),
+                          s[8 * i + z], s[8 * i + z + 1]);
             }
           }
         tc_fence_before();
@@ -770,16 +780,19 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             }
         }
         // the rows' references: the first unit's maxima, and new ones where a score passes them by far
-        const bool first = u == x.u0 && !x.goes_on;
+        const bool first = u == x.u0;
         bool move = first;
         if (!first) {
           float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 8 * PX_MINE; i += 4)
             if (i < 8 * mine) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.m[first_row(i >> 3) + (i & 4)]);
-              top = fmaxf(fmaxf(top, fmaf(s[i], c, -m.x)), fmaf(s[i + 1], c, -m.y));
-              top = fmaxf(fmaxf(top, fmaf(s[i + 2], c, -m.z)), fmaf(s[i + 3], c, -m.w));
+              const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sm.minus_m[first_row(i >> 3) + (i & 4)]);
+              float a, b;
+              f2_unpack(f2_fma(f2_pack(s[i], s[i + 1]), c2, m.x), a, b);
+              top = fmaxf(fmaxf(top, a), b);
+              f2_unpack(f2_fma(f2_pack(s[i + 2], s[i + 3]), c2, m.y), a, b);
+              top = fmaxf(fmaxf(top, a), b);
             }
           move = px_bar_or(1 + wg, top > PX_LAZY);
         }
@@ -807,19 +820,21 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             top = px_unorder(sm.top[now_at][my_row]) * c;
             const float old = first ? PX_UNSET : m_mine;
             m_mine = top == -INFINITY ? old : fmaxf(old, top);
-            sm.m[my_row] = m_mine;
+            sm.minus_m[my_row] = -m_mine;
             sm.by[my_row] = px_ex2(old - m_mine);
           }
           __syncwarp();
           if (!first) {
-            if (x.goes_on) ready(&sm.o_empty[(seg - 1) & 1], ((seg - 1) >> 1) & 1);   // the total is complete
-            ready(&sm.p_empty, (k - 1) & 1);   // and O holds the units before
+            // O holds the run's units before, the total the runs before
+            const int runs = (u - x.u0) / PX_RUN, now = run0 + runs, total = runs > 0;
+            if (total) ready(&sm.o_empty[(now - 1) & 1], ((now - 1) >> 1) & 1);
+            ready(&sm.p_empty, (k - 1) & 1);
 #pragma unroll 1
-            for (int part = u > x.u0 ? 0 : p_parts; part < p_parts + x.goes_on; ++part)
+            for (int part = (u - x.u0) % PX_RUN ? 0 : p_parts; part < p_parts + total; ++part)
 #pragma unroll 1
               for (int i = 0; i < mine; ++i) {
                 const uint32_t at =
-                    tmem + lanes + first_row(i) + (part < p_parts ? PX_O + PX_O_STEP * x.o_at + part * cols : PX_TOTAL);
+                    tmem + lanes + first_row(i) + (part < p_parts ? PX_O + (x.rows <= PX_TWICE ? PX_O_STEP * (now & 1) : 0) + part * cols : PX_TOTAL);
                 float o[8];
                 px_ld8(at, o);
                 tmem_wait_ld();
@@ -837,26 +852,28 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll
         for (int i = 0; i < PX_MINE; ++i)
           if (i < mine) {
-            float v[8];
+            uint64_t v[4];
 #pragma unroll
-            for (int z = 0; z < 8; z += 4) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.m[first_row(i) + z]);
-              v[z] = px_ex2(fmaf(s[8 * i + z], c, -m.x));
-              v[z + 1] = px_ex2(fmaf(s[8 * i + z + 1], c, -m.y));
-              v[z + 2] = px_ex2(fmaf(s[8 * i + z + 2], c, -m.z));
-              v[z + 3] = px_ex2(fmaf(s[8 * i + z + 3], c, -m.w));
+            for (int z = 0; z < 4; z += 2) {
+              const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sm.minus_m[first_row(i) + 2 * z]);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int at = 8 * i + 2 * (z + y);
+                float a, b;
+                f2_unpack(f2_fma(f2_pack(s[at], s[at + 1]), c2, y ? m.y : m.x), a, b);
+                v[z + y] = f2_pack(px_ex2(a), px_ex2(b));
+                f2_unpack(f2_add(f2_pack(l[at], l[at + 1]), v[z + y]), l[at], l[at + 1]);
+              }
             }
-#pragma unroll
-            for (int z = 0; z < 8; ++z) l[8 * i + z] += v[z];
 #pragma unroll
             for (int part = 0; part < PX_PARTS; ++part) {
               if (part < p_parts) {   // B's columns: the parts side by side
                 const int ch = part * cols / 8 + wg + PX_GROUPS * i;
                 uint4 o;
-                o.x = px_part(v[0], v[1]);
-                o.y = px_part(v[2], v[3]);
-                o.z = px_part(v[4], v[5]);
-                o.w = px_part(v[6], v[7]);
+                o.x = px_part(v[0]);
+                o.y = px_part(v[1]);
+                o.z = px_part(v[2]);
+                o.w = px_part(v[3]);
                 *reinterpret_cast<uint4*>(Ps + (ch >> 3) * C::P_PART + e * 128 + (((ch & 7) ^ (e & 7)) << 4)) = o;
               }
             }
@@ -881,17 +898,16 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         arrive(&sm.p_full);
       }
       // ---- the rows' references and sums (a warp's part of them) for the results
-      if (!x.more) {
-        const size_t row = scratch_row(x);
+      const size_t row = scratch_row(x);
 #pragma unroll
-        for (int i = 0; i < PX_MINE; ++i)
-          if (i < mine) {
-            const float sum = px_across(l + 8 * i, lane, [](float a, float b) { return a + b; });
-            const int r = first_row(i) + lane;
-            if (lane < 8 && r < x.rows) reinterpret_cast<float*>(scratch.l + row + r)[warp & 3] = sum;
-          }
-        if ((warp & 3) == 0 && lane < 8 * mine && my_row < x.rows) scratch.m[row + my_row] = m_mine;
-      }
+      for (int i = 0; i < PX_MINE; ++i)
+        if (i < mine) {
+          const float sum = px_across(l + 8 * i, lane, [](float a, float b) { return a + b; });
+          const int r = first_row(i) + lane;
+          if (lane < 8 && r < x.rows) reinterpret_cast<float*>(scratch.l + row + r)[warp & 3] = sum;
+        }
+      if ((warp & 3) == 0 && lane < 8 * mine && my_row < x.rows) scratch.m[row + my_row] = m_mine;
+      run0 += (x.u1 - x.u0 + PX_RUN - 1) / PX_RUN;
       arrive(&sm.seg_empty[seg % PX_SEGS]);
     }
   }
@@ -980,13 +996,13 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
   const size_t op = (size_t)r * p.H * HD + (size_t)h * HD + E * lane;
 #pragma unroll
   for (int i = 0; i < E; i += 2) {
-    float a = o[i], b = o[i + 1];
-    const uint32_t hi = px_part(a, b);
+    uint64_t v = f2_pack(o[i], o[i + 1]);
+    const uint32_t hi = px_part(v);
     if (p.bf16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + out + i) = hi;
     else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + out + i) = make_float2(o[i], o[i + 1]);
     if (p.out_hi) {
       *reinterpret_cast<uint32_t*>(p.out_hi + op + i) = hi;
-      *reinterpret_cast<uint32_t*>(p.out_lo + op + i) = px_part(a, b);
+      *reinterpret_cast<uint32_t*>(p.out_lo + op + i) = px_part(v);
     }
   }
 }
