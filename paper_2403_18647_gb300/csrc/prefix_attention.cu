@@ -13,8 +13,8 @@
 //
 // Work: items are (cache head, tile of up to PX_ROWS rows) of the shared pages and (sequence, cache
 // head, tile) of the others; units are 128 slots of an item.  The units, items in order, are divided
-// evenly among the CTAs (one on an SM), so that every CTA streams the same bytes; an item's partial
-// results from the CTAs that share it are merged by a second kernel, a warp for each row and head.
+// among the CTAs (one on an SM) by what they cost; an item's partial results from the CTAs that share it
+// are merged by a second kernel, a warp for each row and head.
 //
 // Per unit, on tcgen05 in the form that puts the slots on the 128 lanes (the rows, often few, are
 // the N of the products, so they do not pad to 128):
@@ -91,19 +91,31 @@ struct PxCfg {
   static constexpr size_t OFF_MISC = OFF_Q + HALVES * Q_HALF;
 };
 
-// what the CTAs agree on; the first one leaves it for the merge
+// What the CTAs agree on; the first one leaves it for the merge.  Shares are counted in places: those of an
+// item are some for its start and then some for each of its units, which belongs to the CTA that has its
+// first one.
+struct PxCost {
+  int start, unit;
+};
 struct PxSched {
   int shared;              // pages that all sequences share, whole and committed
-  int up;                  // units of an item of the shared pages
-  int tp;                  // units of all of them
-  int total;
-  int q, r;                // units of a CTA's share; the first r CTAs have one more
-  int cum[PX_MAX_B + 1];   // units of the items of the sequences before
+  int q, r;                // places of a CTA's share; the first r CTAs have one more
+  int tp;                  // places of the items of the shared pages
+  int units;               // units of one of them
+  PxCost cost[2];          // of the items of the shared pages, of the others
+  int cum[PX_MAX_B + 1];   // places of the items of the sequences before
   __device__ int begin(int c) const { return c * q + min(c, r); }
+  __device__ int places(int k, int units) const { return units > 0 ? cost[k].start + units * cost[k].unit : 0; }
 };
+// What an item of that many rows costs: 1.3 us a unit and as much for the start with up to 32 rows, 2 us
+// (1.65 of 16 bits) and 2.6 with more, by the ends of the CTAs of four cases.  (16x4 rows of 7B heads
+// after 16500 slots: 101 us, 106 with shares of as many units; 64 rows of 16 bits after 8200: 57, 65.)
+__device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
+  return rows > 32 ? PxCost{8, bf16 ? 5 : 6} : PxCost{4, 4};
+}
 // n / d for n < 2^16, inv = px_inv(d)
 __device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
-__device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has unit g
+__device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has place g
   const int x = g - (q + 1) * r;
   return x < 0 ? g / (q + 1) : r + x / q;
 }
@@ -136,43 +148,41 @@ struct PxMisc {
   uint32_t pages_ok[8];    // by unit: its pages are in the pool (bits 0, 1)
 };
 
-// the segment that starts at unit g and ends at the item's end or at gend; `near`: no later sequence
-// than its own
-__device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int g, int gend, int& near) {
-  const int G = p.G;
-  PxSeg e;
-  int U, rt;
-  if (g < sc.tp) {
-    const PxTiles& t = p.tiles[0];
-    U = sc.up;
-    const int item = g / U;
-    e.u0 = g - item * U;
-    e.hk = item / t.n;
-    rt = item - e.hk * t.n;
-    e.s = -1;
-    e.row0 = rt * t.rows;
-    e.rows = min(t.rows, p.b * p.nq * G - e.row0);
-    e.slot0 = 0;
-    e.end = e.len = sc.shared * KV_PAGE;
-  } else {
-    const PxTiles& t = p.tiles[1];
-    int x = g - sc.tp;
+// the segment that starts at place g and ends at the item's end or at gend, where g goes (it may have no
+// units); `near`: no later sequence than its own
+__device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const int* len, int& g, int gend, int& near) {
+  const int k = g < sc.tp ? 0 : 1;
+  const PxTiles& t = p.tiles[k];
+  PxSeg e{};
+  int x = g, places = sc.places(0, sc.units), units = sc.units;
+  if (k) {
+    x -= sc.tp;
 #pragma unroll 1
     while (sc.cum[near + 1] <= x) ++near;
     x -= sc.cum[near];
-    U = (sc.cum[near + 1] - sc.cum[near]) / (p.Hk * t.n);
-    const int item = x / U;
-    e.u0 = x - item * U;
-    e.hk = item / t.n;
-    rt = item - e.hk * t.n;
+    places = (sc.cum[near + 1] - sc.cum[near]) / (p.Hk * t.n);
+    units = (places - sc.cost[1].start) / sc.cost[1].unit;
+  }
+  const int item = x / places, at = x - item * places, n = min(places - at, gend - g), rt = item % t.n;
+  e.hk = item / t.n;
+  if (k) {
     e.s = near;
-    e.row0 = near * p.nq * G + rt * t.rows;
-    e.rows = min(t.rows, p.nq * G - rt * t.rows);
+    e.row0 = near * p.nq * p.G + rt * t.rows;
+    e.rows = min(t.rows, p.nq * p.G - rt * t.rows);
     e.slot0 = sc.shared * KV_PAGE;
     e.len = len[near];
     e.end = min(e.len + p.nq, p.ld * KV_PAGE);
+  } else {
+    e.s = -1;
+    e.row0 = rt * t.rows;
+    e.rows = min(t.rows, p.b * p.nq * p.G - e.row0);
+    e.end = e.len = sc.shared * KV_PAGE;
   }
-  e.u1 = min(U, e.u0 + gend - g);
+  const PxCost c = sc.cost[k];
+  auto unit = [&](int place) { return min(units, (max(0, place - c.start) + c.unit - 1) / c.unit); };   // the first one from there on
+  e.u0 = unit(at);
+  e.u1 = unit(at + n);
+  g += n;
   return e;
 }
 
@@ -422,9 +432,16 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       if (s1 < p.b) shared = min(shared, min(__ldcg(p.common + s1), n1 / KV_PAGE));
       shared = max(0, __reduce_min_sync(0xffffffffu, shared));
     }
-    const int per = p.Hk * p.tiles[1].n;
-    auto units = [&](int n) { return per * ((min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
-    const int u0 = s0 < p.b ? units(n0) : 0, u1 = s1 < p.b ? units(n1) : 0;
+    // With few units they are the places (a CTA's share has to hold the places of any unit, or some CTA
+    // within an item would have none of its units), and with very many, for the places' range.
+    const int per = p.Hk * p.tiles[1].n, first = p.Hk * p.tiles[0].n, shared_units = (shared + 1) / 2;
+    auto units = [&](int n) { return max(0, (min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
+    const int units0 = s0 < p.b ? units(n0) : 0, units1 = s1 < p.b ? units(n1) : 0;
+    const int all = first * shared_units + per * (int)__reduce_add_sync(0xffffffffu, (unsigned)(units0 + units1));
+    const bool weighed = all > 2 * (int)gridDim.x && all < 1 << 27;
+    if (lane < 2) sm.sched.cost[lane] = weighed ? px_cost(p.tiles[lane].rows, p.bf16) : PxCost{0, 1};
+    __syncwarp();
+    const int u0 = per * sm.sched.places(1, units0), u1 = per * sm.sched.places(1, units1);
     int x = u0 + u1;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -438,10 +455,9 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
     if (lane == 31) {
       sm.sched.cum[0] = 0;
       sm.sched.shared = shared;
-      sm.sched.up = (shared + 1) / 2;
-      sm.sched.tp = p.Hk * p.tiles[0].n * sm.sched.up;
+      sm.sched.units = shared_units;
+      sm.sched.tp = first * sm.sched.places(0, shared_units);
       const int total = sm.sched.tp + x;
-      sm.sched.total = total;
       sm.sched.q = total / (int)gridDim.x;
       sm.sched.r = total % (int)gridDim.x;
     }
@@ -493,8 +509,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll 1
       for (int i = 0, g = sm.sched.begin(blockIdx.x);; ++i) {
         PxSeg e{};
-        if (g < g1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
-        g += e.u1 - e.u0;
+        while (g < g1 && e.u0 == e.u1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
         e.q_at = q_at = e.rows <= PX_TWICE ? q_at ^ 1 : 0;
         e.whole = max(rows, e.rows) > PX_TWICE;
         rows = e.rows;
@@ -930,26 +945,29 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
   if (w >= p.b * p.nq * p.H) return;
   const PxScratch scratch(p);
   const int r = w / p.H, h = w - r * p.H, s = px_div(r, p.inv_nq), hk = px_div(h, p.inv_g);
-  const int shared = __ldcg(&scratch.sched->shared), up = __ldcg(&scratch.sched->up), tp = __ldcg(&scratch.sched->tp),
-            q = __ldcg(&scratch.sched->q), rest = __ldcg(&scratch.sched->r), c_s = __ldcg(&scratch.sched->cum[s]),
-            c_e = __ldcg(&scratch.sched->cum[s + 1]);
+  const PxSched* sc = scratch.sched;
+  const int q = __ldcg(&sc->q), rest = __ldcg(&sc->r), tp = __ldcg(&sc->tp), units = __ldcg(&sc->units), c_s = __ldcg(&sc->cum[s]),
+            c_e = __ldcg(&sc->cum[s + 1]);
+  PxCost cost[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) cost[k] = PxCost{__ldcg(&sc->cost[k].start), __ldcg(&sc->cost[k].unit)};
   const int R = p.b * p.nq * p.G, rr = r * p.G + h - hk * p.G;
   // of the shared pages, of the others: parts, the first one's row of the scratch (an item's own), and
   // how far the second one's (a CTA's) is from 0, the later ones PX_ROWS on each
   const int all = p.b * p.nq * p.H, mine = hk * R + rr;
   int n[2] = {0, 0}, next[2] = {0, 0};
-  auto item = [&](int k, int first, int U, int at) {   // its first unit, units, and the row of the tile
-    const int c0 = px_owner(first, q, rest);
-    n[k] = px_owner(first + U - 1, q, rest) - c0 + 1;
+  auto item = [&](int k, int base, int units, int at) {   // its first place, units, and the row of the tile
+    const int first = base + cost[k].start, c0 = px_owner(first, q, rest);
+    n[k] = px_owner(first + (units - 1) * cost[k].unit, q, rest) - c0 + 1;
     next[k] = 2 * all + PX_ROWS * c0 + at;
   };
-  if (shared > 0) {
+  if (units > 0) {
     const int t = rr / p.tiles[0].rows;
-    item(0, (hk * p.tiles[0].n + t) * up, up, rr - t * p.tiles[0].rows);
+    item(0, (hk * p.tiles[0].n + t) * (cost[0].start + units * cost[0].unit), units, rr - t * p.tiles[0].rows);
   }
   if (c_e > c_s) {
-    const int x = rr - s * p.nq * p.G, t = x / p.tiles[1].rows, U = (c_e - c_s) / (p.Hk * p.tiles[1].n);
-    item(1, tp + c_s + (hk * p.tiles[1].n + t) * U, U, x - t * p.tiles[1].rows);
+    const int x = rr - s * p.nq * p.G, t = x / p.tiles[1].rows, places = (c_e - c_s) / (p.Hk * p.tiles[1].n);
+    item(1, tp + c_s + (hk * p.tiles[1].n + t) * places, (places - cost[1].start) / cost[1].unit, x - t * p.tiles[1].rows);
   }
   const int parts = n[0] + n[1];
   float M = PX_UNSET, L = 0.f, o[E];
