@@ -91,8 +91,7 @@ struct PxCfg {
   static constexpr size_t OFF_MISC = OFF_Q + HALVES * Q_HALF;
 };
 
-// What the CTAs agree on; the first one leaves it for the merge.  Shares are counted in places: those of an
-// item are some for its start and then some for each of its units, which belongs to the CTA that has its
+// What the CTAs, and the merge after them, agree on.  Shares are counted in places: those of an item are some for its start and then some for each of its units, which belongs to the CTA that has its
 // first one.
 struct PxCost {
   int start, unit;
@@ -112,6 +111,50 @@ struct PxSched {
 // after 16500 slots: 101 us, 106 with shares of as many units; 64 rows of 16 bits after 8200: 57, 65.)
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
   return rows > 32 ? PxCost{8, bf16 ? 5 : 6} : PxCost{4, 4};
+}
+// ... from the lengths, by a warp; `end`: the places up to the sequences 2 lane and 2 lane + 1 and theirs,
+// `len` their lengths
+struct PxPlan {
+  int shared, q, r, tp, units, end[2], len[2];
+  PxCost cost[2];
+};
+__device__ PxPlan px_plan(const PrefixAttnParams& p, int ctas, int lane) {
+  PxPlan a;
+  const int s0 = 2 * lane, s1 = s0 + 1;
+  a.len[0] = s0 < p.b ? max(0, __ldcg(p.len + s0)) : 0;
+  a.len[1] = s1 < p.b ? max(0, __ldcg(p.len + s1)) : 0;
+  a.shared = 0;
+  if (p.common && p.b > 1) {
+    a.shared = p.ld;
+    if (s0 < p.b) a.shared = min(a.shared, min(__ldcg(p.common + s0), a.len[0] / KV_PAGE));
+    if (s1 < p.b) a.shared = min(a.shared, min(__ldcg(p.common + s1), a.len[1] / KV_PAGE));
+    a.shared = max(0, __reduce_min_sync(0xffffffffu, a.shared));
+  }
+  const int per = p.Hk * p.tiles[1].n, first = p.Hk * p.tiles[0].n;
+  auto units = [&](int n) { return max(0, (min(n + p.nq, p.ld * KV_PAGE) - a.shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
+  a.units = (a.shared + 1) / 2;
+  const int units0 = s0 < p.b ? units(a.len[0]) : 0, units1 = s1 < p.b ? units(a.len[1]) : 0;
+  const int all = first * a.units + per * (int)__reduce_add_sync(0xffffffffu, (unsigned)(units0 + units1));
+  // With few units they are the places (a CTA's share has to hold the places of any unit, or some CTA
+  // within an item would have none of its units), and with very many, for the places' range.
+  const bool weighed = all > 2 * ctas && all < 1 << 27;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) a.cost[k] = weighed ? px_cost(p.tiles[k].rows, p.bf16) : PxCost{0, 1};
+  auto places = [&](int k, int units) { return units > 0 ? a.cost[k].start + units * a.cost[k].unit : 0; };
+  const int u1 = per * places(1, units1);
+  int x = per * places(1, units0) + u1;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  a.end[0] = x - u1;
+  a.end[1] = x;
+  a.tp = first * places(0, a.units);
+  const int total = a.tp + __shfl_sync(0xffffffffu, x, 31);
+  a.q = total / ctas;
+  a.r = total - a.q * ctas;
+  return a;
 }
 // n / d for n < 2^16, inv = px_inv(d)
 __device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
@@ -314,17 +357,14 @@ struct PxScratch {
   float* o;        // [2 * row heads + PX_ROWS * CTAs][hd]
   float* m;        // the same rows' references
   float4* l;       // and sums, in four parts
-  PxSched* sched;
   static __host__ __device__ size_t rows(size_t row_heads, int ctas) { return (2 * row_heads + (size_t)PX_ROWS * ctas + 31) / 32 * 32; }
   __host__ __device__ PxScratch(const PrefixAttnParams& p) {
     const size_t n = rows((size_t)p.b * p.nq * p.H, p.ctas);
-    sched = reinterpret_cast<PxSched*>(p.part);
-    l = reinterpret_cast<float4*>(p.part + 256);
-    m = p.part + 256 + 4 * n;
+    l = reinterpret_cast<float4*>(p.part);
+    m = p.part + 4 * n;
     o = m + n;
   }
 };
-static_assert(sizeof(PxSched) <= 1024, "the schedule's place");
 
 // a segment's queries (thread i of n) into shared memory, rows past its own as zeros; the loads of
 // two pieces of eight dimensions are in flight together
@@ -422,44 +462,22 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   if (tid < PX_ROWS) sm.top[0][tid] = 0;
   pdl_wait();   // q, lengths, tables and rows come from the kernels before
   pdl_trigger();
-  if (warp == 2) {   // the schedule: two sequences a lane
-    const int s0 = 2 * lane, s1 = s0 + 1;
-    const int n0 = s0 < p.b ? max(0, __ldcg(p.len + s0)) : 0, n1 = s1 < p.b ? max(0, __ldcg(p.len + s1)) : 0;
-    int shared = 0;
-    if (p.common && p.b > 1) {
-      shared = p.ld;
-      if (s0 < p.b) shared = min(shared, min(__ldcg(p.common + s0), n0 / KV_PAGE));
-      if (s1 < p.b) shared = min(shared, min(__ldcg(p.common + s1), n1 / KV_PAGE));
-      shared = max(0, __reduce_min_sync(0xffffffffu, shared));
-    }
-    // With few units they are the places (a CTA's share has to hold the places of any unit, or some CTA
-    // within an item would have none of its units), and with very many, for the places' range.
-    const int per = p.Hk * p.tiles[1].n, first = p.Hk * p.tiles[0].n, shared_units = (shared + 1) / 2;
-    auto units = [&](int n) { return max(0, (min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
-    const int units0 = s0 < p.b ? units(n0) : 0, units1 = s1 < p.b ? units(n1) : 0;
-    const int all = first * shared_units + per * (int)__reduce_add_sync(0xffffffffu, (unsigned)(units0 + units1));
-    const bool weighed = all > 2 * (int)gridDim.x && all < 1 << 27;
-    if (lane < 2) sm.sched.cost[lane] = weighed ? px_cost(p.tiles[lane].rows, p.bf16) : PxCost{0, 1};
-    __syncwarp();
-    const int u0 = per * sm.sched.places(1, units0), u1 = per * sm.sched.places(1, units1);
-    int x = u0 + u1;
+  if (warp == 2) {
+    const PxPlan a = px_plan(p, gridDim.x, lane);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
+    for (int z = 0; z < 2; ++z) {
+      sm.len[2 * lane + z] = a.len[z];
+      sm.sched.cum[2 * lane + z + 1] = a.end[z];
     }
-    sm.len[s0] = n0;
-    sm.len[s1] = n1;
-    sm.sched.cum[s0 + 1] = x - u1;
-    sm.sched.cum[s1 + 1] = x;
-    if (lane == 31) {
+    if (lane == 0) {
       sm.sched.cum[0] = 0;
-      sm.sched.shared = shared;
-      sm.sched.units = shared_units;
-      sm.sched.tp = first * sm.sched.places(0, shared_units);
-      const int total = sm.sched.tp + x;
-      sm.sched.q = total / (int)gridDim.x;
-      sm.sched.r = total % (int)gridDim.x;
+      sm.sched.shared = a.shared;
+      sm.sched.units = a.units;
+      sm.sched.tp = a.tp;
+      sm.sched.q = a.q;
+      sm.sched.r = a.r;
+      sm.sched.cost[0] = a.cost[0];
+      sm.sched.cost[1] = a.cost[1];
     }
   }
   tc_fence_before();
@@ -467,7 +485,6 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   const PxScratch scratch(p);
-  if (blockIdx.x == 0 && tid < (int)(sizeof(PxSched) / 4)) reinterpret_cast<int*>(scratch.sched)[tid] = reinterpret_cast<int*>(&sm.sched)[tid];
   const int q_parts = p.bf16 ? 1 : PX_PARTS, p_parts = p.bf16 ? 2 : PX_PARTS;
   // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
   // return: one that ran out has set the error bit, and the results are invalid.
@@ -935,22 +952,23 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 }
 
 // A warp for each row and head: its partial results by weight, the loads of PX_JOIN of them in flight.
-constexpr int PX_JOIN = 8;
+// Where they are is worked out before the wait for them (the lengths are those that the kernel before has
+// waited for); small CTAs, as one wave has to hold them all.  (48 rows of 32 heads: 6.1 us with neither.)
+constexpr int PX_JOIN = 8, PX_MERGE = 128;
 template <int HD>
-__global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant__ PrefixAttnParams p) {
+__global__ void __launch_bounds__(PX_MERGE) prefix_merge_kernel(const __grid_constant__ PrefixAttnParams p) {
   constexpr int E = HD / 32;
   pdl_trigger();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, w = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, w = blockIdx.x * (PX_MERGE / 32) + (threadIdx.x >> 5);
   if (w >= p.b * p.nq * p.H) return;
   const PxScratch scratch(p);
   const int r = w / p.H, h = w - r * p.H, s = px_div(r, p.inv_nq), hk = px_div(h, p.inv_g);
-  const PxSched* sc = scratch.sched;
-  const int q = __ldcg(&sc->q), rest = __ldcg(&sc->r), tp = __ldcg(&sc->tp), units = __ldcg(&sc->units), c_s = __ldcg(&sc->cum[s]),
-            c_e = __ldcg(&sc->cum[s + 1]);
-  PxCost cost[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) cost[k] = PxCost{__ldcg(&sc->cost[k].start), __ldcg(&sc->cost[k].unit)};
+  const PxPlan a = px_plan(p, p.ctas, lane);
+  const int q = a.q, rest = a.r, tp = a.tp, units = a.units;
+  const PxCost* cost = a.cost;
+  const int e0 = __shfl_sync(0xffffffffu, a.end[0], s >> 1), e1 = __shfl_sync(0xffffffffu, a.end[1], s >> 1),
+            e_was = __shfl_sync(0xffffffffu, a.end[1], max(0, (s >> 1) - 1));
+  const int c_e = s & 1 ? e1 : e0, c_s = s & 1 ? e0 : s ? e_was : 0;
   const int R = p.b * p.nq * p.G, rr = r * p.G + h - hk * p.G;
   // of the shared pages, of the others: parts, the first one's row of the scratch (an item's own), and
   // how far the second one's (a CTA's) is from 0, the later ones PX_ROWS on each
@@ -970,6 +988,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const __grid_constant
     item(1, tp + c_s + (hk * p.tiles[1].n + t) * places, (places - cost[1].start) / cost[1].unit, x - t * p.tiles[1].rows);
   }
   const int parts = n[0] + n[1];
+  pdl_wait();
   float M = PX_UNSET, L = 0.f, o[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) o[i] = 0.f;
@@ -1045,8 +1064,8 @@ cudaError_t px_launch(const PrefixAttnParams& p, cudaStream_t st, bool pdl) {
   cfg.numAttrs = pdl ? 1 : 0;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_attention_kernel<HD>, p);
   if (e != cudaSuccess) return e;
-  cfg.gridDim = dim3((p.b * p.nq * p.H + 7) / 8);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3((p.b * p.nq * p.H + PX_MERGE / 32 - 1) / (PX_MERGE / 32));
+  cfg.blockDim = dim3(PX_MERGE);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<HD>, p);
 }
@@ -1068,7 +1087,7 @@ static uint32_t px_inv(int d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + 
 // floats for row_heads rows of hd (twice as many of half the size)
 size_t prefix_attention_scratch(int row_heads, int hd, int num_sms) {
   const size_t most = hd < 128 ? (size_t)row_heads * 2 : row_heads;
-  return std::max(256 + PxScratch::rows(row_heads, num_sms) * (5 + std::max(hd, 128)), 256 + PxScratch::rows(most, num_sms) * (5 + 64));
+  return std::max(PxScratch::rows(row_heads, num_sms) * (5 + std::max(hd, 128)), PxScratch::rows(most, num_sms) * (5 + 64));
 }
 
 cudaError_t prefix_attention_prepare() {
