@@ -238,6 +238,20 @@ __device__ __forceinline__ void px_ld8(uint32_t taddr, float* v) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void px_ld4(uint32_t taddr, float* v) {
+  uint32_t r[4];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(taddr)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void px_st4(uint32_t taddr, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(__float_as_uint(v[0])),
+               "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3]))
+               : "memory");
+}
 __device__ __forceinline__ void px_st8(uint32_t taddr, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
                "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
@@ -484,7 +498,6 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  const PxScratch scratch(p);
   const int q_parts = p.bf16 ? 1 : PX_PARTS, p_parts = p.bf16 ? 2 : PX_PARTS;
   // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
   // return: one that ran out has set the error bit, and the results are invalid.
@@ -617,8 +630,10 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll 1
         for (int u = e.u0; u < e.u1; ++u, ++k) {
           const int slot = (2 * k) % NS;
-          ready(&sm.full[slot], ((2 * k) / NS) & 1);
-          if (k > 0) ready(&sm.s_empty, (k - 1) & 1);
+          wait(&sm.full[slot], ((2 * k) / NS) & 1);
+          if (k > 0) wait(&sm.s_empty, (k - 1) & 1);
+          __syncwarp();
+          tc_fence_after();
           const uint64_t a0 = kd + (uint64_t)(slot * (C::TILE >> 4));
           if (!sm.abort) {
 #pragma unroll 1
@@ -651,7 +666,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           }
           const int slot = (2 * k + 1) % NS, steps = (min(PX_UNIT, e.end - e.slot0 - u * PX_UNIT) + 15) / 16;   // 16 slots each
           const uint64_t a0 = vd + (uint64_t)(slot * (C::TILE >> 4));
-          ready(&sm.full[slot], ((2 * k + 1) / NS) & 1);
+          wait(&sm.full[slot], ((2 * k + 1) / NS) & 1);
           ready(&sm.p_full, k & 1);
           if (!sm.abort) {
 #pragma unroll 1
@@ -733,7 +748,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             px_st8(total, o);
             continue;
           }
-          float* dst = scratch.o + (row + r) * HD + st;
+          float* dst = PxScratch(p).o + (row + r) * HD + st;
 #pragma unroll
           for (int z = 0; z < 8; ++z)
             if (r + z < x.rows && st < HD) dst[z * HD] = o[z];
@@ -745,9 +760,9 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
     }
   } else {
-    const int st = tid - 128, wg = st >> 7, e = st & 127;   // softmax thread, group, slot of the unit
+    const int wg = (warp >> 2) - 1, e = tid & 127;   // softmax thread, group, slot of the unit
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const float c = rsqrtf((float)HD) * 1.4426950408889634f;
+    constexpr float c = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.4426950408889634f;
     const uint64_t c2 = f2_pack(c, c);
     auto ready = [&](uint64_t* bar, uint32_t parity) {
       wait(bar, parity);
@@ -778,18 +793,19 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         for (int i = 0; i < PX_MINE; ++i)
           if (i < mine) {
             const uint32_t at = tmem + lanes + first_row(i);
-            float a[8], b[8];   // the second and third parts' products
+            float a[8];   // the second and third parts' products
             px_ld8(at, s + 8 * i);
-            if (q_parts > 1) {
-              px_ld8(at + cols, a);
-              px_ld8(at + 2 * cols, b);
-            }
+            if (q_parts > 1) px_ld8(at + cols, a);
             tmem_wait_ld();
             if (q_parts > 1) {
 #pragma unroll
               for (int z = 0; z < 8; z += 2)
-                f2_unpack(f2_add(f2_pack(s[8 * i + z], s[8 * i + z + 1]), f2_add(f2_pack(a[z], a[z + 1]), f2_pack(b[z], b[z + 1]))),
-                          s[8 * i + z], s[8 * i + z + 1]);
+                f2_unpack(f2_add(f2_pack(s[8 * i + z], s[8 * i + z + 1]), f2_pack(a[z], a[z + 1])), s[8 * i + z], s[8 * i + z + 1]);
+              px_ld8(at + 2 * cols, a);
+              tmem_wait_ld();
+#pragma unroll
+              for (int z = 0; z < 8; z += 2)
+                f2_unpack(f2_add(f2_pack(s[8 * i + z], s[8 * i + z + 1]), f2_pack(a[z], a[z + 1])), s[8 * i + z], s[8 * i + z + 1]);
             }
           }
         tc_fence_before();
@@ -830,8 +846,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         }
         if (move) {
           // three places in turn: all have read one before any comes to its next use
-          const int now_at = moves % 3, next_at = (moves + 1) % 3;
-          ++moves;
+          const int now_at = moves, next_at = moves == 2 ? 0 : moves + 1;
+          moves = next_at;
           float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < PX_MINE; ++i)
@@ -864,15 +880,16 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll 1
             for (int part = (u - x.u0) % PX_RUN ? 0 : p_parts; part < p_parts + total; ++part)
 #pragma unroll 1
-              for (int i = 0; i < mine; ++i) {
-                const uint32_t at =
-                    tmem + lanes + first_row(i) + (part < p_parts ? PX_O + (x.rows <= PX_TWICE ? PX_O_STEP * (now & 1) : 0) + part * cols : PX_TOTAL);
-                float o[8];
-                px_ld8(at, o);
+              for (int i = 0; i < 2 * mine; ++i) {   // four rows
+                const int r = first_row(i >> 1) + 4 * (i & 1);
+                const uint32_t at = tmem + lanes + r +
+                                    (part < p_parts ? PX_O + (x.rows <= PX_TWICE ? PX_O_STEP * (now & 1) : 0) + part * cols : PX_TOTAL);
+                float o[4];
+                px_ld4(at, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int z = 0; z < 8; ++z) o[z] *= sm.by[first_row(i) + z];
-                px_st8(at, o);
+                for (int z = 0; z < 4; ++z) o[z] *= sm.by[r + z];
+                px_st4(at, o);
               }
 #pragma unroll
             for (int i = 0; i < 8 * PX_MINE; ++i)
@@ -931,6 +948,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
       }
       // ---- the rows' references and sums (a warp's part of them) for the results
       const size_t row = scratch_row(x);
+      const PxScratch scratch(p);
 #pragma unroll
       for (int i = 0; i < PX_MINE; ++i)
         if (i < mine) {
