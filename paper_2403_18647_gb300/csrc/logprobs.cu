@@ -51,6 +51,19 @@ __device__ __forceinline__ float lp_ex2(float x) {
   return y;
 }
 
+// 1 if x >= lo (no NaN), else 0
+__device__ __forceinline__ float lp_ge(float x, float lo) {
+  float r;
+  asm("set.ge.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(lo));
+  return r;
+}
+// the same of two bf16 values, added to two sums in bf16
+__device__ __forceinline__ uint32_t lp_count2(uint32_t sums, uint32_t x, uint32_t lo) {
+  const __nv_bfloat162 one = __hge2(reinterpret_cast<__nv_bfloat162&>(x), reinterpret_cast<__nv_bfloat162&>(lo)),
+                       r = __hadd2(reinterpret_cast<__nv_bfloat162&>(sums), one);
+  return reinterpret_cast<const uint32_t&>(r);
+}
+
 // larger key = earlier alternative: the logit's order in the high half, the id's inverse in the low
 // (every key is above 0)
 __device__ __forceinline__ unsigned long long lp_key(float x, int id) {
@@ -231,9 +244,10 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
     }
     const float lt = !given ? INFINITY : fetched ? lt_next : logit(t);
     // x comes before the token iff x >= lt at lower ids, x >= the next value above lt at higher ones
+    constexpr uint32_t step1 = BF16 ? 0x10000u : 1u;
     const float above = lt == INFINITY ? NAN
-                        : lt == 0.f    ? __uint_as_float(1u)
-                                       : __uint_as_float(__float_as_uint(lt) + (lt > 0.f ? 1u : 0xFFFFFFFFu));
+                        : lt == 0.f    ? __uint_as_float(step1)
+                                       : __uint_as_float(__float_as_uint(lt) + (lt > 0.f ? step1 : 0u - step1));
     // this thread's value among the row's ends, which no whole vector holds (fewer than 2 E)
     const int end_id = tid < run.head ? tid : run.tail + tid - run.head;
     const bool end_mine = rank == 0 && tid < 2 * E && end_id < p.V;
@@ -267,6 +281,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
         if (at < LP_NOTED) sm.noted[at] = lp_key(x, id);
       };
       int round = 0;
+      uint64_t count2 = 0;   // logits before the token, in two sums
       for (int v = run.v0 + tid; v - tid < run.v1; v += LP_ROUND, ++round) {
         uint4 r[LP_UNROLL];
         constexpr uint32_t none = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
@@ -274,6 +289,18 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
 #pragma unroll
           for (int u = 0; u < LP_UNROLL; ++u)
             r[u] = v + u * LP_THREADS < run.v1 ? __ldcg(run.vec() + v + u * LP_THREADS) : make_uint4(none, none, none, none);
+#pragma unroll
+          for (int u = 0; u < LP_UNROLL; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {   // (a NaN is -inf)
+              uint32_t& w = (&r[u].x)[k];
+              if constexpr (BF16) {
+                const __nv_bfloat162 h = __hmax2(reinterpret_cast<__nv_bfloat162&>(w), reinterpret_cast<const __nv_bfloat162&>(none));
+                w = reinterpret_cast<const uint32_t&>(h);
+              } else {
+                w = __float_as_uint(fmaxf(__uint_as_float(w), -INFINITY));
+              }
+            }
         } else {
           mbar_wait_bounded(&sm.full[it % LP_STAGES], (it / LP_STAGES) & 1, &sm.abort, p.err);
           const uint4* stage = sm.ring[it % LP_STAGES] + tid;
@@ -284,9 +311,6 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
             for (int u = 0; u < LP_UNROLL; ++u)
               if (v + u * LP_THREADS >= run.v1) r[u] = make_uint4(none, none, none, none);
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.empty[it % LP_STAGES]);
-          ++it;
         }
         float vtop[LP_UNROLL];   // the largest of each vector (a NaN is passed over)
 #pragma unroll
@@ -314,8 +338,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
           for (int u = 0; u < LP_UNROLL; ++u)
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-              const float x = value(r[u], k);
-              add(isnan(x) ? -INFINITY : x);
+              add(value(r[u], k));
             }
         } else {
           const uint64_t m2 = f2_pack(-s.m, -s.m), c2 = f2_pack(c, c);
@@ -338,37 +361,62 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
           f2_unpack(E2, s.E, b);
           s.E += b;
         }
-        // the logits before the token, and those to note: most vectors have neither
+        // the logits before the token, and those to note
         if (top >= lt) {
+          uint64_t half = 0;   // (16 bits: counted in bf16, at most 16 a round and half)
 #pragma unroll
           for (int u = 0; u < LP_UNROLL; ++u) {
             const int at = v + u * LP_THREADS, id0 = run.head + at * E;
-            if (vtop[u] < lt || at >= run.v1) continue;
-            const float lo = id0 + E <= t ? lt : above;
+            const float lo = at >= run.v1 ? NAN : id0 + E <= t ? lt : above;
+            if constexpr (BF16) {
+              const uint32_t lo2 = __float_as_uint(lo) >> 16 | (__float_as_uint(lo) & 0xFFFF0000u);
 #pragma unroll
-            for (int k = 0; k < E; ++k) {
-              float x = value(r[u], k);
-              if (CLEAN && isnan(x)) x = -INFINITY;
-              s.before += x >= lo;
+              for (int k = 0; k < 4; ++k) half = lp_count2((uint32_t)half, (&r[u].x)[k], lo2);
+            } else {
+#pragma unroll
+              for (int k = 0; k < E; k += 2)
+                count2 = f2_add(count2, f2_pack(lp_ge(value(r[u], k), lo), lp_ge(value(r[u], k + 1), lo)));
             }
-            if (id0 <= t && t < id0 + E)   // equal logits before the token in its own vector
+            if (id0 <= t && t < id0 + E && at < run.v1)   // equal logits before the token in its own vector
               for (int k = 0; id0 + k < t; ++k) s.before += logit(id0 + k) == lt;
           }
+          if constexpr (BF16)
+            count2 = f2_add(count2, f2_pack(__uint_as_float((uint32_t)half << 16), __uint_as_float((uint32_t)half & 0xFFFF0000u)));
         }
         if (top >= bound) {
+          uint32_t hit = 0;   // vectors
 #pragma unroll
-          for (int u = 0; u < LP_UNROLL; ++u) {
-            const int at = v + u * LP_THREADS, id0 = run.head + at * E;
-            if (vtop[u] < bound || at >= run.v1) continue;
+          for (int u = 0; u < LP_UNROLL; ++u) hit |= (uint32_t)(vtop[u] >= bound && v + u * LP_THREADS < run.v1) << u;
+#pragma unroll 1
+          while (hit) {
+            const int at = v + (__ffs(hit) - 1) * LP_THREADS, id0 = run.head + at * E;
+            hit &= hit - 1;
+            const uint4* w = CLEAN ? run.vec() + at : sm.ring[it % LP_STAGES] + (at - v + tid);
+            const uint4 x4 = *w;
+            uint32_t which = 0;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-              float x = value(r[u], k);
+              const float x = value(x4, k);
+              which |= (uint32_t)(x >= bound || (CLEAN && bound == -INFINITY)) << k;   // (a NaN is -inf)
+            }
+#pragma unroll 1
+            for (; which; which &= which - 1) {
+              const int k = __ffs(which) - 1;
+              float x = BF16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(w)[k]) : reinterpret_cast<const float*>(w)[k];
               if (CLEAN && isnan(x)) x = -INFINITY;
-              if (x >= bound) note(x, id0 + k);
+              note(x, id0 + k);
             }
           }
         }
+        if (!CLEAN) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.empty[it % LP_STAGES]);
+          ++it;
+        }
       }
+      float b0, b1;
+      f2_unpack(count2, b0, b1);
+      s.before += (int)b0 + (int)b1;
       if (end_mine) {
         const float x = isnan(end_raw) ? -INFINITY : end_raw;
         if (x > s.m) grow(x);
