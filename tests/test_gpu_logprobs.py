@@ -120,6 +120,21 @@ def test_ties_go_to_the_lowest_id(ctx):
     check(run(ctx, x.cuda(), t, 32), reference(x, t, 32, 1.0))
 
 
+@pytest.mark.parametrize("type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [19, 4099, 40003])
+def test_ranks_among_neighbouring_values(ctx, type, vocab):
+    """Tokens of every value of a set of zeros, smallest ones and values next to one another."""
+    one = torch.tensor([0.0, 1.0, -1.0, 3.5, -0.25]).to(type)
+    near = torch.cat([one, torch.nextafter(one, torch.full_like(one, math.inf)), torch.nextafter(one, torch.full_like(one, -math.inf)),
+                      torch.tensor([-0.0, -math.inf, 2.0, -2.0]).to(type)])
+    g = torch.Generator().manual_seed(11)
+    x = near[torch.randint(0, near.numel(), (2 * near.numel(), vocab), generator=g)]
+    t = torch.randint(0, vocab, (2 * near.numel(),), generator=g, dtype=torch.int32)
+    x[torch.arange(t.numel()), t.long()] = near.repeat(2)
+    check(run(ctx, x.cuda(), t, 5), reference(x, t, 5, 1.0))
+    assert ctx.get_error() == 0
+
+
 def test_masked_and_infinite_logits(ctx):
     """Banned ids, the type's lowest value, rows with fewer ids left than alternatives, rows with none, +inf."""
     V = 9000
