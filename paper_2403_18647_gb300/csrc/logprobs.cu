@@ -20,7 +20,13 @@
 //    logits from it on are noted, in shared memory: about n after each of these of random logits.  At
 //    the end each noted one's place is the number of larger ones.  Where too many are noted (equal
 //    logits, long runs of -inf), they are noted again from a better bound on (another pass, over L2).
+//  - the rank: logits before the token are counted two at a time, where a round has any; an if for each
+//    was a quarter of the time with tokens of any rank.
 // The row's ends that are not whole vectors (rows may start anywhere) are read value by value.
+// Measured: 4096 rows of 32016 fp32 logits, 2 alternatives 96 us (5.4 TB/s, 0.80 of the copy rate);
+// 1000 rows of 128003 of 16 bits, 20 alternatives 78 us (3.3 TB/s: the instructions, 17 a logit before the
+// counting and the noting were short, and the last third of the rows' turns, which 88 CTAs have); 48
+// rows of 32016 7.1 us, 6 of 4104 4.7 (launch, chain of barriers).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -502,7 +508,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
       lp_bar();   // the warps' sums
     }
     // Many noted ones (those of the early rounds, from lower bounds on): the whole run's bound keeps
-    // about n of them.  2000 rows of 32016, 32 alternatives: 79 us, 87 without.
+    // about n of them (2000 rows of 32016, 32 alternatives: 8 us less of 87).
     if (count > LP_FEW) {
       const unsigned long long low = lp_key(nth_group(mine, false), INT_MAX);
       const unsigned long long k0 = tid < count ? sm.noted[tid] : 0, k1 = tid + LP_THREADS < count ? sm.noted[tid + LP_THREADS] : 0;

@@ -33,20 +33,24 @@
 // The tensor cores cut off what an addition to their fp32 accumulator cannot hold, so that an error of
 // half a unit in the last place grows with every 16 slots added.  After PX_RUN units O is therefore
 // added, rounded, to a total in TMEM and begun anew (16x4 rows of 7B heads after 16500 slots: an error of
-// 0.9e-6 and 107 us; 1.4e-6 and 104 with 8 units, 2.4e-6 and 102 with 16, 5.9e-6 without; fp32
-// products in a row 2.5e-6).
+// 0.9e-6; 1.4e-6 and 2 % less time with 8 units, 2.4e-6 and 4 % with 16, 5.9e-6 without; fp32 products
+// in a row 2.5e-6).
 //
 // The three parts are side by side in B (N = three times the rows) and their products in columns of
 // their own, added up when they are read: 8 MMAs a tile of K or V instead of 24.  An MMA takes N / 2
 // cycles from N = 96 on and 50 below.
 //
-// Warps: 0 TMA (pages by the table), 1 and 3 MMA issue (a whole warp, one lane's instructions), 2 the
-// segments, ahead of their use, 4-19 softmax, 20-23 queries and results, so that a segment's queries are
-// in place before the one ahead of it ends and its results leave while the next one runs.  What bounds
-// a unit of 64 rows is the softmax' chain of loads, barriers and stores, 3700 cycles, against 1600 of
-// the tensor cores'; on one warp the products' issue, 1500 and 1950 cycles for a unit's scores and
-// values beside busy warps, was as long (8x6 rows after 2048 slots, 7B heads: 36 us, 32 on two warps;
-// 64 rows of 16 bits over 8200 slots: 96 us, 62).
+// Warps: 0 TMA (pages by the table), 1 and 3 MMA issue (a whole warp, one lane's instructions; one warp
+// took 1500 cycles for a unit's scores and 1950 for its values beside the busy ones, and bounded all),
+// 2 the segments, ahead of their use, 4-19 softmax, 20-23 queries and results, so that a segment's
+// queries are in place before the one ahead of it ends and its results leave while the next one runs.
+//
+// What bounds it: a unit of an SM takes 1.6 us with up to 32 rows when all SMs stream (1.47 at its share of
+// the copy rate), 1.9 with 64 (the softmax: 47 % of the issue slots, the rest its chain of loads, votes
+// and waits; two halves of the rows in turn, with twice the MMAs to issue, took 2.2).  Beside them the
+// starts: 2.5 us from the launch to the first scores, 1.3 us an item, 4 us for the merge.  Measured: 8x6
+// rows after 2048 slots of 7B heads 25 us, 16x4 after 16500 94 us (4.3 TB/s).  Registers are what the
+// softmax has least of: 44 spilled bytes fewer were worth 4 % to 7 %.
 // Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: S and two O.
 #include <algorithm>
 
@@ -107,8 +111,8 @@ struct PxSched {
   __device__ int places(int k, int units) const { return units > 0 ? cost[k].start + units * cost[k].unit : 0; }
 };
 // What an item of that many rows costs: 1.3 us a unit and as much for the start with up to 32 rows, 2 us
-// (1.65 of 16 bits) and 2.6 with more, by the ends of the CTAs of four cases.  (16x4 rows of 7B heads
-// after 16500 slots: 101 us, 106 with shares of as many units; 64 rows of 16 bits after 8200: 57, 65.)
+// (1.65 of 16 bits) and 2.6 with more, by the ends of the CTAs of four cases.  (Shares of as many units
+// each: 5 % more time for 16x4 rows after 16500 slots, 15 % for 64 rows of 16 bits after 8200.)
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
   return rows > 32 ? PxCost{8, bf16 ? 5 : 6} : PxCost{4, 4};
 }
@@ -971,7 +975,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 
 // A warp for each row and head: its partial results by weight, the loads of PX_JOIN of them in flight.
 // Where they are is worked out before the wait for them (the lengths are those that the kernel before has
-// waited for); small CTAs, as one wave has to hold them all.  (48 rows of 32 heads: 6.1 us with neither.)
+// waited for); small CTAs, as one wave has to hold them all.  (48 rows of 32 heads: 3.3 us less for both.)
 constexpr int PX_JOIN = 8, PX_MERGE = 128;
 template <int HD>
 __global__ void __launch_bounds__(PX_MERGE) prefix_merge_kernel(const __grid_constant__ PrefixAttnParams p) {
