@@ -148,14 +148,23 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_kinds = None
+
+
 def _rows(t):
-    """(address, values from one row to the next, element type) of a CUDA matrix whose rows are contiguous."""
-    import torch
-    if not t.is_cuda or t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16):
+    """(address, values from one row to the next, element type, rows, columns) of a CUDA matrix whose rows are
+    contiguous."""
+    global _kinds
+    if _kinds is None:
+        import torch
+        _kinds = {torch.float32: FP32, torch.bfloat16: BF16}
+    kind = _kinds.get(t.dtype)
+    if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError("expected a float32 or bfloat16 CUDA matrix")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    (rows, columns), (ld, step) = t.shape, t.stride()
+    if step != 1 and columns > 1:
         raise ValueError("expected contiguous rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1], BF16 if t.dtype == torch.bfloat16 else FP32
+    return t.data_ptr(), ld if rows > 1 else columns, kind, rows, columns
 
 
 def _check(status: int, what: str):
@@ -506,25 +515,25 @@ class Context:
         [b][columns]; shared (leading columns equal to sequence 0's, may be None) and lens int32 [b]; anc int32 [b*qn]
         block-row masks of a tree block."""
         self._bind_stream()
-        (qp, q_ld, kind), (op, out_ld, kind_out) = _rows(q), _rows(out)
+        (qp, q_ld, kind, q_rows, _), (op, out_ld, kind_out, out_rows, _) = _rows(q), _rows(out)
         if kind != kind_out:
             raise ValueError("q and out are of different types")
-        if table.shape[0] < b or q.shape[0] < b * qn or out.shape[0] < b * qn:
+        sequences, columns = table.shape
+        if sequences < b or q_rows < b * qn or out_rows < b * qn:
             raise ValueError("fewer rows than b or b * qn")
-        _check(_lib().sdsat_op_prefix_attention(self.handle, qp, q_ld, _ptr(k), _ptr(v), k.shape[0], _ptr(table),
-                                                table.shape[1], _ptr(shared), _ptr(lens), _ptr(anc), b, qn, H, Hk, hd, op,
-                                                out_ld, kind), "sdsat_op_prefix_attention")
+        _check(_lib().sdsat_op_prefix_attention(self.handle, qp, q_ld, _ptr(k), _ptr(v), k.size(0), _ptr(table), columns,
+                                                _ptr(shared), _ptr(lens), _ptr(anc), b, qn, H, Hk, hd, op, out_ld, kind),
+               "sdsat_op_prefix_attention")
 
     def op_logprobs(self, logits, tokens=None, logp=None, entropy=None, rank=None, top_ids=None, top_logp=None,
                     temperature: float = 1.0):
         """logits [rows][vocab] fp32 or bf16 (rows any distance apart); tokens, rank int32 and logp, entropy fp32 [rows];
         top_ids int32 and top_logp fp32 [rows][n]."""
         self._bind_stream()
-        lp, ld, kind = _rows(logits)
-        n = 0 if top_ids is None else top_ids.shape[1]
-        _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, logits.shape[0], logits.shape[1], _ptr(tokens),
-                                        temperature, n, _ptr(logp), _ptr(entropy), _ptr(rank), _ptr(top_ids),
-                                        _ptr(top_logp)), "sdsat_op_logprobs")
+        lp, ld, kind, rows, vocab = _rows(logits)
+        n = 0 if top_ids is None else top_ids.size(1)
+        _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, rows, vocab, _ptr(tokens), temperature, n, _ptr(logp),
+                                        _ptr(entropy), _ptr(rank), _ptr(top_ids), _ptr(top_logp)), "sdsat_op_logprobs")
 
     def debug_workspace(self, which: int, rows: int):
         """Last-layer workspace of the last forward: 0 h, 1 q, 2 attention out, 3 SwiGLU act."""
