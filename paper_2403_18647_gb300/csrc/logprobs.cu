@@ -57,17 +57,11 @@ __device__ __forceinline__ float lp_ex2(float x) {
   return y;
 }
 
-// 1 if x >= lo (no NaN), else 0
-__device__ __forceinline__ float lp_ge(float x, float lo) {
-  float r;
-  asm("set.ge.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(lo));
+// per half: all bits where x >= lo (no NaN), of two bf16 values
+__device__ __forceinline__ uint32_t lp_ge2(uint32_t x, uint32_t lo) {
+  uint32_t r;
+  asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(lo));
   return r;
-}
-// the same of two bf16 values, added to two sums in bf16
-__device__ __forceinline__ uint32_t lp_count2(uint32_t sums, uint32_t x, uint32_t lo) {
-  const __nv_bfloat162 one = __hge2(reinterpret_cast<__nv_bfloat162&>(x), reinterpret_cast<__nv_bfloat162&>(lo)),
-                       r = __hadd2(reinterpret_cast<__nv_bfloat162&>(sums), one);
-  return reinterpret_cast<const uint32_t&>(r);
 }
 
 // larger key = earlier alternative: the logit's order in the high half, the id's inverse in the low
@@ -287,7 +281,6 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
         if (at < LP_NOTED) sm.noted[at] = lp_key(x, id);
       };
       int round = 0;
-      uint64_t count2 = 0;   // logits before the token, in two sums
       for (int v = run.v0 + tid; v - tid < run.v1; v += LP_ROUND, ++round) {
         uint4 r[LP_UNROLL];
         constexpr uint32_t none = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
@@ -369,25 +362,44 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
         }
         // the logits before the token, and those to note
         if (top >= lt) {
-          uint64_t half = 0;   // (16 bits: counted in bf16, at most 16 a round and half)
-#pragma unroll
-          for (int u = 0; u < LP_UNROLL; ++u) {
-            const int at = v + u * LP_THREADS, id0 = run.head + at * E;
-            const float lo = at >= run.v1 ? NAN : id0 + E <= t ? lt : above;
-            if constexpr (BF16) {
+          const int id0 = run.head + (v - tid) * E, id1 = run.head + min(v - tid + LP_ROUND, run.v1) * E;   // the round's
+          if (!CLEAN && (id1 <= t || id0 > t) && lt > -INFINITY) {
+            // the same comparison for all of them (vectors past the run's end are -inf; +inf ends in the slower pass)
+            const float lo = id1 <= t ? lt : above;
+            uint32_t sum = 0;
+            if constexpr (BF16) {   // a low half's mask counts 1 - 2^16, a high one's 2^16
               const uint32_t lo2 = __float_as_uint(lo) >> 16 | (__float_as_uint(lo) & 0xFFFF0000u);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) half = lp_count2((uint32_t)half, (&r[u].x)[k], lo2);
-            } else {
+              for (int u = 0; u < LP_UNROLL; ++u)
 #pragma unroll
-              for (int k = 0; k < E; k += 2)
-                count2 = f2_add(count2, f2_pack(lp_ge(value(r[u], k), lo), lp_ge(value(r[u], k + 1), lo)));
+                for (int k = 0; k < 4; ++k) sum -= lp_ge2((&r[u].x)[k], lo2);
+              s.before += 2 * (int)(sum & 0xFFFFu) + ((int)sum >> 16);
+            } else {   // x - lo has a sign where x < lo (-0 - -0 has none)
+              const float minus = lo == 0.f ? 0.f : -lo;
+              const uint64_t minus2 = f2_pack(minus, minus);
+#pragma unroll
+              for (int u = 0; u < LP_UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < E; k += 2) {
+                  float a, b;
+                  f2_unpack(f2_add(f2_pack(value(r[u], k), value(r[u], k + 1)), minus2), a, b);
+                  sum += __float_as_uint(a) >> 31;
+                  sum += __float_as_uint(b) >> 31;
+                }
+              s.before += LP_UNROLL * E - (int)sum;
             }
-            if (id0 <= t && t < id0 + E && at < run.v1)   // equal logits before the token in its own vector
-              for (int k = 0; id0 + k < t; ++k) s.before += logit(id0 + k) == lt;
+          } else {
+#pragma unroll 1
+            for (int at = v; at < min(v - tid + LP_ROUND, run.v1); at += LP_THREADS) {
+              const int first = run.head + at * E;
+              const float lo = first + E <= t ? lt : above;
+              const uint4 w = CLEAN ? __ldcg(run.vec() + at) : sm.ring[it % LP_STAGES][at - v + tid];
+#pragma unroll
+              for (int k = 0; k < E; ++k) s.before += (CLEAN ? fmaxf(value(w, k), -INFINITY) : value(w, k)) >= lo;
+              if (first <= t && t < first + E)   // equal logits before the token in its own vector
+                for (int k = 0; first + k < t; ++k) s.before += logit(first + k) == lt;
+            }
           }
-          if constexpr (BF16)
-            count2 = f2_add(count2, f2_pack(__uint_as_float((uint32_t)half << 16), __uint_as_float((uint32_t)half & 0xFFFF0000u)));
         }
         if (top >= bound) {
           uint32_t hit = 0;   // vectors
@@ -400,10 +412,11 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
             const uint4* w = CLEAN ? run.vec() + at : sm.ring[it % LP_STAGES] + (at - v + tid);
             const uint4 x4 = *w;
             uint32_t which = 0;
+            if (CLEAN && bound == -INFINITY) {   // (a NaN is -inf)
+              which = (1u << E) - 1u;
+            } else {
 #pragma unroll
-            for (int k = 0; k < E; ++k) {
-              const float x = value(x4, k);
-              which |= (uint32_t)(x >= bound || (CLEAN && bound == -INFINITY)) << k;   // (a NaN is -inf)
+              for (int k = 0; k < E; ++k) which |= (uint32_t)(value(x4, k) >= bound) << k;
             }
 #pragma unroll 1
             for (; which; which &= which - 1) {
@@ -420,9 +433,6 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
           ++it;
         }
       }
-      float b0, b1;
-      f2_unpack(count2, b0, b1);
-      s.before += (int)b0 + (int)b1;
       if (end_mine) {
         const float x = isnan(end_raw) ? -INFINITY : end_raw;
         if (x > s.m) grow(x);
