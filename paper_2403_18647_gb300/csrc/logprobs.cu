@@ -16,17 +16,17 @@
 // put together.  Nothing of a row is kept:
 //  - maximum, sums: each thread rescales its running (m, S, E) when a round's maximum passes m;
 //  - alternatives: the n-th largest of the LP_GROUPS maxima that groups of threads have met is a lower
-//    bound of the run's n-th largest logit.  It is taken after the rounds 1, 2, 4, 8, ..., and only
-//    logits from it on are noted, in shared memory: about n after each of these of random logits.  At
-//    the end each noted one's place is the number of larger ones.  Where too many are noted (equal
+//    bound of the run's n-th largest logit.  It is taken in the rounds 0, 3 and 24 (each time costs
+//    more than the notes that more of them would spare: 4096 rows of 32016, 10 alternatives 102 us, 104 with
+//    0, 2, 8 and 32, 109 with every power of two), and only logits from it on are noted, in shared memory.
+//    At the end each noted one's place is the number of larger ones.  Where too many are noted (equal
 //    logits, long runs of -inf), they are noted again from a better bound on (another pass, over L2).
 //  - the rank: logits before the token are counted two at a time, where a round has any; an if for each
 //    was a quarter of the time with tokens of any rank.
 // The row's ends that are not whole vectors (rows may start anywhere) are read value by value.
-// Measured: 4096 rows of 32016 fp32 logits, 2 alternatives 96 us (5.4 TB/s, 0.80 of the copy rate);
-// 1000 rows of 128003 of 16 bits, 20 alternatives 78 us (3.3 TB/s: the instructions, 17 a logit before the
-// counting and the noting were short, and the last third of the rows' turns, which 88 CTAs have); 48
-// rows of 32016 7.1 us, 6 of 4104 4.7 (launch, chain of barriers).
+// Measured: 4096 rows of 32016 fp32 logits, 2 alternatives 91 us (5.8 TB/s, 0.85 of the copy rate);
+// 1000 rows of 128003 of 16 bits, 20 alternatives 74 us (3.5 TB/s: the instructions, and the last third
+// of the rows' turns, which 88 CTAs have); 48 rows of 32016 7 us, 6 of 4104 4.6 (launch, chain of barriers).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, LP_PER_SM) logprobs_kernel(co
         const float top = fmaxf(fmaxf(vtop[0], vtop[1]), fmaxf(vtop[2], vtop[3]));
         static_assert(LP_UNROLL == 4, "the round's maximum");
         // (the same for every thread)
-        if (round == 0 || (n && (bound == -INFINITY || round == 2 || round == 8 || round == 32))) {
+        if (round == 0 || (n && (bound == -INFINITY || round == 3 || round == 24))) {
           const float old = s.S > 0.f ? s.m : -INFINITY;
           const float low = nth_group(fmaxf(old, top), round == 0);
           if (n) bound = fmaxf(bound, low);
