@@ -116,12 +116,32 @@ struct PxSched {
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
   return rows > 32 ? PxCost{8, bf16 ? 5 : 6} : PxCost{4, 4};
 }
+// n / d for n < 2^16, inv = px_inv(d)
+__device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
+// n / d for 0 <= n < 1.9e9, quotients below 2^30 (the first one is off by 2^-21 of itself at most, the
+// second one's operand is exact): a third of the instructions, which are fetched cold here
+__device__ __forceinline__ int px_quot(int n, int d) {
+  const float inv = __fdividef(1.0f, (float)d);
+  int q = __float2int_rz((float)n * inv), r = n - q * d;
+  const int more = __float2int_rd((float)r * inv);
+  q += more;
+  r -= more * d;
+  return q + (r >= d) - (r < 0);
+}
+__device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has place g
+  const int x = g - (q + 1) * r;
+  return x < 0 ? px_quot(g, q + 1) : r + px_quot(x, q);
+}
 // ... from the lengths, by a warp; `end`: the places up to the sequences 2 lane and 2 lane + 1 and theirs,
 // `len` their lengths
 struct PxPlan {
   int shared, q, r, tp, units, end[2], len[2];
   PxCost cost[2];
 };
+// units of a sequence of n committed slots beyond the shared pages
+__device__ __forceinline__ int px_units(const PrefixAttnParams& p, int n, int shared) {
+  return max(0, (min(n + p.nq, p.ld * KV_PAGE) - shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT);
+}
 __device__ PxPlan px_plan(const PrefixAttnParams& p, int ctas, int lane) {
   PxPlan a;
   const int s0 = 2 * lane, s1 = s0 + 1;
@@ -135,7 +155,7 @@ __device__ PxPlan px_plan(const PrefixAttnParams& p, int ctas, int lane) {
     a.shared = max(0, __reduce_min_sync(0xffffffffu, a.shared));
   }
   const int per = p.Hk * p.tiles[1].n, first = p.Hk * p.tiles[0].n;
-  auto units = [&](int n) { return max(0, (min(n + p.nq, p.ld * KV_PAGE) - a.shared * KV_PAGE + PX_UNIT - 1) / PX_UNIT); };
+  auto units = [&](int n) { return px_units(p, n, a.shared); };
   a.units = (a.shared + 1) / 2;
   const int units0 = s0 < p.b ? units(a.len[0]) : 0, units1 = s1 < p.b ? units(a.len[1]) : 0;
   const int all = first * a.units + per * (int)__reduce_add_sync(0xffffffffu, (unsigned)(units0 + units1));
@@ -156,17 +176,10 @@ __device__ PxPlan px_plan(const PrefixAttnParams& p, int ctas, int lane) {
   a.end[1] = x;
   a.tp = first * places(0, a.units);
   const int total = a.tp + __shfl_sync(0xffffffffu, x, 31);
-  a.q = total / ctas;
+  a.q = px_quot(total, ctas);
   a.r = total - a.q * ctas;
   return a;
 }
-// n / d for n < 2^16, inv = px_inv(d)
-__device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
-__device__ __forceinline__ int px_owner(int g, int q, int r) {   // the CTA that has place g
-  const int x = g - (q + 1) * r;
-  return x < 0 ? g / (q + 1) : r + x / q;
-}
-
 // a CTA's units of one item
 struct PxSeg {
   int s;                   // sequence, or -1: the shared pages
@@ -207,11 +220,12 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
 #pragma unroll 1
     while (sc.cum[near + 1] <= x) ++near;
     x -= sc.cum[near];
-    places = (sc.cum[near + 1] - sc.cum[near]) / (p.Hk * t.n);
-    units = (places - sc.cost[1].start) / sc.cost[1].unit;
+    units = px_units(p, len[near], sc.shared);
+    places = sc.places(1, units);
   }
-  const int item = x / places, at = x - item * places, n = min(places - at, gend - g), rt = item % t.n;
-  e.hk = item / t.n;
+  const int item = px_quot(x, places), at = x - item * places, n = min(places - at, gend - g);
+  e.hk = px_quot(item, t.n);
+  const int rt = item - e.hk * t.n;
   if (k) {
     e.s = near;
     e.row0 = near * p.nq * p.G + rt * t.rows;
@@ -226,7 +240,7 @@ __device__ PxSeg px_segment(const PrefixAttnParams& p, const PxSched& sc, const 
     e.end = e.len = sc.shared * KV_PAGE;
   }
   const PxCost c = sc.cost[k];
-  auto unit = [&](int place) { return min(units, (max(0, place - c.start) + c.unit - 1) / c.unit); };   // the first one from there on
+  auto unit = [&](int place) { return min(units, px_quot(max(0, place - c.start) + c.unit - 1, c.unit)); };   // the first one from there on
   e.u0 = unit(at);
   e.u1 = unit(at + n);
   g += n;
@@ -984,13 +998,13 @@ __global__ void __launch_bounds__(PX_MERGE) prefix_merge_kernel(const __grid_con
   const int lane = threadIdx.x & 31, w = blockIdx.x * (PX_MERGE / 32) + (threadIdx.x >> 5);
   if (w >= p.b * p.nq * p.H) return;
   const PxScratch scratch(p);
-  const int r = w / p.H, h = w - r * p.H, s = px_div(r, p.inv_nq), hk = px_div(h, p.inv_g);
+  const int r = px_quot(w, p.H), h = w - r * p.H, s = px_div(r, p.inv_nq), hk = px_div(h, p.inv_g);
   const PxPlan a = px_plan(p, p.ctas, lane);
   const int q = a.q, rest = a.r, tp = a.tp, units = a.units;
   const PxCost* cost = a.cost;
-  const int e0 = __shfl_sync(0xffffffffu, a.end[0], s >> 1), e1 = __shfl_sync(0xffffffffu, a.end[1], s >> 1),
+  const int e0 = __shfl_sync(0xffffffffu, a.end[0], s >> 1),
             e_was = __shfl_sync(0xffffffffu, a.end[1], max(0, (s >> 1) - 1));
-  const int c_e = s & 1 ? e1 : e0, c_s = s & 1 ? e0 : s ? e_was : 0;
+  const int c_s = s & 1 ? e0 : s ? e_was : 0, own = px_units(p, __shfl_sync(0xffffffffu, s & 1 ? a.len[1] : a.len[0], s >> 1), a.shared);
   const int R = p.b * p.nq * p.G, rr = r * p.G + h - hk * p.G;
   // of the shared pages, of the others: parts, the first one's row of the scratch (an item's own), and
   // how far the second one's (a CTA's) is from 0, the later ones PX_ROWS on each
@@ -1002,12 +1016,12 @@ __global__ void __launch_bounds__(PX_MERGE) prefix_merge_kernel(const __grid_con
     next[k] = 2 * all + PX_ROWS * c0 + at;
   };
   if (units > 0) {
-    const int t = rr / p.tiles[0].rows;
+    const int t = px_quot(rr, p.tiles[0].rows);
     item(0, (hk * p.tiles[0].n + t) * (cost[0].start + units * cost[0].unit), units, rr - t * p.tiles[0].rows);
   }
-  if (c_e > c_s) {
-    const int x = rr - s * p.nq * p.G, t = x / p.tiles[1].rows, places = (c_e - c_s) / (p.Hk * p.tiles[1].n);
-    item(1, tp + c_s + (hk * p.tiles[1].n + t) * places, (places - cost[1].start) / cost[1].unit, x - t * p.tiles[1].rows);
+  if (own > 0) {
+    const int x = rr - s * p.nq * p.G, t = px_quot(x, p.tiles[1].rows);
+    item(1, tp + c_s + (hk * p.tiles[1].n + t) * (cost[1].start + own * cost[1].unit), own, x - t * p.tiles[1].rows);
   }
   const int parts = n[0] + n[1];
   pdl_wait();
