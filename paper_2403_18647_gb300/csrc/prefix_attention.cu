@@ -48,8 +48,8 @@
 // What bounds it: a unit of an SM takes 1.6 us with up to 32 rows when all SMs stream (1.47 at its share of
 // the copy rate), 1.9 with 64 (the softmax: 47 % of the issue slots, the rest its chain of loads, votes
 // and waits; two halves of the rows in turn, with twice the MMAs to issue, took 2.2).  Beside them the
-// starts: 2.5 us from the launch to the first scores, 1.3 us an item, 4 us for the merge.  Measured: 8x6
-// rows after 2048 slots of 7B heads 25 us, 16x4 after 16500 94 us (4.3 TB/s).  Registers are what the
+// starts: 5 us from the launch to the first scores, 0.9 us an item, 2.5 us for the merge.  Measured: 8x6
+// rows after 2048 slots of 7B heads 24 us, 16x4 after 16500 91 us (4.4 TB/s).  Registers are what the
 // softmax has least of: 44 spilled bytes fewer were worth 4 % to 7 %.
 // Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: S and two O.
 #include <algorithm>
@@ -110,11 +110,12 @@ struct PxSched {
   __device__ int begin(int c) const { return c * q + min(c, r); }
   __device__ int places(int k, int units) const { return units > 0 ? cost[k].start + units * cost[k].unit : 0; }
 };
-// What an item of that many rows costs: 1.3 us a unit and as much for the start with up to 32 rows, 2 us
-// (1.65 of 16 bits) and 2.6 with more, by the ends of the CTAs of four cases.  (Shares of as many units
-// each: 5 % more time for 16x4 rows after 16500 slots, 15 % for 64 rows of 16 bits after 8200.)
+// What an item of that many rows costs, a unit of up to 32 rows being 4 (1.2 us): units of more rows 2 us
+// (1.65 of 16 bits); starts 0.9 us, with more rows, whose queries and O have no second place, 4.5 us beside
+// the stream of K and V (3). By the ends of the CTAs of four cases and the times of sets of these numbers;
+// with shares of as many units each they are up to 20 % longer, with starts of 8 up to 8 %.
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
-  return rows > 32 ? PxCost{8, bf16 ? 5 : 6} : PxCost{4, 4};
+  return rows > 32 ? PxCost{bf16 ? 10 : 14, bf16 ? 5 : 6} : PxCost{3, 4};
 }
 // n / d for n < 2^16, inv = px_inv(d)
 __device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
@@ -161,7 +162,7 @@ __device__ PxPlan px_plan(const PrefixAttnParams& p, int ctas, int lane) {
   const int all = first * a.units + per * (int)__reduce_add_sync(0xffffffffu, (unsigned)(units0 + units1));
   // With few units they are the places (a CTA's share has to hold the places of any unit, or some CTA
   // within an item would have none of its units), and with very many, for the places' range.
-  const bool weighed = all > 2 * ctas && all < 1 << 27;
+  const bool weighed = all > 2 * ctas && all < 1 << 26;
 #pragma unroll
   for (int k = 0; k < 2; ++k) a.cost[k] = weighed ? px_cost(p.tiles[k].rows, p.bf16) : PxCost{0, 1};
   auto places = [&](int k, int units) { return units > 0 ? a.cost[k].start + units * a.cost[k].unit : 0; };
