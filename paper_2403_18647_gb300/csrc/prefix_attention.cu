@@ -495,6 +495,15 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   if (tid < PX_ROWS) sm.top[0][tid] = 0;
   pdl_wait();   // q, lengths, tables and rows come from the kernels before
   pdl_trigger();
+  if (warp >= 4) {
+    // All queries on their way to L2, a line a thread, before they are loaded: from memory that takes
+    // 0.8 us, and 2 us beside the stream of K and V.
+    const int lines = p.H * HD * (p.bf16 ? 2 : 4) / 128, z = (tid - 128) * gridDim.x + blockIdx.x, r = px_quot(z, lines);
+    if (r < p.b * p.nq) {
+      const char* at = static_cast<const char*>(p.q) + r * p.q_ld * (p.bf16 ? 2 : 4) + (z - r * lines) * 128;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+    }
+  }
   if (warp == 2) {
     const PxPlan a = px_plan(p, gridDim.x, lane);
 #pragma unroll
@@ -551,34 +560,21 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   if (warp >= 4) first_queries(tid - 128);
 
   if (warp == 2) {
-    // ---- the segments.  Their queries are on their way to L2 long before they are loaded: beside the
-    // stream of K and V a load from memory takes 2 us.
-    const int g1 = sm.sched.begin(blockIdx.x + 1);
-    int g = sm.sched.begin(blockIdx.x), near = 0, rows = 0, q_at = 1;
-    const int bytes = p.bf16 ? 2 : 4, lines = HD * bytes / 128;   // of a row and head
+    // ---- the segments
+    if (lane == 0) {
+      const int g1 = sm.sched.begin(blockIdx.x + 1);
+      int near = 0, rows = 0, q_at = 1;
 #pragma unroll 1
-    for (int i = 0;; ++i) {
-      wait(&sm.seg_empty[i % PX_SEGS], ((i / PX_SEGS) & 1) ^ 1);
-      if (lane == 0) {
+      for (int i = 0, g = sm.sched.begin(blockIdx.x);; ++i) {
         PxSeg e{};
         while (g < g1 && e.u0 == e.u1) e = px_segment(p, sm.sched, sm.len, g, g1, near);
         e.q_at = q_at = e.rows <= PX_TWICE ? q_at ^ 1 : 0;
         e.whole = max(rows, e.rows) > PX_TWICE;
         rows = e.rows;
+        wait(&sm.seg_empty[i % PX_SEGS], ((i / PX_SEGS) & 1) ^ 1);
         sm.seg[i % PX_SEGS] = e;
         mbar_arrive(&sm.seg_full[i % PX_SEGS]);
-      }
-      __syncwarp();
-      // (in place until the next segment but two: this warp writes it)
-      const PxSeg& e = sm.seg[i % PX_SEGS];
-      if (e.u0 == e.u1) break;
-      if (i > 0) {
-#pragma unroll 1
-        for (int z = lane; z < e.rows * lines; z += 32) {
-          const int r = z / lines, rr = e.row0 + r, tr = px_div(rr, p.inv_g);
-          const char* at = static_cast<const char*>(p.q) + (tr * p.q_ld + (e.hk * p.G + rr - tr * p.G) * HD) * bytes + (z - r * lines) * 128;
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
-        }
+        if (e.u0 == e.u1) break;
       }
     }
   } else if (warp == 0) {
