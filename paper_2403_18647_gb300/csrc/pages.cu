@@ -50,22 +50,25 @@ __device__ int block_scan(int v, int* warp_sums, int* sum) {
 }
 static_assert(PG_WARPS == 32, "one warp adds the warps up");
 
-// common[s] = leading pages that sequence s holds together with sequence 0 (a warp per sequence)
+// common[s] = leading pages that sequence s holds together with sequence 0 (a warp per sequence, the
+// loads of 128 columns in flight)
 __device__ void common_pages(const PagesParams& p) {
+  constexpr int N = 4;
   const int lane = threadIdx.x & 31;
   for (int s = threadIdx.x >> 5; s < p.batch; s += PG_WARPS) {
     int n = p.ld;
-    for (int j0 = 0; j0 < p.ld; j0 += 32) {
-      const int j = j0 + lane;
-      bool same = false;
-      if (j < p.ld) {
-        const int a = __ldcg(p.table + j);
-        same = a >= 0 && a == __ldcg(p.table + (size_t)s * p.ld + j);
+    for (int j0 = 0; j0 < p.ld && n == p.ld; j0 += 32 * N) {
+      int a[N], z[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = j0 + 32 * i + lane;
+        a[i] = j < p.ld ? __ldcg(p.table + j) : -1;
+        z[i] = j < p.ld ? __ldcg(p.table + (size_t)s * p.ld + j) : -1;
       }
-      const unsigned differ = __ballot_sync(0xffffffffu, !same);
-      if (differ) {
-        n = min(p.ld, j0 + __ffs(differ) - 1);
-        break;
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i) {   // (the first one that differs is what stays)
+        const unsigned differ = __ballot_sync(0xffffffffu, a[i] < 0 || a[i] != z[i]);
+        if (differ) n = min(p.ld, j0 + 32 * i + __ffs(differ) - 1);
       }
     }
     if (lane == 0) p.common[s] = n;
@@ -76,11 +79,11 @@ __device__ void common_pages(const PagesParams& p) {
 // A round of columns: every sequence's entries are read before any of them is written, so the
 // table can be permuted in place.
 __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const __grid_constant__ PagesParams p) {
-  __shared__ int src_s[PAGES_MAX_BATCH];
-  __shared__ int len_s[PAGES_MAX_BATCH];
+  __shared__ int src_s[PAGES_MAX_BATCH], len_all[PAGES_MAX_BATCH];
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, nb = p.src ? p.nb : 1;
+  for (int s = tid; s < p.batch; s += PG_THREADS) len_all[s] = __ldcg(p.len + s);
   for (int s = tid; s < nb; s += PG_THREADS) {
     int a = p.src ? __ldcg(p.src + s) : -1;
     if (a >= p.batch) {   // there is no such sequence: s stays as it is
@@ -88,10 +91,9 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const __grid_con
       a = p.seq0 + s;
     }
     src_s[s] = a;
-    len_s[s] = a < 0 ? 0 : __ldcg(p.len + a);
   }
   __syncthreads();
-  for (int s = tid; s < nb; s += PG_THREADS) p.len[p.seq0 + s] = len_s[s];
+  for (int s = tid; s < nb; s += PG_THREADS) p.len[p.seq0 + s] = src_s[s] < 0 ? 0 : len_all[src_s[s]];
   const int cols = PG_THREADS / nb;   // (nb <= PAGES_MAX_BATCH: a thread has one entry a round)
   for (int c0 = 0; c0 < p.ld; c0 += cols) {
     const int s = tid / cols, j = c0 + tid % cols;
