@@ -367,14 +367,13 @@ struct PrefixAttnParams {
   int b, nq, H, Hk, hd;
   void* out;                // [b*q][out_ld], the type of q
   __nv_bfloat16 *out_hi, *out_lo;   // [b*q][H*hd], or null: the O projection's operand
-  float* part;              // scratch: prefix_attention_scratch() floats, 1024-byte aligned
+  float* part;              // scratch: prefix_attention_scratch() floats (prefix_scratch.h), 1024-byte aligned
   int ctas;                 // set by launch_prefix_attention, as the next three
   int G;                    // H / Hk
   uint32_t inv_g, inv_nq;   // of G and nq, for divisions
   PxTiles tiles[2];         // of a cache head's rows: of the batch, of a sequence
   uint32_t* err;
 };
-size_t prefix_attention_scratch(int row_heads, int hd, int num_sms);
 cudaError_t prefix_attention_prepare();
 cudaError_t launch_prefix_attention(const PrefixAttnParams& p, int num_sms, cudaStream_t st, bool pdl);
 

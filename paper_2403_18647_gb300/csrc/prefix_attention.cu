@@ -52,16 +52,14 @@
 // rows after 2048 slots of 7B heads 24 us, 16x4 after 16500 91 us (4.4 TB/s).  Registers are what the
 // softmax has least of: 44 spilled bytes fewer were worth 4 % to 7 %.
 // Shared memory: a ring of K and V tiles, P and Q in three parts; TMEM: S and two O.
-#include <algorithm>
-
 #include "common.cuh"
 #include "internal.h"
+#include "prefix_scratch.h"
 
 namespace sdsat {
 namespace {
 
 constexpr int PX_UNIT = 128;      // slots of a unit: two pages
-constexpr int PX_ROWS = 64;       // rows of a tile
 constexpr int PX_PARTS = 3;       // bf16 parts of fp32 queries and of their probabilities
 constexpr int PX_GROUPS = 4;      // softmax groups of 128 threads
 constexpr int PX_SOFTMAX = 128 * PX_GROUPS;
@@ -390,9 +388,8 @@ struct PxScratch {
   float* o;        // [2 * row heads + PX_ROWS * CTAs][hd]
   float* m;        // the same rows' references
   float4* l;       // and sums, in four parts
-  static __host__ __device__ size_t rows(size_t row_heads, int ctas) { return (2 * row_heads + (size_t)PX_ROWS * ctas + 31) / 32 * 32; }
-  __host__ __device__ PxScratch(const PrefixAttnParams& p) {
-    const size_t n = rows((size_t)p.b * p.nq * p.H, p.ctas);
+  __device__ PxScratch(const PrefixAttnParams& p) {
+    const size_t n = px_scratch_rows((size_t)p.b * p.nq * p.H, p.ctas);
     l = reinterpret_cast<float4*>(p.part);
     m = p.part + 4 * n;
     o = m + n;
@@ -1129,12 +1126,6 @@ static PxTiles px_tiles(int all) {
 
 // for px_div: n * (inv d - 2^32) < 2^32
 static uint32_t px_inv(int d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
-
-// floats for row_heads rows of hd (twice as many of half the size)
-size_t prefix_attention_scratch(int row_heads, int hd, int num_sms) {
-  const size_t most = hd < 128 ? (size_t)row_heads * 2 : row_heads;
-  return std::max(PxScratch::rows(row_heads, num_sms) * (5 + std::max(hd, 128)), PxScratch::rows(most, num_sms) * (5 + 64));
-}
 
 cudaError_t prefix_attention_prepare() {
   const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;

@@ -19,6 +19,7 @@
 
 #include "sdsat.h"
 #include "internal.h"
+#include "prefix_scratch.h"
 
 using namespace sdsat;
 static_assert(TRACE_WORDS == SDSAT_TRACE_WORDS, "trace record size");
@@ -797,7 +798,7 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
             dalloc(c, &c->acc_counters, rows) && dalloc(c, &c->adaptive, SDSAT_MAX_ADAPTIVE) &&
             dalloc(c, &c->tree_pos, rows) && dalloc(c, &c->tree_anc, rows) &&
             dalloc(c, &c->tree_ws, (size_t)rows * TREE_WS_STRIDE) &&
-            dalloc(c, &c->prefix_part, prefix_attention_scratch(rows * cfg->n_heads, cfg->head_dim, c->num_sms)) &&
+            dalloc(c, &c->prefix_part, prefix_attention_scratch((size_t)rows * cfg->n_heads * cfg->head_dim, c->num_sms)) &&
             dalloc(c, &c->err, 1) && dalloc(c, &c->xop_hi, (size_t)OP_MAX_M * OP_MAX_K) &&
             dalloc(c, &c->ssq, (size_t)rows * ((d + 127) / 128)) &&
             dalloc(c, &c->xop_lo, (size_t)OP_MAX_M * OP_MAX_K);
