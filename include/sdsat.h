@@ -445,8 +445,8 @@ SDSAT_API sdsat_status sdsat_op_attention(sdsat_ctx* ctx, const float* q_dev, co
  *   len_dev    int32 [b] committed lengths
  * A slot on a page outside [0, n_pages) is not attended to and sets device bit PAGE.  hd 64 or
  * 128, H a multiple of Hk, b*q <= SDSAT_MAX_ROWS, b*q*H*hd <= SDSAT_MAX_ROWS rows of the
- * context's heads, b*q*H*table_ld <= 2^30; pointers 16-byte aligned, rows a multiple of 16 bytes
- * apart.  Errors: EINVAL. */
+ * context's heads, b*q*H*table_ld <= 2^30, max(b*q*G, H)*G < 2^32 for G = H/Hk; pointers
+ * 16-byte aligned, rows a multiple of 16 bytes apart.  Errors: EINVAL. */
 SDSAT_API sdsat_status sdsat_op_prefix_attention(sdsat_ctx* ctx, const void* q_dev, int64_t q_ld, const void* k_dev,
                                                  const void* v_dev, int n_pages, const int32_t* table_dev,
                                                  int table_ld, const int32_t* shared_dev, const int32_t* len_dev,

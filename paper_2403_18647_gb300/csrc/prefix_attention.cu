@@ -115,7 +115,7 @@ struct PxSched {
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
   return rows > 32 ? PxCost{bf16 ? 10 : 14, bf16 ? 5 : 6} : PxCost{3, 4};
 }
-// n / d for n < 2^16, inv = px_inv(d)
+// n / d for n d < 2^32 (rows and heads by a cache head's query heads: checked by the caller), inv = px_inv(d)
 __device__ __forceinline__ int px_div(int n, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)n, inv) : n; }
 // n / d for 0 <= n < 1.9e9, quotients below 2^30 (the first one is off by 2^-21 of itself at most, the
 // second one's operand is exact): a third of the instructions, which are fetched cold here
@@ -1124,7 +1124,7 @@ static PxTiles px_tiles(int all) {
   return t;
 }
 
-// for px_div: n * (inv d - 2^32) < 2^32
+// for px_div: n (inv d - 2^32) < n d < 2^32
 static uint32_t px_inv(int d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
 
 cudaError_t prefix_attention_prepare() {

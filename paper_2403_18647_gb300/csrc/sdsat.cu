@@ -1429,7 +1429,8 @@ sdsat_status sdsat_op_prefix_attention(sdsat_ctx* c, const void* q_dev, int64_t 
   const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
   if (q_ld < (long long)H * hd || out_ld < (long long)H * hd || q_ld % per16 || out_ld % per16) return SDSAT_EINVAL;
   if ((size_t)b * q * H * hd > (size_t)SDSAT_MAX_ROWS * c->cfg.n_heads * c->cfg.head_dim) return SDSAT_EINVAL;
-  const long long rows = (long long)n_pages * Hk * KV_PAGE;
+  const long long rows = (long long)n_pages * Hk * KV_PAGE, G = H / Hk;
+  if (std::max<long long>(b * q * G, H) * G >= 1ll << 32) return SDSAT_EINVAL;   // (rows and heads are divided by G through a 32-bit reciprocal)
   if (rows > 0x7FFFFFFFll || (long long)b * q * H * table_ld > 1ll << 30) return SDSAT_EINVAL;   // (units are counted in 32 bits)
   PrefixAttnParams a;
   std::memset(&a, 0, sizeof(a));

@@ -26,3 +26,22 @@ def test_heads_of_half_the_size_on_a_context_of_many(sd):
     c.dims, c.x, c.k, c.v = (4, 16, 50, 50, 64), some(c.x), c.k[:, 7::40], c.v[:, 7::40]
     c.check(some(out))
     assert ctx.get_error() == 0
+
+
+def test_cache_heads_of_more_queries_than_a_reciprocal_divides_are_refused(sd):
+    """Rows of a cache head are divided by its query heads with 32-bit reciprocals: their number times G < 2^32."""
+    ctx = sd.Context(synth.ModelShape("wide", 1, 128, 1000, 128, 256, 256, 0), None, max_position=64)
+
+    def call(H, Hk=1):
+        c = Case(19, 1, 1, H, Hk, 64, [2], 0)
+        return c, c.run(ctx)
+
+    for H, Hk in ((65536, 1), (128000, 1), (128000, 2)):
+        with pytest.raises(sd.SdsatError) as e:
+            call(H, Hk)
+        assert e.value.status == 1
+    c, out = call(65535)
+    some = lambda x: x.view(1, 65535, 64)[:, 65500:].reshape(1, -1)  # noqa: E731
+    c.dims, c.x = (1, 1, 35, 1, 64), some(c.x)
+    c.check(some(out))
+    assert ctx.get_error() == 0
