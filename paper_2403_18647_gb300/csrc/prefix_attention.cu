@@ -527,7 +527,8 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
   // Every role goes through every segment, unit, wait and barrier of the share, whatever the waits
   // return: one that ran out has set the error bit, and the results are invalid.
   auto wait = [&](uint64_t* bar, uint32_t parity) { px_wait(bar, parity, &sm.abort, p.err); };
-  // the i-th segment's description (in place until each role has arrived at seg_empty)
+  // the i-th segment's description (in place until each role has arrived at seg_empty, all lanes of its warps
+  // having read it: `arrive`)
   auto segment = [&](int i) -> const PxSeg& {
     wait(&sm.seg_full[i % PX_SEGS], (i / PX_SEGS) & 1);
     return sm.seg[i % PX_SEGS];
@@ -581,8 +582,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
 #pragma unroll 1
     for (int seg = 0;; ++seg) {
       const PxSeg e = segment(seg);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      arrive(&sm.seg_empty[seg % PX_SEGS]);
       if (e.u0 == e.u1) break;
       const int* row = p.table + (size_t)max(e.s, 0) * p.ld;
       const int j0 = e.slot0 / KV_PAGE + 2 * e.u0, j1 = min((e.end + KV_PAGE - 1) / KV_PAGE, e.slot0 / KV_PAGE + 2 * e.u1);
@@ -670,7 +670,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
           commit(&sm.empty[slot]);
         }
         commit(&sm.q_empty[seg & 1]);
-        if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+        arrive(&sm.seg_empty[seg % PX_SEGS]);
       }
     } else {
       const uint64_t vd = px_desc_mn(smem_u32(smem), C::HALF), pd = px_desc_mn(smem_u32(Ps), C::P_PART);
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
             ++run;
           }
         }
-        if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+        arrive(&sm.seg_empty[seg % PX_SEGS]);
       }
     }
     if (sm.abort) {   // wait for issued MMAs before shared memory goes away
@@ -782,7 +782,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1) prefix_attention_kernel(const _
         tc_fence_before();
         arrive(&sm.o_empty[run & 1]);
       }
-      if (lane == 0) mbar_arrive(&sm.seg_empty[seg % PX_SEGS]);
+      arrive(&sm.seg_empty[seg % PX_SEGS]);
     }
   } else {
     const int wg = (warp >> 2) - 1, e = tid & 127;   // softmax thread, group, slot of the unit

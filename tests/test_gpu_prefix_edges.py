@@ -45,3 +45,16 @@ def test_cache_heads_of_more_queries_than_a_reciprocal_divides_are_refused(sd):
     c.dims, c.x = (1, 1, 35, 1, 64), some(c.x)
     c.check(some(out))
     assert ctx.get_error() == 0
+
+
+@pytest.mark.parametrize("H,hd,type", [(40, 128, torch.float32), (64, 64, torch.float32), (40, 128, torch.bfloat16)])
+def test_many_short_segments_on_every_sm(sd, H, hd, type):
+    """Some twenty items of one unit for each CTA, so that the segments' descriptions go round several times: every
+    call gives the same bits."""
+    ctx = sd.Context(synth.SHAPES["13b"], None, max_position=64)
+    c = Case(20, 64, 1, H, H, hd, [s % 5 for s in range(64)], 0, type)
+    out = c.run(ctx)
+    c.check(out)
+    for _ in range(100):
+        assert torch.equal(c.run(ctx), out)
+    assert ctx.get_error() == 0
