@@ -318,6 +318,22 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         tmem_st16(ts + 64 + i / 2, lo);
       }
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      // The product reads steps of 16 keys.  Slots behind the CTA's last key may hold anything (a paged
+      // cache's pages what their last owner left), and 0 times NaN is NaN: their values become zeros, the
+      // same ones from each tile that reads the block.  (The slot of V held K of block j - 1, whose S is
+      // complete: its next phase is V's.)
+      const int there = keys(nt - 1) - j * PA_ROWS;   // keys of the block
+      if (there < PA_ROWS && there % 16) {
+        constexpr int CHUNKS = HD / 8;   // of 16 bytes, of a key
+        const int vs = (2 * j + 1) % PA_SLOTS;
+        ok = mbar_wait_bounded(&full[vs], ((2 * j + 1) / PA_SLOTS) & 1, abort_flag, p.err);
+        for (int z = there * CHUNKS + (threadIdx.x & 127); z < (there + 15) / 16 * 16 * CHUNKS; z += 128) {
+          const int at = z / CHUNKS, i = z % CHUNKS;
+          *reinterpret_cast<uint4*>(ring + (size_t)vs * C::TILE + (i >> 3) * C::HALF + at * 128 + (((i & 7) ^ (at & 7)) << 4)) =
+              make_uint4(0u, 0u, 0u, 0u);
+        }
+        fence_proxy_async_smem();
+      }
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(&p_full[t]);
