@@ -21,6 +21,12 @@
 // 64-position blocks, whose K and V fragments each warp read from shared memory again), 2047
 // 81 (256), 512 23 (43), 99 12.3 (20); at 4095 1.08 PFLOP/s executed.
 //
+// Values that no position may see take part with P = 0: the slots behind the last key, up to the 16 keys
+// of a product's step, and pages that are not there.  They may hold anything (a paged cache's pages what
+// their last owner left), and 0 times NaN is NaN, so they are made zeros in the ring before the product, by the
+// warp that loads, which has nothing left to load by then: 1 % of a launch at 2047 positions.  (By the
+// softmax warps, whose registers are all taken, 4 %; by warp 2, which has to be told when, 2.5 %.)
+//
 // Warps 0-3: TMA (warp 0), MMA issue and TMEM (warp 1), two idle; warps 4-7 and 8-11: softmax
 // and output of tile 0 and 1.  Shared memory: Q 64 KB per tile, a ring of three 32 KB slots in
 // which K and V blocks alternate (hd 128).
@@ -36,6 +42,7 @@ constexpr int PA_ROWS = 128;      // chunk positions per tile, and keys per bloc
 constexpr int PA_SLOTS = 3;
 constexpr int PA_THREADS = 384;
 constexpr float PA_LAZY = 8.0f;   // log2 of the growth of a row maximum that is left unscaled
+constexpr float PA_UNSET = -1e30f;   // reference of a row that has seen no key
 
 template <int HD>
 struct PaCfg {
@@ -45,8 +52,8 @@ struct PaCfg {
   static constexpr int TILE = HALVES * HALF;                // Q hi, Q lo, K or V: 128 rows
   static constexpr size_t OFF_RING = 2 * 2 * (size_t)TILE;  // after Q hi + lo of two tiles
   static constexpr size_t OFF_BAR = OFF_RING + (size_t)PA_SLOTS * TILE;
-  static constexpr int NBAR = 2 * PA_SLOTS + 2 * 4 + 1;
-  static constexpr size_t SMEM = 1024 + OFF_BAR + NBAR * 8 + 16;
+  static constexpr int NBAR = 2 * PA_SLOTS + 2 * 5 + 1;
+  static constexpr size_t SMEM = 1024 + OFF_BAR + NBAR * 8 + 32;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
 };
 
@@ -107,7 +114,8 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(rb), "f"(ra));
 }
 
-template <int HD>
+// PAGED: pages by a table (an instance of its own, as the scores' registers are all taken)
+template <int HD, bool PAGED>
 __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const __grid_constant__ PfAttnParams p) {
   using C = PaCfg<HD>;
   extern __shared__ uint8_t smem_raw[];
@@ -119,9 +127,15 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
   uint64_t* s_full = q_full + 2;          // [2] S of a block is complete (and everything issued before it)
   uint64_t* p_full = s_full + 2;          // [2] P is in TMEM, O is rescaled (128 threads)
   uint64_t* o_full = p_full + 2;          // [2] the last product is complete
-  uint64_t* drain = o_full + 2;
+  // [2] by block parity: values that no position may see are zeros (V of the block after the next one is not
+  // asked for before this one's products are issued)
+  uint64_t* z_done = o_full + 2;
+  uint64_t* drain = z_done + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // [4] by block: which of its two pages there are (bits 0, 1).  The next block that uses an entry is loaded
+  // when the products of this one's values are done.
+  uint32_t* pages_ok = tmem_slot + 2;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rows = p.tiles * PA_ROWS, nqb = (p.M + rows - 1) / rows;
@@ -137,6 +151,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
       mbar_init(&s_full[t], 1);
       mbar_init(&p_full[t], 128);
       mbar_init(&o_full[t], 1);
+      mbar_init(&z_done[t], 1);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -158,6 +173,24 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
   auto keys = [&](int t) { return len + min(q0 + (t + 1) * PA_ROWS, p.M); };
   auto blocks = [&](int t) { return (keys(t) + PA_ROWS - 1) / PA_ROWS; };
   const int nb = blocks(nt - 1);
+  // blocks with values that no position may see: the last one, where a step of 16 keys runs past its end,
+  // and those with a page that is not there
+  const bool tail = keys(nt - 1) % 16 != 0;
+  auto zeros = [&](int j) { return (tail && j == nb - 1) || (PAGED && pages_ok[j & 3] != 3u); };
+  // ... made zeros, by thread i0 of n
+  auto make_zeros = [&](int j, int i0, int n) {
+    const int vs = (2 * j + 1) % PA_SLOTS, there = min(PA_ROWS, keys(nt - 1) - j * PA_ROWS);   // keys of the block
+    if (!mbar_wait_bounded(&full[vs], ((2 * j + 1) / PA_SLOTS) & 1, abort_flag, p.err)) return;
+    const uint32_t ok_pages = PAGED ? pages_ok[j & 3] : 3u;
+    constexpr int CHUNKS = HD / 8;   // of 16 bytes, of a key
+    for (int z = (ok_pages != 3u ? 0 : there * CHUNKS) + i0; z < (there + 15) / 16 * 16 * CHUNKS; z += n) {
+      const int at = z / CHUNKS, i = z % CHUNKS;
+      if (at >= there || !((ok_pages >> (at / KV_PAGE)) & 1u))
+        *reinterpret_cast<uint4*>(ring + (size_t)vs * C::TILE + (i >> 3) * C::HALF + at * 128 + (((i & 7) ^ (at & 7)) << 4)) =
+            make_uint4(0u, 0u, 0u, 0u);
+    }
+    fence_proxy_async_smem();
+  };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -174,18 +207,27 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
       for (; it < 2 * nb; ++it) {   // K of block 0, V of block 0, K of block 1, ...
         const int s = it % PA_SLOTS;
         if (!mbar_wait_bounded(&empty[s], ((it / PA_SLOTS) & 1) ^ 1, abort_flag, p.err)) break;
-        mbar_arrive_expect_tx(&full[s], C::TILE);
         const CUtensorMap* map = (it & 1) ? &p.vmap : &p.kmap;
         int row[2] = {rowbase + (it >> 1) * PA_ROWS, rowbase + (it >> 1) * PA_ROWS + 64};
-        if (p.pages.table) {   // (a box past the sequence's pages holds no visible key: any page does)
+        if (PAGED) {   // (for a page that is not there, or holds no visible key, any one is loaded)
+          uint32_t there = 0;
           for (int b = 0; b < 2; ++b) {
-            const int j = (it & ~1) + b, page = j < p.pages.ld ? __ldcg(p.pages.table + (size_t)p.seq * p.pages.ld + j) : 0;
-            row[b] = p.row0 + (min(max(page, 0), p.pages.n - 1) * p.H + h) * KV_PAGE;
+            const int j = (it & ~1) + b, page = j < p.pages.ld ? __ldcg(p.pages.table + (size_t)p.seq * p.pages.ld + j) : -1;
+            const bool in = page >= 0 && page < p.pages.n;
+            row[b] = p.row0 + ((in ? page : 0) * p.H + h) * KV_PAGE;
+            if (in || j * KV_PAGE >= keys(nt - 1)) there |= 1u << b;
+            else set_error(p.err, ERR_PAGE);
           }
+          pages_ok[(it >> 1) & 3] = there;
         }
+        mbar_arrive_expect_tx(&full[s], C::TILE);
         for (int hh = 0; hh < C::HALVES; ++hh)
           for (int b = 0; b < 2; ++b)
             tma_load_2d(ring + (size_t)s * C::TILE + hh * C::HALF + b * C::BOX, map, &full[s], hh * 64, row[b], pol);
+        if (PAGED && (it & 1) && (it >> 1) < nb - 1 && zeros(it >> 1)) {
+          make_zeros(it >> 1, 0, 1);
+          mbar_arrive(&z_done[(it >> 1) & 1]);
+        }
       }
       if (*abort_flag) {   // let the copies in flight land before the CTA exits
         auto land = [&](uint64_t* bar, uint32_t parity) {
@@ -196,6 +238,12 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         for (int t = 0; t < nt; ++t) land(&q_full[t], 0);
         for (int i = max(0, it - PA_SLOTS); i < it; ++i) land(&full[i % PA_SLOTS], (i / PA_SLOTS) & 1);
       }
+    }
+    __syncwarp();
+    if (zeros(nb - 1)) {
+      make_zeros(nb - 1, lane, 32);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&z_done[(nb - 1) & 1]);
     }
   } else if (warp == 1) {
     if (lane == 0) {
@@ -231,15 +279,18 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         if (j == blocks(t) - 1) umma_commit(&o_full[t]);
       };
       for (int t = 0; t < nt && ok; ++t) wait(&q_full[t], 0);
+      uint32_t zeroed = 0;   // the phases of z_done
       // step j: per tile, block j - 1's P V and then block j's S over the P it has read; the last
       // tile has every block, so its products release V of block j - 1 and K of block j
       for (int j = 0; j <= nb && ok; ++j) {
         const int ks = (2 * j) % PA_SLOTS, vs = (2 * j + PA_SLOTS - 1) % PA_SLOTS;
         for (int t = 0; t < nt && ok; ++t) {
           const int n = blocks(t);
-          if (j > 0 && j <= n && wait(&full[vs], ((2 * j - 1) / PA_SLOTS) & 1) && wait(&p_full[t], (j - 1) & 1)) {
+          if (j > 0 && j <= n && wait(&full[vs], ((2 * j - 1) / PA_SLOTS) & 1) &&
+              (!zeros(j - 1) || wait(&z_done[(j - 1) & 1], (zeroed >> ((j - 1) & 1)) & 1)) && wait(&p_full[t], (j - 1) & 1)) {
             pv(t, j - 1);
             if (t == nt - 1) umma_commit(&empty[vs]);
+            if (PAGED && t == nt - 1 && zeros(j - 1)) zeroed ^= 1u << ((j - 1) & 1);
           }
           if (j < n && ok && wait(&full[ks], (2 * j / PA_SLOTS) & 1)) {
             qk(t, j);
@@ -278,12 +329,19 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         for (int i = 0; i < PA_ROWS; ++i)
           if (i > last) s[i] = -INFINITY;
       }
+      const uint32_t ok_pages = PAGED ? pages_ok[j & 3] : 3u;
+      if (ok_pages != 3u) {   // keys without a page are not attended to
+#pragma unroll
+        for (int i = 0; i < PA_ROWS; ++i)
+          if (!((ok_pages >> (i / KV_PAGE)) & 1u)) s[i] = -INFINITY;
+      }
       float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
       for (int i = 4; i < PA_ROWS; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[i]);
-      const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+      float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+      if (ok_pages != 3u) mb = fmaxf(mb, PA_UNSET);
       if (j == 0) {
-        m = mb;   // block 0 holds key 0, which every row sees
+        m = mb;   // block 0 holds key 0, which every row sees (if it has a page)
       } else {
         // the S that is ready was issued after block j - 1's P V product: O holds blocks 0 .. j-1
         const bool grow = mb > m + PA_LAZY;
@@ -318,22 +376,6 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
         tmem_st16(ts + 64 + i / 2, lo);
       }
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      // The product reads steps of 16 keys.  Slots behind the CTA's last key may hold anything (a paged
-      // cache's pages what their last owner left), and 0 times NaN is NaN: their values become zeros, the
-      // same ones from each tile that reads the block.  (The slot of V held K of block j - 1, whose S is
-      // complete: its next phase is V's.)
-      const int there = keys(nt - 1) - j * PA_ROWS;   // keys of the block
-      if (there < PA_ROWS && there % 16) {
-        constexpr int CHUNKS = HD / 8;   // of 16 bytes, of a key
-        const int vs = (2 * j + 1) % PA_SLOTS;
-        ok = mbar_wait_bounded(&full[vs], ((2 * j + 1) / PA_SLOTS) & 1, abort_flag, p.err);
-        for (int z = there * CHUNKS + (threadIdx.x & 127); z < (there + 15) / 16 * 16 * CHUNKS; z += 128) {
-          const int at = z / CHUNKS, i = z % CHUNKS;
-          *reinterpret_cast<uint4*>(ring + (size_t)vs * C::TILE + (i >> 3) * C::HALF + at * 128 + (((i & 7) ^ (at & 7)) << 4)) =
-              make_uint4(0u, 0u, 0u, 0u);
-        }
-        fence_proxy_async_smem();
-      }
       tmem_wait_st();
       tc_fence_before();
       mbar_arrive(&p_full[t]);
@@ -341,7 +383,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
     ok = ok && mbar_wait_bounded(&o_full[t], 0, abort_flag, p.err);
     if (__all_sync(0xffffffffu, ok)) {
       tc_fence_after();
-      const float inv = 1.0f / l;
+      const float inv = PAGED && l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
 #pragma unroll 1
       for (int i = 0; i < HD; i += 16) {
         float o[16];
@@ -371,12 +413,17 @@ __global__ void __launch_bounds__(PA_THREADS, 1) prefill_attention_kernel(const 
   }
 }
 
+template <int HD, bool PAGED>
+static cudaError_t pa_prepare() {
+  const auto kernel = prefill_attention_kernel<HD, PAGED>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PaCfg<HD>::SMEM);
+  return e == cudaSuccess ? prefer_shared(kernel) : e;
+}
 cudaError_t prefill_attention_prepare() {
-  const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(prefill_attention_kernel<64>, a, (int)PaCfg<64>::SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_attention_kernel<128>, a, (int)PaCfg<128>::SMEM);
-  if (e == cudaSuccess) e = prefer_shared(prefill_attention_kernel<64>);
-  if (e == cudaSuccess) e = prefer_shared(prefill_attention_kernel<128>);
+  cudaError_t e = pa_prepare<64, false>();
+  if (e == cudaSuccess) e = pa_prepare<128, false>();
+  if (e == cudaSuccess) e = pa_prepare<64, true>();
+  if (e == cudaSuccess) e = pa_prepare<128, true>();
   return e;
 }
 
@@ -393,8 +440,11 @@ cudaError_t launch_prefill_attention(PfAttnParams& p, int num_sms, cudaStream_t 
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
-  return p.hd == 64 ? cudaLaunchKernelEx(&cfg, prefill_attention_kernel<64>, p)
-                    : cudaLaunchKernelEx(&cfg, prefill_attention_kernel<128>, p);
+  if (p.pages.table)
+    return p.hd == 64 ? cudaLaunchKernelEx(&cfg, prefill_attention_kernel<64, true>, p)
+                      : cudaLaunchKernelEx(&cfg, prefill_attention_kernel<128, true>, p);
+  return p.hd == 64 ? cudaLaunchKernelEx(&cfg, prefill_attention_kernel<64, false>, p)
+                    : cudaLaunchKernelEx(&cfg, prefill_attention_kernel<128, false>, p);
 }
 
 }  // namespace sdsat
