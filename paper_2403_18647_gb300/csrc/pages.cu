@@ -50,6 +50,14 @@ __device__ int block_scan(int v, int* warp_sums, int* sum) {
 }
 static_assert(PG_WARPS == 32, "one warp adds the warps up");
 
+// a table entry as a page of the pool, or -1 for none (the table can be written from outside: a number that is
+// neither is reported and counts as none)
+__device__ __forceinline__ int pool_page(const PagesParams& p, int entry) {
+  if (entry >= -1 && entry < p.n_pages) return entry;
+  set_error(p.err, ERR_PAGE);
+  return -1;
+}
+
 // common[s] = leading pages that sequence s holds together with sequence 0 (a warp per sequence, the
 // loads of 128 columns in flight)
 __device__ void common_pages(const PagesParams& p) {
@@ -98,16 +106,17 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const __grid_con
   for (int c0 = 0; c0 < p.ld; c0 += cols) {
     const int s = tid / cols, j = c0 + tid % cols;
     const bool mine = s < nb && j < p.ld;
-    int was = -1, now = -1;
+    int there = -1, now = -1;
     int* entry = nullptr;
     if (mine) {
       entry = p.table + (size_t)(p.seq0 + s) * p.ld + j;
-      was = __ldcg(entry);
+      there = __ldcg(entry);
       const int a = src_s[s];
-      now = a < 0 ? -1 : __ldcg(p.table + (size_t)a * p.ld + j);
+      now = a < 0 ? -1 : pool_page(p, __ldcg(p.table + (size_t)a * p.ld + j));
     }
     __syncthreads();
-    if (mine && was != now) {
+    if (mine && there != now) {
+      const int was = pool_page(p, there);
       __stcg(entry, now);
       if (was >= 0) atomicSub(p.refs + was, 1);
       if (now >= 0) atomicAdd(p.refs + now, 1);
@@ -150,7 +159,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
       const int j = j0 + lane;
       int kind = KEEP, page = -1;
       if (j < end_s[s]) {
-        page = __ldcg(p.table + (size_t)(p.seq0 + s) * p.ld + j);
+        page = pool_page(p, __ldcg(p.table + (size_t)(p.seq0 + s) * p.ld + j));
         if (page < 0) {
           kind = FRESH;
         } else {
@@ -282,7 +291,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const __grid_
   // the committed slots of the pages past the front
   const long long entries = (long long)p.batch * p.ld;
   for (long long i = tid; i < entries && holes; i += PG_THREADS) {
-    const int page = __ldcg(p.table + i);
+    const int page = pool_page(p, __ldcg(p.table + i));
     if (page >= used) {
       const int s = (int)(i / p.ld), rows = min(KV_PAGE, __ldcg(p.len + s) - (int)(i - (long long)s * p.ld) * KV_PAGE);
       if (rows > 0) atomicMax(p.kinds + page, rows);
@@ -318,7 +327,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const __grid_
   __syncthreads();
   for (long long i = tid; i < entries && holes; i += PG_THREADS) {
     const int page = __ldcg(p.table + i);
-    if (page >= used) __stcg(p.table + i, __ldcg(p.kinds + page));
+    if (page >= used && page < p.n_pages) __stcg(p.table + i, __ldcg(p.kinds + page));
   }
   if (tid == 0) p.copies[0] = copies;
 }

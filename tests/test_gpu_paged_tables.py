@@ -1,0 +1,80 @@
+"""Paged caches whose tables and lengths, which are handed out as writable memory, hold numbers that no call wrote: reported,
+counted as none, and nothing beside them changes."""
+import pytest
+import torch
+
+import synth
+
+pytestmark = pytest.mark.gpu
+
+PAGE = 64
+
+
+@pytest.fixture(scope="module")
+def sd():
+    import paper_2403_18647_gb300 as sd
+    return sd
+
+
+@pytest.fixture(scope="module")
+def model(sd):
+    shape = synth.SHAPES["tiny"]
+    return shape, sd.Context(shape, synth.make_model(shape, seed=0, device="cuda", gain_std=0.1), max_position=1024)
+
+
+def i32(x):
+    return torch.tensor(list(x), dtype=torch.int32, device="cuda")
+
+
+def cache(ctx):
+    """Three sequences of 2, 1 and 3 pages, in this order, of a pool of 10."""
+    kv = ctx.kv_paged(3, 256, 10)
+    for s, n in ((0, 100), (1, 20), (2, 190)):
+        ctx.kv_reserve(kv, 1, n, seq=s)
+    ctx.kv_commit(kv, i32([100, 20, 190]), 3)
+    assert kv.table.tolist() == [[0, 1, -1, -1], [2, -1, -1, -1], [3, 4, 5, -1]]
+    return kv
+
+
+OUTSIDE = [10, 11, 5000, 2 ** 31 - 1, -2, -2 ** 31]
+
+
+@pytest.mark.parametrize("page", OUTSIDE)
+def test_fork_and_free_drop_pages_outside_the_pool(sd, model, page):
+    _, ctx = model
+    kv = cache(ctx)
+    kv.table[2, 1] = page
+    ctx.kv_fork(kv, i32([2, 1]))
+    assert ctx.get_error() == sd.DEV_PAGE
+    assert kv.table.tolist() == [[3, -1, 5, -1], [2, -1, -1, -1], [3, page, 5, -1]]
+    assert kv.refs.tolist() == [0, 0, 1, 2, 1, 2, 0, 0, 0, 0]
+    ctx.kv_free(kv, 2)
+    assert ctx.get_error() == sd.DEV_PAGE
+    assert kv.table.tolist() == [[3, -1, 5, -1], [2, -1, -1, -1], [-1] * 4]
+    assert kv.refs.tolist() == [0, 0, 1, 1, 1, 1, 0, 0, 0, 0]
+    assert kv.lens.tolist() == [190, 20, 0]
+
+
+@pytest.mark.parametrize("page", OUTSIDE)
+def test_reserve_gives_a_page_in_their_place(sd, model, page):
+    _, ctx = model
+    kv = cache(ctx)
+    kv.table[2, 2] = page
+    ctx.kv_reserve(kv, 3, 6)
+    assert ctx.get_error() == sd.DEV_PAGE
+    assert kv.table.tolist() == [[0, 1, -1, -1], [2, -1, -1, -1], [3, 4, 6, 7]]
+    assert kv.refs.tolist() == [1] * 8 + [0, 0]
+
+
+@pytest.mark.parametrize("page", OUTSIDE)
+def test_compact_leaves_them(sd, model, page):
+    _, ctx = model
+    kv = cache(ctx)
+    ctx.kv_free(kv, 0)
+    kv.table[1, 3] = page
+    used = i32([0])
+    ctx.kv_compact(kv, used)
+    assert ctx.get_error() == sd.DEV_PAGE
+    assert used.item() == 4
+    assert kv.table.tolist() == [[-1] * 4, [2, -1, -1, page], [3, 0, 1, -1]]
+    assert kv.refs.tolist() == [1] * 4 + [0] * 6
