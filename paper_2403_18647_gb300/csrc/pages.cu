@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const __grid_con
   for (int s = tid; s < p.batch; s += PG_THREADS) len_all[s] = __ldcg(p.len + s);
   for (int s = tid; s < nb; s += PG_THREADS) {
     int a = p.src ? __ldcg(p.src + s) : -1;
-    if (a >= p.batch) {   // there is no such sequence: s stays as it is
+    if (a < -1 || a >= p.batch) {   // there is no such sequence: s stays as it is
       set_error(p.err, ERR_PAGE);
       a = p.seq0 + s;
     }

@@ -78,3 +78,14 @@ def test_compact_leaves_them(sd, model, page):
     assert used.item() == 4
     assert kv.table.tolist() == [[-1] * 4, [2, -1, -1, page], [3, 0, 1, -1]]
     assert kv.refs.tolist() == [1] * 4 + [0] * 6
+
+
+@pytest.mark.parametrize("src", [-2, -100, 3, 2 ** 31 - 1])
+def test_sequences_outside_the_batch_are_not_forked_from(sd, model, src):
+    """-1 alone empties a sequence."""
+    _, ctx = model
+    kv = cache(ctx)
+    before = kv.table.tolist(), kv.refs.tolist(), kv.lens.tolist()
+    ctx.kv_fork(kv, i32([0, src, 2]))
+    assert ctx.get_error() == sd.DEV_PAGE
+    assert (kv.table.tolist(), kv.refs.tolist(), kv.lens.tolist()) == before
