@@ -59,10 +59,10 @@ struct PageMap {
   int ld, n;
 };
 // Element offset within a layer of (sequence, head 0, slot, dimension 0), -1 where the slot must not
-// be written: past the capacity, without a page, or on a page that other sequences hold too.
+// be written: outside the capacity, without a page, or on a page that other sequences hold too.
 // (Heads are KV_PAGE rows apart in a paged cache, cap rows in a contiguous one.)
 __device__ __forceinline__ long long cache_row(const PageMap& pg, int seq, int slot, int H, int cap, int hd) {
-  if (slot >= cap) return -1;
+  if ((unsigned)slot >= (unsigned)cap) return -1;
   if (!pg.table) return ((long long)seq * H * cap + slot) * hd;
   const int page = __ldcg(pg.table + (size_t)seq * pg.ld + slot / KV_PAGE);
   if (page < 0 || page >= pg.n || __ldcg(pg.refs + page) != 1) return -1;

@@ -138,11 +138,11 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const __grid_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int refs_mine = tid < p.n_pages ? __ldcg(p.refs + tid) : 1;   // (needed later; on its way now)
   for (int s = tid; s < p.nb; s += PG_THREADS) {
-    const int len = __ldcg(p.len + p.seq0 + s);
+    const int was = __ldcg(p.len + p.seq0 + s), len = min(max(was, 0), p.cap);
     long long end = (long long)len + p.n;
-    if (end > p.cap) {   // the slots past the capacity get no page
+    if (end > p.cap || len != was) {   // the slots past the capacity get no page
       set_error(p.err, ERR_CAPACITY);
-      end = p.cap;
+      end = min(end, (long long)p.cap);
     }
     first_s[s] = len / KV_PAGE;
     part_s[s] = len % KV_PAGE;

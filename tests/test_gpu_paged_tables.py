@@ -89,3 +89,26 @@ def test_sequences_outside_the_batch_are_not_forked_from(sd, model, src):
     ctx.kv_fork(kv, i32([0, src, 2]))
     assert ctx.get_error() == sd.DEV_PAGE
     assert (kv.table.tolist(), kv.refs.tolist(), kv.lens.tolist()) == before
+
+
+@pytest.mark.parametrize("n", [-1, -70, -2 ** 31, 257, 10 ** 6, 2 ** 31 - 100])
+def test_lengths_outside_the_capacity(sd, model, n):
+    """Pages from slot 0 on, or none; a block's rows outside the capacity are not written."""
+    shape, ctx = model
+    kv = cache(ctx)
+    kv.lens[1] = n
+    ctx.kv_reserve(kv, 1, 70, seq=1)
+    assert ctx.get_error() == sd.DEV_CAPACITY
+    assert kv.table.tolist() == [[0, 1, -1, -1], [2, 6, -1, -1] if n < 0 else [2, -1, -1, -1], [3, 4, 5, -1]]
+    assert kv.refs.tolist() == [1] * 6 + [1 if n < 0 else 0] + [0] * 3
+    kv.lens[1] = n if n != -1 else -7            # (a block of six rows ends below 0)
+    ctx.kv_reserve(kv, 1, 6, seq=2)
+    ctx.get_error()
+    kv.k.fill_(1.0), kv.v.fill_(1.0)
+    lg = torch.empty(18, shape.vocab, device="cuda")
+    ctx.block_forward(kv, synth.prompt_ids(0, 41, 18, 4096).cuda(), lg, 3, 6)
+    assert ctx.get_error() & sd.DEV_CAPACITY
+    written = kv.table[0, 1].item(), kv.table[2, 2].item(), kv.table[2, 3].item()    # the rows of the others
+    rest = [i for i in range(10) if i not in written]
+    assert (kv.k[:, rest] == 1).all() and (kv.v[:, rest] == 1).all()
+    assert all((kv.k[:, i] != 1).any() for i in written)
