@@ -151,7 +151,9 @@ SDSAT_API void sdsat_kv_destroy(sdsat_kv* kv);
  * to `max_len` slots each, which may share pages.  Every call that takes a cache takes a
  * paged one, with two differences: the slots that a call writes (block rows, a prompt,
  * sdsat_kv_write) need pages that their sequence alone holds (sdsat_kv_reserve), and a row
- * without one is not written and sets device bit CAPACITY; and block forwards read the
+ * without one is not written and sets device bit CAPACITY (sdsat_prefill, and an accept call
+ * with commit, leave the length as it was where a row that they would commit has none;
+ * sdsat_kv_commit sets any length); and block forwards read the
  * leading pages that all their sequences share once for all of them.
  * Synchronous.  Errors: EINVAL (batch > 256), ENOMEM, ECAPACITY (as sdsat_kv_create),
  * EUNSUPPORTED (n_layers * n_pages * n_heads * SDSAT_PAGE >= 2^31). */

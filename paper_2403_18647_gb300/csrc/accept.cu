@@ -618,8 +618,9 @@ __global__ void __launch_bounds__(ACC_THREADS, 4) accept_kernel(const AcceptPara
   }
   p.accepted_len[sl] = 1 + m;
   if (p.commit) {
-    const int nl = __ldcg(p.len + s) + 1 + m;
-    if (nl <= p.cap) p.len[s] = nl;
+    // (rows without a page of the sequence's own have not been written; at most SDSAT_ATT_MAXQ slots: two pages)
+    const int l0 = __ldcg(p.len + s), nl = l0 + 1 + m;
+    if (nl <= p.cap && (!p.pages.table || (l0 >= 0 && own_page(p.pages, s, l0) && own_page(p.pages, s, nl - 1)))) p.len[s] = nl;
     else set_error(p.err, ERR_CAPACITY);
     if (p.emitted) p.emitted[s] += 1 + m;
   }
@@ -905,18 +906,35 @@ cudaError_t launch_commit(int* len, const int* new_len, int nb, int cap, uint32_
   return cudaLaunchKernelEx(&cfg, commit_kernel, len, new_len, nb, cap, err);
 }
 
-__global__ void add_len_kernel(int* len, int seq, int n, int cap, uint32_t* err) {
+// A prompt's rows, `n` more of them.  On a paged cache (one warp): the last ones commit the prompt if every
+// slot of it is on a page that the sequence alone holds; rows on others have not been written, and the
+// length goes back to what it was before the first ones (*start, where they leave it).
+__global__ void __launch_bounds__(32) add_len_kernel(int* len, int seq, int n, int cap, PageMap pages, int* start, int first, int last,
+                                                     uint32_t* err) {
   pdl_wait();
   pdl_trigger();
-  const int v = __ldcg(len + seq) + n;
-  if (v > cap) set_error(err, ERR_CAPACITY);
-  len[seq] = v > cap ? cap : v;
+  const int lane = threadIdx.x, was = __ldcg(len + seq), v = min(was + n, cap);
+  int now = v;
+  if (pages.table) {
+    const int from = first ? was : __ldcg(start);
+    bool own = from >= 0;
+    for (int slot = from / KV_PAGE * KV_PAGE + lane * KV_PAGE; last && own && slot < v; slot += 32 * KV_PAGE) own = own_page(pages, seq, slot);
+    if (!__all_sync(0xffffffffu, own)) {
+      now = from;
+      if (lane == 0) set_error(err, ERR_CAPACITY);
+    }
+    if (first && lane == 0) *start = from;
+  }
+  if (lane != 0) return;
+  if (was + n > cap) set_error(err, ERR_CAPACITY);
+  len[seq] = now;
 }
 
-cudaError_t launch_add_len(int* len, int seq, int n, int cap, uint32_t* err, cudaStream_t st, bool pdl) {
+cudaError_t launch_add_len(int* len, int seq, int n, int cap, const PageMap& pages, int* start, bool first, bool last, uint32_t* err,
+                           cudaStream_t st, bool pdl) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = make_cfg(dim3(1), dim3(1), st, pdl, attr);
-  return cudaLaunchKernelEx(&cfg, add_len_kernel, len, seq, n, cap, err);
+  cudaLaunchConfig_t cfg = make_cfg(dim3(1), dim3(32), st, pdl, attr);
+  return cudaLaunchKernelEx(&cfg, add_len_kernel, len, seq, n, cap, pages, start, first ? 1 : 0, last ? 1 : 0, err);
 }
 
 __global__ void exp_kernel(const float* in, float* out, int n) {

@@ -69,6 +69,13 @@ __device__ __forceinline__ long long cache_row(const PageMap& pg, int seq, int s
   return ((long long)page * H * KV_PAGE + slot % KV_PAGE) * hd;
 }
 
+// Whether rows for slot `slot` (within the capacity) were, or would be, written: on a page that the sequence
+// alone holds.
+__device__ __forceinline__ bool own_page(const PageMap& pg, int seq, int slot) {
+  const int page = __ldcg(pg.table + (size_t)seq * pg.ld + slot / KV_PAGE);
+  return page >= 0 && page < pg.n && __ldcg(pg.refs + page) == 1;
+}
+
 // ---- skinny weight-streaming GEMM --------------------------------------------
 // CTAs per SM of the skinny GEMM's grid (compile-time tuning).
 // Every user of the grid size (the split-K partials, the fixed scratch of the
@@ -278,6 +285,7 @@ struct AcceptParams {
   int top_k;
   int* len;                 // [B] committed lengths
   int cap;
+  PageMap pages;            // of a paged cache
   int commit;
   int* accepted_len;        // [nb]
   int* out_tokens;          // [nb*q]
@@ -319,7 +327,9 @@ cudaError_t launch_tree_compact(const int* ws, int nb, int L, int H, int hd, int
                                 __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t st, bool pdl);
 cudaError_t launch_commit(int* len, const int* new_len, int nb, int cap, uint32_t* err, cudaStream_t st,
                           bool pdl);
-cudaError_t launch_add_len(int* len, int seq, int n, int cap, uint32_t* err, cudaStream_t st, bool pdl);
+// commit n more rows of a prompt; first, last: of its rows (*start: scratch)
+cudaError_t launch_add_len(int* len, int seq, int n, int cap, const PageMap& pages, int* start, bool first, bool last, uint32_t* err,
+                           cudaStream_t st, bool pdl);
 cudaError_t launch_exp(const float* in, float* out, int n, cudaStream_t st);
 // a bounded wait that nothing satisfies: sets ERR_TIMEOUT after WAIT_LIMIT_NS (test hook)
 cudaError_t launch_wait_timeout(uint32_t* err, cudaStream_t st);

@@ -135,6 +135,7 @@ struct sdsat_ctx {
   int* tree_ws = nullptr;      // [SDSAT_MAX_ROWS][TREE_WS_STRIDE] tree commit: len, m, path
   int* adaptive = nullptr;
   float* prefix_part = nullptr;   // partial results of the prefix attention
+  int* prompt_start = nullptr;    // [1] a prompt's sequence's length before it
   uint32_t* err = nullptr;
   // prefill workspaces (chunks of up to pf_rows positions; allocated with the weights)
   int pf_rows = 0;
@@ -606,9 +607,18 @@ sdsat_status forward(sdsat_ctx* c, sdsat_kv* kv, int seq0, int nb, int q, const 
   return SDSAT_OK;
 }
 
+// M more rows of a prompt are committed (first, last: of its rows)
+sdsat_status commit_rows(sdsat_ctx* c, sdsat_kv* kv, int seq, int M, bool first, bool last) {
+  return timed(c, K_PREFILL_COMMIT, [&] {
+           return launch_add_len(kv->len, seq, M, kv->cap, kv->map(), c->prompt_start, first, last, c->err, c->stream, c->pdl);
+         }) == cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
+}
+
 // one prefill chunk: M <= pf_rows prompt positions of sequence seq through every layer, then
 // committed
-sdsat_status prefill_chunk(sdsat_ctx* c, sdsat_kv* kv, int seq, const int32_t* tokens, int M) {
+sdsat_status prefill_chunk(sdsat_ctx* c, sdsat_kv* kv, int seq, const int32_t* tokens, int M, bool first, bool last) {
   const sdsat_config& cf = c->cfg;
   const int H = cf.n_heads, hd = cf.head_dim, R = H * hd, xi = prefill_tok(M) == 64;
   Tiled t{};
@@ -644,11 +654,7 @@ sdsat_status prefill_chunk(sdsat_ctx* c, sdsat_kv* kv, int seq, const int32_t* t
     a.err = c->err;
     return timed(c, K_PF_ATTENTION, [&] { return launch_prefill_attention(a, c->num_sms, c->stream, c->pdl); });
   });
-  if (s != SDSAT_OK) return s;
-  return timed(c, K_PREFILL_COMMIT,
-               [&] { return launch_add_len(kv->len, seq, M, kv->cap, c->err, c->stream, c->pdl); }) == cudaSuccess
-             ? SDSAT_OK
-             : SDSAT_ECUDA;
+  return s != SDSAT_OK ? s : commit_rows(c, kv, seq, M, first, last);
 }
 
 sdsat_status accept_common(sdsat_ctx* c, sdsat_kv* kv, const float* logits, const int32_t* drafts, int b, int q,
@@ -677,6 +683,7 @@ sdsat_status accept_common(sdsat_ctx* c, sdsat_kv* kv, const float* logits, cons
   p.top_k = top_k;
   p.len = kv->len;
   p.cap = kv->cap;
+  p.pages = kv->map();
   p.commit = commit;
   p.accepted_len = acc;
   p.out_tokens = out;
@@ -799,7 +806,7 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
             dalloc(c, &c->tree_pos, rows) && dalloc(c, &c->tree_anc, rows) &&
             dalloc(c, &c->tree_ws, (size_t)rows * TREE_WS_STRIDE) &&
             dalloc(c, &c->prefix_part, prefix_attention_scratch((size_t)rows * cfg->n_heads * cfg->head_dim, c->num_sms)) &&
-            dalloc(c, &c->err, 1) && dalloc(c, &c->xop_hi, (size_t)OP_MAX_M * OP_MAX_K) &&
+            dalloc(c, &c->prompt_start, 1) && dalloc(c, &c->err, 1) && dalloc(c, &c->xop_hi, (size_t)OP_MAX_M * OP_MAX_K) &&
             dalloc(c, &c->ssq, (size_t)rows * ((d + 127) / 128)) &&
             dalloc(c, &c->xop_lo, (size_t)OP_MAX_M * OP_MAX_K);
   const int xcols[X_COUNT] = {d, R, F};
@@ -1095,18 +1102,14 @@ sdsat_status sdsat_prefill(sdsat_ctx* c, sdsat_kv* kv, int seq, const int32_t* t
   if (n > kv->cap) return SDSAT_ECAPACITY;
   if (n > 0 && n <= SDSAT_MAX_Q) {   // fits one block
     const sdsat_status s = forward(c, kv, seq, 1, n, tokens_dev, nullptr, nullptr);
-    if (s != SDSAT_OK) return s;
-    return timed(c, K_PREFILL_COMMIT, [&] { return launch_add_len(kv->len, seq, n, kv->cap, c->err, c->stream, c->pdl); }) ==
-                   cudaSuccess
-               ? SDSAT_OK
-               : SDSAT_ECUDA;
+    return s != SDSAT_OK ? s : commit_rows(c, kv, seq, n, true, true);
   }
   // Chunks of equal size up to the position block: every chunk streams all the weights, so
   // none is left with a few positions (8191: 4096 + 4095; 4100: 2176 + 1924).
   const int chunks = (n + c->pf_rows - 1) / c->pf_rows;
   const int per = chunks ? ((n + chunks - 1) / chunks + 127) / 128 * 128 : 0;
   for (int i = 0; i < n; i += per) {
-    const sdsat_status s = prefill_chunk(c, kv, seq, tokens_dev + i, std::min(per, n - i));
+    const sdsat_status s = prefill_chunk(c, kv, seq, tokens_dev + i, std::min(per, n - i), i == 0, i + per >= n);
     if (s != SDSAT_OK) return s;
   }
   return SDSAT_OK;
