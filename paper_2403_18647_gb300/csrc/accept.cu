@@ -889,7 +889,7 @@ cudaError_t launch_wait_timeout(uint32_t* err, cudaStream_t st) {
 __global__ void commit_kernel(int* len, const int* new_len, int nb, int cap, uint32_t* err) {
   pdl_wait();
   pdl_trigger();
-  const int s = threadIdx.x;
+  const int s = blockIdx.x * blockDim.x + threadIdx.x;
   if (s >= nb) return;
   int v = __ldcg(new_len + s);
   if (v < 0 || v > cap) {
@@ -902,7 +902,7 @@ __global__ void commit_kernel(int* len, const int* new_len, int nb, int cap, uin
 cudaError_t launch_commit(int* len, const int* new_len, int nb, int cap, uint32_t* err, cudaStream_t st,
                           bool pdl) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = make_cfg(dim3(1), dim3(64), st, pdl, attr);
+  cudaLaunchConfig_t cfg = make_cfg(dim3((nb + 63) / 64), dim3(64), st, pdl, attr);
   return cudaLaunchKernelEx(&cfg, commit_kernel, len, new_len, nb, cap, err);
 }
 

@@ -1148,7 +1148,7 @@ sdsat_status sdsat_accept_pipelined(sdsat_ctx* c, sdsat_kv* kv, const float* log
 }
 
 sdsat_status sdsat_kv_commit(sdsat_ctx* c, sdsat_kv* kv, const int32_t* new_len_dev, int b) {
-  if (!c || !kv || kv->ctx != c || !new_len_dev || b < 1 || b > kv->batch || b > 64) return SDSAT_EINVAL;
+  if (!c || !kv || kv->ctx != c || !new_len_dev || b < 1 || b > kv->batch) return SDSAT_EINVAL;
   return timed(c, K_KV_COMMIT, [&] { return launch_commit(kv->len, new_len_dev, b, kv->cap, c->err, c->stream, c->pdl); }) ==
                  cudaSuccess
              ? SDSAT_OK

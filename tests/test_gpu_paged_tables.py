@@ -112,3 +112,22 @@ def test_lengths_outside_the_capacity(sd, model, n):
     rest = [i for i in range(10) if i not in written]
     assert (kv.k[:, rest] == 1).all() and (kv.v[:, rest] == 1).all()
     assert all((kv.k[:, i] != 1).any() for i in written)
+
+
+@pytest.mark.parametrize("b", [1, 63, 64, 65, 200, 256])
+def test_lengths_of_every_sequence_are_committed_and_rolled_back(sd, model, b):
+    """A paged cache takes up to 256 sequences; so does a commit, and a contiguous cache's takes as many as it has."""
+    _, ctx = model
+    for kv in (ctx.kv_paged(256, 128, 600), ctx.kv(256, 128)):
+        if isinstance(kv, sd.PagedKV):
+            ctx.kv_reserve(kv, 256, 100)
+        new = torch.tensor([(37 * s) % 101 for s in range(256)], dtype=torch.int32, device="cuda")
+        ctx.kv_commit(kv, new, b)
+        assert ctx.kv_lengths(kv).tolist() == new.tolist()[:b] + [0] * (256 - b)
+        back = new // 2
+        ctx.kv_commit(kv, back, b)
+        assert ctx.kv_lengths(kv).tolist() == back.tolist()[:b] + [0] * (256 - b)
+        assert ctx.get_error() == 0
+        with pytest.raises(sd.SdsatError) as e:
+            ctx.kv_commit(kv, new, 257)
+        assert e.value.status == 1
