@@ -267,7 +267,9 @@ class PagedKV(KV):
     """A library-owned cache of `n_pages` pages of PAGE slots, which sequences may share."""
 
     def __init__(self, ctx: "Context", batch: int, max_len: int, n_pages: int):
+        import torch
         self.ctx = ctx
+        self.device = torch.device("cuda", torch.cuda.current_device())   # where the library allocates it
         h = ctypes.c_void_p()
         _check(_lib().sdsat_kv_create_paged(ctx.handle, batch, max_len, n_pages, ctypes.byref(h)),
                "sdsat_kv_create_paged")
@@ -284,7 +286,7 @@ class PagedKV(KV):
     # the cache's own memory as tensors (what it holds is read on the stream of the calls before)
     def _view(self, address, shape, typestr="<i4"):
         import torch
-        return torch.as_tensor(_Memory(self, address, shape, typestr), device="cuda")
+        return torch.as_tensor(_Memory(self, address, shape, typestr), device=self.device)
 
     @property
     def table(self):
