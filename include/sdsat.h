@@ -198,7 +198,8 @@ SDSAT_API sdsat_status sdsat_kv_info(const sdsat_kv* kv, void** k_dev, void** v_
  * src / dst are bf16 [n_heads][n][head_dim] device buffers; rows land at slots
  * slot0 .. slot0+n-1.  Asynchronous on the context stream.  Used to load a
  * snapshot (or synthetic contents) and to inspect what a block forward wrote.
- * Errors: EINVAL (null pointer, layer/seq/slot range). */
+ * On a paged cache a slot without a page reads as zeros and sets device bit CAPACITY.
+ * Errors: EINVAL (null pointer, layer/seq/slot range, buffers not aligned to their values). */
 SDSAT_API sdsat_status sdsat_kv_write(sdsat_ctx* ctx, sdsat_kv* kv, int layer, int seq, int slot0, int n,
                                       const void* k_src_dev, const void* v_src_dev);
 SDSAT_API sdsat_status sdsat_kv_read(sdsat_ctx* ctx, const sdsat_kv* kv, int layer, int seq, int slot0, int n,

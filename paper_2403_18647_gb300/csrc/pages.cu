@@ -423,12 +423,14 @@ __global__ void __launch_bounds__(32) pages_copy_kernel(const __grid_constant__ 
 }
 
 // ---- rows in and out -----------------------------------------------------------------------------
-// src / dst [H][n][hd] <-> slots slot0 .. of one (layer, sequence); one 16-byte piece a thread
+// src / dst [H][n][hd] <-> slots slot0 .. of one (layer, sequence); one piece a thread, of 16 bytes where the
+// buffers allow it, or of one value
+template <typename T>
 __global__ void __launch_bounds__(256) pages_rows_kernel(const __grid_constant__ PagesParams p, int layer, int slot0,
-                                                         uint4* kx, uint4* vx, int write) {
+                                                         T* kx, T* vx, int write) {
   pdl_wait();
   pdl_trigger();
-  const int chunks = p.hd / 8;
+  const int chunks = p.hd * 2 / (int)sizeof(T);
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x, total = 2ll * p.H * p.n * chunks;
   if (i >= total) return;
   const int c = (int)(i % chunks);
@@ -437,15 +439,15 @@ __global__ void __launch_bounds__(256) pages_rows_kernel(const __grid_constant__
   const int h = (int)(r / p.n % p.H);
   const bool v = r / p.n >= p.H;
   const int page = __ldcg(p.table + (size_t)p.seq0 * p.ld + slot / KV_PAGE);
-  uint4* buf = (v ? vx : kx) + ((long long)h * p.n + x) * chunks + c;
+  T* buf = (v ? vx : kx) + ((long long)h * p.n + x) * chunks + c;
   // no page, or (to write) one that others hold too
   const bool ok = page >= 0 && page < p.n_pages && (!write || __ldcg(p.refs + page) == 1);
   if (!ok) {
     if (c == 0 && h == 0 && !v) set_error(p.err, ERR_CAPACITY);
-    if (!write) *buf = make_uint4(0u, 0u, 0u, 0u);
+    if (!write) *buf = T{};
     return;
   }
-  uint4* row = reinterpret_cast<uint4*>((v ? p.v : p.k) + ((((long long)layer * p.n_pages + page) * p.H + h) * KV_PAGE + slot % KV_PAGE) * p.hd) + c;
+  T* row = reinterpret_cast<T*>((v ? p.v : p.k) + ((((long long)layer * p.n_pages + page) * p.H + h) * KV_PAGE + slot % KV_PAGE) * p.hd) + c;
   if (write) *row = __ldcg(buf);
   else *buf = __ldcg(row);
 }
@@ -475,7 +477,8 @@ cudaError_t pages_prepare() {
   if (e == cudaSuccess) e = prefer_shared(pages_copy_kernel);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(pages_copy_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pages_copy_smem(128));
-  if (e == cudaSuccess) e = prefer_shared(pages_rows_kernel);
+  if (e == cudaSuccess) e = prefer_shared(pages_rows_kernel<uint4>);
+  if (e == cudaSuccess) e = prefer_shared(pages_rows_kernel<unsigned short>);
   return e;
 }
 
@@ -493,9 +496,13 @@ cudaError_t launch_pages_copy(const PagesParams& p, int num_sms, cudaStream_t st
 }
 cudaError_t launch_pages_rows(const PagesParams& p, int layer, int slot0, void* k, void* v, bool write, cudaStream_t st,
                               bool pdl) {
-  const long long pieces = 2ll * p.H * p.n * (p.hd / 8);
-  return launch_pages(pages_rows_kernel, dim3((unsigned)((pieces + 255) / 256)), 256, 0, st, pdl, p, layer, slot0,
-                      static_cast<uint4*>(k), static_cast<uint4*>(v), write ? 1 : 0);
+  const bool whole = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15) == 0;
+  const long long pieces = 2ll * p.H * p.n * (p.hd / (whole ? 8 : 1));
+  const dim3 grid((unsigned)((pieces + 255) / 256));
+  return whole ? launch_pages(pages_rows_kernel<uint4>, grid, 256, 0, st, pdl, p, layer, slot0, static_cast<uint4*>(k),
+                              static_cast<uint4*>(v), write ? 1 : 0)
+               : launch_pages(pages_rows_kernel<unsigned short>, grid, 256, 0, st, pdl, p, layer, slot0,
+                              static_cast<unsigned short*>(k), static_cast<unsigned short*>(v), write ? 1 : 0);
 }
 
 }  // namespace sdsat

@@ -1037,7 +1037,8 @@ static sdsat_status kv_copy(sdsat_ctx* c, const sdsat_kv* kv, int layer, int seq
   const int H = c->cfg.n_heads, hd = c->cfg.head_dim;
   if (kv->pages) {
     const bool write = ks || vs;
-    if (!aligned16(write ? ks : kd) || !aligned16(write ? vs : vd)) return SDSAT_EINVAL;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(write ? ks : kd) | reinterpret_cast<uintptr_t>(write ? vs : vd);
+    if (at % sizeof(__nv_bfloat16)) return SDSAT_EINVAL;
     PagesParams p = pages_params(c, const_cast<sdsat_kv*>(kv));
     p.seq0 = seq;
     p.n = n;

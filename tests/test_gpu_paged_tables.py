@@ -131,3 +131,30 @@ def test_lengths_of_every_sequence_are_committed_and_rolled_back(sd, model, b):
         with pytest.raises(sd.SdsatError) as e:
             ctx.kv_commit(kv, new, 257)
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("offset", [0, 1, 3, 7, 8])
+@pytest.mark.parametrize("slot0,n", [(0, 1), (60, 70), (0, 200)])
+def test_rows_to_and_from_buffers_of_any_alignment(sd, model, offset, slot0, n):
+    """Buffers that start anywhere, as contiguous caches take them, beside values that must stay."""
+    shape, ctx = model
+    kv = ctx.kv_paged(2, 256, 9)
+    ctx.kv_reserve(kv, 2, 256)
+    size = shape.n_heads * n * shape.head_dim
+    x = [torch.randn(size + 20, device="cuda").bfloat16() for _ in range(2)]
+    at = lambda t: t[offset:offset + size].view(shape.n_heads, n, shape.head_dim)  # noqa: E731
+    ctx.kv_write(kv, 1, 1, slot0, at(x[0]), at(x[1]))
+    got = ctx.kv_read(kv, 1, 1, slot0, n)
+    assert torch.equal(got[0], at(x[0])) and torch.equal(got[1], at(x[1]))
+    back = [torch.full_like(t, 9.0) for t in x]
+    assert sd.lib().sdsat_kv_read(ctx.handle, kv.handle, 1, 1, slot0, n, at(back[0]).data_ptr(), at(back[1]).data_ptr()) == 0
+    for b, t in zip(back, x):
+        assert torch.equal(b[offset:offset + size], t[offset:offset + size])
+        assert (b[:offset] == 9).all() and (b[offset + size:] == 9).all()
+    assert ctx.get_error() == 0
+    ctx.kv_free(kv, 1)
+    ctx.kv_write(kv, 1, 1, slot0, at(x[0]), at(x[1]))
+    assert ctx.get_error() == sd.DEV_CAPACITY
+    assert sd.lib().sdsat_kv_read(ctx.handle, kv.handle, 1, 1, slot0, n, at(back[0]).data_ptr(), at(back[1]).data_ptr()) == 0
+    assert (at(back[0]) == 0).all() and (at(back[1]) == 0).all()
+    assert ctx.get_error() == sd.DEV_CAPACITY
