@@ -1031,7 +1031,7 @@ sdsat_status sdsat_kv_compact(sdsat_ctx* c, sdsat_kv* kv, int32_t* used_dev) {
 static sdsat_status kv_copy(sdsat_ctx* c, const sdsat_kv* kv, int layer, int seq, int slot0, int n, const void* ks,
                             const void* vs, void* kd, void* vd) {
   if (!c || !kv || kv->ctx != c || layer < 0 || layer >= c->cfg.n_layers || seq < 0 || seq >= kv->batch ||
-      slot0 < 0 || n < 0 || slot0 + n > kv->cap)
+      slot0 < 0 || n < 0 || n > kv->cap - slot0)
     return SDSAT_EINVAL;
   if (n == 0) return SDSAT_OK;
   const int H = c->cfg.n_heads, hd = c->cfg.head_dim;

@@ -158,3 +158,14 @@ def test_rows_to_and_from_buffers_of_any_alignment(sd, model, offset, slot0, n):
     assert sd.lib().sdsat_kv_read(ctx.handle, kv.handle, 1, 1, slot0, n, at(back[0]).data_ptr(), at(back[1]).data_ptr()) == 0
     assert (at(back[0]) == 0).all() and (at(back[1]) == 0).all()
     assert ctx.get_error() == sd.DEV_CAPACITY
+
+
+@pytest.mark.parametrize("slot0,n", [(256, 1), (255, 2), (2 ** 31 - 1, 1), (2 ** 31 - 100, 200), (1, 2 ** 31 - 1), (-1, 1), (0, -1)])
+def test_rows_outside_the_capacity_are_refused(sd, model, slot0, n):
+    """Slots whose sum with the number of rows does not fit 32 bits, too."""
+    _, ctx = model
+    x = torch.zeros(64, dtype=torch.bfloat16, device="cuda").data_ptr()
+    for kv in (ctx.kv(2, 256), ctx.kv_paged(2, 256, 9)):
+        for f in (sd.lib().sdsat_kv_write, sd.lib().sdsat_kv_read):
+            assert f(ctx.handle, kv.handle, 0, 0, slot0, n, x, x) == 1
+    assert ctx.get_error() == 0
