@@ -467,7 +467,8 @@ SDSAT_API sdsat_status sdsat_op_prefix_attention(sdsat_ctx* ctx, const void* q_d
  * NULL.  Any output but the two of n_top > 0 may be NULL.  A NaN logit counts as -inf (device
  * bit NAN_LOGITS), a token outside the vocabulary as id 0 (TOKEN); a logit of +inf shares the
  * mass with the others of +inf; a row of -inf alone has probabilities 0 and entropy 0.
- * Errors: EINVAL (temperature <= 0, n_top > 32 or > vocab, rows > 2^27), EUNSUPPORTED (vocab > 262144). */
+ * Errors: EINVAL (temperature <= 0, infinite or below 4.3e-39, n_top > 32 or > vocab, rows >
+ * 2^27), EUNSUPPORTED (vocab > 262144). */
 SDSAT_API sdsat_status sdsat_op_logprobs(sdsat_ctx* ctx, const void* logits_dev, int64_t ld, int type, int rows,
                                          int vocab, const int32_t* tokens_dev, float temperature, int n_top,
                                          float* logp_dev, float* entropy_dev, int32_t* rank_dev,

@@ -1467,7 +1467,9 @@ sdsat_status sdsat_op_logprobs(sdsat_ctx* c, const void* logits_dev, int64_t ld,
                                const int32_t* tokens_dev, float temperature, int n_top, float* logp_dev,
                                float* entropy_dev, int32_t* rank_dev, int32_t* top_ids_dev, float* top_logp_dev) {
   if (!c || rows < 0 || rows > LP_MAX_ROWS || vocab < 1 || ld < vocab || (type != SDSAT_FP32 && type != SDSAT_BF16)) return SDSAT_EINVAL;
-  if (!(temperature > 0.f) || std::isinf(temperature) || n_top < 0 || n_top > LP_MAX_TOP || n_top > vocab) return SDSAT_EINVAL;
+  // (the kernel's exponents are differences times log2(e) / temperature)
+  if (!(temperature > 0.f) || std::isinf(temperature) || std::isinf(1.0f / temperature * 1.4426950408889634f)) return SDSAT_EINVAL;
+  if (n_top < 0 || n_top > LP_MAX_TOP || n_top > vocab) return SDSAT_EINVAL;
   if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
   if (!logits_dev || reinterpret_cast<uintptr_t>(logits_dev) % (type == SDSAT_BF16 ? 2 : 4)) return SDSAT_EINVAL;
   if (!tokens_dev && (logp_dev || rank_dev)) return SDSAT_EINVAL;
