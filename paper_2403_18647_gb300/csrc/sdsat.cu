@@ -883,6 +883,10 @@ static sdsat_status kv_create(sdsat_ctx* c, int batch, int max_len, int pages, s
   kv->page_ld = (max_len + KV_PAGE - 1) / KV_PAGE;
   const long long rows = c->cfg.n_layers * kv->layer_rows(c->cfg.n_heads);
   const size_t n = (size_t)rows * c->cfg.head_dim;
+  if (pages && rows > 0x7FFFFFFFll) {   // (no memory holds so many, but it is not memory that they lack)
+    delete kv;
+    return SDSAT_EUNSUPPORTED;
+  }
   const size_t entries = (size_t)batch * kv->page_ld, list = 4 + 5 * (size_t)pages;
   const size_t page_ints = pages ? list + entries + 2 * (size_t)pages + batch + std::max<size_t>(pages, entries) : 0;
   void *k = nullptr, *v = nullptr, *len = nullptr, *em = nullptr, *pm = nullptr;

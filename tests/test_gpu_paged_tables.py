@@ -169,3 +169,12 @@ def test_rows_outside_the_capacity_are_refused(sd, model, slot0, n):
         for f in (sd.lib().sdsat_kv_write, sd.lib().sdsat_kv_read):
             assert f(ctx.handle, kv.handle, 0, 0, slot0, n, x, x) == 1
     assert ctx.get_error() == 0
+
+
+def test_pools_of_more_rows_than_the_kernels_count(sd, model):
+    """2 layers, 4 heads: 2^31 rows of K are 2^22 pages."""
+    _, ctx = model
+    for pages in (2 ** 22, 2 ** 22 + 1, 2 ** 31 - 1):
+        with pytest.raises(sd.SdsatError) as e:
+            ctx.kv_paged(1, 64, pages)
+        assert e.value.status == 6, pages
