@@ -23,8 +23,9 @@ def best_of_n(ctx, shape, prompt, n: int, k: int, loops: int, max_len: int, temp
     `loops` two-step loops: each emits a token of draft step 1 and 1 to k + 1 of draft step 2."""
     q, P = k + 1, prompt.numel()
     kv = ctx.kv_paged(n + 1, max_len, -(-P // 64) + n * (-(-(max_len - P) // 64) + 1))
-    ctx.kv_reserve(kv, 1, P - 1, seq=n)
-    ctx.prefill(kv, n, prompt[:-1])                      # the last prompt token opens the first block
+    if P > 1:
+        ctx.kv_reserve(kv, 1, P - 1, seq=n)
+        ctx.prefill(kv, n, prompt[:-1])                  # the last prompt token opens the first block
     ctx.kv_fork(kv, torch.full((n,), n, dtype=torch.int32, device="cuda"))
 
     new = lambda *s, t=torch.int32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
