@@ -148,22 +148,15 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-_kinds = None
-
-
-def _types():
-    """{tensor type: element type} of _rows, and the types float32, bfloat16, int32 (asked for once)."""
-    global _kinds
-    if _kinds is None:
-        import torch
-        _kinds = {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.bfloat16, torch.int32
-    return _kinds
+_kinds = _f32 = _bf16 = _i32 = None   # tensor types, once torch is there (the first call of _rows)
 
 
 def _rows(t):
     """(address, values from one row to the next, element type, rows, columns) of a CUDA matrix whose rows are
     contiguous."""
-    kind = _types()[0].get(t.dtype)
+    if _kinds is None:
+        _types()
+    kind = _kinds.get(t.dtype)
     if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError("expected a float32 or bfloat16 CUDA matrix")
     (rows, columns), (ld, step) = t.shape, t.stride()
@@ -172,15 +165,25 @@ def _rows(t):
     return t.data_ptr(), ld if rows > 1 else columns, kind, rows, columns
 
 
+def _types():
+    global _kinds, _f32, _bf16, _i32
+    import torch
+    _kinds, _f32, _bf16, _i32 = {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.bfloat16, torch.int32
+
+
 def _array(t, dtype, n: int):
     """The address of a contiguous CUDA tensor of n values or more of a type (None and addresses as they are)."""
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype is not dtype or t.numel() < n:
-        raise ValueError("expected %d values of %s, got %d of %s" % (n, dtype, t.numel(), t.dtype))
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous CUDA tensor")
-    return t.data_ptr()
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.numel() >= n and t.is_cuda and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+        raise
+    raise ValueError("expected %d values of %s in a contiguous CUDA tensor, got %d of %s on %s"
+                     % (n, dtype, t.numel(), t.dtype, t.device))
 
 
 def _check(status: int, what: str):
@@ -357,8 +360,10 @@ class Context:
     def kv_fork(self, kv: PagedKV, src, b: int = None):
         """Sequence s takes the pages and the length of sequence src[s] (int32 CUDA tensor [b]; -1: none)."""
         self._bind_stream()
+        if _kinds is None:
+            _types()
         b = src.numel() if b is None else b
-        _check(_lib().sdsat_kv_fork(self.handle, kv.handle, _array(src, _types()[3], min(b, kv.batch)), b), "sdsat_kv_fork")
+        _check(_lib().sdsat_kv_fork(self.handle, kv.handle, _array(src, _i32, min(b, kv.batch)), b), "sdsat_kv_fork")
 
     def kv_free(self, kv: PagedKV, seq: int):
         self._bind_stream()
@@ -372,7 +377,9 @@ class Context:
     def kv_compact(self, kv: PagedKV, used=None):
         """Pages in use move to the front of the pool; used: int32 CUDA tensor [1] for their number."""
         self._bind_stream()
-        _check(_lib().sdsat_kv_compact(self.handle, kv.handle, _array(used, _types()[3], 1)), "sdsat_kv_compact")
+        if _kinds is None:
+            _types()
+        _check(_lib().sdsat_kv_compact(self.handle, kv.handle, _array(used, _i32, 1)), "sdsat_kv_compact")
 
     def kv_write(self, kv: KV, layer: int, seq: int, slot0: int, k, v):
         """k, v: bf16 CUDA tensors [n_heads, n, head_dim] written to slots slot0 .. slot0+n-1."""
@@ -537,18 +544,19 @@ class Context:
         (qp, q_ld, kind, q_rows, q_cols), (op, out_ld, kind_out, out_rows, out_cols) = _rows(q), _rows(out)
         if kind != kind_out:
             raise ValueError("q and out are of different types")
-        _, _, bf16, i32 = _types()
         (sequences, columns), pages = table.shape, k.size(0)
         if sequences < b or q_rows < b * qn or out_rows < b * qn:
             raise ValueError("fewer rows than b or b * qn")
         if H > 0 and Hk > 0 and H % Hk == 0 and hd in (64, 128):   # (the library refuses other heads)
             if q_cols < H * hd or out_cols < H * hd:
                 raise ValueError("fewer columns than H * hd")
-            if k.shape != (pages, Hk, PAGE, hd) or v.shape != k.shape:
+            want = (pages, Hk, PAGE, hd)
+            if k.shape != want or v.shape != want:
                 raise ValueError("expected pages of [Hk][%d][hd]" % PAGE)
-        _check(_lib().sdsat_op_prefix_attention(self.handle, qp, q_ld, _array(k, bf16, 0), _array(v, bf16, 0), pages, _array(table, i32, 0), columns,
-                                                _array(shared, i32, b), _array(lens, i32, b), _array(anc, i32, b * qn), b, qn, H, Hk,
-                                                hd, op, out_ld, kind), "sdsat_op_prefix_attention")
+        _check(_lib().sdsat_op_prefix_attention(self.handle, qp, q_ld, _array(k, _bf16, 0), _array(v, _bf16, 0), pages,
+                                                _array(table, _i32, 0), columns, _array(shared, _i32, b), _array(lens, _i32, b),
+                                                _array(anc, _i32, b * qn), b, qn, H, Hk, hd, op, out_ld, kind),
+               "sdsat_op_prefix_attention")
 
     def op_logprobs(self, logits, tokens=None, logp=None, entropy=None, rank=None, top_ids=None, top_logp=None,
                     temperature: float = 1.0):
@@ -556,13 +564,12 @@ class Context:
         top_ids int32 and top_logp fp32 [rows][n]."""
         self._bind_stream()
         lp, ld, kind, rows, vocab = _rows(logits)
-        _, f32, _, i32 = _types()
         n = 0 if top_ids is None else top_ids.size(1)
-        if n and top_logp is not None and top_logp.shape != top_ids.shape:
-            raise ValueError("top_ids and top_logp are of different shapes")
-        _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, rows, vocab, _array(tokens, i32, rows), temperature, n,
-                                        _array(logp, f32, rows), _array(entropy, f32, rows), _array(rank, i32, rows),
-                                        _array(top_ids, i32, rows * n), _array(top_logp, f32, rows * n)), "sdsat_op_logprobs")
+        if n and top_logp is not None and top_logp.size(1) != n:
+            raise ValueError("top_ids and top_logp are of different widths")
+        _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, rows, vocab, _array(tokens, _i32, rows), temperature, n,
+                                        _array(logp, _f32, rows), _array(entropy, _f32, rows), _array(rank, _i32, rows),
+                                        _array(top_ids, _i32, rows * n), _array(top_logp, _f32, rows * n)), "sdsat_op_logprobs")
 
     def debug_workspace(self, which: int, rows: int):
         """Last-layer workspace of the last forward: 0 h, 1 q, 2 attention out, 3 SwiGLU act."""
