@@ -22,6 +22,9 @@
  *    (sdsat_set_stream); only sdsat_create, sdsat_kv_create, sdsat_*_destroy
  *    and sdsat_get_error synchronise.  No compute call allocates memory, so
  *    compute calls may be captured into a CUDA graph.
+ *  - The calls of a context share its workspaces (partial results, operands, the
+ *    error word): calls queued on two streams must not overlap.  Order the streams
+ *    by an event, or use a context for each.
  *  - Argument errors are detected on the host and returned synchronously
  *    (nothing is queued).  Errors only the device can see (a NaN logit, a
  *    row past the KV capacity, a timed-out wait) set bits in a device flag
@@ -59,12 +62,12 @@ typedef enum {
 /* device error bits reported by sdsat_get_error */
 #define SDSAT_DEV_NAN_LOGITS 0x1u  /* NaN logit seen; it counted as -inf */
 #define SDSAT_DEV_TIMEOUT 0x2u     /* a bounded in-kernel wait expired; results invalid */
-#define SDSAT_DEV_CAPACITY 0x4u    /* a block row fell past the KV capacity; not written */
+#define SDSAT_DEV_CAPACITY 0x4u    /* a row fell past the KV capacity, or has no page of its own; not written */
 #define SDSAT_DEV_TOKEN 0x8u       /* a token id outside [0, vocab); id 0 used instead */
 #define SDSAT_DEV_POSITION 0x10u   /* a RoPE position outside [0, max_position); clamped */
 #define SDSAT_DEV_TREE 0x20u       /* a tree parent that is not an earlier row; read as the root */
-
-#define SDSAT_DEV_PAGE 0x40u       /* a page outside the pool, or a sequence to fork from outside the batch; skipped */
+#define SDSAT_DEV_PAGE 0x40u       /* a slot to attend to without a page, a page number outside the pool or a
+                                      sequence to fork from outside the batch; skipped */
 
 #define SDSAT_MAX_Q 16           /* block rows per sequence (k <= 15 adaptive tokens) */
 #define SDSAT_MAX_ROWS 64        /* batch * q rows per block forward */
@@ -153,8 +156,10 @@ SDSAT_API void sdsat_kv_destroy(sdsat_kv* kv);
  * sdsat_kv_write) need pages that their sequence alone holds (sdsat_kv_reserve), and a row
  * without one is not written and sets device bit CAPACITY (sdsat_prefill, and an accept call
  * with commit, leave the length as it was where a row that they would commit has none;
- * sdsat_kv_commit sets any length); and block forwards read the
- * leading pages that all their sequences share once for all of them.
+ * sdsat_kv_commit sets any length); and block forwards read the whole, committed leading
+ * pages that all their sequences hold together with sequence 0 once for all of them.  One
+ * sequence of the batch with another prompt, or without pages, and none are: several
+ * prompts' samples share most in a call for each.
  * Synchronous.  Errors: EINVAL (batch > 256), ENOMEM, ECAPACITY (as sdsat_kv_create),
  * EUNSUPPORTED (n_layers * n_pages * n_heads * SDSAT_PAGE >= 2^31). */
 SDSAT_API sdsat_status sdsat_kv_create_paged(sdsat_ctx* ctx, int batch, int max_len, int n_pages, sdsat_kv** out);
@@ -162,6 +167,8 @@ SDSAT_API sdsat_status sdsat_kv_create_paged(sdsat_ctx* ctx, int batch, int max_
 /* Device addresses and geometry of a paged cache: table int32 [batch][table_ld], entry j of
  * a sequence the page of its slots 64 j .. 64 j + 63 (-1: none), and refs int32 [n_pages],
  * the sequences that hold each page (0: free).  Any output pointer may be NULL.
+ * Fork, free and reserve count the pages that sequences share, and block forwards go by that
+ * count: after writing to the table (and refs, which has to agree with it) call one of them.
  * Errors: EINVAL (a contiguous cache). */
 SDSAT_API sdsat_status sdsat_kv_pages(const sdsat_kv* kv, int32_t** table_dev, int32_t** refs_dev, int* n_pages,
                                       int* table_ld);
@@ -169,8 +176,8 @@ SDSAT_API sdsat_status sdsat_kv_pages(const sdsat_kv* kv, int32_t** table_dev, i
 /* Sequence s < b takes the pages and the length that sequence src_dev[s] (any sequence of the
  * cache, its own included) had before the call; -1 leaves it empty.  Pages are shared, not
  * copied; a page that no sequence holds any more is free.  src_dev int32 [b].  The emitted
- * counters stay.  Errors: EINVAL; device bit PAGE where src_dev[s] is not in the batch (s keeps
- * its pages). */
+ * counters stay.  Errors: EINVAL; device bit PAGE where src_dev[s] is neither -1 nor in the
+ * batch (s keeps its pages), and where a table entry is no page of the pool (dropped). */
 SDSAT_API sdsat_status sdsat_kv_fork(sdsat_ctx* ctx, sdsat_kv* kv, const int32_t* src_dev, int b);
 
 /* Sequence seq gives its pages up (length 0).  Errors: EINVAL. */
@@ -181,7 +188,8 @@ SDSAT_API sdsat_status sdsat_kv_free(sdsat_ctx* ctx, sdsat_kv* kv, int seq);
  * page that other sequences hold too is replaced by the lowest free one, into which its
  * committed slots are copied (of several sequences that hold it the last one keeps it).
  * Errors: EINVAL; device bit CAPACITY where a sequence would pass max_len (it gets the pages up
- * to it) or the pool has too few free pages (nothing changes). */
+ * to it) or the pool has too few free pages (nothing changes); PAGE where a table entry is no
+ * page of the pool (replaced). */
 SDSAT_API sdsat_status sdsat_kv_reserve(sdsat_ctx* ctx, sdsat_kv* kv, int seq, int b, int n);
 
 /* Move the pages in use to the ids 0 .. u-1 of the pool: the i-th used page with an id >= u
@@ -263,8 +271,9 @@ SDSAT_API sdsat_status sdsat_accept_nucleus(sdsat_ctx* ctx, sdsat_kv* kv, const 
 /* Explicit commit / rollback (implied by Sec. 2.1.1: after Eq. 3 only the accepted
  * prefix stays in the context; the adaptive positions of draft step 1 and the rejected
  * drafts are dropped): len[s] = new_len_dev[s] for s < b (device values,
- * 0 <= new_len <= max_len; out-of-range values are clamped and set CAPACITY).
- * Errors: EINVAL. */
+ * 0 <= new_len <= max_len; out-of-range values are clamped and set CAPACITY).  On a paged
+ * cache committed slots without a page are not attended to (device bit PAGE).
+ * Errors: EINVAL (b > the cache's batch). */
 SDSAT_API sdsat_status sdsat_kv_commit(sdsat_ctx* ctx, sdsat_kv* kv, const int32_t* new_len_dev, int b);
 
 /* Copy the committed lengths len[0 .. b-1] into lens_dev (int32 [b], device),
@@ -446,7 +455,10 @@ SDSAT_API sdsat_status sdsat_op_attention(sdsat_ctx* ctx, const float* q_dev, co
  *              0's; NULL: none.  The whole pages of committed slots among those that all
  *              sequences share are read once for all of them, through sequence 0's row
  *   len_dev    int32 [b] committed lengths
- * A slot on a page outside [0, n_pages) is not attended to and sets device bit PAGE.  hd 64 or
+ * A slot on a page outside [0, n_pages) is not attended to and sets device bit PAGE.  What a page
+ * holds in slots that no row of a sequence sees does not matter; a block slot that some of its
+ * rows see counts 0 times its value in the others, so a NaN or an infinity there reaches them.
+ * Partial results go through the context's workspace (see the conventions on streams).  hd 64 or
  * 128, H a multiple of Hk, b*q <= SDSAT_MAX_ROWS, b*q*H*hd <= SDSAT_MAX_ROWS rows of the
  * context's heads, b*q*H*table_ld <= 2^30, max(b*q*G, H)*G < 2^32 for G = H/Hk; pointers
  * 16-byte aligned, rows a multiple of 16 bytes apart.  Errors: EINVAL. */

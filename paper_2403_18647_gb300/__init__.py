@@ -267,7 +267,10 @@ class _Memory:
 
 
 class PagedKV(KV):
-    """A library-owned cache of `n_pages` pages of PAGE slots, which sequences may share."""
+    """A library-owned cache of `n_pages` pages of PAGE slots, which sequences may share.
+
+    Its tensors are the cache's own memory.  Block forwards go by the shared pages that kv_fork, kv_free and kv_reserve
+    count: after writing to `table` (and `refs`) call one of them."""
 
     def __init__(self, ctx: "Context", batch: int, max_len: int, n_pages: int):
         import torch

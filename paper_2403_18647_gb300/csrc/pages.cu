@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(const __grid_
 // One thread on an SM drives them, loads PC_AHEAD blocks ahead; the warp's lanes have the next 32
 // blocks' places.  A branch of a 7B-shaped cache into eight, 288 MB to move at the least: 61 us
 // in all, 103 with warps that copied through registers, 32 on an SM; a round of ten samples on a
-// 13B-shaped one, 693 MB: 111 and 208.
+// 13B-shaped one, 693 MB: 112 and 208 replayed as a graph (calls in a row take 114 to 146).
 constexpr int PC_SLOTS = 12, PC_AHEAD = 6;
 __device__ __forceinline__ void bulk_store_s2g(void* dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");

@@ -17,14 +17,14 @@
 // O is rescaled only when a row's maximum has grown by more than 2^8 since the last time
 // (exact: the reference value cancels in the division by the row's sum; P stays below 2^8).
 //
-// Measured, 32 heads x 128, us per launch: 4095 positions 254 (872 with mma.sync m16n8k16 on
+// Measured, 32 heads x 128, us per launch: 4095 positions 257 (872 with mma.sync m16n8k16 on
 // 64-position blocks, whose K and V fragments each warp read from shared memory again), 2047
-// 81 (256), 512 23 (43), 99 12.3 (20); at 4095 1.08 PFLOP/s executed.
+// 82 (256), 512 23 (43), 99 12.3 (20); at 4095 1.07 PFLOP/s executed.
 //
 // Values that no position may see take part with P = 0: the slots behind the last key, up to the 16 keys
 // of a product's step, and pages that are not there.  They may hold anything (a paged cache's pages what
 // their last owner left), and 0 times NaN is NaN, so they are made zeros in the ring before the product, by the
-// warp that loads, which has nothing left to load by then: 1 % of a launch at 2047 positions.  (By the
+// warp that loads, which has nothing left to load by then: up to 1 % of a launch (2047, 4095).  (By the
 // softmax warps, whose registers are all taken, 4 %; by warp 2, which has to be told when, 2.5 %.)
 //
 // Warps 0-3: TMA (warp 0), MMA issue and TMEM (warp 1), two idle; warps 4-7 and 8-11: softmax

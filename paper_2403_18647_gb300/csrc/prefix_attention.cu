@@ -23,7 +23,8 @@
 //   O^T += V^T P^T  A = the V tile read MN-major, B = P (shared memory, MN-major)   hd x N rows
 // K and V are the cache's bf16 values.  fp32 queries and the probabilities enter as three bf16 parts
 // (24 bits: nothing is lost against fp32 products; one part for bf16 queries, whose probabilities
-// have two), one product each into the same fp32 accumulator.
+// have two, 2^-17: the result is rounded to bf16, and 0.2 % of them round to the neighbour of the
+// nearest one, as 0.01 to 0.1 % do with fp32 products), one product each into the same fp32 accumulator.
 //
 // The reference m of a row is its maximum over the first unit; later units only check that no score
 // passes it by more than 2^PX_LAZY, which is rare, and then rescale: a maximum over lanes for each
@@ -93,8 +94,8 @@ struct PxCfg {
   static constexpr size_t OFF_MISC = OFF_Q + HALVES * Q_HALF;
 };
 
-// What the CTAs, and the merge after them, agree on.  Shares are counted in places: those of an item are some for its start and then some for each of its units, which belongs to the CTA that has its
-// first one.
+// What the CTAs, and the merge after them, agree on.  Shares are counted in places: those of an item are
+// some for its start and then some for each of its units, which belongs to the CTA that has its first one.
 struct PxCost {
   int start, unit;
 };
@@ -111,7 +112,8 @@ struct PxSched {
 // What an item of that many rows costs, a unit of up to 32 rows being 4 (1.2 us): units of more rows 2 us
 // (1.65 of 16 bits); starts 0.9 us, with more rows, whose queries and O have no second place, 4.5 us beside
 // the stream of K and V (3). By the ends of the CTAs of four cases and the times of sets of these numbers;
-// with shares of as many units each they are up to 20 % longer, with starts of 8 up to 8 %.
+// with shares of as many units each they are up to 20 % longer, with starts of 8 up to 8 %.  All four have
+// heads of 128: those of 64, whose units are half the bytes, take the same numbers and were not measured.
 __device__ __forceinline__ PxCost px_cost(int rows, bool bf16) {
   return rows > 32 ? PxCost{bf16 ? 10 : 14, bf16 ? 5 : 6} : PxCost{3, 4};
 }
