@@ -197,6 +197,32 @@ SDSAT_API sdsat_status sdsat_kv_reserve(sdsat_ctx* ctx, sdsat_kv* kv, int seq, i
  * *used_dev = u (int32, may be NULL).  Errors: EINVAL. */
 SDSAT_API sdsat_status sdsat_kv_compact(sdsat_ctx* ctx, sdsat_kv* kv, int32_t* used_dev);
 
+/* Rotary position embedding of a model that the context's own table does not describe: part of a head, pairs side by
+ * side, frequencies scaled for long contexts. */
+#define SDSAT_ROPE_PLAIN 0
+#define SDSAT_ROPE_LINEAR 1      /* f_i / factor (position interpolation) */
+#define SDSAT_ROPE_PARTS 2       /* f_i (g_i + (1 - g_i) / factor), g_i = clamp((r_i - low) / (high - low), 0, 1) with
+                                    r_i = original f_i / 2 pi, the turns of pair i in the original context */
+typedef struct {
+  int32_t dims;            /* rotated dimensions of a head, the first ones: even, 2 .. 128; the rest pass through */
+  int32_t interleaved;     /* pairs (2 i, 2 i + 1), else (i, i + dims/2), i < dims/2 */
+  int32_t max_position;    /* positions 0 .. max_position - 1, at most 2^24 */
+  int32_t scaling;         /* SDSAT_ROPE_* */
+  int32_t original;        /* PARTS: positions of the context that the model was trained on */
+  int32_t reserved;        /* 0 */
+  double theta;            /* f_i = theta^(-2 i / dims) radians a position */
+  double factor;           /* LINEAR, PARTS */
+  double low, high;        /* PARTS: turns up to which a pair is interpolated, and from which on it stays */
+  double magnitude;        /* cosines and sines are multiplied by it (1: none) */
+} sdsat_rope_config;
+typedef struct sdsat_rope sdsat_rope;
+
+/* The cosines and sines of every position and pair, fp32, from angles in double: max_position * dims * 4 bytes.
+ * Synchronous.  The calls of its context take it; it may be destroyed before or after that.
+ * Errors: EINVAL (a field out of its range), ENOMEM, ECUDA. */
+SDSAT_API sdsat_status sdsat_rope_create(sdsat_ctx* ctx, const sdsat_rope_config* cfg, sdsat_rope** out);
+SDSAT_API void sdsat_rope_destroy(sdsat_rope* rope);
+
 /* Device addresses and geometry of a KV cache (for tests and benches that fill
  * or inspect it).  Any output pointer may be NULL. */
 SDSAT_API sdsat_status sdsat_kv_info(const sdsat_kv* kv, void** k_dev, void** v_dev, int32_t** len_dev,
@@ -468,6 +494,53 @@ SDSAT_API sdsat_status sdsat_op_prefix_attention(sdsat_ctx* ctx, const void* q_d
                                                  const uint32_t* anc_dev, int b, int q, int H, int Hk, int hd,
                                                  void* out_dev, int64_t out_ld, int type);
 
+/* ---- ragged batches on pages: sequences with new rows of a number of their own --------------- */
+/* The rows of a ragged batch stand one after the other: rows start[s] .. start[s+1]-1 are the new ones of sequence s,
+ * row start[s] + i at slot len[s] + i.  start_dev int32 [b+1] ascends within [0, rows]; rows before start[0] and from
+ * start[b] on belong to no sequence and are left as they are.  len_dev int32 [b]: the committed slots, which the calls do
+ * not advance.  table_dev int32 [b][table_ld] and the pages as in sdsat_op_prefix_attention. */
+
+/* Head norms, rotation and append.  For every new row of every sequence, with x one of its heads of queries or keys:
+ *   x' = x rsqrt(mean x^2 + eps) g                        (with gains; else x' = x)
+ *   (a, z) -> (a cos - z sin, a sin + z cos)              for the pairs of `rope` at the row's position
+ * The queries go to q_out_dev, keys and the values (as they are) as bf16 to the slot's row of the sequence's page.
+ *   q_dev, k_dev, v_dev  [rows] of H*hd, Hk*hd and Hk*hd values of `type` (SDSAT_FP32, SDSAT_BF16), q_ld, k_ld and v_ld
+ *                        values apart: also parts of one matrix.  q_out_dev: the same type, q_out_ld apart; may be q_dev
+ *   q_gain_dev, k_gain_dev  bf16 [hd], or NULL: no norm of those heads
+ *   position_dev         int32 [rows], or NULL: the slots.  A position outside the table counts as its nearest (device
+ *                        bit POSITION)
+ *   k_pages_dev, v_pages_dev  bf16 [n_pages][Hk][SDSAT_PAGE][hd]
+ *   refs_dev             int32 [n_pages], or NULL: a row whose page is not held once is not written
+ * A row past the table's slots or without a page (of its own, with refs) is not written to the cache and sets device
+ * bit CAPACITY; its query is rotated all the same.  Two sequences that write to one page need refs.
+ * hd 64 or 128, dims <= hd, H a multiple of Hk, b <= 65536; q, k, v and q_out 16-byte aligned with rows a multiple of 16
+ * bytes apart, pages 16-byte aligned, gains aligned to their values.  Errors: EINVAL. */
+SDSAT_API sdsat_status sdsat_op_rotary_append(sdsat_ctx* ctx, const sdsat_rope* rope, const void* q_dev, int64_t q_ld,
+                                              const void* k_dev, int64_t k_ld, const void* v_dev, int64_t v_ld, int type,
+                                              int rows, const int32_t* start_dev, const int32_t* len_dev, int b,
+                                              const int32_t* position_dev, const void* q_gain_dev, const void* k_gain_dev,
+                                              float eps, int H, int Hk, int hd, void* q_out_dev, int64_t q_out_ld,
+                                              void* k_pages_dev, void* v_pages_dev, int n_pages, const int32_t* table_dev,
+                                              int table_ld, const int32_t* refs_dev);
+
+/* Causal attention of a ragged batch over pages (its new rows' keys and values among them):
+ * out[start[s]+i][h*hd+d] = sum_t softmax_t(q . k_t / sqrt(hd)) v_t[d] over slots t <= len[s] + i.
+ *   q_dev, out_dev  [rows] of H*hd values of `type` (SDSAT_FP32, SDSAT_BF16), q_ld and out_ld values apart; sums fp32;
+ *                   query head h reads cache head h / (H/Hk)
+ * fp32 queries and probabilities enter the products in three bf16 parts (24 bits), bf16 queries as they are and their
+ * probabilities rounded to bf16.  A slot past the table or on a page outside [0, n_pages) is not attended to and sets
+ * device bit PAGE (a row that sees no slot is 0); what a page holds in slots that no row of the sequence sees does not
+ * matter; a row's invisible slots that a later row sees count 0 times their value.  A start_dev that does not ascend
+ * within [0, rows] leaves out_dev as it is and sets device bit CAPACITY; negative lengths count as 0.  Partial results
+ * go through the context's workspace (see the conventions on streams).
+ * hd 64 or 128, H a multiple of Hk, H/Hk <= 128, b <= 1024, n_pages * Hk * SDSAT_PAGE < 2^31; pointers 16-byte
+ * aligned, rows a multiple of 16 bytes apart.  Errors: EINVAL, EUNSUPPORTED (H/Hk or b above that). */
+SDSAT_API sdsat_status sdsat_op_chunk_attention(sdsat_ctx* ctx, const void* q_dev, int64_t q_ld, int rows,
+                                                const void* k_pages_dev, const void* v_pages_dev, int n_pages,
+                                                const int32_t* table_dev, int table_ld, const int32_t* start_dev,
+                                                const int32_t* len_dev, int b, int H, int Hk, int hd, void* out_dev,
+                                                int64_t out_ld, int type);
+
 /* Log probabilities of rows of logits at a temperature T: with m the row's maximum,
  * d_i = (l_i - m) / T and S = sum_i exp(d_i),
  *   logp[r]    = d_t - log S of the row's token t = tokens_dev[r]
@@ -485,6 +558,33 @@ SDSAT_API sdsat_status sdsat_op_logprobs(sdsat_ctx* ctx, const void* logits_dev,
                                          int vocab, const int32_t* tokens_dev, float temperature, int n_top,
                                          float* logp_dev, float* entropy_dev, int32_t* rank_dev,
                                          int32_t* top_ids_dev, float* top_logp_dev);
+
+/* Rules on the logits of b*q block rows (row j of sequence s at s*q + j) before a token is selected.  With
+ * c(t) the number of times that t was generated and seen(t) whether it was, or is in the prompt:
+ *   l <- seen(t) ? (l > 0 ? l / repetition[s] : l * repetition[s]) : l
+ *   l <- l - frequency[s] c(t) - (c(t) > 0 ? presence[s] : 0)
+ *   l <- l + the bias of t
+ *   l <- allowed(t) ? l : -inf
+ * in fp32, rounded once.  in_dev, out_dev: rows of `vocab` values of `type`, in_ld and out_ld values apart (any
+ * alignment of their values); the same rows, or none in common.
+ *   history_dev       int32 [b][history_ld]: the tokens before the block; history_len_dev int32 [b] of them (clamped to
+ *                     [0, history_ld]), the first prompt_len_dev int32 [b] the prompt (NULL: none); NULL: no history
+ *   tokens_dev        int32 [b*q]: the block's tokens.  Row j comes after tokens 0 .. j of its sequence, or, with anc_dev,
+ *                     after those of the bits of anc_dev[s*q+j]; they count as generated.  NULL: none
+ *   repetition_dev, frequency_dev, presence_dev  fp32 [b]; NULL: 1, 0, 0
+ *   bias_id_dev, bias_dev  int32 and fp32 [b][n_bias]; of an id that is there twice the first counts
+ *   allowed_dev       uint32 [b*q][allowed_ld]: bit t % 32 of word t / 32; NULL: all
+ * Negative ids in history, tokens and biases are places that hold none; ids from vocab on count as none too and set
+ * device bit TOKEN.  NaN logits stay NaN where they are allowed.  q <= SDSAT_MAX_Q, b*q <= 2^20, n_bias <= 1024,
+ * history_ld < 2^19.  Errors: EINVAL, EUNSUPPORTED (history_ld, n_bias or vocab > 2^20). */
+SDSAT_API sdsat_status sdsat_op_adjust_logits(sdsat_ctx* ctx, const void* in_dev, int64_t in_ld, int type, int b, int q,
+                                              int vocab, const int32_t* history_dev, int history_ld,
+                                              const int32_t* history_len_dev, const int32_t* prompt_len_dev,
+                                              const int32_t* tokens_dev, const uint32_t* anc_dev,
+                                              const float* repetition_dev, const float* frequency_dev,
+                                              const float* presence_dev, const int32_t* bias_id_dev, const float* bias_dev,
+                                              int n_bias, const uint32_t* allowed_dev, int allowed_ld, void* out_dev,
+                                              int64_t out_ld);
 
 /* Copy a context workspace of the last block forward into dst_dev (fp32,
  * rows x cols row-major, rows = b*q of that forward): which = 0 the residual

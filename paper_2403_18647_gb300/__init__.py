@@ -33,6 +33,7 @@ DEV_TREE = 0x20
 DEV_PAGE = 0x40
 
 PAGE = 64              # slots of a page of a paged cache
+ROPE_SCALING = {None: 0, "linear": 1, "parts": 2}
 FP32, BF16 = 0, 1      # element types of the kernels that take more than one
 
 
@@ -57,6 +58,13 @@ class KernelStat(ctypes.Structure):
 class LayerWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("attn_norm", "wq", "wk", "wv", "wo", "ffn_norm", "w_gate", "w_up", "w_down")]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("max_position", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("original", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("theta", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
 
 
 class Weights(ctypes.Structure):
@@ -111,6 +119,10 @@ def _lib():
             "sdsat_kv_compact": [P, P, P],
             "sdsat_op_prefix_attention": [P, P, I64, P, P, I, P, I, P, P, P, I, I, I, I, I, P, I64, I],
             "sdsat_op_logprobs": [P, P, I64, I, I, I, P, F, I, P, P, P, P, P],
+            "sdsat_rope_create": [P, ctypes.POINTER(RopeConfig), ctypes.POINTER(P)],
+            "sdsat_op_rotary_append": [P, P, P, I64, P, I64, P, I64, I, I, P, P, I, P, P, P, F, I, I, I, P, I64, P, P, I, P, I, P],
+            "sdsat_op_chunk_attention": [P, P, I64, I, P, P, I, P, I, P, P, I, I, I, I, P, I64, I],
+            "sdsat_op_adjust_logits": [P, P, I64, I, I, I, I, P, I, P, P, P, P, P, P, P, P, P, I, P, I, P, I64],
             "sdsat_debug_workspace": [P, I, I, P],
             "sdsat_debug_wait_timeout": [P],
             "sdsat_attention_grid": [I, P, I, I, ctypes.POINTER(I), ctypes.POINTER(I)],
@@ -123,6 +135,8 @@ def _lib():
         lib.sdsat_destroy.restype = None
         lib.sdsat_kv_destroy.argtypes = [P]
         lib.sdsat_kv_destroy.restype = None
+        lib.sdsat_rope_destroy.argtypes = [P]
+        lib.sdsat_rope_destroy.restype = None
         lib.sdsat_kernel_class_name.argtypes = [ctypes.c_int]
         lib.sdsat_kernel_class_name.restype = ctypes.c_char_p
         lib.sdsat_status_string.argtypes = [ctypes.c_int]
@@ -184,6 +198,14 @@ def _array(t, dtype, n: int):
         raise
     raise ValueError("expected %d values of %s in a contiguous CUDA tensor, got %d of %s on %s"
                      % (n, dtype, t.numel(), t.dtype, t.device))
+
+
+def _pages(k, v, Hk: int, hd: int) -> int:
+    """The number of pages of two pools of cache heads."""
+    shape = tuple(k.shape)
+    if len(shape) != 4 or shape[1:] != (Hk, PAGE, hd) or tuple(v.shape) != shape:
+        raise ValueError("expected pages of [Hk][%d][hd]" % PAGE)
+    return shape[0]
 
 
 def _check(status: int, what: str):
@@ -323,6 +345,27 @@ class PagedKV(KV):
     @property
     def v(self):
         return self._pool(1)
+
+
+class Rope:
+    """The cosines and sines of a rotation: max_position rows of dims / 2 pairs, fp32."""
+
+    def __init__(self, ctx: "Context", cfg: RopeConfig):
+        self.ctx, self.dims, self.max_position = ctx, cfg.dims, cfg.max_position
+        h = ctypes.c_void_p()
+        _check(_lib().sdsat_rope_create(ctx.handle, ctypes.byref(cfg), ctypes.byref(h)), "sdsat_rope_create")
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _lib().sdsat_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Context:
@@ -573,6 +616,80 @@ class Context:
         _check(_lib().sdsat_op_logprobs(self.handle, lp, ld, kind, rows, vocab, _array(tokens, _i32, rows), temperature, n,
                                         _array(logp, _f32, rows), _array(entropy, _f32, rows), _array(rank, _i32, rows),
                                         _array(top_ids, _i32, rows * n), _array(top_logp, _f32, rows * n)), "sdsat_op_logprobs")
+
+    # ---- ragged batches on pages: rows starts[s] .. starts[s + 1] - 1 are sequence s's new ones ----
+    def rope(self, dims: int, max_position: int, theta: float = 1e4, interleaved: bool = False, scaling: str = None,
+             factor: float = 1.0, low: float = 1.0, high: float = 32.0, original: int = 0, magnitude: float = 1.0) -> Rope:
+        """The rotation of the first `dims` dimensions of a head; scaling None, "linear" or "parts" (see sdsat.h)."""
+        if scaling not in ROPE_SCALING:
+            raise ValueError("scaling: expected one of %s" % list(ROPE_SCALING))
+        self._bind_stream()
+        return Rope(self, RopeConfig(dims, int(interleaved), max_position, ROPE_SCALING[scaling], original, 0, theta, factor, low,
+                                     high, magnitude))
+
+    def op_rotary_append(self, rope: Rope, q, k, v, q_out, k_pages, v_pages, table, lens, starts, H: int, Hk: int, hd: int,
+                         positions=None, q_gain=None, k_gain=None, eps: float = 1e-5, refs=None):
+        """q, q_out [rows][H*hd], k and v [rows][Hk*hd], all fp32 or all bf16 (rows any distance apart); k_pages, v_pages bf16
+        [pages][Hk][PAGE][hd]; table int32 [b][columns]; lens int32 [b]; starts int32 [b + 1]; positions int32 [rows];
+        gains bf16 [hd]; refs int32 [pages]."""
+        self._bind_stream()
+        (qp, q_ld, kind, rows, cols), (op, o_ld, o_kind, o_rows, o_cols) = _rows(q), _rows(q_out)
+        (kp, k_ld, k_kind, k_rows, k_cols), (vp, v_ld, v_kind, v_rows, v_cols) = _rows(k), _rows(v)
+        if not kind == o_kind == k_kind == v_kind:
+            raise ValueError("q, k, v and q_out are of different types")
+        if k_rows < rows or v_rows < rows or o_rows < rows:
+            raise ValueError("k, v or q_out of fewer rows than q")
+        if cols < H * hd or o_cols < H * hd or k_cols < Hk * hd or v_cols < Hk * hd:
+            raise ValueError("fewer columns than heads * hd")
+        (b, columns), pages = table.shape, _pages(k_pages, v_pages, Hk, hd)
+        _check(_lib().sdsat_op_rotary_append(self.handle, rope.handle, qp, q_ld, kp, k_ld, vp, v_ld, kind, rows,
+                                             _array(starts, _i32, b + 1), _array(lens, _i32, b), b, _array(positions, _i32, rows),
+                                             _array(q_gain, _bf16, hd), _array(k_gain, _bf16, hd), eps, H, Hk, hd, op, o_ld,
+                                             _array(k_pages, _bf16, 0), _array(v_pages, _bf16, 0), pages,
+                                             _array(table, _i32, 0), columns, _array(refs, _i32, pages)), "sdsat_op_rotary_append")
+
+    def op_chunk_attention(self, q, k_pages, v_pages, table, lens, starts, H: int, Hk: int, hd: int, out):
+        """q, out [rows][H*hd], both fp32 or bf16 (rows any distance apart); k_pages, v_pages bf16 [pages][Hk][PAGE][hd];
+        table int32 [b][columns]; lens int32 [b]; starts int32 [b + 1]."""
+        self._bind_stream()
+        (qp, q_ld, kind, rows, cols), (op, o_ld, o_kind, o_rows, o_cols) = _rows(q), _rows(out)
+        if kind != o_kind:
+            raise ValueError("q and out are of different types")
+        if o_rows < rows:
+            raise ValueError("out of fewer rows than q")
+        if cols < H * hd or o_cols < H * hd:
+            raise ValueError("fewer columns than H * hd")
+        (b, columns), pages = table.shape, _pages(k_pages, v_pages, Hk, hd)
+        _check(_lib().sdsat_op_chunk_attention(self.handle, qp, q_ld, rows, _array(k_pages, _bf16, 0), _array(v_pages, _bf16, 0), pages,
+                                               _array(table, _i32, 0), columns, _array(starts, _i32, b + 1), _array(lens, _i32, b), b,
+                                               H, Hk, hd, op, o_ld, kind), "sdsat_op_chunk_attention")
+
+    def op_adjust_logits(self, logits, out, q: int = 1, history=None, history_lens=None, prompt_lens=None, tokens=None, anc=None,
+                         repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, allowed=None):
+        """logits, out [b*q][vocab], both fp32 or bf16 (rows any distance apart); history int32 [b][n]; history_lens, prompt_lens
+        int32 [b]; tokens, anc int32 [b*q]; repetition, frequency, presence fp32 [b]; bias_ids int32 and bias fp32 [b][m];
+        allowed int32 [b*q][words of 32 ids]."""
+        self._bind_stream()
+        (ip, i_ld, kind, rows, vocab), (op, o_ld, o_kind, o_rows, o_cols) = _rows(logits), _rows(out)
+        if kind != o_kind:
+            raise ValueError("logits and out are of different types")
+        if q < 1 or rows % q:
+            raise ValueError("rows are no multiple of q")
+        if o_rows < rows or o_cols < vocab:
+            raise ValueError("out is smaller than logits")
+        b = rows // q
+        n = 0 if history is None else history.size(1)
+        m = 0 if bias_ids is None else bias_ids.size(1)
+        if (bias is None) != (bias_ids is None) or m and bias.shape[1] != m:
+            raise ValueError("bias_ids and bias are of different widths")
+        words = 0 if allowed is None else allowed.size(1)
+        if allowed is not None and words < -(-vocab // 32):
+            raise ValueError("allowed is narrower than the vocabulary")
+        _check(_lib().sdsat_op_adjust_logits(self.handle, ip, i_ld, kind, b, q, vocab, _array(history, _i32, b * n), n,
+                                             _array(history_lens, _i32, b), _array(prompt_lens, _i32, b), _array(tokens, _i32, rows),
+                                             _array(anc, _i32, rows), _array(repetition, _f32, b), _array(frequency, _f32, b),
+                                             _array(presence, _f32, b), _array(bias_ids, _i32, b * m), _array(bias, _f32, b * m), m,
+                                             _array(allowed, _i32, rows * words), words, op, o_ld), "sdsat_op_adjust_logits")
 
     def debug_workspace(self, which: int, rows: int):
         """Last-layer workspace of the last forward: 0 h, 1 q, 2 attention out, 3 SwiGLU act."""

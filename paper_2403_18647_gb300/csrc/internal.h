@@ -409,4 +409,83 @@ struct LogprobParams {
 cudaError_t logprobs_prepare();
 cudaError_t launch_logprobs(const LogprobParams& p, int num_sms, cudaStream_t st, bool pdl);
 
+// ---- ragged batches: rows start[s] .. start[s+1]-1 of sequence s at slots len[s] .. -----
+// Head norms, rotation and append (rotary.cu)
+constexpr int ROPE_MAX_POSITION = 1 << 24;
+constexpr int ROTARY_MAX_BATCH = 1 << 16;
+struct RopeTable {
+  const float2* turn;       // [n][dims/2] cosines and sines
+  int dims, n, interleaved;
+};
+struct RopeBuild {
+  double f[64];             // radians a position
+  double magnitude;
+};
+cudaError_t launch_rope_table(const RopeBuild& f, float2* turn, int n, int pairs, cudaStream_t st);
+struct RotaryParams {
+  RopeTable rope;
+  const void *q, *k, *v;    // [rows][ld] fp32 or bf16
+  void* q_out;
+  long long q_ld, k_ld, v_ld, out_ld;
+  bool bf16;
+  int rows, b;
+  const int *start, *len;   // [b+1], [b]
+  const int* positions;     // [rows], or null: the slots
+  const __nv_bfloat16 *q_gain, *k_gain;   // [hd] or null
+  float eps;
+  int H, Hk, hd;
+  __nv_bfloat16 *k_pages, *v_pages;       // [pages.n][Hk][KV_PAGE][hd]
+  PageMap pages;            // refs may be null
+  uint32_t* err;
+};
+cudaError_t rotary_prepare();
+cudaError_t launch_rotary_append(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl);
+
+// Causal attention of a ragged batch (chunk_attention.cu)
+constexpr int CHUNK_MAX_BATCH = 1024;
+struct ChunkAttnParams {
+  CUtensorMap kmap, vmap;   // as PrefixAttnParams
+  const void* q;            // [rows][q_ld] fp32 or bf16
+  void* out;
+  long long q_ld, out_ld;
+  bool bf16;
+  const int *start, *len;
+  const int* table;         // [b][ld]
+  int rows, b, ld, n_pages;
+  int H, Hk, hd;
+  float* part;              // scratch: chunk_attention_scratch() floats, 16-byte aligned
+  const __nv_bfloat16 *k, *v;
+  uint32_t* err;
+};
+size_t chunk_attention_scratch(int num_sms);
+cudaError_t chunk_attention_prepare();
+cudaError_t launch_chunk_attention(const ChunkAttnParams& p, int num_sms, cudaStream_t st, bool pdl);
+
+// Penalties, biases and masks of logits (adjust.cu)
+constexpr int ADJ_MAX_BIAS = 1024;
+constexpr int ADJ_MAX_HISTORY = (1 << 19) - 1;
+constexpr int ADJ_MAX_VOCAB = 1 << 20;
+constexpr int ADJ_MAX_ROWS = 1 << 20;
+struct AdjustParams {
+  const void* in;           // [b*q][in_ld] fp32 or bf16
+  void* out;
+  long long in_ld, out_ld;
+  bool bf16;
+  int b, q, V;
+  const int* history;       // [b][history_ld] or null
+  int history_ld;
+  const int *history_len, *prompt_len;    // [b]; prompt_len may be null
+  const int* tokens;        // [b*q] or null
+  const uint32_t* anc;      // [b*q] or null
+  const float *repetition, *frequency, *presence;   // [b] or null
+  const int* bias_id;       // [b][n_bias]
+  const float* bias;
+  int n_bias;
+  const uint32_t* allowed;  // [b*q][allowed_ld] or null
+  int allowed_ld;
+  uint32_t* err;
+};
+cudaError_t adjust_prepare();
+cudaError_t launch_adjust(const AdjustParams& p, int num_sms, cudaStream_t st, bool pdl);
+
 }  // namespace sdsat

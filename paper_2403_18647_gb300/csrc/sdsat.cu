@@ -91,12 +91,14 @@ struct LayerMaps {
 enum KClass : int {
   K_RMSNORM = 0, K_GEMM_QKV, K_ATTENTION, K_GEMM_O, K_GEMM_GATEUP, K_GEMM_DOWN, K_GEMM_LM_HEAD, K_ACCEPT,
   K_BUILD_BLOCK, K_KV_COMMIT, K_PREFILL_COMMIT, K_GEMM_OP, K_ATTENTION_OP, K_TREE_PREP, K_TREE_COMPACT,
-  K_PF_GEMM, K_PF_ATTENTION, K_PAGES, K_PREFIX_ATTENTION, K_LOGPROBS, K_COUNT
+  K_PF_GEMM, K_PF_ATTENTION, K_PAGES, K_PREFIX_ATTENTION, K_LOGPROBS, K_ROTARY_APPEND,
+  K_CHUNK_ATTENTION, K_ADJUST_LOGITS, K_COUNT
 };
 const char* const KCLASS_NAME[K_COUNT] = {"rmsnorm", "gemm_qkv", "attention", "gemm_o", "gemm_gateup", "gemm_down",
                                           "gemm_lm_head", "accept", "build_block", "kv_commit", "prefill_commit",
                                           "gemm_op", "attention_op", "tree_prep", "tree_compact", "prefill_gemm",
-                                          "prefill_attention", "pages", "prefix_attention", "logprobs"};
+                                          "prefill_attention", "pages", "prefix_attention", "logprobs", "rotary_append",
+                                          "chunk_attention", "adjust_logits"};
 
 static_assert(SDSAT_MAX_ROWS == 64, "block rows fill one 64-row tile of the prefill GEMM");
 constexpr int MAX_GEMM_TILES = 1 << 16;
@@ -135,6 +137,7 @@ struct sdsat_ctx {
   int* tree_ws = nullptr;      // [SDSAT_MAX_ROWS][TREE_WS_STRIDE] tree commit: len, m, path
   int* adaptive = nullptr;
   float* prefix_part = nullptr;   // partial results of the prefix attention
+  float* chunk_part = nullptr;    // ... of the chunk attention
   int* prompt_start = nullptr;    // [1] a prompt's sequence's length before it
   uint32_t* err = nullptr;
   // prefill workspaces (chunks of up to pf_rows positions; allocated with the weights)
@@ -163,6 +166,12 @@ struct sdsat_ctx {
   std::vector<cudaEvent_t> prof_events;
   std::vector<int> prof_class;
   size_t prof_used = 0;
+};
+
+struct sdsat_rope {
+  sdsat_ctx* ctx = nullptr;
+  float2* turn = nullptr;   // [max_position][dims/2]
+  RopeTable table{};
 };
 
 struct sdsat_kv {
@@ -750,7 +759,8 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
       cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
       gemm_prepare() != cudaSuccess || attention_prepare() != cudaSuccess || prefill_prepare() != cudaSuccess ||
       prefill_attention_prepare() != cudaSuccess || accept_prepare() != cudaSuccess || pages_prepare() != cudaSuccess ||
-      prefix_attention_prepare() != cudaSuccess || logprobs_prepare() != cudaSuccess) {
+      prefix_attention_prepare() != cudaSuccess || logprobs_prepare() != cudaSuccess ||
+      rotary_prepare() != cudaSuccess || chunk_attention_prepare() != cudaSuccess || adjust_prepare() != cudaSuccess) {
     delete c;
     return SDSAT_ECUDA;
   }
@@ -806,6 +816,7 @@ sdsat_status sdsat_create(const sdsat_config* cfg, const sdsat_weights* w, void*
             dalloc(c, &c->tree_pos, rows) && dalloc(c, &c->tree_anc, rows) &&
             dalloc(c, &c->tree_ws, (size_t)rows * TREE_WS_STRIDE) &&
             dalloc(c, &c->prefix_part, prefix_attention_scratch((size_t)rows * cfg->n_heads * cfg->head_dim, c->num_sms)) &&
+            dalloc(c, &c->chunk_part, chunk_attention_scratch(c->num_sms)) &&
             dalloc(c, &c->prompt_start, 1) && dalloc(c, &c->err, 1) && dalloc(c, &c->xop_hi, (size_t)OP_MAX_M * OP_MAX_K) &&
             dalloc(c, &c->ssq, (size_t)rows * ((d + 127) / 128)) &&
             dalloc(c, &c->xop_lo, (size_t)OP_MAX_M * OP_MAX_K);
@@ -1496,6 +1507,198 @@ sdsat_status sdsat_op_logprobs(sdsat_ctx* c, const void* logits_dev, int64_t ld,
   p.top_logp = top_logp_dev;
   p.err = c->err;
   return timed(c, K_LOGPROBS, [&] { return launch_logprobs(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_rope_create(sdsat_ctx* c, const sdsat_rope_config* f, sdsat_rope** out) {
+  if (!c || !f || !out) return SDSAT_EINVAL;
+  *out = nullptr;
+  auto positive = [](double x) { return x > 0. && std::isfinite(x); };
+  if (f->dims < 2 || f->dims > 128 || f->dims % 2 || f->max_position < 1 || f->max_position > ROPE_MAX_POSITION ||
+      (f->interleaved != 0 && f->interleaved != 1) || f->scaling < SDSAT_ROPE_PLAIN || f->scaling > SDSAT_ROPE_PARTS ||
+      !positive(f->theta) || !positive(f->magnitude))
+    return SDSAT_EINVAL;
+  if (f->scaling != SDSAT_ROPE_PLAIN && !positive(f->factor)) return SDSAT_EINVAL;
+  if (f->scaling == SDSAT_ROPE_PARTS && (f->original < 1 || !std::isfinite(f->low) || !std::isfinite(f->high) || !(f->low < f->high)))
+    return SDSAT_EINVAL;
+  const int pairs = f->dims / 2;
+  RopeBuild build;
+  std::memset(&build, 0, sizeof(build));
+  build.magnitude = f->magnitude;
+  for (int i = 0; i < pairs; ++i) {
+    const double w = std::pow(f->theta, -2.0 * i / f->dims);
+    double keep = f->scaling == SDSAT_ROPE_PLAIN ? 1.0 : 0.0;
+    if (f->scaling == SDSAT_ROPE_PARTS)
+      keep = std::min(1.0, std::max(0.0, (f->original * w / 6.283185307179586476925 - f->low) / (f->high - f->low)));
+    build.f[i] = f->scaling == SDSAT_ROPE_PLAIN ? w : w * (keep + (1.0 - keep) / f->factor);
+  }
+  sdsat_rope* r = new (std::nothrow) sdsat_rope();
+  if (!r) return SDSAT_ENOMEM;
+  r->ctx = c;
+  void* turn = nullptr;
+  if (cudaMalloc(&turn, (size_t)f->max_position * pairs * sizeof(float2)) != cudaSuccess) {
+    cudaGetLastError();   // clear the runtime's record of the failed allocation (not sticky)
+    delete r;
+    return SDSAT_ENOMEM;
+  }
+  r->turn = static_cast<float2*>(turn);
+  r->table = RopeTable{r->turn, f->dims, f->max_position, f->interleaved};
+  if (launch_rope_table(build, r->turn, f->max_position, pairs, c->stream) != cudaSuccess ||
+      cudaStreamSynchronize(c->stream) != cudaSuccess) {
+    cudaFree(turn);
+    delete r;
+    return SDSAT_ECUDA;
+  }
+  *out = r;
+  return SDSAT_OK;
+}
+
+void sdsat_rope_destroy(sdsat_rope* r) {
+  if (!r) return;
+  cudaFree(r->turn);   // (waits for the device; the context may be gone)
+  delete r;
+}
+
+sdsat_status sdsat_op_rotary_append(sdsat_ctx* c, const sdsat_rope* rope, const void* q_dev, int64_t q_ld, const void* k_dev,
+                                    int64_t k_ld, const void* v_dev, int64_t v_ld, int type, int rows,
+                                    const int32_t* start_dev, const int32_t* len_dev, int b, const int32_t* position_dev,
+                                    const void* q_gain_dev, const void* k_gain_dev, float eps, int H, int Hk, int hd,
+                                    void* q_out_dev, int64_t q_out_ld, void* k_pages_dev, void* v_pages_dev, int n_pages,
+                                    const int32_t* table_dev, int table_ld, const int32_t* refs_dev) {
+  if (!c || !rope || rope->ctx != c || (type != SDSAT_FP32 && type != SDSAT_BF16) || rows < 0 || b < 1 ||
+      b > ROTARY_MAX_BATCH || (hd != 64 && hd != 128) || H < 1 || Hk < 1 || H % Hk || rope->table.dims > hd || n_pages < 1 ||
+      table_ld < 1 || !(eps >= 0.f) || std::isinf(eps))
+    return SDSAT_EINVAL;
+  const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
+  const long long R = (long long)H * hd, Rk = (long long)Hk * hd;
+  if (q_ld < R || q_out_ld < R || k_ld < Rk || v_ld < Rk || (q_ld | q_out_ld | k_ld | v_ld) % per16) return SDSAT_EINVAL;
+  if (R + 2 * Rk > 1 << 24 || (long long)table_ld * KV_PAGE > 0x7FFFFFFFll || (long long)rows * ((R + 2 * Rk) / 64) >= 1ll << 31)
+    return SDSAT_EINVAL;   // (heads of rows, and slots, are counted in 32 bits)
+  if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
+  if (!aligned16(q_dev) || !aligned16(k_dev) || !aligned16(v_dev) || !aligned16(q_out_dev) || !aligned16(k_pages_dev) ||
+      !aligned16(v_pages_dev) || !start_dev || !len_dev || !table_dev || reinterpret_cast<uintptr_t>(q_gain_dev) % 2 ||
+      reinterpret_cast<uintptr_t>(k_gain_dev) % 2)
+    return SDSAT_EINVAL;
+  RotaryParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.rope = rope->table;
+  p.q = q_dev;
+  p.k = k_dev;
+  p.v = v_dev;
+  p.q_out = q_out_dev;
+  p.q_ld = q_ld;
+  p.k_ld = k_ld;
+  p.v_ld = v_ld;
+  p.out_ld = q_out_ld;
+  p.bf16 = type == SDSAT_BF16;
+  p.rows = rows;
+  p.b = b;
+  p.start = start_dev;
+  p.len = len_dev;
+  p.positions = position_dev;
+  p.q_gain = static_cast<const __nv_bfloat16*>(q_gain_dev);
+  p.k_gain = static_cast<const __nv_bfloat16*>(k_gain_dev);
+  p.eps = eps;
+  p.H = H;
+  p.Hk = Hk;
+  p.hd = hd;
+  p.k_pages = static_cast<__nv_bfloat16*>(k_pages_dev);
+  p.v_pages = static_cast<__nv_bfloat16*>(v_pages_dev);
+  p.pages = PageMap{table_dev, refs_dev, table_ld, n_pages};
+  p.err = c->err;
+  return timed(c, K_ROTARY_APPEND, [&] { return launch_rotary_append(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_op_chunk_attention(sdsat_ctx* c, const void* q_dev, int64_t q_ld, int rows, const void* k_pages_dev,
+                                      const void* v_pages_dev, int n_pages, const int32_t* table_dev, int table_ld,
+                                      const int32_t* start_dev, const int32_t* len_dev, int b, int H, int Hk, int hd,
+                                      void* out_dev, int64_t out_ld, int type) {
+  if (!c || (type != SDSAT_FP32 && type != SDSAT_BF16) || rows < 0 || b < 1 || (hd != 64 && hd != 128) || H < 1 || Hk < 1 ||
+      H % Hk || n_pages < 1 || table_ld < 1)
+    return SDSAT_EINVAL;
+  const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
+  if (q_ld < (long long)H * hd || out_ld < (long long)H * hd || q_ld % per16 || out_ld % per16) return SDSAT_EINVAL;
+  const long long pool = (long long)n_pages * Hk * KV_PAGE;
+  if (pool > 0x7FFFFFFFll || (long long)table_ld * KV_PAGE > 0x3FFFFFFFll || (long long)H * hd > 1 << 24 || rows > 1 << 28)
+    return SDSAT_EINVAL;   // (pool rows and slots are counted in 32 bits)
+  if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
+  if (!aligned16(q_dev) || !aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !aligned16(out_dev) || !start_dev || !len_dev ||
+      !table_dev)
+    return SDSAT_EINVAL;
+  if (H / Hk > 128 || b > CHUNK_MAX_BATCH) return SDSAT_EUNSUPPORTED;
+  ChunkAttnParams p;
+  std::memset(&p, 0, sizeof(p));
+  if (!make_kvmap(&p.kmap, k_pages_dev, pool, hd) || !make_kvmap(&p.vmap, v_pages_dev, pool, hd)) return SDSAT_ECUDA;
+  p.q = q_dev;
+  p.out = out_dev;
+  p.q_ld = q_ld;
+  p.out_ld = out_ld;
+  p.bf16 = type == SDSAT_BF16;
+  p.start = start_dev;
+  p.len = len_dev;
+  p.table = table_dev;
+  p.rows = rows;
+  p.b = b;
+  p.ld = table_ld;
+  p.n_pages = n_pages;
+  p.H = H;
+  p.Hk = Hk;
+  p.hd = hd;
+  p.part = c->chunk_part;
+  p.k = static_cast<const __nv_bfloat16*>(k_pages_dev);
+  p.v = static_cast<const __nv_bfloat16*>(v_pages_dev);
+  p.err = c->err;
+  return timed(c, K_CHUNK_ATTENTION, [&] { return launch_chunk_attention(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
+             ? SDSAT_OK
+             : SDSAT_ECUDA;
+}
+
+sdsat_status sdsat_op_adjust_logits(sdsat_ctx* c, const void* in_dev, int64_t in_ld, int type, int b, int q, int vocab,
+                                    const int32_t* history_dev, int history_ld, const int32_t* history_len_dev,
+                                    const int32_t* prompt_len_dev, const int32_t* tokens_dev, const uint32_t* anc_dev,
+                                    const float* repetition_dev, const float* frequency_dev, const float* presence_dev,
+                                    const int32_t* bias_id_dev, const float* bias_dev, int n_bias,
+                                    const uint32_t* allowed_dev, int allowed_ld, void* out_dev, int64_t out_ld) {
+  if (!c || (type != SDSAT_FP32 && type != SDSAT_BF16) || b < 0 || q < 1 || q > SDSAT_MAX_Q || vocab < 1 || in_ld < vocab ||
+      out_ld < vocab || history_ld < 0 || n_bias < 0 || b > ADJ_MAX_ROWS / q)
+    return SDSAT_EINVAL;
+  if (allowed_dev && allowed_ld < (vocab + 31) / 32) return SDSAT_EINVAL;
+  if (b == 0) return SDSAT_OK;   // (no rows need no memory)
+  const unsigned value = type == SDSAT_BF16 ? 2 : 4;
+  if (!in_dev || !out_dev || reinterpret_cast<uintptr_t>(in_dev) % value || reinterpret_cast<uintptr_t>(out_dev) % value)
+    return SDSAT_EINVAL;
+  if (history_dev && history_ld && !history_len_dev) return SDSAT_EINVAL;
+  if (n_bias && (!bias_id_dev || !bias_dev)) return SDSAT_EINVAL;
+  if (vocab > ADJ_MAX_VOCAB || n_bias > ADJ_MAX_BIAS || history_ld > ADJ_MAX_HISTORY) return SDSAT_EUNSUPPORTED;
+  AdjustParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.in = in_dev;
+  p.out = out_dev;
+  p.in_ld = in_ld;
+  p.out_ld = out_ld;
+  p.bf16 = type == SDSAT_BF16;
+  p.b = b;
+  p.q = q;
+  p.V = vocab;
+  p.history = history_ld ? history_dev : nullptr;
+  p.history_ld = history_ld;
+  p.history_len = history_len_dev;
+  p.prompt_len = prompt_len_dev;
+  p.tokens = tokens_dev;
+  p.anc = anc_dev;
+  p.repetition = repetition_dev;
+  p.frequency = frequency_dev;
+  p.presence = presence_dev;
+  p.bias_id = bias_id_dev;
+  p.bias = bias_dev;
+  p.n_bias = n_bias;
+  p.allowed = allowed_dev;
+  p.allowed_ld = allowed_ld;
+  p.err = c->err;
+  return timed(c, K_ADJUST_LOGITS, [&] { return launch_adjust(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
              ? SDSAT_OK
              : SDSAT_ECUDA;
 }
