@@ -445,6 +445,7 @@ cudaError_t launch_rotary_append(const RotaryParams& p, int num_sms, cudaStream_
 constexpr int CHUNK_MAX_BATCH = 1024;
 struct ChunkAttnParams {
   CUtensorMap kmap, vmap;   // as PrefixAttnParams
+  CUtensorMap qmap;         // bf16 queries as [rows][H][hd], boxes of 128 / G rows x G heads x 64 dims
   const void* q;            // [rows][q_ld] fp32 or bf16
   void* out;
   long long q_ld, out_ld;
@@ -454,7 +455,6 @@ struct ChunkAttnParams {
   int rows, b, ld, n_pages;
   int H, Hk, hd;
   float* part;              // scratch: chunk_attention_scratch() floats, 16-byte aligned
-  const __nv_bfloat16 *k, *v;
   uint32_t* err;
 };
 size_t chunk_attention_scratch(int num_sms);

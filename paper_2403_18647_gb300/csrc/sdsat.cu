@@ -78,6 +78,18 @@ bool make_kvmap(CUtensorMap* map, const void* ptr, long long rows, int hd) {
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// bf16 queries [rows][ld] as [rows][H][hd], boxes of n rows x G heads x 64 dimensions, 128-byte swizzle
+bool make_qmap(CUtensorMap* map, const void* ptr, int rows, long long ld, int H, int hd, int G, int n) {
+  if (!get_encode()) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)H, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)ld * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)n};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr int N_MPADS = sizeof(GEMM_MPADS) / sizeof(GEMM_MPADS[0]);
 int mpad_index(int M) { return (int)(std::find(GEMM_MPADS, GEMM_MPADS + N_MPADS, gemm_mpad(M)) - GEMM_MPADS); }
 
@@ -1631,7 +1643,9 @@ sdsat_status sdsat_op_chunk_attention(sdsat_ctx* c, const void* q_dev, int64_t q
   if (H / Hk > 128 || b > CHUNK_MAX_BATCH) return SDSAT_EUNSUPPORTED;
   ChunkAttnParams p;
   std::memset(&p, 0, sizeof(p));
-  if (!make_kvmap(&p.kmap, k_pages_dev, pool, hd) || !make_kvmap(&p.vmap, v_pages_dev, pool, hd)) return SDSAT_ECUDA;
+  if (!make_kvmap(&p.kmap, k_pages_dev, pool, hd) || !make_kvmap(&p.vmap, v_pages_dev, pool, hd) ||
+      (type == SDSAT_BF16 && !make_qmap(&p.qmap, q_dev, rows, q_ld, H, hd, H / Hk, 128 / (H / Hk))))
+    return SDSAT_ECUDA;
   p.q = q_dev;
   p.out = out_dev;
   p.q_ld = q_ld;
@@ -1648,8 +1662,6 @@ sdsat_status sdsat_op_chunk_attention(sdsat_ctx* c, const void* q_dev, int64_t q
   p.Hk = Hk;
   p.hd = hd;
   p.part = c->chunk_part;
-  p.k = static_cast<const __nv_bfloat16*>(k_pages_dev);
-  p.v = static_cast<const __nv_bfloat16*>(v_pages_dev);
   p.err = c->err;
   return timed(c, K_CHUNK_ATTENTION, [&] { return launch_chunk_attention(p, c->num_sms, c->stream, c->pdl); }) == cudaSuccess
              ? SDSAT_OK
