@@ -98,15 +98,41 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[tmem] * B[smem]: A's rows on the lanes, two bf16 of K per column
-__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                             uint32_t accumulate) {
+// The products are issued by a whole warp, in step, of which one lane's instruction counts (`mine`): issued from a
+// branch that one lane took, each MMA cost some 90 cycles.
+__device__ __forceinline__ uint32_t ch_elect() {
+  uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r;
+}
+// D[tmem] (+)= A[smem] * B[smem]^T
+__device__ __forceinline__ void ch_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t mine) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine)
       : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A's rows on the lanes, two bf16 of K per column
+__device__ __forceinline__ void ch_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t mine) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine)
+      : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 // MN-major operand in the 128-byte swizzle layout: atoms of 64 dims (128 bytes) x 8 keys;
 // `lead` bytes to the next 64 dims, 1024 to the next 8 keys
@@ -491,94 +517,104 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     // ---- products
     constexpr uint32_t idesc_s = idesc_bf16_f32(128, CH_BLK);
     constexpr uint32_t idesc_o = idesc_bf16_f32(128, HD) | (1u << 16);   // B is MN-major
+    const uint32_t mine = ch_elect();
+    const uint64_t q_desc = sdesc_sw128(smem_u32(smem)), k_desc = sdesc_sw128(smem_u32(ring)), v_desc = sdesc_sw128_mn(smem_u32(ring), C::HALF);
     bool ok = true;
     uint32_t n = 0, qn[2] = {0, 0}, pn[2] = {0, 0}, zn = 0;   // blocks; per tile: Q tiles, P's; z_done phases (bits)
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && mbar_wait_bounded(bar, parity, abort_flag, p.err);
-      if (ok) tc_fence_after();
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
+      tc_fence_after();
       return ok;
     };
+    auto commit = [&](uint64_t* bar) {
+      if (mine) umma_commit(bar);
+      __syncwarp();
+    };
     auto qk = [&](int t, uint32_t blk) {
-      const uint32_t k = smem_u32(ring + (size_t)((2 * blk) % SLOTS) * C::TILE);
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) {
-        const uint32_t q = smem_u32(smem + (size_t)(PARTS * t + part) * C::TILE);
+      const uint64_t k = k_desc + (uint64_t)((2 * blk) % SLOTS) * (C::TILE >> 4), q = q_desc + (uint64_t)(PARTS * t) * (C::TILE >> 4);
+#pragma unroll 1
+      for (int part = PARTS - 1; part >= 0; --part)   // (small ones first: the sums round less)
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t o = (kk >> 2) * C::HALF + (kk & 3) * 32;
-          umma_bf16(tmem + C::S_COL(t), sdesc_sw128(q + o), sdesc_sw128(k + o), idesc_s, part | kk ? 1u : 0u);
+          const uint32_t o = (kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2;
+          ch_mma(tmem + C::S_COL(t), q + part * (C::TILE >> 4) + o, k + o, idesc_s, part < PARTS - 1 || kk ? 1u : 0u, mine);
         }
-      }
-      umma_commit(&s_full[t]);
+      commit(&s_full[t]);
     };
     auto pv = [&](int t, uint32_t blk, int steps, bool first) {
-      const uint32_t v = smem_u32(ring + (size_t)((2 * blk + 1) % SLOTS) * C::TILE);
-      for (int part = 0; part < PARTS; ++part)
-        for (int kk = 0; kk < steps; ++kk)
-          umma_bf16_ta(tmem + C::O_COL(t), tmem + C::P_COL(t) + part * 64 + kk * 8, sdesc_sw128_mn(v + kk * 2048, C::HALF), idesc_o,
-                       !first || part || kk ? 1u : 0u);
+      const uint64_t v = v_desc + (uint64_t)((2 * blk + 1) % SLOTS) * (C::TILE >> 4);
+#pragma unroll 1
+      for (int part = PARTS - 1; part >= 0; --part) {
+        const uint32_t a = tmem + C::P_COL(t) + part * 64;
+        const uint32_t acc = !first || part < PARTS - 1 ? 1u : 0u;
+        if (steps == CH_BLK / 16) {
+#pragma unroll
+          for (int kk = 0; kk < CH_BLK / 16; ++kk) ch_mma_ta(tmem + C::O_COL(t), a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
+        } else {
+#pragma unroll 1
+          for (int kk = 0; kk < steps; ++kk) ch_mma_ta(tmem + C::O_COL(t), a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
+        }
+      }
     };
     ChItem it;
     while (ok && next_item(it)) {
-      if (lane == 0) {
-        const int nt = item_tiles(it);
-        int end[2] = {item_end(it, 0), item_end(it, nt - 1)};
-        for (int t = 0; t < nt && ok; ++t)
-          if (end[t] > it.kb0) wait(&q_full[t], qn[t]++ & 1);
-        const uint32_t n0 = n;   // block kb0 is the ring's n0-th
-        auto wait_v = [&](uint32_t blk, int j) {
-          const int vs = (2 * blk + 1) % SLOTS;
-          if (!wait(&full[vs], ((2 * blk + 1) / SLOTS) & 1)) return false;
-          if (flags[blk % CH_FLAGS] == 3u && !item_tail(it, j)) return true;
-          return wait(&z_done[vs], (zn >> vs) & 1);
-        };
-        auto used_v = [&](uint32_t blk, int j) {   // by the last product of a block
-          const int vs = (2 * blk + 1) % SLOTS;
-          if (flags[blk % CH_FLAGS] != 3u || item_tail(it, j)) zn ^= 1u << vs;
-          umma_commit(&empty[vs]);
-        };
-        auto steps = [&](int t, int j) { return min(CH_BLK / 16, (item_keys(it, t) - j * CH_BLK + 15) / 16); };
-        // step j: per tile, block j - 1's P V and then block j's S over the P that it has read (one tile: block j's S, into a
-        // place of its own, and then block j - 1's P V); the last tile has every block, so its products release V of block
-        // j - 1 and K of block j
-        for (int j = it.kb0; j <= it.kb1 && ok; ++j) {
-          const uint32_t blk = n0 + (j - it.kb0);
-          for (int t = 0; t < nt && ok; ++t) {
-            const bool has_pv = j > it.kb0 && j <= end[t], has_qk = j < end[t];
-            auto do_pv = [&]() {
-              if (!wait_v(blk - 1, j - 1)) return;
-              if (PARTS == 1 && !wait(&p_full[t], pn[t]++ & 1)) return;
-              pv(t, blk - 1, steps(t, j - 1), j - 1 == it.kb0);
-              if (PARTS != 1) umma_commit(pv_done);
-              else if (j == end[t]) umma_commit(&o_full[t]);
-              if (t == nt - 1) used_v(blk - 1, j - 1);
-            };
-            auto do_qk = [&]() {
-              const int ks = (2 * blk) % SLOTS;
-              if (!wait(&full[ks], (2 * blk / SLOTS) & 1)) return;
-              qk(t, blk);
-              if (j == end[t] - 1) umma_commit(&q_empty[t]);
-              if (t == nt - 1) umma_commit(&empty[ks]);
-            };
-            if (PARTS == 1) {
-              if (has_pv) do_pv();
-              if (has_qk && ok) do_qk();
-            } else {
-              if (has_pv) wait(&p_full[t], pn[t]++ & 1);   // (S has been read, too)
-              if (has_qk && ok) do_qk();
-              if (has_pv && ok) do_pv();
+      const int nt = item_tiles(it);
+      const int end[2] = {item_end(it, 0), item_end(it, nt - 1)};
+#pragma unroll
+      for (int t = 0; t < C::TILES; ++t)
+        if (t < nt && end[t] > it.kb0) wait(&q_full[t], qn[t]++ & 1);
+      const uint32_t n0 = n;   // block kb0 is the ring's n0-th
+      auto has_zeros = [&](uint32_t blk, int j) { return flags[blk % CH_FLAGS] != 3u || item_tail(it, j); };
+      // step j: per tile, block j - 1's P V and then block j's S over the P that it has read (one tile: block j's S, into a
+      // place of its own, and then block j - 1's P V); the last tile has every block, so its products release V of block
+      // j - 1 and K of block j
+#pragma unroll 1
+      for (int j = it.kb0; j <= it.kb1 && ok; ++j) {
+        const uint32_t blk = n0 + (j - it.kb0);
+#pragma unroll
+        for (int t = 0; t < C::TILES; ++t) {
+          if (t >= nt) break;
+          const bool has_pv = j > it.kb0 && j <= end[t], has_qk = j < end[t];
+          auto do_pv = [&]() {
+            const int vs = (2 * blk - 1) % SLOTS;
+            if (!wait(&full[vs], ((2 * blk - 1) / SLOTS) & 1)) return;
+            const bool zeros = has_zeros(blk - 1, j - 1);
+            if (zeros && !wait(&z_done[vs], (zn >> vs) & 1)) return;
+            if (PARTS == 1 && !wait(&p_full[t], pn[t]++ & 1)) return;
+            pv(t, blk - 1, min(CH_BLK / 16, (item_keys(it, t) - (j - 1) * CH_BLK + 15) / 16), j - 1 == it.kb0);
+            if (PARTS != 1) commit(pv_done);
+            else if (j == end[t]) commit(&o_full[t]);
+            if (t == nt - 1) {
+              if (zeros) zn ^= 1u << vs;
+              commit(&empty[vs]);
             }
+          };
+          auto do_qk = [&]() {
+            const int ks = (2 * blk) % SLOTS;
+            if (!wait(&full[ks], (2 * blk / SLOTS) & 1)) return;
+            qk(t, blk);
+            if (j == end[t] - 1) commit(&q_empty[t]);
+            if (t == nt - 1) commit(&empty[ks]);
+          };
+          if (PARTS == 1) {
+            if (has_pv) do_pv();
+            if (has_qk && ok) do_qk();
+          } else {
+            if (has_pv) wait(&p_full[t], pn[t]++ & 1);   // (S has been read, too)
+            if (has_qk && ok) do_qk();
+            if (has_pv && ok) do_pv();
           }
         }
-        n = n0 + (it.kb1 - it.kb0);
       }
-      ok = __all_sync(0xffffffffu, ok);
+      n = n0 + (it.kb1 - it.kb0);
     }
-    if (lane == 0 && *abort_flag) {   // wait for issued MMAs before shared memory goes away
-      umma_commit(drain);
-      const uint64_t t0 = globaltimer_ns();
-      while (!mbar_try_wait(drain, 0))
-        if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
+    if (*abort_flag) {   // wait for issued MMAs before shared memory goes away
+      commit(drain);
+      if (lane == 0) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(drain, 0))
+          if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
+      }
     }
     __syncwarp();
   } else if (warp >= 4 && (warp >> 2) - 1 < C::TILES) {
@@ -620,8 +656,10 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int x = 4; x < CH_BLK; ++x) mx[x & 3] = fmaxf(mx[x & 3], s[x]);
-        const float mb = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c, CH_UNSET);
+        for (int x = 4; x < CH_BLK - 4; x += 8)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[x + 2 * y], s[x + 2 * y + 1]);
+        const float mb = fmaxf(max3(max3(mx[0], s[CH_BLK - 4], s[CH_BLK - 3]), max3(mx[1], s[CH_BLK - 2], s[CH_BLK - 1]), fmaxf(mx[2], mx[3])) * c, CH_UNSET);
         // two tiles: the S that is ready was issued after block j - 1's P V; one tile: that is waited for
         if (PARTS != 1 && j > it.kb0) {
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(pv_done, vn++ & 1, abort_flag, p.err));
@@ -648,22 +686,27 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
             }
           }
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint64_t sum[2] = {0, 0};
+        const uint64_t c2 = f2_pack(c, c), m2 = f2_pack(-m, -m);
 #pragma unroll
         for (int x = 0; x < CH_BLK; x += 32) {
           uint32_t u[PARTS][16];
 #pragma unroll
           for (int y = 0; y < 16; ++y) {
-            float a = ex2(fmaf(s[x + 2 * y], c, -m)), b = ex2(fmaf(s[x + 2 * y + 1], c, -m));
-            sum[(2 * y) & 3] += a;
-            sum[(2 * y + 1) & 3] += b;
+            float a, b;
+            f2_unpack(f2_fma(f2_pack(s[x + 2 * y], s[x + 2 * y + 1]), c2, m2), a, b);
+            a = ex2(a);
+            b = ex2(b);
+            sum[y & 1] = f2_add(sum[y & 1], f2_pack(a, b));
 #pragma unroll
             for (int q = 0; q < PARTS; ++q) u[q][y] = q + 1 < PARTS ? take_bf16(a, b) : pack_bf16(a, b);
           }
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) tmem_st16(tp + 64 * q + x / 2, u[q]);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float l0, l1;
+        f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
+        l += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&p_full[t]);
@@ -754,57 +797,96 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
 }
 
 // Joins the parts of the items that several CTAs shared: item a is the one that goes on behind CTA a's stretch, its parts
-// those of a (slot 1) and of the CTAs that follow (slot 0) up to the one that ends it.  A warp for each row.
-constexpr int CM_ROWS = 8;
+// those of a (slot 1) and of the CTAs that follow (slot 0) up to the one that ends it.  A warp takes CM_ROWS rows, whose
+// loads are in flight together; the parts' references and sums are on its lanes.
+constexpr int CM_WARPS = 8, CM_ROWS = 4;
 template <int HD, bool BF16>
-__global__ void __launch_bounds__(CM_ROWS * 32) chunk_merge_kernel(const __grid_constant__ ChunkAttnParams p, int ctas, int tiles) {
+__global__ void __launch_bounds__(CM_WARPS * 32) chunk_merge_kernel(const __grid_constant__ ChunkAttnParams p, int ctas, int tiles) {
   constexpr int E = HD / 32;
   const int lane = threadIdx.x & 31;
-  const int groups = tiles * CH_BLK / CM_ROWS, a = blockIdx.x / groups, rr = blockIdx.x % groups * CM_ROWS + (threadIdx.x >> 5);
-  const int G = p.H / p.Hk, pt1 = CH_BLK / G, t = rr / CH_BLK, gi = rr % CH_BLK / G, g = rr % CH_BLK % G, i = t * pt1 + gi;
+  const int groups = tiles * CH_BLK / (CM_WARPS * CM_ROWS), a = blockIdx.x / groups;
+  const int rr0 = (blockIdx.x % groups * CM_WARPS + (threadIdx.x >> 5)) * CM_ROWS;
+  const int G = p.H / p.Hk, pt1 = CH_BLK / G;
   pdl_trigger();
   pdl_wait();
   const ChRec* recs = reinterpret_cast<const ChRec*>(p.part);
   const float2* part_ml = reinterpret_cast<const float2*>(recs + 2 * ctas);
   const float* part_o = reinterpret_cast<const float*>(part_ml + 2 * ctas * 2 * CH_BLK);
-  const int4 r4 = __ldcg(reinterpret_cast<const int4*>(recs + 2 * a + 1));
-  const ChRec r = {r4.x, r4.y, r4.z, r4.w};
-  if (gi >= pt1 || i >= r.npos) return;
+  const int4 r = __ldcg(reinterpret_cast<const int4*>(recs + 2 * a + 1));   // row0, npos, hk
+  int i[CM_ROWS];   // positions in the item, -1: no row of it
+  bool some = false;
+#pragma unroll
+  for (int y = 0; y < CM_ROWS; ++y) {
+    const int rr = rr0 + y, gi = rr % CH_BLK / G;
+    i[y] = gi < pt1 && rr / CH_BLK * pt1 + gi < r.y ? rr / CH_BLK * pt1 + gi : -1;
+    some |= i[y] >= 0;
+  }
+  if (!some) return;
   // the last of the parts' CTAs
   int last = a;
   for (int c0 = a + 1; last == a && c0 < ctas; c0 += 32) {
     const int c = c0 + lane;
-    const unsigned ends = __ballot_sync(0xffffffffu, c < ctas && __ldcg(reinterpret_cast<const int4*>(recs + 2 * c)).w);
+    const unsigned ends = __ballot_sync(0xffffffffu, c < ctas && __ldcg(reinterpret_cast<const int4*>(recs + 2 * min(c, ctas - 1))).w);
     if (ends) last = c0 + __ffs(ends) - 1;
   }
   const int n = 1 + last - a;
-  auto place = [&](int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1) * 2 * CH_BLK + rr; };
-  float m = CH_UNSET;
-  for (int k = lane; k < n; k += 32) {
-    const float2 ml = __ldcg(part_ml + place(k));
-    if (ml.y > 0.f) m = fmaxf(m, ml.x);
+  auto place = [&](int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1) * 2 * CH_BLK + rr0; };
+  float m[CM_ROWS], l[CM_ROWS], acc[CM_ROWS][E];
+#pragma unroll
+  for (int y = 0; y < CM_ROWS; ++y) {
+    m[y] = CH_UNSET;
+    l[y] = 0.f;
+#pragma unroll
+    for (int x = 0; x < E; ++x) acc[y][x] = 0.f;
+  }
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    const int here = min(32, n - k0);
+    float w[CM_ROWS];
+#pragma unroll
+    for (int y = 0; y < CM_ROWS; ++y) {
+      const float2 ml = lane < here && i[y] >= 0 ? __ldcg(part_ml + place(k0 + lane) + y) : make_float2(CH_UNSET, 0.f);
+      float top = ml.y > 0.f ? fmaxf(ml.x, m[y]) : m[y];   // (a part that saw no key of the row has a sum of 0)
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      w[y] = ml.y > 0.f ? ex2(ml.x - top) : 0.f;
+      float sum = ml.y * w[y];
+#pragma unroll
+      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float f = ex2(m[y] - top);
+      l[y] = fmaf(l[y], f, sum);
+      m[y] = top;
+#pragma unroll
+      for (int x = 0; x < E; ++x) acc[y][x] *= f;
+    }
+#pragma unroll 4
+    for (int k = 0; k < here; ++k)
+#pragma unroll
+      for (int y = 0; y < CM_ROWS; ++y) {
+        const float f = __shfl_sync(0xffffffffu, w[y], k);
+        if (f == 0.f) continue;   // (and maybe nothing was written)
+        const float* o = part_o + (place(k0 + k) + y) * HD + lane * E;
+        float v[E];
+        if (E == 4) {
+          const float4 q = __ldcg(reinterpret_cast<const float4*>(o));
+          v[0] = q.x, v[1] = q.y, v[E - 2] = q.z, v[E - 1] = q.w;
+        } else {
+          const float2 q = __ldcg(reinterpret_cast<const float2*>(o));
+          v[0] = q.x, v[1] = q.y;
+        }
+#pragma unroll
+        for (int x = 0; x < E; ++x) acc[y][x] = fmaf(v[x], f, acc[y][x]);
+      }
   }
 #pragma unroll
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float l = 0.f, acc[E];
+  for (int y = 0; y < CM_ROWS; ++y) {
+    if (i[y] < 0) continue;
+    const float inv = l[y] == 0.f ? 0.f : 1.0f / l[y];
+    const long long at = (long long)(r.x + i[y]) * p.out_ld + (r.z * G + (rr0 + y) % CH_BLK % G) * HD + lane * E;
 #pragma unroll
-  for (int x = 0; x < E; ++x) acc[x] = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < n; ++k) {
-    const float2 ml = __ldcg(part_ml + place(k));
-    if (!(ml.y > 0.f)) continue;   // (no key, and maybe nothing written)
-    const float f = ex2(ml.x - m);
-    l = fmaf(ml.y, f, l);
-    const float* o = part_o + place(k) * HD + lane * E;
-#pragma unroll
-    for (int x = 0; x < E; ++x) acc[x] = fmaf(__ldcg(o + x), f, acc[x]);
-  }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const long long at = (long long)(r.row0 + i) * p.out_ld + (r.hk * G + g) * HD + lane * E;
-#pragma unroll
-  for (int x = 0; x < E; x += 2) {
-    if (BF16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + at + x) = pack_bf16(acc[x] * inv, acc[x + 1] * inv);
-    else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at + x) = make_float2(acc[x] * inv, acc[x + 1] * inv);
+    for (int x = 0; x < E; x += 2) {
+      if (BF16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + at + x) = pack_bf16(acc[y][x] * inv, acc[y][x + 1] * inv);
+      else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at + x) = make_float2(acc[y][x] * inv, acc[y][x + 1] * inv);
+    }
   }
 }
 
@@ -839,8 +921,8 @@ static cudaError_t ch_launch(const ChunkAttnParams& p, int num_sms, cudaStream_t
   // (an item of fewer than four blocks is not split)
   if (e != cudaSuccess || ((long long)p.ld * KV_PAGE + CH_BLK - 1) / CH_BLK < 4) return e;
   constexpr int TILES = ChCfg<HD, PARTS>::TILES;
-  cfg.gridDim = dim3(num_sms * (TILES * CH_BLK / CM_ROWS));
-  cfg.blockDim = dim3(CM_ROWS * 32);
+  cfg.gridDim = dim3(num_sms * (TILES * CH_BLK / (CM_WARPS * CM_ROWS)));
+  cfg.blockDim = dim3(CM_WARPS * 32);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<HD, PARTS == 1>, p, num_sms, TILES);
 }
