@@ -3,26 +3,29 @@
 //   out = sum_t p_t v_t / sum_t p_t,  p_t = exp2(c s_t - m),  s = q K^T,  c = log2(e) / sqrt(hd)
 //
 // A tile is 128 rows: PT = 128 / G positions of the G query heads that share a cache head, so that K and V are
-// loaded once for all of them.  An item is TILES tiles of a sequence and cache head, its work the blocks of 128 keys that its
-// rows see.  The items stand in a line, weighed by their keys and a start's cost, and every CTA (one on an SM) takes an
-// equal stretch of it, wherever that begins: few rows of long sequences are split along their keys, and causal tiles of
-// unequal length leave no SM idle.  An item that several CTAs share leaves partial results (m, sum, O), which a second
-// kernel joins in order.  Sequences, lengths and pages are device values, so the plan is made on the device, by one
-// warp of each CTA (a scan over the sequences), which then hands items to the others.
+// loaded once for all of them.  An item is TILES tiles of a sequence and cache head, its work the steps of 64 keys (a page)
+// that its rows see.  The items stand in a line, weighed by their keys and a start's cost, and every CTA (one on an SM)
+// takes an equal stretch of it, wherever that begins: few rows of long sequences are split along their keys, and causal
+// tiles of unequal length leave no SM idle.  An item that several CTAs share leaves partial results (m, sum, O), which
+// a second kernel joins in order.  Sequences, lengths and pages are device values, so the plan is made on the device,
+// by one warp of each CTA (a scan over the sequences), which then hands items to the others.
 //
-// bf16 (PARTS = 1, TILES = 2): S, O of both tiles fill TMEM, P lies over its S.  While one tile's 128 threads (a row
-// each, no shuffles) work on its scores, the tensor cores run the other tile's products.
-// fp32 (PARTS = 3, TILES = 1): queries and probabilities as three bf16 parts (24 bits); P beside S, so that the next
-// block's S is computed while this one's P is made.
+// Scores have two places in TMEM, by the step's parity: S of step i + 2 is issued behind P V of step i, so that the
+// softmax (a thread for each row, no shuffles) always has the next step's scores.  The entries of the ring go by
+// what is issued together: entry e of an item is V of step e - 2 and K of step e.
+// bf16 (PARTS = 1, TILES = 2): P lies over its S; a warp for each tile issues its products (a wait, even one that is over,
+// costs such a warp 100 cycles or more, and each MMA 44).  Tensor cycles of a step: 8 x 48 (N = 64) and 4 x 64.
+// fp32 (PARTS = 3, TILES = 1): queries and probabilities as three bf16 parts (24 bits), smallest first; P beside S.  The
+// tensor cores' accumulator truncates, so O holds one step, and 4 more warps add it to a rounded total in registers.
 //
-// O is rescaled only when a row's maximum has grown by more than 2^8 since the last time (exact: the reference value
-// cancels in the division by the row's sum).
+// A row's reference m is moved only when its maximum has grown by more than 2^8 since the last time (exact: it cancels
+// in the division by the row's sum), so that O (the total) is seldom rescaled.
 //
 // Values that no row may see (behind the last key, up to the 16 keys of a product's step; pages that are not there) take
 // part with P = 0 and may hold NaN: they are made zeros in the ring before the product, by the warp that loads.
 //
-// Warps: 0 loads (TMA), 1 issues the products, 2 plans, 4-7 softmax and output of tile 0, 8-11 of tile 1, or, with one
-// tile, the next item's queries.
+// Warps: 0 loads (TMA), 1 and 3 issue the products of tile 0 and 1, 2 plans; 4-7 softmax and output of tile 0, 8-11 of
+// tile 1; with one tile 4-7 bring the queries, too, and 8-11 keep the total and write the output.
 #include <algorithm>
 
 #include "common.cuh"
@@ -31,10 +34,12 @@
 namespace sdsat {
 
 static_assert(KV_PAGE == 64, "a page is one box of keys");
-constexpr int CH_BLK = 128;           // keys of a block, rows of a tile
+constexpr int CH_ROWS = 128;          // rows of a tile
+constexpr int CH_STEP = KV_PAGE;      // keys of a step: a page
 constexpr int CH_THREADS = 384;
 constexpr int CH_DESC = 4;            // items handed out ahead
-constexpr int CH_FLAGS = 8;           // blocks whose pages' presence is kept
+constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
+constexpr int CH_PART = 4;            // steps that a part of an item has at least
 constexpr int CH_START = 192;         // what an item's start costs, in keys
 constexpr int CH_LEAST = 384;         // keys (and starts) for which a CTA is worth its while
 constexpr float CH_LAZY = 8.0f;       // log2 of the growth of a row maximum that is left unscaled
@@ -46,32 +51,38 @@ struct ChRec {
 };
 struct ChItem {
   int row0, npos, pos0, hk;           // first row, positions, slot of the first; cache head (-1: no more items)
-  int seq, kb0, kb1, slot;            // blocks; partial results' place or -1
+  int seq, kb0, kb1, slot;            // steps; partial results' place or -1
 };
 
 template <int HD, int PARTS>
 struct ChCfg {
   static constexpr int TILES = PARTS == 1 ? 2 : 1;
   static constexpr int HALVES = HD / 64;
-  static constexpr int BOX = 64 * 128;                      // one TMA box of K or V: 64 keys x 64 dims
-  static constexpr int HALF = CH_BLK * 128;                 // 128 rows x 64 dims, 128-byte swizzle
+  static constexpr int HALF = CH_ROWS * 128;                // Q: 128 rows x 64 dims, 128-byte swizzle
   static constexpr int TILE = HALVES * HALF;
-  static constexpr int SLOTS = HD == 128 ? 4 : 8;
+  static constexpr int BOX = CH_STEP * 128;                 // K or V: 64 keys x 64 dims, a TMA box
+  static constexpr int SLOT = HALVES * BOX;                 // a step's K or V
+  static constexpr int SLOTS = HD == 128 ? 4 : 8;           // entries of the ring: V, K
+  static_assert(CH_FLAGS >= SLOTS + 2, "flags outlast the loads ahead");
   static constexpr size_t OFF_RING = (size_t)TILES * PARTS * TILE;
-  static constexpr size_t OFF_BAR = OFF_RING + (size_t)SLOTS * TILE;
-  static constexpr int NBAR = 3 * SLOTS + 5 * 2 + 2 + 2 * CH_DESC;
+  static constexpr size_t OFF_BAR = OFF_RING + (size_t)SLOTS * 2 * SLOT;
+  static constexpr int NBAR = 2 * SLOTS + 21 + 2 * CH_DESC;
   static constexpr size_t OFF_ITEMS = OFF_BAR + (NBAR + 1) / 2 * 16;
   static constexpr size_t SMEM = 1024 + OFF_ITEMS + CH_DESC * sizeof(ChItem) + CH_FLAGS * 4 + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
   static_assert(OFF_RING >= (CHUNK_MAX_BATCH + 1) * 8, "the plan lies over the queries");
-  // TMEM columns
+  // TMEM columns: S and P of step i, by its parity
   static constexpr int S_COL(int t) { return 128 * t; }
   static constexpr int P_COL(int t) { return PARTS == 1 ? 128 * t : 128; }
+  static constexpr int P_STEP = PARTS == 1 ? 64 : 96;
   static constexpr int O_COL(int t) { return PARTS == 1 ? 256 + 128 * t : 320; }
+  // one tile: what the softmax tells those who keep the total; by step's parity the total's factor, by item's parity the
+  // sum and the reference
+  static constexpr int F_COL = 448, L_COL = 450, M_COL = 452;
 };
 
 size_t chunk_attention_scratch(int num_sms) {
-  return (size_t)2 * num_sms * (sizeof(ChRec) / 4 + 2 * CH_BLK * (2 + 128));
+  return (size_t)2 * num_sms * (sizeof(ChRec) / 4 + 2 * CH_ROWS * (2 + 128));
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
@@ -96,6 +107,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v)) : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+  return __uint_as_float(r);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // The products are issued by a whole warp, in step, of which one lane's instruction counts (`mine`): issued from a
@@ -128,6 +152,31 @@ __device__ __forceinline__ void ch_mma_ta(uint32_t d, uint32_t a, uint64_t b, ui
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(mine)
       : "memory");
+}
+__device__ __forceinline__ void ch_commit(uint32_t bar, uint32_t mine) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(mine)
+      : "memory");
+}
+// whether the phases of two barriers are both complete: one round trip for both
+__device__ __forceinline__ bool ch_try_both(uint32_t a, uint32_t pa, uint32_t b, uint32_t pb) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+      "and.pred p, p, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(a), "r"(pa), "r"(b), "r"(pb)
+      : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ bool ch_wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t* err) {
+  return mbar_wait_bounded(bar, parity, abort, err);
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -203,44 +252,51 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem + C::OFF_RING;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);   // [SLOTS] K or V block landed
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);   // [SLOTS] an entry landed
   uint64_t* empty = full + SLOTS;         // [SLOTS] its products are done
-  uint64_t* z_done = empty + SLOTS;       // [SLOTS] values that no row may see are zeros (of blocks that have some)
-  uint64_t* q_full = z_done + SLOTS;      // [2] per tile: Q is there
-  uint64_t* q_empty = q_full + 2;         // [2] the item's last S is complete
-  uint64_t* s_full = q_empty + 2;         // [2] S of a block is complete (and everything issued before it)
-  uint64_t* p_full = s_full + 2;          // [2] P is in TMEM, O is rescaled (128 threads)
-  uint64_t* o_full = p_full + 2;          // [2] two tiles: the item's last product is complete
-  uint64_t* pv_done = o_full + 2;         // one tile: a block's P V is complete
-  uint64_t* drain = pv_done + 1;
-  uint64_t* d_full = drain + 1;           // [CH_DESC] an item's description is there
+  uint64_t* z_full = empty + SLOTS;       // an entry landed in which values have to be made zeros
+  uint64_t* q_full = z_full + 1;          // [2] per tile: Q is there
+  uint64_t* q_empty = q_full + 2;         // [2] two tiles: the item's last S is complete
+  uint64_t* s_full = q_empty + 2;         // [2][2] per tile and entry's parity: S of its step, and P V of the one before the last, are complete
+  uint64_t* p_full = s_full + 4;          // [2][2] P is in TMEM, O is rescaled (128 threads)
+  uint64_t* pv_done = p_full + 4;         // one tile: a step's P V is complete
+  uint64_t* o_free = pv_done + 1;         // one tile: O of a step has been read (128 threads)
+  uint64_t* l_full = o_free + 1;          // [2] one tile, by item's parity: the rows' sums are there (128 threads)
+  uint64_t* l_free = l_full + 2;          // [2] ... and have been read
+  uint64_t* drain = l_free + 2;           // [2]
+  uint64_t* d_full = drain + 2;           // [CH_DESC] an item's description is there
   uint64_t* d_empty = d_full + CH_DESC;   // [CH_DESC] all have read it
   ChItem* items = reinterpret_cast<ChItem*>(smem + C::OFF_ITEMS);
-  uint32_t* flags = reinterpret_cast<uint32_t*>(items + CH_DESC);   // [CH_FLAGS] by block: which of its two pages there are
+  uint32_t* flags = reinterpret_cast<uint32_t*>(items + CH_DESC);   // [CH_FLAGS] by entry: whether there is the page of its K
   uint32_t* tmem_slot = flags + CH_FLAGS;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   long long* plan = reinterpret_cast<long long*>(smem);             // [b + 1] cost before each sequence
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int G = p.H / p.Hk, pt1 = CH_BLK / G, pt = C::TILES * pt1, cap = p.ld * KV_PAGE;
+  const int G = p.H / p.Hk, pt1 = CH_ROWS / G, pt = C::TILES * pt1, cap = p.ld * KV_PAGE;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
-      mbar_init(&z_done[s], 1);
+      mbar_init(&empty[s], C::TILES);
     }
+    mbar_init(z_full, 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&q_full[t], PARTS == 1 ? 1 : 128);
       mbar_init(&q_empty[t], 1);
-      mbar_init(&s_full[t], 1);
-      mbar_init(&p_full[t], 128);
-      mbar_init(&o_full[t], 1);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&s_full[2 * t + b], 1);
+        mbar_init(&p_full[2 * t + b], 128);
+      }
+      mbar_init(&l_full[t], 128);
+      mbar_init(&l_free[t], 128);
     }
     mbar_init(pv_done, 1);
+    mbar_init(o_free, 128);
     mbar_init(drain, 1);
+    mbar_init(drain + 1, 1);
     for (int i = 0; i < CH_DESC; ++i) {
       mbar_init(&d_full[i], 1);
-      mbar_init(&d_empty[i], 10);
+      mbar_init(&d_empty[i], 9 + C::TILES);
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -258,17 +314,17 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
 
   ChRec* recs = reinterpret_cast<ChRec*>(p.part);                             // [2 ctas]
   float2* part_ml = reinterpret_cast<float2*>(recs + 2 * gridDim.x);          // [2 ctas][256]
-  float* part_o = reinterpret_cast<float*>(part_ml + 2 * gridDim.x * 2 * CH_BLK);   // [2 ctas][256][HD]
+  float* part_o = reinterpret_cast<float*>(part_ml + 2 * gridDim.x * 2 * CH_ROWS);   // [2 ctas][256][HD]
 
   // an item's geometry
   auto item_keys = [&](const ChItem& it, int t) { return (int)min((long long)cap, (long long)it.pos0 + min(it.npos, (t + 1) * pt1)); };
   auto item_tiles = [&](const ChItem& it) { return C::TILES == 2 && it.npos > pt1 ? 2 : 1; };
-  // blocks of tile t up to which this part goes
-  auto item_end = [&](const ChItem& it, int t) { return min(it.kb1, (item_keys(it, t) + CH_BLK - 1) / CH_BLK); };
-  // the last tile's block has values behind its last key in a step of 16
+  // the step up to which this part of tile t goes
+  auto item_end = [&](const ChItem& it, int t) { return min(it.kb1, (item_keys(it, t) + CH_STEP - 1) / CH_STEP); };
+  // the last tile's step j has values behind its last key in 16 of a product
   auto item_tail = [&](const ChItem& it, int j) {
     const int k = item_keys(it, item_tiles(it) - 1);
-    return k % 16 != 0 && j == k / CH_BLK;
+    return k % 16 != 0 && j == k / CH_STEP;
   };
   uint32_t d_phase = 0;   // items read
   auto next_item = [&](ChItem& it) {   // by a warp
@@ -354,11 +410,10 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         else hi = mid;
       }
       a.t = lo;
-      // parts of at least two blocks
-      const int blocks = (ch_keys(q, pt, cap, a.t) + CH_BLK - 1) / CH_BLK;
-      const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + CH_BLK / 2) / CH_BLK;
-      a.kb = kb < 2 ? 0 : (int)kb;
-      if (a.kb > blocks - 2 && a.kb > 0) a = after(a, q);
+      const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
+      const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + CH_STEP / 2) / CH_STEP;
+      a.kb = kb < CH_PART ? 0 : (int)kb;
+      if (a.kb > steps - CH_PART && a.kb > 0) a = after(a, q);
       return a;
     };
     const ChRec none = {0, 0, 0, 0};
@@ -379,7 +434,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       bool stop = true;
       if (more) {
         q = ch_sequence(p, a.s);
-        const int blocks = (ch_keys(q, pt, cap, a.t) + CH_BLK - 1) / CH_BLK;
+        const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
         it.row0 = q.first + a.t * pt;
         it.npos = min(pt, q.n - a.t * pt);
         it.pos0 = q.len + a.t * pt;
@@ -387,11 +442,11 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         it.seq = a.s;
         it.kb0 = a.kb;
         stop = a.s == end.s && a.hk == end.hk && a.t == end.t;
-        it.kb1 = stop ? end.kb : blocks;
+        it.kb1 = stop ? end.kb : steps;
         if (it.kb0 > 0) {
           it.slot = 2 * cta;
-          left = ChRec{it.row0, it.npos, it.hk, it.kb1 == blocks};
-        } else if (it.kb1 < blocks) {
+          left = ChRec{it.row0, it.npos, it.hk, it.kb1 == steps};
+        } else if (it.kb1 < steps) {
           it.slot = 2 * cta + 1;
           right = ChRec{it.row0, it.npos, it.hk, 0};
         }
@@ -415,25 +470,24 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   } else if (warp == 0) {
     // ---- loads
     const uint64_t pol = l2_policy_evict_normal();
-    uint32_t n = 0, qn[2] = {0, 0};   // ring entries used, Q tiles loaded
+    uint32_t n = 0, qn[2] = {0, 0}, zn = 0;   // entries, Q tiles loaded, entries with zeros
     bool ok = true;
-    // a block whose values wait to be made zeros
-    int z_slot = -1, z_there = 0;
-    uint32_t z_parity = 0, z_pages = 3;
+    // the entry whose values wait to be made zeros, keys z_from .. z_to - 1 of its V
+    int z_slot = -1, z_from = 0, z_to = 0;
     auto make_zeros = [&]() {
       if (z_slot < 0) return;
-      if (mbar_wait_bounded(&full[z_slot], z_parity, abort_flag, p.err)) {
+      if (mbar_wait_bounded(z_full, zn & 1, abort_flag, p.err)) {
         constexpr int CHUNKS = HD / 8;   // of 16 bytes, of a key
-        for (int z = lane; z < (z_there + 15) / 16 * 16 * CHUNKS; z += 32) {
+        for (int z = z_from * CHUNKS + lane; z < z_to * CHUNKS; z += 32) {
           const int at = z / CHUNKS, i = z % CHUNKS;
-          if (at >= z_there || !((z_pages >> (at / KV_PAGE)) & 1u))
-            *reinterpret_cast<uint4*>(ring + (size_t)z_slot * C::TILE + (i >> 3) * C::HALF + at * 128 + (((i & 7) ^ (at & 7)) << 4)) =
-                make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(ring + (size_t)z_slot * 2 * C::SLOT + (i >> 3) * C::BOX + at * 128 + (((i & 7) ^ (at & 7)) << 4)) =
+              make_uint4(0u, 0u, 0u, 0u);
         }
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&z_done[z_slot]);
+      if (lane == 0) mbar_arrive(&full[z_slot]);
+      ++zn;
       z_slot = -1;
     };
     // (values that a product waits for are made zeros before anything waits for that product)
@@ -461,44 +515,41 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
           }
         }
       }
-      // the pages of 16 blocks at a time, the next ones asked for ahead
+      // 32 pages at a time, the next ones asked for ahead
       const int* row = p.table + (size_t)it.seq * p.ld;
-      auto pages = [&](int j) { return 2 * j + lane < p.ld ? __ldcg(row + 2 * j + lane) : -1; };
-      int now = pages(it.kb0), next = pages(it.kb0 + 16), base = it.kb0;
-      for (int j = it.kb0; j < it.kb1 && ok; ++j) {
-        if (j == base + 16) base = j, now = next, next = pages(j + 16);
-        int page[2];
-        uint32_t there = 0, load = 0;
-        for (int b = 0; b < 2; ++b) {
-          page[b] = __shfl_sync(0xffffffffu, now, 2 * (j - base) + b);
-          const bool wanted = j * CH_BLK + b * KV_PAGE < keys, in = page[b] >= 0 && page[b] < p.n_pages;
-          if (wanted && in) load |= 1u << b;
-          if (!wanted || in) there |= 1u << b;
-          else if (lane == 0) set_error(p.err, ERR_PAGE);
-        }
-        const uint32_t bytes = __popc(load) * C::HALVES * C::BOX;
-        for (int which = 0; which < 2; ++which, ++n) {
-          const int s = n % SLOTS;
-          if (!acquire(&empty[s], ((n / SLOTS) & 1) ^ 1)) break;
-          if (lane == 0) {
-            if (which == 0) flags[(n / 2) % CH_FLAGS] = there;
-            mbar_arrive_expect_tx(&full[s], bytes);
-            for (int b = 0; b < 2; ++b)
-              if ((load >> b) & 1u)
-                for (int hh = 0; hh < C::HALVES; ++hh)
-                  tma_load_2d(ring + (size_t)s * C::TILE + hh * C::HALF + b * C::BOX, which ? &p.vmap : &p.kmap, &full[s], hh * 64,
-                              (page[b] * p.Hk + it.hk) * KV_PAGE, pol);
-          }
-          __syncwarp();
-        }
-        if (!ok) break;
-        if (there != 3u || item_tail(it, j)) {
+      auto pages = [&](int j) { return j + lane < p.ld ? __ldcg(row + j + lane) : -1; };
+      int now = pages(it.kb0), next = pages(it.kb0 + 32), base = it.kb0;
+      int before[2] = {0, 0};   // the pages of the last two steps
+      for (int j = it.kb0; j < it.kb1 + 2 && ok; ++j, ++n) {   // K of step j, V of step j - 2
+        if (j == base + 32) base = j, now = next, next = pages(j + 32);
+        const int page = __shfl_sync(0xffffffffu, now, j - base), v_page = before[0];
+        const bool has_k = j < it.kb1, has_v = j >= it.kb0 + 2;
+        const bool k_there = has_k && page >= 0 && page < p.n_pages, v_there = has_v && v_page >= 0 && v_page < p.n_pages;
+        before[0] = before[1];
+        before[1] = page;
+        const int s = n % SLOTS;
+        if (!acquire(&empty[s], ((n / SLOTS) & 1) ^ 1)) break;
+        const bool zeros = has_v && (!v_there || item_tail(it, j - 2));
+        if (zeros) {
           make_zeros();   // (one at a time)
-          z_slot = (n - 1) % SLOTS;
-          z_parity = ((n - 1) / SLOTS) & 1;
-          z_there = min(CH_BLK, keys - j * CH_BLK);
-          z_pages = there;
+          const int seen = min(CH_STEP, keys - (j - 2) * CH_STEP);
+          z_slot = s;
+          z_from = v_there ? seen : 0;
+          z_to = (seen + 15) / 16 * 16;
         }
+        if (lane == 0) {
+          uint64_t* bar = zeros ? z_full : &full[s];
+          flags[n % CH_FLAGS] = k_there;
+          if (has_k && !k_there) set_error(p.err, ERR_PAGE);
+          mbar_arrive_expect_tx(bar, (k_there ? C::SLOT : 0) + (v_there ? C::SLOT : 0));
+          uint8_t* at = ring + (size_t)s * 2 * C::SLOT;
+#pragma unroll
+          for (int hh = 0; hh < C::HALVES; ++hh) {
+            if (v_there) tma_load_2d(at + hh * C::BOX, &p.vmap, bar, hh * 64, (v_page * p.Hk + it.hk) * KV_PAGE, pol);
+            if (k_there) tma_load_2d(at + C::SLOT + hh * C::BOX, &p.kmap, bar, hh * 64, (page * p.Hk + it.hk) * KV_PAGE, pol);
+          }
+        }
+        __syncwarp();
       }
     }
     make_zeros();
@@ -511,280 +562,316 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       if (PARTS == 1)
         for (int t = 0; t < 2; ++t)
           if (qn[t]) land(&q_full[t], (qn[t] - 1) & 1);
+      if (zn) land(z_full, (zn - 1) & 1);
       for (uint32_t i = n > SLOTS ? n - SLOTS : 0; i < n; ++i) land(&full[i % SLOTS], (i / SLOTS) & 1);
     }
-  } else if (warp == 1) {
-    // ---- products
-    constexpr uint32_t idesc_s = idesc_bf16_f32(128, CH_BLK);
+  } else if (warp == 1 || (warp == 3 && C::TILES == 2)) {
+    // ---- products of a tile
+    const int t = warp >> 1;
+    constexpr uint32_t idesc_s = idesc_bf16_f32(128, CH_STEP);
     constexpr uint32_t idesc_o = idesc_bf16_f32(128, HD) | (1u << 16);   // B is MN-major
     const uint32_t mine = ch_elect();
-    const uint64_t q_desc = sdesc_sw128(smem_u32(smem)), k_desc = sdesc_sw128(smem_u32(ring)), v_desc = sdesc_sw128_mn(smem_u32(ring), C::HALF);
+    const uint64_t q_desc = sdesc_sw128(smem_u32(smem)) + (uint64_t)(PARTS * t) * (C::TILE >> 4);
+    const uint64_t v_desc = sdesc_sw128_mn(smem_u32(ring), C::BOX), k_desc = sdesc_sw128(smem_u32(ring) + C::SLOT);
+    const uint32_t ts = tmem + C::S_COL(t), tp = tmem + C::P_COL(t), to = tmem + C::O_COL(t);
     bool ok = true;
-    uint32_t n = 0, qn[2] = {0, 0}, pn[2] = {0, 0}, zn = 0;   // blocks; per tile: Q tiles, P's; z_done phases (bits)
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
+    uint32_t n = 0, x = 0, qn = 0, pn = 0;   // entries of the ring and of the tile, Q tiles, P's
+    const uint32_t full_at = smem_u32(full), empty_at = smem_u32(empty), s_at = smem_u32(s_full + 2 * t), p_at = smem_u32(p_full + 2 * t),
+                   qe_at = smem_u32(q_empty + t), pv_at = smem_u32(pv_done);
+    auto wait = [&](uint64_t* bar, uint32_t parity) {   // (the lanes agree before the products)
+      ok = ok && mbar_wait_bounded(bar, parity, abort_flag, p.err);
+    };
+    auto agree = [&]() {
+      ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       return ok;
     };
-    auto commit = [&](uint64_t* bar) {
-      if (mine) umma_commit(bar);
-      __syncwarp();
-    };
-    auto qk = [&](int t, uint32_t blk) {
-      const uint64_t k = k_desc + (uint64_t)((2 * blk) % SLOTS) * (C::TILE >> 4), q = q_desc + (uint64_t)(PARTS * t) * (C::TILE >> 4);
-#pragma unroll 1
-      for (int part = PARTS - 1; part >= 0; --part)   // (small ones first: the sums round less)
-#pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t o = (kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2;
-          ch_mma(tmem + C::S_COL(t), q + part * (C::TILE >> 4) + o, k + o, idesc_s, part < PARTS - 1 || kk ? 1u : 0u, mine);
-        }
-      commit(&s_full[t]);
-    };
-    auto pv = [&](int t, uint32_t blk, int steps, bool first) {
-      const uint64_t v = v_desc + (uint64_t)((2 * blk + 1) % SLOTS) * (C::TILE >> 4);
-#pragma unroll 1
-      for (int part = PARTS - 1; part >= 0; --part) {
-        const uint32_t a = tmem + C::P_COL(t) + part * 64;
-        const uint32_t acc = !first || part < PARTS - 1 ? 1u : 0u;
-        if (steps == CH_BLK / 16) {
-#pragma unroll
-          for (int kk = 0; kk < CH_BLK / 16; ++kk) ch_mma_ta(tmem + C::O_COL(t), a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
-        } else {
-#pragma unroll 1
-          for (int kk = 0; kk < steps; ++kk) ch_mma_ta(tmem + C::O_COL(t), a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
-        }
-      }
-    };
     ChItem it;
     while (ok && next_item(it)) {
-      const int nt = item_tiles(it);
-      const int end[2] = {item_end(it, 0), item_end(it, nt - 1)};
-#pragma unroll
-      for (int t = 0; t < C::TILES; ++t)
-        if (t < nt && end[t] > it.kb0) wait(&q_full[t], qn[t]++ & 1);
-      const uint32_t n0 = n;   // block kb0 is the ring's n0-th
-      auto has_zeros = [&](uint32_t blk, int j) { return flags[blk % CH_FLAGS] != 3u || item_tail(it, j); };
-      // step j: per tile, block j - 1's P V and then block j's S over the P that it has read (one tile: block j's S, into a
-      // place of its own, and then block j - 1's P V); the last tile has every block, so its products release V of block
-      // j - 1 and K of block j
+      const int nt = item_tiles(it), keys = item_keys(it, t) - it.kb0 * CH_STEP, all = it.kb1 - it.kb0 + 2;
+      const int steps = t < nt ? max(0, item_end(it, t) - it.kb0) : 0, mine_too = steps ? steps + 2 : 0;
+      if (steps) wait(&q_full[t], qn++ & 1);
+      // entry e: P V of step e - 2, then S of step e over the scores that it has used
 #pragma unroll 1
-      for (int j = it.kb0; j <= it.kb1 && ok; ++j) {
-        const uint32_t blk = n0 + (j - it.kb0);
-#pragma unroll
-        for (int t = 0; t < C::TILES; ++t) {
-          if (t >= nt) break;
-          const bool has_pv = j > it.kb0 && j <= end[t], has_qk = j < end[t];
-          auto do_pv = [&]() {
-            const int vs = (2 * blk - 1) % SLOTS;
-            if (!wait(&full[vs], ((2 * blk - 1) / SLOTS) & 1)) return;
-            const bool zeros = has_zeros(blk - 1, j - 1);
-            if (zeros && !wait(&z_done[vs], (zn >> vs) & 1)) return;
-            if (PARTS == 1 && !wait(&p_full[t], pn[t]++ & 1)) return;
-            pv(t, blk - 1, min(CH_BLK / 16, (item_keys(it, t) - (j - 1) * CH_BLK + 15) / 16), j - 1 == it.kb0);
-            if (PARTS != 1) commit(pv_done);
-            else if (j == end[t]) commit(&o_full[t]);
-            if (t == nt - 1) {
-              if (zeros) zn ^= 1u << vs;
-              commit(&empty[vs]);
-            }
-          };
-          auto do_qk = [&]() {
-            const int ks = (2 * blk) % SLOTS;
-            if (!wait(&full[ks], (2 * blk / SLOTS) & 1)) return;
-            qk(t, blk);
-            if (j == end[t] - 1) commit(&q_empty[t]);
-            if (t == nt - 1) commit(&empty[ks]);
-          };
-          if (PARTS == 1) {
-            if (has_pv) do_pv();
-            if (has_qk && ok) do_qk();
-          } else {
-            if (has_pv) wait(&p_full[t], pn[t]++ & 1);   // (S has been read, too)
-            if (has_qk && ok) do_qk();
-            if (has_pv && ok) do_pv();
-          }
+      for (int e = 0; e < mine_too; ++e, ++n, ++x) {
+        const uint32_t s = n % SLOTS, b = x & 1, full_parity = (n / SLOTS) & 1;
+        bool ready;
+        if (e >= 2) {
+          ready = ch_try_both(full_at + 8 * s, full_parity, p_at + 8 * (pn & 1), (pn >> 1) & 1);
+          if (PARTS != 1 && pn > 0) ready = ready && mbar_try_wait(o_free, (pn - 1) & 1);
+        } else {
+          ready = mbar_try_wait(&full[s], full_parity);
         }
+        if (!__all_sync(0xffffffffu, ready && ok)) {
+          ok = ok && ch_wait_slow(&full[s], full_parity, abort_flag, p.err);
+          if (e >= 2) {
+            if (PARTS != 1 && pn > 0) ok = ok && ch_wait_slow(o_free, (pn - 1) & 1, abort_flag, p.err);
+            ok = ok && ch_wait_slow(&p_full[2 * t + (pn & 1)], (pn >> 1) & 1, abort_flag, p.err);
+          }
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        }
+        tc_fence_after();
+        if (e >= 2) {
+          ++pn;
+          const uint64_t v = v_desc + s * (2 * C::SLOT >> 4);
+          const int sixteens = min(4, (keys - (e - 2) * CH_STEP + 15) / 16);
+#pragma unroll 1
+          for (int part = PARTS - 1; part >= 0; --part) {
+            const uint32_t a = tp + C::P_STEP * b + part * 32, acc = (PARTS == 1 && e > 2) || part < PARTS - 1 ? 1u : 0u;   // (else over O's old values)
+            if (sixteens == 4) {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) ch_mma_ta(to, a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
+            } else {
+#pragma unroll 1
+              for (int kk = 0; kk < sixteens; ++kk) ch_mma_ta(to, a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
+            }
+          }
+          if (PARTS != 1) ch_commit(pv_at, mine);
+        }
+        if (e < steps) {
+          const uint64_t k = k_desc + s * (2 * C::SLOT >> 4);
+#pragma unroll 1
+          for (int part = PARTS - 1; part >= 0; --part)   // (small ones first: the sums round less)
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk)
+              ch_mma(ts + CH_STEP * b, q_desc + part * (C::TILE >> 4) + (kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2,
+                     k + (kk >> 2) * (C::BOX >> 4) + (kk & 3) * 2, idesc_s, part < PARTS - 1 || kk ? 1u : 0u, mine);
+        }
+        ch_commit(s_at + 8 * b, mine);
+        ch_commit(empty_at + 8 * s, mine);
+        if (PARTS == 1 && e == steps - 1) ch_commit(qe_at, mine);
       }
-      n = n0 + (it.kb1 - it.kb0);
+      // the entries that only the other tile uses
+#pragma unroll 1
+      for (int e = mine_too; e < all && ok; ++e, ++n) {
+        wait(&full[n % SLOTS], (n / SLOTS) & 1);
+        if (!agree()) break;
+        if (lane == 0) mbar_arrive(&empty[n % SLOTS]);
+      }
     }
     if (*abort_flag) {   // wait for issued MMAs before shared memory goes away
-      commit(drain);
+      if (mine) umma_commit(&drain[t]);
+      __syncwarp();
       if (lane == 0) {
         const uint64_t t0 = globaltimer_ns();
-        while (!mbar_try_wait(drain, 0))
+        while (!mbar_try_wait(&drain[t], 0))
           if (globaltimer_ns() - t0 > WAIT_LIMIT_NS) break;
       }
     }
     __syncwarp();
   } else if (warp >= 4 && (warp >> 2) - 1 < C::TILES) {
-    // ---- softmax and output: a thread for each row
+    // ---- softmax (and output, or queries): a thread for each row
     const int t = (warp >> 2) - 1, e = warp & 3, rr = e * 32 + lane, gi = rr / G, g = rr % G;
-    const uint32_t lane_off = (uint32_t)(e * 32) << 16;
-    const uint32_t ts = tmem + lane_off + C::S_COL(t), tp = tmem + lane_off + C::P_COL(t), to = tmem + lane_off + C::O_COL(t);
+    const uint32_t tl = tmem + ((uint32_t)(e * 32) << 16), ts = tl + C::S_COL(t), tp = tl + C::P_COL(t), to = tl + C::O_COL(t);
     const float c = rsqrtf((float)HD) * 1.4426950408889634f;
-    uint32_t sn = 0, on = 0, vn = 0;   // S's read, items done, P V's waited for
-    uint32_t bn = 0;                   // blocks of the items before (for flags)
+    const uint64_t c2 = f2_pack(c, c);
+    uint32_t bn = 0, x = 0, pn = 0, in = 0;   // entries of the ring and of the tile, P's, items
+    float m, l;                        // reference exponent (log2) and the row's sum relative to it
+    // largest of 64 scores, as an exponent
+    auto top = [&](const float (&s)[64]) {
+      float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+      for (int x = 4; x < 60; x += 8)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[x + 2 * y], s[x + 2 * y + 1]);
+      return fmaxf(max3(max3(mx[0], s[60], s[61]), max3(mx[1], s[62], s[63]), fmaxf(mx[2], mx[3])) * c, CH_UNSET);
+    };
+    // keys that the row does not see; last: of the 64
+    auto hide = [&](float (&s)[64], int last) {
+#pragma unroll
+      for (int x = 0; x < 64; ++x)
+        if (x >= last) s[x] = -INFINITY;
+    };
+    // P of a step, and its share of the sum
+    auto probabilities = [&](const float (&s)[64], uint32_t at) {
+      uint64_t sum[2] = {0, 0};
+      const uint64_t m2 = f2_pack(-m, -m);
+      constexpr int STEP = PARTS == 1 ? 32 : 16;
+#pragma unroll
+      for (int x = 0; x < 64; x += STEP) {
+        uint32_t u[PARTS][STEP / 2];
+#pragma unroll
+        for (int y = 0; y < STEP / 2; ++y) {
+          float a, b;
+          f2_unpack(f2_fma(f2_pack(s[x + 2 * y], s[x + 2 * y + 1]), c2, m2), a, b);
+          a = ex2(a);
+          b = ex2(b);
+          sum[y & 1] = f2_add(sum[y & 1], f2_pack(a, b));
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) u[q][y] = q + 1 < PARTS ? take_bf16(a, b) : pack_bf16(a, b);
+        }
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+          if constexpr (PARTS == 1) tmem_st16(at + x / 2, u[q]);
+          else tmem_st8(at + 32 * q + x / 2, u[q]);
+        }
+      }
+      float l0, l1;
+      f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
+      l += l0 + l1;
+    };
+    auto rescale = [&](float f) {
+#pragma unroll 1
+      for (int x = 0; x < HD; x += 16) {
+        float o[16];
+        uint32_t u[16];
+        tmem_ld16(to + x, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int y = 0; y < 16; ++y) u[y] = __float_as_uint(o[y] * f);
+        tmem_st16(to + x, u);
+      }
+    };
     ChItem it;
     bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
+      tc_fence_after();
+      return ok;
+    };
     while (ok && next_item(it)) {
       const int i = t * pt1 + gi;                              // this row's position in the item
       const bool mine = gi < pt1 && i < it.npos;
       const int lim = mine ? (int)min((long long)cap, (long long)it.pos0 + i + 1) : 0x7FFFFFFF;   // keys that it sees
       const int least = __reduce_min_sync(0xffffffffu, lim);
       const int end = item_tiles(it) > t ? item_end(it, t) : 0;
-      float m = CH_UNSET, l = 0.f;   // reference exponent (log2) and the row's sum relative to it
-      for (int j = it.kb0; j < end; ++j) {
-        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[t], sn++ & 1, abort_flag, p.err));
-        if (!ok) break;
-        tc_fence_after();
-        float s[CH_BLK];
+      if (PARTS != 1) {   // the row's query (the last item's S have all been read here)
+        const float* src = static_cast<const float*>(p.q) + (long long)(it.row0 + gi) * p.q_ld + (it.hk * G + g) * HD;
+#pragma unroll 4
+        for (int x = 0; x < HD; x += 8) {
+          float4 f[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+          if (mine) {
+            f[0] = __ldcg(reinterpret_cast<const float4*>(src + x));
+            f[1] = __ldcg(reinterpret_cast<const float4*>(src + x + 4));
+          }
 #pragma unroll
-        for (int x = 0; x < 4; ++x) tmem_ld32(ts + 32 * x, s + 32 * x);
-        tmem_wait_ld();
-        if ((j + 1) * CH_BLK > least) {
-          const int last = lim - j * CH_BLK;
-#pragma unroll
-          for (int x = 0; x < CH_BLK; ++x)
-            if (x >= last) s[x] = -INFINITY;
+          for (int q = 0; q < PARTS; ++q) {
+            const uint4 u = make_uint4(take_bf16(f[0].x, f[0].y), take_bf16(f[0].z, f[0].w), take_bf16(f[1].x, f[1].y), take_bf16(f[1].z, f[1].w));
+            *reinterpret_cast<uint4*>(smem + (size_t)q * C::TILE + (x >> 6) * C::HALF + rr * 128 + ((((x >> 3) & 7) ^ (rr & 7)) << 4)) = u;
+          }
         }
-        const uint32_t there = flags[(bn + (j - it.kb0)) % CH_FLAGS];
-        if (there != 3u) {   // keys without a page are not attended to
-#pragma unroll
-          for (int x = 0; x < CH_BLK; ++x)
-            if (!((there >> (x / KV_PAGE)) & 1u)) s[x] = -INFINITY;
-        }
-        float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-        for (int x = 4; x < CH_BLK - 4; x += 8)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], s[x + 2 * y], s[x + 2 * y + 1]);
-        const float mb = fmaxf(max3(max3(mx[0], s[CH_BLK - 4], s[CH_BLK - 3]), max3(mx[1], s[CH_BLK - 2], s[CH_BLK - 1]), fmaxf(mx[2], mx[3])) * c, CH_UNSET);
-        // two tiles: the S that is ready was issued after block j - 1's P V; one tile: that is waited for
-        if (PARTS != 1 && j > it.kb0) {
-          ok = __all_sync(0xffffffffu, mbar_wait_bounded(pv_done, vn++ & 1, abort_flag, p.err));
-          if (!ok) break;
-          tc_fence_after();
-        }
-        if (j == it.kb0) {
-          m = mb;
-        } else {
-          const bool grow = mb > m + CH_LAZY;
-          if (__any_sync(0xffffffffu, grow)) {
-            const float f = grow ? ex2(m - mb) : 1.f;
-            l *= f;
-            if (grow) m = mb;
+        fence_proxy_async_smem();
+        mbar_arrive(q_full);
+      }
+      m = CH_UNSET, l = 0.f;
 #pragma unroll 1
-            for (int x = 0; x < HD; x += 16) {
-              float o[16];
-              uint32_t u[16];
-              tmem_ld16(to + x, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int y = 0; y < 16; ++y) u[y] = __float_as_uint(o[y] * f);
-              tmem_st16(to + x, u);
-            }
+      for (int j = it.kb0; j < end; ++j, ++x, ++pn) {
+        if (!wait(&s_full[2 * t + (x & 1)], (x >> 1) & 1)) break;
+        const bool there = flags[(bn + (j - it.kb0)) % CH_FLAGS];   // (keys without a page are not attended to)
+        float s[CH_STEP];
+        tmem_ld32(ts + CH_STEP * (x & 1), s);
+        tmem_ld32(ts + CH_STEP * (x & 1) + 32, s + 32);
+        tmem_wait_ld();
+        if ((j + 1) * CH_STEP > least || !there) hide(s, there ? lim - j * CH_STEP : 0);
+        const float mb = top(s);
+        const bool grow = mb > m + CH_LAZY;
+        float f = 1.f;
+        if (__any_sync(0xffffffffu, grow)) {
+          if (grow) f = ex2(m - mb), m = mb;
+          l *= f;
+          if (PARTS == 1 && j > it.kb0) {   // O of the steps before: the last P V came with the next entry
+            if (!wait(&s_full[2 * t + ((x + 1) & 1)], ((x + 1) >> 1) & 1)) break;
+            rescale(f);
           }
         }
-        uint64_t sum[2] = {0, 0};
-        const uint64_t c2 = f2_pack(c, c), m2 = f2_pack(-m, -m);
-#pragma unroll
-        for (int x = 0; x < CH_BLK; x += 32) {
-          uint32_t u[PARTS][16];
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            float a, b;
-            f2_unpack(f2_fma(f2_pack(s[x + 2 * y], s[x + 2 * y + 1]), c2, m2), a, b);
-            a = ex2(a);
-            b = ex2(b);
-            sum[y & 1] = f2_add(sum[y & 1], f2_pack(a, b));
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) u[q][y] = q + 1 < PARTS ? take_bf16(a, b) : pack_bf16(a, b);
-          }
-#pragma unroll
-          for (int q = 0; q < PARTS; ++q) tmem_st16(tp + 64 * q + x / 2, u[q]);
-        }
-        float l0, l1;
-        f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
-        l += l0 + l1;
+        if (PARTS != 1) tmem_st1(tl + C::F_COL + (pn & 1), f);   // what the total is multiplied by first
+        // (over S, or in P's place of two steps ago: its P V came with this entry)
+        probabilities(s, tp + C::P_STEP * (x & 1));
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&p_full[t]);
+        mbar_arrive(&p_full[2 * t + (pn & 1)]);
       }
-      bn += it.kb1 - it.kb0;
+      if (end > it.kb0) {   // the last two P V's
+        for (int y = 0; y < 2; ++y, ++x) wait(&s_full[2 * t + (x & 1)], (x >> 1) & 1);
+      }
+      bn += it.kb1 - it.kb0 + 2;
       if (!ok) break;
-      if (end > it.kb0) {
-        ok = __all_sync(0xffffffffu, PARTS == 1 ? mbar_wait_bounded(&o_full[t], on++ & 1, abort_flag, p.err)
-                                                : mbar_wait_bounded(pv_done, vn++ & 1, abort_flag, p.err));
-        if (!ok) break;
-        tc_fence_after();
-      }
-      if (it.slot >= 0) {
-        const size_t at = (size_t)it.slot * 2 * CH_BLK + t * CH_BLK + rr;
-        if (mine) part_ml[at] = make_float2(m, l);
+      if constexpr (PARTS != 1) {   // the sums and the reference, to those who write
+        const int b = in & 1;
+        if (!wait(&l_free[b], ((in >> 1) & 1) ^ 1)) break;
+        tmem_st1(tl + C::L_COL + b, l);
+        tmem_st1(tl + C::M_COL + b, m);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&l_full[b]);
+        ++in;
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
+        const size_t part = (size_t)it.slot * 2 * CH_ROWS + t * CH_ROWS + rr;
+        const long long at = (long long)(it.row0 + i) * p.out_ld + (it.hk * G + g) * HD;
+        if (it.slot >= 0 && mine) part_ml[part] = make_float2(m, l);
         if (end > it.kb0) {
 #pragma unroll 1
           for (int x = 0; x < HD; x += 16) {
             float o[16];
             tmem_ld16(to + x, o);
             tmem_wait_ld();
-            if (mine)
+            if (mine && it.slot >= 0) {
 #pragma unroll
-              for (int y = 0; y < 16; y += 4) *reinterpret_cast<float4*>(part_o + at * HD + x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
-          }
-        }
-      } else if (end > it.kb0) {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
-        const long long at = (long long)(it.row0 + i) * p.out_ld + (it.hk * G + g) * HD;
-#pragma unroll 1
-        for (int x = 0; x < HD; x += 16) {
-          float o[16];
-          tmem_ld16(to + x, o);
-          tmem_wait_ld();
-          if (mine) {
-            if (PARTS == 1) {
+              for (int y = 0; y < 16; y += 4)
+                *reinterpret_cast<float4*>(part_o + part * HD + x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            } else if (mine) {
               uint32_t u[8];
 #pragma unroll
               for (int y = 0; y < 8; ++y) u[y] = pack_bf16(o[2 * y] * inv, o[2 * y + 1] * inv);
               uint4* d = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + at + x);
               d[0] = make_uint4(u[0], u[1], u[2], u[3]);
               d[1] = make_uint4(u[4], u[5], u[6], u[7]);
-            } else {
-#pragma unroll
-              for (int y = 0; y < 16; y += 4)
-                *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at + x + y) =
-                    make_float4(o[y] * inv, o[y + 1] * inv, o[y + 2] * inv, o[y + 3] * inv);
             }
           }
         }
+        tc_fence_before();   // (O is read: the next item's products may overwrite it once its P has come)
       }
-      tc_fence_before();   // (O is read: the next item's products may overwrite it once its P has come)
     }
   } else if (PARTS != 1 && warp >= 8) {
-    // ---- queries in three parts: a thread for each row
-    const int rr = (int)threadIdx.x - 256, gi = rr / G, g = rr % G;
-    uint32_t qn = 0;
+    // ---- one tile: the total of O and the output, a thread for each row
+    const int e = warp & 3, rr = e * 32 + lane, gi = rr / G, g = rr % G;
+    const uint32_t tl = tmem + ((uint32_t)(e * 32) << 16), to = tl + C::O_COL(0);
+    uint32_t pn = 0, in = 0;   // steps, items
     ChItem it;
-    while (next_item(it)) {
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
+      tc_fence_after();
+      return ok;
+    };
+    while (ok && next_item(it)) {
       const bool mine = gi < pt1 && gi < it.npos;
-      const float* src = static_cast<const float*>(p.q) + (long long)(it.row0 + gi) * p.q_ld + (it.hk * G + g) * HD;
-      if (!__all_sync(0xffffffffu, mbar_wait_bounded(q_empty, (qn & 1) ^ 1, abort_flag, p.err))) break;
-      ++qn;
-#pragma unroll 2
-      for (int x = 0; x < HD; x += 8) {
-        float4 f[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-        if (mine) {
-          f[0] = __ldcg(reinterpret_cast<const float4*>(src + x));
-          f[1] = __ldcg(reinterpret_cast<const float4*>(src + x + 4));
-        }
+      float total[HD];
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) {
-          const uint4 u = make_uint4(take_bf16(f[0].x, f[0].y), take_bf16(f[0].z, f[0].w), take_bf16(f[1].x, f[1].y), take_bf16(f[1].z, f[1].w));
-          *reinterpret_cast<uint4*>(smem + (size_t)q * C::TILE + (x >> 6) * C::HALF + rr * 128 + ((((x >> 3) & 7) ^ (rr & 7)) << 4)) = u;
+      for (int x = 0; x < HD; ++x) total[x] = 0.f;
+#pragma unroll 1
+      for (int j = it.kb0; j < it.kb1; ++j, ++pn) {
+        if (!wait(pv_done, pn & 1)) break;
+        const float f = tmem_ld1(tl + C::F_COL + (pn & 1));
+#pragma unroll
+        for (int x = 0; x < HD; x += 16) {
+          float o[16];
+          tmem_ld16(to + x, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int y = 0; y < 16; ++y) total[x + y] = fmaf(total[x + y], f, o[y]);
         }
+        tc_fence_before();
+        mbar_arrive(o_free);
       }
-      fence_proxy_async_smem();
-      mbar_arrive(q_full);
+      const int b = in & 1;
+      if (!ok || !wait(&l_full[b], (in >> 1) & 1)) break;
+      const float l = tmem_ld1(tl + C::L_COL + b), m = tmem_ld1(tl + C::M_COL + b);
+      tmem_wait_ld();
+      tc_fence_before();
+      mbar_arrive(&l_free[b]);
+      ++in;
+      const float scale = it.slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
+      const size_t part = (size_t)it.slot * 2 * CH_ROWS + rr;
+      float* out = it.slot >= 0 ? part_o + part * HD : static_cast<float*>(p.out) + (long long)(it.row0 + gi) * p.out_ld + (it.hk * G + g) * HD;
+      if (mine) {
+        if (it.slot >= 0) part_ml[part] = make_float2(m, l);
+#pragma unroll
+        for (int x = 0; x < HD; x += 4)
+          *reinterpret_cast<float4*>(out + x) = make_float4(total[x] * scale, total[x + 1] * scale, total[x + 2] * scale, total[x + 3] * scale);
+      }
     }
   }
 
@@ -804,21 +891,21 @@ template <int HD, bool BF16>
 __global__ void __launch_bounds__(CM_WARPS * 32) chunk_merge_kernel(const __grid_constant__ ChunkAttnParams p, int ctas, int tiles) {
   constexpr int E = HD / 32;
   const int lane = threadIdx.x & 31;
-  const int groups = tiles * CH_BLK / (CM_WARPS * CM_ROWS), a = blockIdx.x / groups;
+  const int groups = tiles * CH_ROWS / (CM_WARPS * CM_ROWS), a = blockIdx.x / groups;
   const int rr0 = (blockIdx.x % groups * CM_WARPS + (threadIdx.x >> 5)) * CM_ROWS;
-  const int G = p.H / p.Hk, pt1 = CH_BLK / G;
+  const int G = p.H / p.Hk, pt1 = CH_ROWS / G;
   pdl_trigger();
   pdl_wait();
   const ChRec* recs = reinterpret_cast<const ChRec*>(p.part);
   const float2* part_ml = reinterpret_cast<const float2*>(recs + 2 * ctas);
-  const float* part_o = reinterpret_cast<const float*>(part_ml + 2 * ctas * 2 * CH_BLK);
+  const float* part_o = reinterpret_cast<const float*>(part_ml + 2 * ctas * 2 * CH_ROWS);
   const int4 r = __ldcg(reinterpret_cast<const int4*>(recs + 2 * a + 1));   // row0, npos, hk
   int i[CM_ROWS];   // positions in the item, -1: no row of it
   bool some = false;
 #pragma unroll
   for (int y = 0; y < CM_ROWS; ++y) {
-    const int rr = rr0 + y, gi = rr % CH_BLK / G;
-    i[y] = gi < pt1 && rr / CH_BLK * pt1 + gi < r.y ? rr / CH_BLK * pt1 + gi : -1;
+    const int rr = rr0 + y, gi = rr % CH_ROWS / G;
+    i[y] = gi < pt1 && rr / CH_ROWS * pt1 + gi < r.y ? rr / CH_ROWS * pt1 + gi : -1;
     some |= i[y] >= 0;
   }
   if (!some) return;
@@ -830,7 +917,7 @@ __global__ void __launch_bounds__(CM_WARPS * 32) chunk_merge_kernel(const __grid
     if (ends) last = c0 + __ffs(ends) - 1;
   }
   const int n = 1 + last - a;
-  auto place = [&](int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1) * 2 * CH_BLK + rr0; };
+  auto place = [&](int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1) * 2 * CH_ROWS + rr0; };
   float m[CM_ROWS], l[CM_ROWS], acc[CM_ROWS][E];
 #pragma unroll
   for (int y = 0; y < CM_ROWS; ++y) {
@@ -881,7 +968,7 @@ __global__ void __launch_bounds__(CM_WARPS * 32) chunk_merge_kernel(const __grid
   for (int y = 0; y < CM_ROWS; ++y) {
     if (i[y] < 0) continue;
     const float inv = l[y] == 0.f ? 0.f : 1.0f / l[y];
-    const long long at = (long long)(r.x + i[y]) * p.out_ld + (r.z * G + (rr0 + y) % CH_BLK % G) * HD + lane * E;
+    const long long at = (long long)(r.x + i[y]) * p.out_ld + (r.z * G + (rr0 + y) % CH_ROWS % G) * HD + lane * E;
 #pragma unroll
     for (int x = 0; x < E; x += 2) {
       if (BF16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + at + x) = pack_bf16(acc[y][x] * inv, acc[y][x + 1] * inv);
@@ -918,10 +1005,9 @@ static cudaError_t ch_launch(const ChunkAttnParams& p, int num_sms, cudaStream_t
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, chunk_attention_kernel<HD, PARTS>, p);
-  // (an item of fewer than four blocks is not split)
-  if (e != cudaSuccess || ((long long)p.ld * KV_PAGE + CH_BLK - 1) / CH_BLK < 4) return e;
+  if (e != cudaSuccess || p.ld < 2 * CH_PART) return e;   // (no item is split)
   constexpr int TILES = ChCfg<HD, PARTS>::TILES;
-  cfg.gridDim = dim3(num_sms * (TILES * CH_BLK / (CM_WARPS * CM_ROWS)));
+  cfg.gridDim = dim3(num_sms * (TILES * CH_ROWS / (CM_WARPS * CM_ROWS)));
   cfg.blockDim = dim3(CM_WARPS * 32);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<HD, PARTS == 1>, p, num_sms, TILES);
