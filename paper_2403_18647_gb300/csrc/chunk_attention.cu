@@ -6,8 +6,9 @@
 // loaded once for all of them.  An item is TILES tiles of a sequence and cache head, its work the steps of 64 keys (a page)
 // that its rows see.  The items stand in a line, weighed by their keys and a start's cost, and every CTA (one on an SM)
 // takes an equal stretch of it, wherever that begins: few rows of long sequences are split along their keys, and causal
-// tiles of unequal length leave no SM idle.  An item that several CTAs share leaves partial results (m, sum, O), which
-// a second kernel joins in order.  Sequences, lengths and pages are device values, so the plan is made on the device,
+// tiles of unequal length leave no SM idle.  Of an item that several CTAs share each writes
+// its partial results (m, sum, O), and the one that comes last joins them, always in the same order (a second kernel for
+// that took 15 us behind a prompt of 4095 positions on 32 heads, 126 in all).  Sequences, lengths and pages are device values, so the plan is made on the device,
 // by one warp of each CTA (a scan over the sequences), which then hands items to the others.
 //
 // Scores have two places in TMEM, by the step's parity: S of step i + 2 is issued behind P V of step i, so that the
@@ -40,18 +41,19 @@ constexpr int CH_THREADS = 384;
 constexpr int CH_DESC = 4;            // items handed out ahead
 constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
 constexpr int CH_PART = 4;            // steps that a part of an item has at least
-constexpr int CH_START = 192;         // what an item's start costs, in keys
-constexpr int CH_LEAST = 384;         // keys (and starts) for which a CTA is worth its while
+constexpr int CH_START = 512;         // what an item's start costs, in keys
+constexpr int CH_LEAST = 768;         // keys (and starts) for which a CTA is worth its while
 constexpr float CH_LAZY = 8.0f;       // log2 of the growth of a row maximum that is left unscaled
 constexpr float CH_UNSET = -1e30f;    // reference of a row that has seen no key
 
-// partial results of a CTA: slot 0 an item that began in another, slot 1 one that goes on in the next
-struct ChRec {
-  int row0, npos, hk, last;           // npos 0: none; last: the item ends here
-};
 struct ChItem {
   int row0, npos, pos0, hk;           // first row, positions, slot of the first; cache head (-1: no more items)
-  int seq, kb0, kb1, slot;            // steps; partial results' place or -1
+  int seq, kb0, kb1, part;            // steps; of an item in parts, which one this is, else -1
+  int head, parts, unused[2];         // the CTA of its first part, their number
+};
+
+struct ChSeq {
+  int first, n, len;
 };
 
 template <int HD, int PARTS>
@@ -66,11 +68,11 @@ struct ChCfg {
   static_assert(CH_FLAGS >= SLOTS + 2, "flags outlast the loads ahead");
   static constexpr size_t OFF_RING = (size_t)TILES * PARTS * TILE;
   static constexpr size_t OFF_BAR = OFF_RING + (size_t)SLOTS * 2 * SLOT;
-  static constexpr int NBAR = 2 * SLOTS + 21 + 2 * CH_DESC;
+  static constexpr int NBAR = 2 * SLOTS + 23 + 2 * CH_DESC;
   static constexpr size_t OFF_ITEMS = OFF_BAR + (NBAR + 1) / 2 * 16;
   static constexpr size_t SMEM = 1024 + OFF_ITEMS + CH_DESC * sizeof(ChItem) + CH_FLAGS * 4 + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
-  static_assert(OFF_RING >= (CHUNK_MAX_BATCH + 1) * 8, "the plan lies over the queries");
+  static_assert(OFF_RING + SLOTS * 2 * SLOT >= (CHUNK_MAX_BATCH + 2) * (8 + sizeof(ChSeq)), "the plan lies over the queries and the ring");
   // TMEM columns: S and P of step i, by its parity
   static constexpr int S_COL(int t) { return 128 * t; }
   static constexpr int P_COL(int t) { return PARTS == 1 ? 128 * t : 128; }
@@ -81,9 +83,9 @@ struct ChCfg {
   static constexpr int F_COL = 448, L_COL = 450, M_COL = 452;
 };
 
-size_t chunk_attention_scratch(int num_sms) {
-  return (size_t)2 * num_sms * (sizeof(ChRec) / 4 + 2 * CH_ROWS * (2 + 128));
-}
+// Two places for partial results a CTA (an item that goes on in the next one, an item that began before), and a counter
+// of an item's parts that have come, zero between launches
+size_t chunk_attention_scratch(int num_sms) { return (size_t)2 * num_sms * (2 + 2 * CH_ROWS * (2 + 128)); }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
   uint32_t r[32];
@@ -220,9 +222,6 @@ __device__ __forceinline__ uint32_t take_bf16(float& a, float& b) {
 }
 
 // ---- the plan: sequences of n new positions after `len` slots, items of pt positions -----------
-struct ChSeq {
-  int first, n, len;
-};
 __device__ __forceinline__ ChSeq ch_sequence(const ChunkAttnParams& p, int s) {
   ChSeq q;
   q.first = __ldcg(p.start + s);
@@ -243,6 +242,7 @@ __device__ __forceinline__ int ch_keys(const ChSeq& q, int pt, int cap, int t) {
 
 struct ChPlace {
   int s, hk, t, kb;   // s = b: behind the last item
+  long long cost;     // before the item
 };
 
 template <int HD, int PARTS>
@@ -261,7 +261,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   uint64_t* p_full = s_full + 4;          // [2][2] P is in TMEM, O is rescaled (128 threads)
   uint64_t* pv_done = p_full + 4;         // one tile: a step's P V is complete
   uint64_t* o_free = pv_done + 1;         // one tile: O of a step has been read (128 threads)
-  uint64_t* l_full = o_free + 1;          // [2] one tile, by item's parity: the rows' sums are there (128 threads)
+  uint64_t* part_full = o_free + 1;       // partial results are written (by all who write)
+  uint64_t* part_go = part_full + 1;      // ... and whether they are to be joined here is known
+  uint64_t* l_full = part_go + 1;          // [2] one tile, by item's parity: the rows' sums are there (128 threads)
   uint64_t* l_free = l_full + 2;          // [2] ... and have been read
   uint64_t* drain = l_free + 2;           // [2]
   uint64_t* d_full = drain + 2;           // [CH_DESC] an item's description is there
@@ -270,7 +272,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   uint32_t* flags = reinterpret_cast<uint32_t*>(items + CH_DESC);   // [CH_FLAGS] by entry: whether there is the page of its K
   uint32_t* tmem_slot = flags + CH_FLAGS;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* joins = abort_flag + 1;   // this CTA's part was the item's last
   long long* plan = reinterpret_cast<long long*>(smem);             // [b + 1] cost before each sequence
+  ChSeq* plan_seq = reinterpret_cast<ChSeq*>(plan + CHUNK_MAX_BATCH + 2);   // [b]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = p.H / p.Hk, pt1 = CH_ROWS / G, pt = C::TILES * pt1, cap = p.ld * KV_PAGE;
@@ -292,6 +296,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     }
     mbar_init(pv_done, 1);
     mbar_init(o_free, 128);
+    mbar_init(part_full, C::TILES * 128);
+    mbar_init(part_go, 1);
     mbar_init(drain, 1);
     mbar_init(drain + 1, 1);
     for (int i = 0; i < CH_DESC; ++i) {
@@ -312,9 +318,13 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   pdl_trigger();
   pdl_wait();
 
-  ChRec* recs = reinterpret_cast<ChRec*>(p.part);                             // [2 ctas]
-  float2* part_ml = reinterpret_cast<float2*>(recs + 2 * gridDim.x);          // [2 ctas][256]
-  float* part_o = reinterpret_cast<float*>(part_ml + 2 * gridDim.x * 2 * CH_ROWS);   // [2 ctas][256][HD]
+  int* arrived = reinterpret_cast<int*>(p.part);                              // [4 ctas]
+  float2* part_ml = reinterpret_cast<float2*>(arrived + 4 * gridDim.x);       // [2 ctas][256]
+  float4* part_o = reinterpret_cast<float4*>(part_ml + 2 * gridDim.x * 2 * CH_ROWS);   // [2 ctas][HD / 4][256]: a thread for each row
+  // where part k of the item whose first part is CTA a's leaves its results
+  auto part_at = [&](int a, int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1); };
+  auto ml_of = [&](size_t at, int rr) { return part_ml + at * 2 * CH_ROWS + rr; };
+  auto o_of = [&](size_t at, int rr, int x) { return part_o + (at * (HD / 4) + x / 4) * 2 * CH_ROWS + rr; };
 
   // an item's geometry
   auto item_keys = [&](const ChItem& it, int t) { return (int)min((long long)cap, (long long)it.pos0 + min(it.npos, (t + 1) * pt1)); };
@@ -338,6 +348,113 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     return it.hk >= 0;
   };
 
+  // Partial results have been written by warps w0 .. w0 + W - 1, all of which call this: the one whose part is the item's
+  // last joins the parts.  False: a wait ran out.
+  uint32_t part_phase = 0;
+  auto join = [&](const ChItem& it, int w0) {
+    constexpr int W = 4 * C::TILES, E = HD / 32;   // warps; values of a lane
+    auto wait = [&](uint64_t* bar) { return (bool)__all_sync(0xffffffffu, mbar_wait_bounded(bar, part_phase & 1, abort_flag, p.err)); };
+    __threadfence();
+    mbar_arrive(part_full);
+    if (warp == w0) {
+      if (!wait(part_full)) return false;
+      if (lane == 0) {
+        const bool last = atomic_add_acq_rel_gpu(arrived + it.head, 1) == it.parts - 1;
+        if (last) arrived[it.head] = 0;
+        *joins = last;
+        mbar_arrive(part_go);
+      }
+      __syncwarp();
+    }
+    if (!wait(part_go)) return false;
+    ++part_phase;
+    if (!*joins) return true;
+    auto position = [&](int rr) {   // of a row in the item, -1: no row of it
+      const int gi = rr % CH_ROWS / G, i = rr / CH_ROWS * pt1 + gi;
+      return gi < pt1 && i < it.npos ? i : -1;
+    };
+    if (it.npos * G > W * 8) {   // a thread for each row
+      const int rr = (int)threadIdx.x - w0 * 32, i = position(rr);
+      if (i < 0) return true;
+      float m = CH_UNSET, l = 0.f;
+#pragma unroll 2
+      for (int k = 0; k < it.parts; ++k) {   // (a part that saw no key of the row has a sum of 0, and maybe nothing was written)
+        const float2 ml = __ldcg(ml_of(part_at(it.head, k), rr));
+        const float now = ml.y > 0.f ? fmaxf(m, ml.x) : m;
+        l = l * ex2(m - now) + (ml.y > 0.f ? ml.y * ex2(ml.x - now) : 0.f);
+        m = now;
+      }
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      const long long to = (long long)(it.row0 + i) * p.out_ld + (it.hk * G + rr % CH_ROWS % G) * HD;
+#pragma unroll 1
+      for (int x = 0; x < HD; x += 32) {
+        float acc[32];
+#pragma unroll
+        for (int y = 0; y < 32; ++y) acc[y] = 0.f;
+#pragma unroll 2
+        for (int k = 0; k < it.parts; ++k) {
+          const size_t at = part_at(it.head, k);
+          const float2 ml = __ldcg(ml_of(at, rr));
+          float4 v[8];
+#pragma unroll
+          for (int y = 0; y < 8; ++y) v[y] = __ldcg(o_of(at, rr, x + 4 * y));
+          const float w = ex2(ml.x - m);
+          if (ml.y > 0.f)
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              acc[4 * y] = fmaf(v[y].x, w, acc[4 * y]);
+              acc[4 * y + 1] = fmaf(v[y].y, w, acc[4 * y + 1]);
+              acc[4 * y + 2] = fmaf(v[y].z, w, acc[4 * y + 2]);
+              acc[4 * y + 3] = fmaf(v[y].w, w, acc[4 * y + 3]);
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < 32; y += 8) {
+          if (PARTS == 1)
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + to + x + y) =
+                make_uint4(pack_bf16(acc[y] * inv, acc[y + 1] * inv), pack_bf16(acc[y + 2] * inv, acc[y + 3] * inv),
+                           pack_bf16(acc[y + 4] * inv, acc[y + 5] * inv), pack_bf16(acc[y + 6] * inv, acc[y + 7] * inv));
+          else
+#pragma unroll
+            for (int z = y; z < y + 8; z += 4)
+              *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to + x + z) = make_float4(acc[z] * inv, acc[z + 1] * inv, acc[z + 2] * inv, acc[z + 3] * inv);
+        }
+      }
+      return true;
+    }
+    // few rows, often in many parts: a warp for each
+#pragma unroll 1
+    for (int q = warp - w0; q < it.npos * G; q += W) {
+      const int rr = q / (pt1 * G) * CH_ROWS + q % (pt1 * G), i = position(rr);
+      float m = CH_UNSET, l = 0.f, acc[E];
+#pragma unroll
+      for (int y = 0; y < E; ++y) acc[y] = 0.f;
+#pragma unroll 8
+      for (int k = 0; k < it.parts; ++k) {
+        const size_t at = part_at(it.head, k);
+        const float2 ml = __ldcg(ml_of(at, rr));
+        const float* v = reinterpret_cast<const float*>(o_of(at, rr, lane * E)) + lane * E % 4;
+        float u[E];
+#pragma unroll
+        for (int y = 0; y < E; ++y) u[y] = __ldcg(v + y);
+        const bool seen = ml.y > 0.f;
+        const float now = seen ? fmaxf(m, ml.x) : m, f = ex2(m - now), w = seen ? ex2(ml.x - now) : 0.f;
+        m = now;
+        l = fmaf(l, f, ml.y * w);
+#pragma unroll
+        for (int y = 0; y < E; ++y) acc[y] = fmaf(acc[y], f, seen ? u[y] * w : 0.f);
+      }
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      const long long to = (long long)(it.row0 + i) * p.out_ld + (it.hk * G + rr % CH_ROWS % G) * HD + lane * E;
+#pragma unroll
+      for (int y = 0; y < E; y += 2) {
+        if (PARTS == 1) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + to + y) = pack_bf16(acc[y] * inv, acc[y + 1] * inv);
+        else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + to + y) = make_float2(acc[y] * inv, acc[y + 1] * inv);
+      }
+    }
+    return true;
+  };
+
   if (warp == 2) {
     // ---- the plan
     long long total = 0;
@@ -351,6 +468,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         past |= z > a && (long long)max(len, 0) + (z - a) > cap;
         ChSeq q = {a, z - a, min(max(len, 0), cap)};
         if (z >= a) cost = ch_cost(q, pt) * p.Hk;
+        plan_seq[s] = q;
       }
       long long sum = cost;
 #pragma unroll
@@ -370,16 +488,19 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     }
     __syncwarp();
     const int ctas = (int)max(1ll, min((long long)gridDim.x, total / CH_LEAST)), cta = blockIdx.x;
-    // the first sequence from s on that has rows (b: none); the plan is gone once items are handed out
+    // the first sequence from s on that has rows (b: none); the plan is gone once items are handed out (out)
+    bool out = false;
     auto with_rows = [&](int s) {
       for (; s < p.b; s += 32) {
-        const unsigned some = __ballot_sync(0xffffffffu, s + lane < p.b && __ldcg(p.start + min(s + lane, p.b - 1)) < __ldcg(p.start + min(s + lane, p.b - 1) + 1));
+        const unsigned some = __ballot_sync(0xffffffffu, s + lane < p.b && (out ? __ldcg(p.start + min(s + lane, p.b - 1)) < __ldcg(p.start + min(s + lane, p.b - 1) + 1)
+                                                                                 : plan_seq[min(s + lane, p.b - 1)].n > 0));
         if (some) return s + __ffs(some) - 1;
       }
       return p.b;
     };
     auto after = [&](ChPlace a, const ChSeq& q) {   // the item that follows
       a.kb = 0;
+      a.cost += q.len + CH_START + min((long long)q.n, (long long)(a.t + 1) * pt);
       if (++a.t * pt >= q.n) {
         a.t = 0;
         if (++a.hk == p.Hk) a.hk = 0, a.s = with_rows(a.s + 1);
@@ -388,7 +509,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     };
     // the c-th of the borders between the CTAs' stretches
     auto border = [&](int c) {
-      ChPlace a = {p.b, 0, 0, 0};
+      ChPlace a = {p.b, 0, 0, 0, 0};
       if (c >= ctas || total == 0) return a;
       const long long x = total / ctas * c + total % ctas * c / ctas;
       int lo = 0, hi = p.b;   // the last sequence whose cost before it is at most x
@@ -398,7 +519,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         else hi = mid;
       }
       a.s = lo;
-      const ChSeq q = ch_sequence(p, lo);
+      const ChSeq q = plan_seq[lo];
       const long long of_head = ch_cost(q, pt);
       long long rem = x - plan[lo];
       a.hk = (int)(rem / of_head);
@@ -410,30 +531,33 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         else hi = mid;
       }
       a.t = lo;
+      a.cost = x - rem + ch_before(q, pt, lo);
       const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
       const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + CH_STEP / 2) / CH_STEP;
       a.kb = kb < CH_PART ? 0 : (int)kb;
       if (a.kb > steps - CH_PART && a.kb > 0) a = after(a, q);
       return a;
     };
-    const ChRec none = {0, 0, 0, 0};
-    ChRec left = none, right = none;
-    ChPlace a = {p.b, 0, 0, 0}, z = a;
+    // the last CTA whose stretch begins at most y behind the start of the line
+    auto cta_at = [&](long long y) { return (int)min((long long)ctas - 1, ((y + 1) * ctas - 1) / total); };
+    ChPlace a = {p.b, 0, 0, 0, 0}, z = a;
     if (!bad && cta < ctas) {
       a = border(cta);
       z = border(cta + 1);
     }
-    fence_proxy_async_smem();   // the plan's place is the queries': read before, written by TMA after
     uint32_t n = 0;
     ChPlace end = z;
+    ChSeq q = {0, 0, 0};
+    int it_seq = -1;
     bool ok = true;
     while (ok) {
       const bool more = a.s < p.b && !(a.s == end.s && a.hk == end.hk && a.t == end.t && a.kb >= end.kb);
-      ChItem it = {0, 0, 0, -1, 0, 0, 0, -1};
-      ChSeq q = {0, 0, 0};
+      ChItem it = {0, 0, 0, -1, 0, 0, 0, -1, 0, 0, {0, 0}};
       bool stop = true;
       if (more) {
-        q = ch_sequence(p, a.s);
+        if (!out) q = plan_seq[a.s];
+        else if (a.s != it_seq) q = ch_sequence(p, a.s);
+        it_seq = a.s;
         const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
         it.row0 = q.first + a.t * pt;
         it.npos = min(pt, q.n - a.t * pt);
@@ -443,29 +567,26 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         it.kb0 = a.kb;
         stop = a.s == end.s && a.hk == end.hk && a.t == end.t;
         it.kb1 = stop ? end.kb : steps;
-        if (it.kb0 > 0) {
-          it.slot = 2 * cta;
-          left = ChRec{it.row0, it.npos, it.hk, it.kb1 == steps};
-        } else if (it.kb1 < steps) {
-          it.slot = 2 * cta + 1;
-          right = ChRec{it.row0, it.npos, it.hk, 0};
+        if (it.kb0 > 0 || it.kb1 < steps) {   // (border() takes what is less than CH_PART steps from an end as the end)
+          it.head = cta_at(a.cost + CH_START - CH_STEP / 2 + CH_PART * CH_STEP - 1);
+          it.parts = cta_at(a.cost + CH_START - CH_STEP / 2 + (long long)(steps - CH_PART + 1) * CH_STEP - 1) - it.head + 1;
+          it.part = cta - it.head;
         }
       }
       const int d = n % CH_DESC;
       ok = __all_sync(0xffffffffu, mbar_wait_bounded(&d_empty[d], ((n / CH_DESC) & 1) ^ 1, abort_flag, p.err));
       if (!ok) break;
+      if (!out) fence_proxy_async_smem();   // (the plan's place: read before, written by TMA after)
+      out = true;
+      __syncwarp();
       if (lane == 0) {
         items[d] = it;
         mbar_arrive(&d_full[d]);
       }
       ++n;
       if (!more) break;
-      if (stop) a = z = end = ChPlace{p.b, 0, 0, 0};
+      if (stop) a = z = end = ChPlace{p.b, 0, 0, 0, 0};
       else a = after(a, q);
-    }
-    if (lane == 0) {
-      recs[2 * cta] = left;
-      recs[2 * cta + 1] = right;
     }
   } else if (warp == 0) {
     // ---- loads
@@ -798,19 +919,20 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         ++in;
       } else {
         const float inv = l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
-        const size_t part = (size_t)it.slot * 2 * CH_ROWS + t * CH_ROWS + rr;
         const long long at = (long long)(it.row0 + i) * p.out_ld + (it.hk * G + g) * HD;
-        if (it.slot >= 0 && mine) part_ml[part] = make_float2(m, l);
+        const size_t part = it.part >= 0 ? part_at(it.head, it.part) : 0;
+        const int pr = t * CH_ROWS + rr;
+        if (it.part >= 0 && mine) *ml_of(part, pr) = make_float2(m, l);
         if (end > it.kb0) {
 #pragma unroll 1
           for (int x = 0; x < HD; x += 16) {
             float o[16];
             tmem_ld16(to + x, o);
             tmem_wait_ld();
-            if (mine && it.slot >= 0) {
+            if (mine && it.part >= 0) {
 #pragma unroll
               for (int y = 0; y < 16; y += 4)
-                *reinterpret_cast<float4*>(part_o + part * HD + x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                *o_of(part, pr, x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
             } else if (mine) {
               uint32_t u[8];
 #pragma unroll
@@ -821,6 +943,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
             }
           }
         }
+        if (it.part >= 0 && !join(it, 4)) break;
         tc_fence_before();   // (O is read: the next item's products may overwrite it once its P has come)
       }
     }
@@ -863,15 +986,18 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       tc_fence_before();
       mbar_arrive(&l_free[b]);
       ++in;
-      const float scale = it.slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
-      const size_t part = (size_t)it.slot * 2 * CH_ROWS + rr;
-      float* out = it.slot >= 0 ? part_o + part * HD : static_cast<float*>(p.out) + (long long)(it.row0 + gi) * p.out_ld + (it.hk * G + g) * HD;
-      if (mine) {
-        if (it.slot >= 0) part_ml[part] = make_float2(m, l);
+      if (mine && it.part >= 0) {
+        const size_t part = part_at(it.head, it.part);
+        *ml_of(part, rr) = make_float2(m, l);
 #pragma unroll
-        for (int x = 0; x < HD; x += 4)
-          *reinterpret_cast<float4*>(out + x) = make_float4(total[x] * scale, total[x + 1] * scale, total[x + 2] * scale, total[x + 3] * scale);
+        for (int x = 0; x < HD; x += 4) *o_of(part, rr, x) = make_float4(total[x], total[x + 1], total[x + 2], total[x + 3]);
+      } else if (mine) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;   // (0: no key of the row has a page)
+        float* out = static_cast<float*>(p.out) + (long long)(it.row0 + gi) * p.out_ld + (it.hk * G + g) * HD;
+#pragma unroll
+        for (int x = 0; x < HD; x += 4) *reinterpret_cast<float4*>(out + x) = make_float4(total[x] * inv, total[x + 1] * inv, total[x + 2] * inv, total[x + 3] * inv);
       }
+      if (it.part >= 0 && !join(it, 8)) break;
     }
   }
 
@@ -883,106 +1009,11 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   }
 }
 
-// Joins the parts of the items that several CTAs shared: item a is the one that goes on behind CTA a's stretch, its parts
-// those of a (slot 1) and of the CTAs that follow (slot 0) up to the one that ends it.  A warp takes CM_ROWS rows, whose
-// loads are in flight together; the parts' references and sums are on its lanes.
-constexpr int CM_WARPS = 8, CM_ROWS = 4;
-template <int HD, bool BF16>
-__global__ void __launch_bounds__(CM_WARPS * 32) chunk_merge_kernel(const __grid_constant__ ChunkAttnParams p, int ctas, int tiles) {
-  constexpr int E = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const int groups = tiles * CH_ROWS / (CM_WARPS * CM_ROWS), a = blockIdx.x / groups;
-  const int rr0 = (blockIdx.x % groups * CM_WARPS + (threadIdx.x >> 5)) * CM_ROWS;
-  const int G = p.H / p.Hk, pt1 = CH_ROWS / G;
-  pdl_trigger();
-  pdl_wait();
-  const ChRec* recs = reinterpret_cast<const ChRec*>(p.part);
-  const float2* part_ml = reinterpret_cast<const float2*>(recs + 2 * ctas);
-  const float* part_o = reinterpret_cast<const float*>(part_ml + 2 * ctas * 2 * CH_ROWS);
-  const int4 r = __ldcg(reinterpret_cast<const int4*>(recs + 2 * a + 1));   // row0, npos, hk
-  int i[CM_ROWS];   // positions in the item, -1: no row of it
-  bool some = false;
-#pragma unroll
-  for (int y = 0; y < CM_ROWS; ++y) {
-    const int rr = rr0 + y, gi = rr % CH_ROWS / G;
-    i[y] = gi < pt1 && rr / CH_ROWS * pt1 + gi < r.y ? rr / CH_ROWS * pt1 + gi : -1;
-    some |= i[y] >= 0;
-  }
-  if (!some) return;
-  // the last of the parts' CTAs
-  int last = a;
-  for (int c0 = a + 1; last == a && c0 < ctas; c0 += 32) {
-    const int c = c0 + lane;
-    const unsigned ends = __ballot_sync(0xffffffffu, c < ctas && __ldcg(reinterpret_cast<const int4*>(recs + 2 * min(c, ctas - 1))).w);
-    if (ends) last = c0 + __ffs(ends) - 1;
-  }
-  const int n = 1 + last - a;
-  auto place = [&](int k) { return (size_t)(k ? 2 * (a + k) : 2 * a + 1) * 2 * CH_ROWS + rr0; };
-  float m[CM_ROWS], l[CM_ROWS], acc[CM_ROWS][E];
-#pragma unroll
-  for (int y = 0; y < CM_ROWS; ++y) {
-    m[y] = CH_UNSET;
-    l[y] = 0.f;
-#pragma unroll
-    for (int x = 0; x < E; ++x) acc[y][x] = 0.f;
-  }
-  for (int k0 = 0; k0 < n; k0 += 32) {
-    const int here = min(32, n - k0);
-    float w[CM_ROWS];
-#pragma unroll
-    for (int y = 0; y < CM_ROWS; ++y) {
-      const float2 ml = lane < here && i[y] >= 0 ? __ldcg(part_ml + place(k0 + lane) + y) : make_float2(CH_UNSET, 0.f);
-      float top = ml.y > 0.f ? fmaxf(ml.x, m[y]) : m[y];   // (a part that saw no key of the row has a sum of 0)
-#pragma unroll
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      w[y] = ml.y > 0.f ? ex2(ml.x - top) : 0.f;
-      float sum = ml.y * w[y];
-#pragma unroll
-      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const float f = ex2(m[y] - top);
-      l[y] = fmaf(l[y], f, sum);
-      m[y] = top;
-#pragma unroll
-      for (int x = 0; x < E; ++x) acc[y][x] *= f;
-    }
-#pragma unroll 4
-    for (int k = 0; k < here; ++k)
-#pragma unroll
-      for (int y = 0; y < CM_ROWS; ++y) {
-        const float f = __shfl_sync(0xffffffffu, w[y], k);
-        if (f == 0.f) continue;   // (and maybe nothing was written)
-        const float* o = part_o + (place(k0 + k) + y) * HD + lane * E;
-        float v[E];
-        if (E == 4) {
-          const float4 q = __ldcg(reinterpret_cast<const float4*>(o));
-          v[0] = q.x, v[1] = q.y, v[E - 2] = q.z, v[E - 1] = q.w;
-        } else {
-          const float2 q = __ldcg(reinterpret_cast<const float2*>(o));
-          v[0] = q.x, v[1] = q.y;
-        }
-#pragma unroll
-        for (int x = 0; x < E; ++x) acc[y][x] = fmaf(v[x], f, acc[y][x]);
-      }
-  }
-#pragma unroll
-  for (int y = 0; y < CM_ROWS; ++y) {
-    if (i[y] < 0) continue;
-    const float inv = l[y] == 0.f ? 0.f : 1.0f / l[y];
-    const long long at = (long long)(r.x + i[y]) * p.out_ld + (r.z * G + (rr0 + y) % CH_ROWS % G) * HD + lane * E;
-#pragma unroll
-    for (int x = 0; x < E; x += 2) {
-      if (BF16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + at + x) = pack_bf16(acc[y][x] * inv, acc[y][x + 1] * inv);
-      else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at + x) = make_float2(acc[y][x] * inv, acc[y][x + 1] * inv);
-    }
-  }
-}
-
 template <int HD, int PARTS>
 static cudaError_t ch_prepare() {
   const auto kernel = chunk_attention_kernel<HD, PARTS>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChCfg<HD, PARTS>::SMEM);
-  if (e == cudaSuccess) e = prefer_shared(kernel);
-  return e == cudaSuccess ? prefer_shared(chunk_merge_kernel<HD, PARTS == 1>) : e;
+  return e == cudaSuccess ? prefer_shared(kernel) : e;
 }
 cudaError_t chunk_attention_prepare() {
   cudaError_t e = ch_prepare<64, 1>();
@@ -1004,13 +1035,7 @@ static cudaError_t ch_launch(const ChunkAttnParams& p, int num_sms, cudaStream_t
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, chunk_attention_kernel<HD, PARTS>, p);
-  if (e != cudaSuccess || p.ld < 2 * CH_PART) return e;   // (no item is split)
-  constexpr int TILES = ChCfg<HD, PARTS>::TILES;
-  cfg.gridDim = dim3(num_sms * (TILES * CH_ROWS / (CM_WARPS * CM_ROWS)));
-  cfg.blockDim = dim3(CM_WARPS * 32);
-  cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<HD, PARTS == 1>, p, num_sms, TILES);
+  return cudaLaunchKernelEx(&cfg, chunk_attention_kernel<HD, PARTS>, p);
 }
 cudaError_t launch_chunk_attention(const ChunkAttnParams& p, int num_sms, cudaStream_t st, bool pdl) {
   if (p.bf16) return p.hd == 64 ? ch_launch<64, 1>(p, num_sms, st, pdl) : ch_launch<128, 1>(p, num_sms, st, pdl);
