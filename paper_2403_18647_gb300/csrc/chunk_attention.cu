@@ -68,7 +68,7 @@ struct ChCfg {
   static_assert(CH_FLAGS >= SLOTS + 2, "flags outlast the loads ahead");
   static constexpr size_t OFF_RING = (size_t)TILES * PARTS * TILE;
   static constexpr size_t OFF_BAR = OFF_RING + (size_t)SLOTS * 2 * SLOT;
-  static constexpr int NBAR = 2 * SLOTS + 23 + 2 * CH_DESC;
+  static constexpr int NBAR = 2 * SLOTS + 24 + 2 * CH_DESC;
   static constexpr size_t OFF_ITEMS = OFF_BAR + (NBAR + 1) / 2 * 16;
   static constexpr size_t SMEM = 1024 + OFF_ITEMS + CH_DESC * sizeof(ChItem) + CH_FLAGS * 4 + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
@@ -78,9 +78,10 @@ struct ChCfg {
   static constexpr int P_COL(int t) { return PARTS == 1 ? 128 * t : 128; }
   static constexpr int P_STEP = PARTS == 1 ? 64 : 96;
   static constexpr int O_COL(int t) { return PARTS == 1 ? 256 + 128 * t : 320; }
-  // one tile: what the softmax tells those who keep the total; by step's parity the total's factor, by item's parity the
-  // sum and the reference
-  static constexpr int F_COL = 448, L_COL = 450, M_COL = 452;
+  // one tile: what the softmax tells those who keep the total; the total's factor of a step (four of them: one is read before
+  // the P V of the step after it, which the softmax waits for two steps on), and by item's parity the sum and the reference
+  static constexpr int F_COL(uint32_t step) { return 448 + (step & 3); }
+  static constexpr int L_COL = 452, M_COL = 454;
 };
 
 // Two places for partial results a CTA (an item that goes on in the next one, an item that began before), and a counter
@@ -259,8 +260,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   uint64_t* q_empty = q_full + 2;         // [2] two tiles: the item's last S is complete
   uint64_t* s_full = q_empty + 2;         // [2][2] per tile and entry's parity: S of its step, and P V of the one before the last, are complete
   uint64_t* p_full = s_full + 4;          // [2][2] P is in TMEM, O is rescaled (128 threads)
-  uint64_t* pv_done = p_full + 4;         // one tile: a step's P V is complete
-  uint64_t* o_free = pv_done + 1;         // one tile: O of a step has been read (128 threads)
+  uint64_t* pv_done = p_full + 4;         // [2] one tile, by step's parity: its P V is complete
+  uint64_t* o_free = pv_done + 2;         // one tile: O of a step has been read (128 threads)
   uint64_t* part_full = o_free + 1;       // partial results are written (by all who write)
   uint64_t* part_go = part_full + 1;      // ... and whether they are to be joined here is known
   uint64_t* l_full = part_go + 1;          // [2] one tile, by item's parity: the rows' sums are there (128 threads)
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], C::TILES);
+      mbar_init(&empty[s], 2);
     }
     mbar_init(z_full, 1);
     for (int t = 0; t < 2; ++t) {
@@ -294,7 +295,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       mbar_init(&l_full[t], 128);
       mbar_init(&l_free[t], 128);
     }
-    mbar_init(pv_done, 1);
+    mbar_init(&pv_done[0], 1);
+    mbar_init(&pv_done[1], 1);
     mbar_init(o_free, 128);
     mbar_init(part_full, C::TILES * 128);
     mbar_init(part_go, 1);
@@ -302,7 +304,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     mbar_init(drain + 1, 1);
     for (int i = 0; i < CH_DESC; ++i) {
       mbar_init(&d_full[i], 1);
-      mbar_init(&d_empty[i], 9 + C::TILES);
+      mbar_init(&d_empty[i], 11);
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -686,9 +688,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       if (zn) land(z_full, (zn - 1) & 1);
       for (uint32_t i = n > SLOTS ? n - SLOTS : 0; i < n; ++i) land(&full[i % SLOTS], (i / SLOTS) & 1);
     }
-  } else if (warp == 1 || (warp == 3 && C::TILES == 2)) {
-    // ---- products of a tile
-    const int t = warp >> 1;
+  } else if (warp == 1 || warp == 3) {
+    // ---- products: a tile's or, with one tile, S on one warp and P V on the other
+    const int t = PARTS == 1 ? warp >> 1 : 0;
     constexpr uint32_t idesc_s = idesc_bf16_f32(128, CH_STEP);
     constexpr uint32_t idesc_o = idesc_bf16_f32(128, HD) | (1u << 16);   // B is MN-major
     const uint32_t mine = ch_elect();
@@ -699,6 +701,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     uint32_t n = 0, x = 0, qn = 0, pn = 0;   // entries of the ring and of the tile, Q tiles, P's
     const uint32_t full_at = smem_u32(full), empty_at = smem_u32(empty), s_at = smem_u32(s_full + 2 * t), p_at = smem_u32(p_full + 2 * t),
                    qe_at = smem_u32(q_empty + t), pv_at = smem_u32(pv_done);
+    const bool does_s = PARTS == 1 || warp == 1, does_pv = PARTS == 1 || warp == 3;
     auto wait = [&](uint64_t* bar, uint32_t parity) {   // (the lanes agree before the products)
       ok = ok && mbar_wait_bounded(bar, parity, abort_flag, p.err);
     };
@@ -711,55 +714,67 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     while (ok && next_item(it)) {
       const int nt = item_tiles(it), keys = item_keys(it, t) - it.kb0 * CH_STEP, all = it.kb1 - it.kb0 + 2;
       const int steps = t < nt ? max(0, item_end(it, t) - it.kb0) : 0, mine_too = steps ? steps + 2 : 0;
-      if (steps) wait(&q_full[t], qn++ & 1);
-      // entry e: P V of step e - 2, then S of step e over the scores that it has used
+      if (steps && does_s) wait(&q_full[t], qn++ & 1);
+      // entry e: P V of step e - 2, then S of step e over the scores that it has used (one tile: once they have been read)
 #pragma unroll 1
       for (int e = 0; e < mine_too; ++e, ++n, ++x) {
-        const uint32_t s = n % SLOTS, b = x & 1, full_parity = (n / SLOTS) & 1;
+        const bool has_pv = e >= 2, has_s = e < steps;
+        const uint32_t s = n % SLOTS, full_parity = (n / SLOTS) & 1;
+        // one tile: x counts this warp's steps; S waits for P of the step before the last, P V for its own P
+        if (PARTS != 1 && !(does_s ? has_s : has_pv)) --x;
+        const uint32_t b = x & 1;
+        uint32_t pw = pn;              // the P that is waited for
+        bool wait_p = has_pv;
+        if (PARTS != 1) {
+          wait_p = does_s ? has_s && x >= 2 : has_pv;
+          pw = does_s ? x - 2 : x;
+        }
         bool ready;
-        if (e >= 2) {
-          ready = ch_try_both(full_at + 8 * s, full_parity, p_at + 8 * (pn & 1), (pn >> 1) & 1);
-          if (PARTS != 1 && pn > 0) ready = ready && mbar_try_wait(o_free, (pn - 1) & 1);
+        if (wait_p) {
+          ready = ch_try_both(full_at + 8 * s, full_parity, p_at + 8 * (pw & 1), (pw >> 1) & 1);
+          if (PARTS != 1 && does_pv && x > 0) ready = ready && mbar_try_wait(o_free, (x - 1) & 1);
         } else {
           ready = mbar_try_wait(&full[s], full_parity);
         }
         if (!__all_sync(0xffffffffu, ready && ok)) {
           ok = ok && ch_wait_slow(&full[s], full_parity, abort_flag, p.err);
-          if (e >= 2) {
-            if (PARTS != 1 && pn > 0) ok = ok && ch_wait_slow(o_free, (pn - 1) & 1, abort_flag, p.err);
-            ok = ok && ch_wait_slow(&p_full[2 * t + (pn & 1)], (pn >> 1) & 1, abort_flag, p.err);
+          if (wait_p) {
+            if (PARTS != 1 && does_pv && x > 0) ok = ok && ch_wait_slow(o_free, (x - 1) & 1, abort_flag, p.err);
+            ok = ok && ch_wait_slow(&p_full[2 * t + (pw & 1)], (pw >> 1) & 1, abort_flag, p.err);
           }
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
         }
         tc_fence_after();
-        if (e >= 2) {
+        if (has_pv && does_pv) {
           ++pn;
           const uint64_t v = v_desc + s * (2 * C::SLOT >> 4);
           const int sixteens = min(4, (keys - (e - 2) * CH_STEP + 15) / 16);
-#pragma unroll 1
-          for (int part = PARTS - 1; part >= 0; --part) {
-            const uint32_t a = tp + C::P_STEP * b + part * 32, acc = (PARTS == 1 && e > 2) || part < PARTS - 1 ? 1u : 0u;   // (else over O's old values)
-            if (sixteens == 4) {
+          if (sixteens == 4) {
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk) ch_mma_ta(to, a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
-            } else {
+            for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)   // (the first over O's old values where they are another item's or, with one tile, step's)
+                ch_mma_ta(to, tp + C::P_STEP * b + part * 32 + kk * 8, v + kk * 128, idesc_o, kk || part < PARTS - 1 ? 1u : PARTS == 1 && e > 2, mine);
+          } else {
 #pragma unroll 1
-              for (int kk = 0; kk < sixteens; ++kk) ch_mma_ta(to, a + kk * 8, v + kk * 128, idesc_o, kk ? 1u : acc, mine);
-            }
+            for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll 1
+              for (int kk = 0; kk < sixteens; ++kk)
+                ch_mma_ta(to, tp + C::P_STEP * b + part * 32 + kk * 8, v + kk * 128, idesc_o, kk || part < PARTS - 1 ? 1u : PARTS == 1 && e > 2, mine);
           }
-          if (PARTS != 1) ch_commit(pv_at, mine);
+          if (PARTS != 1) ch_commit(pv_at + 8 * b, mine);
         }
-        if (e < steps) {
+        if (has_s && does_s) {
           const uint64_t k = k_desc + s * (2 * C::SLOT >> 4);
-#pragma unroll 1
+#pragma unroll
           for (int part = PARTS - 1; part >= 0; --part)   // (small ones first: the sums round less)
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk)
               ch_mma(ts + CH_STEP * b, q_desc + part * (C::TILE >> 4) + (kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2,
                      k + (kk >> 2) * (C::BOX >> 4) + (kk & 3) * 2, idesc_s, part < PARTS - 1 || kk ? 1u : 0u, mine);
         }
-        ch_commit(s_at + 8 * b, mine);
+        if (PARTS == 1 || (has_s && does_s)) ch_commit(s_at + 8 * b, mine);
         ch_commit(empty_at + 8 * s, mine);
         if (PARTS == 1 && e == steps - 1) ch_commit(qe_at, mine);
       }
@@ -896,14 +911,14 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
             rescale(f);
           }
         }
-        if (PARTS != 1) tmem_st1(tl + C::F_COL + (pn & 1), f);   // what the total is multiplied by first
-        // (over S, or in P's place of two steps ago: its P V came with this entry)
+        if (PARTS != 1 && pn >= 2 && !wait(&pv_done[pn & 1], ((pn - 2) >> 1) & 1)) break;   // P's place
+        if (PARTS != 1) tmem_st1(tl + C::F_COL(pn), f);   // what the total is multiplied by first
         probabilities(s, tp + C::P_STEP * (x & 1));
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&p_full[2 * t + (pn & 1)]);
       }
-      if (end > it.kb0) {   // the last two P V's
+      if (PARTS == 1 && end > it.kb0) {   // the last two P V's
         for (int y = 0; y < 2; ++y, ++x) wait(&s_full[2 * t + (x & 1)], (x >> 1) & 1);
       }
       bn += it.kb1 - it.kb0 + 2;
@@ -966,8 +981,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       for (int x = 0; x < HD; ++x) total[x] = 0.f;
 #pragma unroll 1
       for (int j = it.kb0; j < it.kb1; ++j, ++pn) {
-        if (!wait(pv_done, pn & 1)) break;
-        const float f = tmem_ld1(tl + C::F_COL + (pn & 1));
+        if (!wait(&pv_done[pn & 1], (pn >> 1) & 1)) break;
+        const float f = tmem_ld1(tl + C::F_COL(pn));
 #pragma unroll
         for (int x = 0; x < HD; x += 16) {
           float o[16];
