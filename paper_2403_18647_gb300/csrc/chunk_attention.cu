@@ -41,8 +41,10 @@ constexpr int CH_THREADS = 384;
 constexpr int CH_DESC = 4;            // items handed out ahead
 constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
 constexpr int CH_PART = 4;            // steps that a part of an item has at least
-constexpr int CH_START = 512;         // what an item's start costs, in keys
-constexpr int CH_LEAST = 768;         // keys (and starts) for which a CTA is worth its while
+// What work costs, in quarters of a key's with one tile: a key with two tiles, an item's start, and that for which a CTA
+// is worth its while.  One tile's steps are bound by memory, two tiles' by the products and the softmax: 48 sequences of up to
+// 8200 slots, two of them with 100 new rows, take 167 us with these, 189 with equal keys, 179 with a start of 64 keys.
+constexpr int CH_TWO = 5, CH_START = 4 * 320, CH_LEAST = 4 * 512;
 constexpr float CH_LAZY = 8.0f;       // log2 of the growth of a row maximum that is left unscaled
 constexpr float CH_UNSET = -1e30f;    // reference of a row that has seen no key
 
@@ -53,7 +55,7 @@ struct ChItem {
 };
 
 struct ChSeq {
-  int first, n, len;
+  int first, n, len, w;               // w: what a key costs
 };
 
 template <int HD, int PARTS>
@@ -223,21 +225,25 @@ __device__ __forceinline__ uint32_t take_bf16(float& a, float& b) {
 }
 
 // ---- the plan: sequences of n new positions after `len` slots, items of pt positions -----------
-__device__ __forceinline__ ChSeq ch_sequence(const ChunkAttnParams& p, int s) {
+__device__ __forceinline__ ChSeq ch_sequence(const ChunkAttnParams& p, int s, int pt1, int tiles) {
   ChSeq q;
   q.first = __ldcg(p.start + s);
   q.n = __ldcg(p.start + s + 1) - q.first;
   q.len = min(max(__ldcg(p.len + s), 0), p.ld * KV_PAGE);
+  q.w = tiles == 2 && q.n > pt1 ? CH_TWO : 4;
   return q;
 }
-// cost of a head's items before item t, and of all of them
+// cost of a head's items before item t, and of item t
 __device__ __forceinline__ long long ch_before(const ChSeq& q, int pt, int t) {
-  return (long long)t * (q.len + CH_START) + (long long)pt * ((long long)t * (t + 1) / 2);
+  return (long long)t * ((long long)q.w * q.len + CH_START) + (long long)q.w * pt * ((long long)t * (t + 1) / 2);
+}
+__device__ __forceinline__ long long ch_item(const ChSeq& q, int pt, int t) {
+  return (long long)q.w * (q.len + min((long long)q.n, (long long)(t + 1) * pt)) + CH_START;
 }
 __device__ __forceinline__ long long ch_cost(const ChSeq& q, int pt) {
   if (q.n <= 0) return 0;
   const int t = (q.n + pt - 1) / pt;
-  return ch_before(q, pt, t - 1) + q.len + CH_START + q.n;
+  return ch_before(q, pt, t - 1) + ch_item(q, pt, t - 1);
 }
 __device__ __forceinline__ int ch_keys(const ChSeq& q, int pt, int cap, int t) { return min((long long)cap, (long long)q.len + min((long long)q.n, (long long)(t + 1) * pt)); }
 
@@ -460,16 +466,18 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   if (warp == 2) {
     // ---- the plan
     long long total = 0;
+    int n_items = 0;
     bool bad = false, past = false;
     for (int s0 = 0; s0 < p.b; s0 += 32) {
       const int s = s0 + lane;
       long long cost = 0;
+      int items_here = 0;
       if (s < p.b) {
         const int a = __ldcg(p.start + s), z = __ldcg(p.start + s + 1), len = __ldcg(p.len + s);
         bad |= a < 0 || z < a || z > p.rows;
         past |= z > a && (long long)max(len, 0) + (z - a) > cap;
-        ChSeq q = {a, z - a, min(max(len, 0), cap)};
-        if (z >= a) cost = ch_cost(q, pt) * p.Hk;
+        const ChSeq q = {a, z - a, min(max(len, 0), cap), C::TILES == 2 && z - a > pt1 ? CH_TWO : 4};
+        if (z >= a) cost = ch_cost(q, pt) * p.Hk, items_here = (int)min(1ll << 15, ((long long)q.n + pt - 1) / pt * p.Hk);
         plan_seq[s] = q;
       }
       long long sum = cost;
@@ -480,6 +488,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       }
       if (s < p.b) plan[s] = total + sum - cost;
       total += __shfl_sync(0xffffffffu, sum, 31);
+      n_items = min(1 << 20, n_items + (int)__reduce_add_sync(0xffffffffu, (unsigned)items_here));
     }
     bad = __any_sync(0xffffffffu, bad);
     past = __any_sync(0xffffffffu, past);
@@ -489,7 +498,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       else if (past) set_error(p.err, ERR_PAGE);
     }
     __syncwarp();
-    const int ctas = (int)max(1ll, min((long long)gridDim.x, total / CH_LEAST)), cta = blockIdx.x;
+    // (of two for each item none takes two of them)
+    const int ctas = (int)max(1ll, min((long long)gridDim.x, max(2ll * n_items, total / CH_LEAST))), cta = blockIdx.x;
     // the first sequence from s on that has rows (b: none); the plan is gone once items are handed out (out)
     bool out = false;
     auto with_rows = [&](int s) {
@@ -502,7 +512,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     };
     auto after = [&](ChPlace a, const ChSeq& q) {   // the item that follows
       a.kb = 0;
-      a.cost += q.len + CH_START + min((long long)q.n, (long long)(a.t + 1) * pt);
+      a.cost += ch_item(q, pt, a.t);
       if (++a.t * pt >= q.n) {
         a.t = 0;
         if (++a.hk == p.Hk) a.hk = 0, a.s = with_rows(a.s + 1);
@@ -535,7 +545,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       a.t = lo;
       a.cost = x - rem + ch_before(q, pt, lo);
       const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
-      const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + CH_STEP / 2) / CH_STEP;
+      const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + q.w * CH_STEP / 2) / (q.w * CH_STEP);
       a.kb = kb < CH_PART ? 0 : (int)kb;
       if (a.kb > steps - CH_PART && a.kb > 0) a = after(a, q);
       return a;
@@ -549,7 +559,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     }
     uint32_t n = 0;
     ChPlace end = z;
-    ChSeq q = {0, 0, 0};
+    ChSeq q = {0, 0, 0, 4};
     int it_seq = -1;
     bool ok = true;
     while (ok) {
@@ -558,7 +568,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       bool stop = true;
       if (more) {
         if (!out) q = plan_seq[a.s];
-        else if (a.s != it_seq) q = ch_sequence(p, a.s);
+        else if (a.s != it_seq) q = ch_sequence(p, a.s, pt1, C::TILES);
         it_seq = a.s;
         const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
         it.row0 = q.first + a.t * pt;
@@ -570,8 +580,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         stop = a.s == end.s && a.hk == end.hk && a.t == end.t;
         it.kb1 = stop ? end.kb : steps;
         if (it.kb0 > 0 || it.kb1 < steps) {   // (border() takes what is less than CH_PART steps from an end as the end)
-          it.head = cta_at(a.cost + CH_START - CH_STEP / 2 + CH_PART * CH_STEP - 1);
-          it.parts = cta_at(a.cost + CH_START - CH_STEP / 2 + (long long)(steps - CH_PART + 1) * CH_STEP - 1) - it.head + 1;
+          const long long from = a.cost + CH_START - q.w * CH_STEP / 2 - 1, step = q.w * CH_STEP;
+          it.head = cta_at(from + CH_PART * step);
+          it.parts = cta_at(from + (steps - CH_PART + 1) * step) - it.head + 1;
           it.part = cta - it.head;
         }
       }
