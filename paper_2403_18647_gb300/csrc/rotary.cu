@@ -4,10 +4,11 @@
 //   dimensions;  queries -> q_out, keys and values -> bf16 rows of the sequence's pages
 //
 // Written as y = x c + partner s with s negated in a pair's first place, one expression serves both layouts.  What
-// bounds it is memory: every row is read and written once.  A warp takes RT_U x (128 / HD) heads of one row, four
-// values a lane, all of them loaded before the row's sequence, slot and page are looked up, so that those
-// dependent loads run beside the wide ones.  Norm and rotation stay in registers (shuffles); sums are fp32, the
-// table's angles are reduced in double (an fp32 angle of position 30000 is off by 1e-3).
+// bounds it is memory, then instructions: rows are read and written once, 16 bytes a lane.  A warp takes heads of one
+// row, RT_U of them on each of its parts at a time, the next ones asked for before these are worked on; the first are
+// asked for before the row's sequence, slot and page are looked up, so that those dependent loads run beside the wide
+// ones.  Norm and rotation stay in registers (shuffles); sums are fp32, the table's angles are reduced in double (an
+// fp32 angle of position 30000 is off by 1e-3).
 #include <algorithm>
 
 #include "common.cuh"
@@ -16,7 +17,10 @@
 namespace sdsat {
 
 constexpr int RT_WARPS = 4;
-constexpr int RT_U = 4;
+constexpr int RT_U = 2;
+// Warps that an SM should have before a warp takes more heads of its row (us: 8500 rows of 32 / 8 bf16 heads 46 at 32, 55 at 128,
+// 73 at 512; 4095 rows of 40 / 40 fp32 heads 81 at 32, 75 at 128 and 512).
+constexpr int rt_fill(bool bf16) { return bf16 ? 32 : 128; }
 
 __global__ void rope_table_kernel(const RopeBuild f, float2* turn, int n, int pairs) {
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
@@ -53,45 +57,34 @@ __device__ __forceinline__ int sequence_of(const int* start, int b, int r, int l
   return s;
 }
 
-__device__ __forceinline__ float one_of(const float (&v)[4], int i) {
-  const float a = i & 1 ? v[1] : v[0], z = i & 1 ? v[3] : v[2];
-  return i & 2 ? z : a;
-}
+enum RotaryLayout : int {
+  ROT_INTERLEAVED = 0,   // the partner of place e is e ^ 1
+  ROT_LANES = 1,         // e + half or e - half, whole lanes away
+  ROT_ANY = 2,           // ... some lanes and places away
+};
 
-template <bool BF16, int HD>
-__global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __grid_constant__ RotaryParams p, int groups) {
-  constexpr int HPW = 128 / HD, LANES = 32 / HPW;   // heads side by side in a warp, lanes of one
-  const int lane = threadIdx.x & 31, sub = lane / LANES, e0 = lane % LANES * 4;
+// heads: how many of a row a warp takes, a multiple of RT_U times its parts
+template <bool BF16, int HD, int LAYOUT, bool NORM>
+__global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __grid_constant__ RotaryParams p, int groups, int heads) {
+  constexpr int E = BF16 ? 8 : 4;                        // values of a lane
+  constexpr int LANES = HD / E, PARTS = 32 / LANES;      // lanes of a head, heads side by side in a warp
+  using Raw = uint4;
+  const int lane = threadIdx.x & 31, part = lane / LANES, e0 = lane % LANES * E;
   const long long w = (long long)blockIdx.x * RT_WARPS + (threadIdx.x >> 5);
-  const int r = (int)(w / groups), g = (int)(w % groups);
+  const int r = (int)(w / groups), h0 = (int)(w % groups) * heads + part;
   pdl_trigger();
   pdl_wait();
   if (r >= p.rows) return;
-  const int NH = p.H + 2 * p.Hk;
-  float x[RT_U][4];
+  const int Hqk = p.H + p.Hk, NH = min(Hqk + p.Hk, h0 - part + heads);
+  constexpr int size = BF16 ? 2 : 4;
+  // where head h of queries, keys or values stands: base + h HD values
+  const char* q_row = static_cast<const char*>(p.q) + (r * p.q_ld + e0) * size;
+  const char* k_row = static_cast<const char*>(p.k) + (r * p.k_ld - (long long)p.H * HD + e0) * size;
+  const char* v_row = static_cast<const char*>(p.v) + (r * p.v_ld - (long long)Hqk * HD + e0) * size;
+  auto load = [&](int h) { return h < NH ? *reinterpret_cast<const Raw*>((h < p.H ? q_row : h < Hqk ? k_row : v_row) + (long long)h * (HD * size)) : make_uint4(0u, 0u, 0u, 0u); };
+  Raw raw[RT_U];
 #pragma unroll
-  for (int u = 0; u < RT_U; ++u) {
-    const int h = (g * RT_U + u) * HPW + sub;
-    const void* src = p.q;
-    long long at = r * p.q_ld + h * HD + e0;
-    if (h >= p.H + p.Hk) src = p.v, at = r * p.v_ld + (h - p.H - p.Hk) * HD + e0;
-    else if (h >= p.H) src = p.k, at = r * p.k_ld + (h - p.H) * HD + e0;
-    if (h < NH) {
-      if (BF16) {
-        const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(src) + at);
-        x[u][0] = __uint_as_float(b.x << 16);
-        x[u][1] = __uint_as_float(b.x & 0xFFFF0000u);
-        x[u][2] = __uint_as_float(b.y << 16);
-        x[u][3] = __uint_as_float(b.y & 0xFFFF0000u);
-      } else {
-        const float4 f = *reinterpret_cast<const float4*>(static_cast<const float*>(src) + at);
-        x[u][0] = f.x, x[u][1] = f.y, x[u][2] = f.z, x[u][3] = f.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[u][i] = 0.f;
-    }
-  }
+  for (int u = 0; u < RT_U; ++u) raw[u] = load(h0 + u * PARTS);
 
   int first = 0;
   const int s = sequence_of(p.start, p.b, r, lane, first);
@@ -99,7 +92,7 @@ __global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __gr
   const long long slot = (long long)__ldcg(p.len + s) + (r - first);
   // the row of the sequence's page, -1: not written
   long long row = -1;
-  if ((g + 1) * RT_U * HPW > p.H) {
+  if (h0 - part + heads > p.H) {
     if (slot >= 0 && slot < (long long)p.pages.ld * KV_PAGE) {
       const int page = __ldcg(p.pages.table + (size_t)s * p.pages.ld + slot / KV_PAGE);
       if (page >= 0 && page < p.pages.n && (!p.pages.refs || __ldcg(p.pages.refs + page) == 1))
@@ -112,75 +105,161 @@ __global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __gr
     if (lane == 0) set_error(p.err, ERR_POSITION);
     pos = pos < 0 ? 0 : p.rope.n - 1;
   }
-  // this lane's four places: y = x c + partner s
-  const int dims = p.rope.dims, half = dims / 2, d = half & 3;
-  float c[4], t[4];
-  bool turned[4];
+  char* out_row = static_cast<char*>(p.q_out) + (r * p.out_ld + e0) * size;
+  __nv_bfloat16* k_slot = p.k_pages + (row - (long long)p.H * KV_PAGE) * HD + e0;
+  __nv_bfloat16* v_slot = p.v_pages + (row - (long long)Hqk * KV_PAGE) * HD + e0;
+
+  // this lane's places: y = x c + partner t
+  const int dims = p.rope.dims, half = dims / 2;
+  const float2* turn = p.rope.turn + pos * half;
+  const int e_pair = LAYOUT == ROT_INTERLEAVED ? e0 >> 1 : e0 < half ? e0 : e0 - half;   // (ROT_LANES: of the first place)
+  float c[E], t[E];
+  const bool turned = e0 < dims;   // (ROT_ANY: some of the places)
+  if (LAYOUT == ROT_ANY) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int e = e0 + i;
-    turned[i] = e < dims;
-    const bool head = p.rope.interleaved ? !(e & 1) : e < half;
-    const int pair = p.rope.interleaved ? e >> 1 : head ? e : e - half;
-    const float2 cs = turned[i] ? __ldg(p.rope.turn + pos * half + pair) : make_float2(1.f, 0.f);
-    c[i] = cs.x;
-    t[i] = head ? -cs.y : cs.y;
-  }
-#pragma unroll
-  for (int u = 0; u < RT_U; ++u) {
-    const int h = (g * RT_U + u) * HPW + sub;
-    const bool is_q = h < p.H, is_v = h >= p.H + p.Hk;
-    float y[4] = {x[u][0], x[u][1], x[u][2], x[u][3]};
-    const __nv_bfloat16* gain = is_q ? p.q_gain : is_v ? nullptr : p.k_gain;
-    float sq = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sq = fmaf(y[i], y[i], sq);
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-    if (gain) {
-      const float f = rsqrtf(sq * (1.0f / HD) + p.eps);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = y[i] * f * __bfloat162float(gain[e0 + i]);
+    for (int i = 0; i < E; ++i) {
+      const int e = e0 + i;
+      const float2 cs = e < dims ? __ldg(turn + (e < half ? e : e - half)) : make_float2(1.f, 0.f);
+      c[i] = cs.x;
+      t[i] = e < half ? -cs.y : cs.y;
     }
-    float z[4];
-    if (p.rope.interleaved) {
+  } else if (LAYOUT == ROT_LANES) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) z[i] = y[i ^ 1];
-    } else {
-      // the partner of place e is e + half or e - half: (half >> 2) lanes on or back, and d places
+    for (int i = 0; i < E; i += 2) {   // (half is even: rows of the table are 16-byte aligned)
+      const float4 cs = turned ? __ldg(reinterpret_cast<const float4*>(turn + e_pair + i)) : make_float4(1.f, 0.f, 1.f, 0.f);
+      c[i] = cs.x, c[i + 1] = cs.z;
+      t[i] = e0 < half ? -cs.y : cs.y, t[i + 1] = e0 < half ? -cs.w : cs.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; i += 2) {
+      const float2 cs = e0 + i < dims ? __ldg(turn + e_pair + i / 2) : make_float2(1.f, 0.f);
+      c[i] = c[i + 1] = cs.x;
+      t[i] = -cs.y, t[i + 1] = cs.y;
+    }
+  }
+  uint32_t gain[2][E / 2];   // of queries and keys
+  if (NORM)
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const uint16_t* from = reinterpret_cast<const uint16_t*>(g ? p.k_gain : p.q_gain);
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) gain[g][i] = from ? (uint32_t)from[e0 + 2 * i] | (uint32_t)from[e0 + 2 * i + 1] << 16 : 0u;
+    }
+  const int on = lane + (e0 < half ? half / E : -(half / E));   // ROT_LANES: the partner's lane
+
+  for (int h_at = h0; h_at - part < NH; h_at += RT_U * PARTS) {
+    Raw now[RT_U];
+#pragma unroll
+    for (int u = 0; u < RT_U; ++u) {
+      now[u] = raw[u];
+      raw[u] = load(h_at + (RT_U + u) * PARTS);
+    }
+#pragma unroll
+    for (int u = 0; u < RT_U; ++u) {
+      const int h = h_at + u * PARTS;
+      const bool is_v = h >= Hqk, is_q = h < p.H;
+      float y[E];
+      const uint32_t word[4] = {now[u].x, now[u].y, now[u].z, now[u].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float on = __shfl_sync(0xffffffffu, one_of(y, (i + d) & 3), lane + (half >> 2) + ((i + d) >> 2));
-        const float back = __shfl_sync(0xffffffffu, one_of(y, (i - d) & 3), lane - (half >> 2) - (i < d ? 1 : 0));
-        z[i] = e0 + i < half ? on : back;
+        if (BF16) {
+          y[(2 * i) % E] = __uint_as_float(word[i] << 16);
+          y[(2 * i + 1) % E] = __uint_as_float(word[i] & 0xFFFF0000u);
+        } else {
+          y[i] = __uint_as_float(word[i]);
+        }
       }
-    }
+      if (NORM) {
+        float sq = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (turned[i] && !is_v) y[i] = fmaf(y[i], c[i], z[i] * t[i]);
-    __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
-    const uint2 packed = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
-    if (is_q) {
-      const long long at = r * p.out_ld + h * HD + e0;
-      if (BF16) *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.q_out) + at) = packed;
-      else *reinterpret_cast<float4*>(static_cast<float*>(p.q_out) + at) = make_float4(y[0], y[1], y[2], y[3]);
-    } else if (h < NH && row >= 0) {
-      const int hk = is_v ? h - p.H - p.Hk : h - p.H;
-      *reinterpret_cast<uint2*>((is_v ? p.v_pages : p.k_pages) + (row + (long long)hk * KV_PAGE) * HD + e0) = packed;
+        for (int i = 0; i < E; ++i) sq = fmaf(y[i], y[i], sq);
+#pragma unroll
+        for (int o = LANES / 2; o; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        if (!is_v && (is_q ? p.q_gain : p.k_gain)) {
+          const float f = rsqrtf(sq * (1.0f / HD) + p.eps);
+#pragma unroll
+          for (int i = 0; i < E; i += 2) {
+            const uint32_t g = is_q ? gain[0][i / 2] : gain[1][i / 2];
+            y[i] = y[i] * f * __uint_as_float(g << 16);
+            y[i + 1] = y[i + 1] * f * __uint_as_float(g & 0xFFFF0000u);
+          }
+        }
+      }
+      float z[E];
+      if (LAYOUT == ROT_INTERLEAVED) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) z[i] = y[i ^ 1];
+      } else if (LAYOUT == ROT_LANES) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) z[i] = __shfl_sync(0xffffffffu, y[i], on);
+      } else {
+        // (half / E) lanes and half % E places on, or back
+        const int d = half % E, lanes = half / E;
+        auto one_of = [&](int i) {
+          float v = y[0];
+#pragma unroll
+          for (int k = 1; k < E; ++k)
+            if (i == k) v = y[k];
+          return v;
+        };
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float f = __shfl_sync(0xffffffffu, one_of((i + d) % E), lane + lanes + (i + d) / E);
+          const float b = __shfl_sync(0xffffffffu, one_of((i + E - d) % E), lane - lanes - (i < d ? 1 : 0));
+          z[i] = e0 + i < half ? f : b;
+        }
+      }
+      if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (LAYOUT == ROT_LANES ? turned : e0 + i < dims) y[i] = fmaf(y[i], c[i], z[i] * t[i]);
+      }
+      if (h >= NH) continue;
+      uint32_t packed[E / 2];
+#pragma unroll
+      for (int i = 0; i < E; i += 2) {
+        const __nv_bfloat162 two = __floats2bfloat162_rn(y[i], y[i + 1]);
+        packed[i / 2] = *reinterpret_cast<const uint32_t*>(&two);
+      }
+      if (is_q && !BF16) {
+        *reinterpret_cast<float4*>(out_row + (long long)h * (HD * size)) = make_float4(y[0], y[1], y[2], y[3]);
+      } else if (is_q || row >= 0) {
+        char* to = is_q ? out_row + (long long)h * (HD * size) : reinterpret_cast<char*>((is_v ? v_slot : k_slot) + (long long)h * (KV_PAGE * HD));
+        if constexpr (BF16) *reinterpret_cast<uint4*>(to) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+        else *reinterpret_cast<uint2*>(to) = make_uint2(packed[0], packed[1]);
+      }
     }
   }
 }
 
+template <bool BF16, int HD, int LAYOUT>
+static cudaError_t rt_prepare() {
+  const cudaError_t e = prefer_shared(rotary_append_kernel<BF16, HD, LAYOUT, false>);
+  return e == cudaSuccess ? prefer_shared(rotary_append_kernel<BF16, HD, LAYOUT, true>) : e;
+}
+template <bool BF16, int HD>
+static cudaError_t rt_prepare() {
+  cudaError_t e = rt_prepare<BF16, HD, ROT_INTERLEAVED>();
+  if (e == cudaSuccess) e = rt_prepare<BF16, HD, ROT_LANES>();
+  return e == cudaSuccess ? rt_prepare<BF16, HD, ROT_ANY>() : e;
+}
 cudaError_t rotary_prepare() {
-  cudaError_t e = prefer_shared(rotary_append_kernel<false, 64>);
-  if (e == cudaSuccess) e = prefer_shared(rotary_append_kernel<false, 128>);
-  if (e == cudaSuccess) e = prefer_shared(rotary_append_kernel<true, 64>);
-  if (e == cudaSuccess) e = prefer_shared(rotary_append_kernel<true, 128>);
-  return e;
+  cudaError_t e = rt_prepare<false, 64>();
+  if (e == cudaSuccess) e = rt_prepare<false, 128>();
+  if (e == cudaSuccess) e = rt_prepare<true, 64>();
+  return e == cudaSuccess ? rt_prepare<true, 128>() : e;
 }
 
-cudaError_t launch_rotary_append(const RotaryParams& p, int, cudaStream_t st, bool pdl) {
-  const int per = RT_U * (128 / p.hd), groups = (p.H + 2 * p.Hk + per - 1) / per;
+template <bool BF16, int HD, int LAYOUT>
+static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
+  constexpr int step = RT_U * (32 * (BF16 ? 8 : 4) / HD);   // heads of a warp at a time
+  const int steps = (p.H + 2 * p.Hk + step - 1) / step;
+  // whole rows to a warp once those fill the SMs, fewer heads while they do not
+  int groups = 1;
+  while (groups < steps && (long long)p.rows * groups < (long long)rt_fill(BF16) * num_sms) ++groups;
+  const int per = (steps + groups - 1) / groups;
+  groups = (steps + per - 1) / per;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(((long long)p.rows * groups + RT_WARPS - 1) / RT_WARPS));
   cfg.blockDim = dim3(RT_WARPS * 32);
@@ -190,11 +269,17 @@ cudaError_t launch_rotary_append(const RotaryParams& p, int, cudaStream_t st, bo
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
-  if (p.bf16)
-    return p.hd == 64 ? cudaLaunchKernelEx(&cfg, rotary_append_kernel<true, 64>, p, groups)
-                      : cudaLaunchKernelEx(&cfg, rotary_append_kernel<true, 128>, p, groups);
-  return p.hd == 64 ? cudaLaunchKernelEx(&cfg, rotary_append_kernel<false, 64>, p, groups)
-                    : cudaLaunchKernelEx(&cfg, rotary_append_kernel<false, 128>, p, groups);
+  return p.q_gain || p.k_gain ? cudaLaunchKernelEx(&cfg, rotary_append_kernel<BF16, HD, LAYOUT, true>, p, groups, per * step)
+                              : cudaLaunchKernelEx(&cfg, rotary_append_kernel<BF16, HD, LAYOUT, false>, p, groups, per * step);
+}
+template <bool BF16, int HD>
+static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
+  if (p.rope.interleaved) return rt_launch<BF16, HD, ROT_INTERLEAVED>(p, num_sms, st, pdl);
+  return p.rope.dims / 2 % (BF16 ? 8 : 4) ? rt_launch<BF16, HD, ROT_ANY>(p, num_sms, st, pdl) : rt_launch<BF16, HD, ROT_LANES>(p, num_sms, st, pdl);
+}
+cudaError_t launch_rotary_append(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
+  if (p.bf16) return p.hd == 64 ? rt_launch<true, 64>(p, num_sms, st, pdl) : rt_launch<true, 128>(p, num_sms, st, pdl);
+  return p.hd == 64 ? rt_launch<false, 64>(p, num_sms, st, pdl) : rt_launch<false, 128>(p, num_sms, st, pdl);
 }
 
 }  // namespace sdsat
