@@ -18,9 +18,8 @@
 
 namespace sdsat {
 
-constexpr int ADJ_THREADS = 256;
 constexpr int ADJ_U = 4;                                      // vectors of a thread in flight
-constexpr int ADJ_STRETCH = 8192;                             // ids of a stretch at most
+constexpr int ADJ_STRETCH = 16384;                            // ids of a stretch at most
 constexpr uint32_t ADJ_PROMPT = 1u << 31;
 constexpr int ADJ_BIAS_SHIFT = 20;                            // 11 bits: ADJ_MAX_BIAS - place, 0: none
 constexpr uint32_t ADJ_COUNT = (1u << ADJ_BIAS_SHIFT) - 1;   // a history and a block's tokens stay below it
@@ -76,13 +75,14 @@ __device__ __forceinline__ void adj_mask(uint4& x, uint32_t ok) {
   }
 }
 
-// rp: rows of a sequence that one CTA takes; ch: ids of a stretch (a multiple of 128)
-template <bool BF16>
-__global__ void __launch_bounds__(ADJ_THREADS, 4) adjust_kernel(const __grid_constant__ AdjustParams p, int rp, int ch, int parts, int chunks) {
+// rp: rows of a sequence that one CTA takes; ch: ids of a stretch (a multiple of 128, ADJ_STRETCH at most)
+template <bool BF16, int ADJ_THREADS>
+__global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel(const __grid_constant__ AdjustParams p, int rp, int ch, int parts, int chunks) {
   extern __shared__ uint4 adj_mem[];
   uint32_t* words = reinterpret_cast<uint32_t*>(adj_mem);            // [ch]
   uint16_t* list = reinterpret_cast<uint16_t*>(words + ch);          // [ch + ADJ_AGAIN]
   int* listed = reinterpret_cast<int*>(list + ch + ADJ_AGAIN);
+  __shared__ uint16_t queue[ADJ_THREADS / 32][64];           // of a warp: tokens of the stretch, bit 15: of the prompt
   constexpr int VEC = BF16 ? 8 : 4;         // values of 16 bytes
   constexpr int size = BF16 ? 2 : 4;
   const int tid = threadIdx.x, lane = tid & 31;
@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(ADJ_THREADS, 4) adjust_kernel(const __grid_con
   if (tid == 0) *listed = 0;
   pdl_trigger();
   pdl_wait();
+  const int n_history = p.history ? __ldg(p.history_len + s) : 0, n_prompt = p.history && p.prompt_len ? __ldg(p.prompt_len + s) : 0;
   int largest = -1;   // of the ids
   auto here = [&](int id) { return (uint32_t)id - (uint32_t)v0 < (uint32_t)nv; };
   auto list_it = [&](uint32_t before, int id) {
@@ -181,22 +182,65 @@ __global__ void __launch_bounds__(ADJ_THREADS, 4) adjust_kernel(const __grid_con
         __syncthreads();
       }
       if (p.history) {
-        const int n = min(max(__ldg(p.history_len + s), 0), p.history_ld), np = p.prompt_len ? __ldg(p.prompt_len + s) : 0;
+        // Few of a history's tokens are in the stretch, but some of a warp's 32 nearly always: they are queued, and
+        // counted when there is one for each lane.
+        const int n = min(max(n_history, 0), p.history_ld);
         const int* text = p.history + (size_t)s * p.history_ld;
-        int i = tid;
+        uint16_t* q = queue[tid >> 5];
+        int held = 0;
+        auto count = [&](uint16_t t) {
+          const int id = v0 + (t & 0x7FFF);
+          list_it(t & 0x8000 ? atomicOr(&words[id - v0], ADJ_PROMPT) : atomicAdd(&words[id - v0], 1u), id);
+        };
+        auto offer = [&](int id, int i) {
+          largest = max(largest, id);
+          const bool mine_too = here(id);
+          const unsigned some = __ballot_sync(0xffffffffu, mine_too);
+          if (!some) return;
+          if (mine_too) q[held + __popc(some & ((1u << lane) - 1u))] = (uint16_t)((id - v0) | (i < n_prompt ? 0x8000 : 0));
+          held += __popc(some);
+          __syncwarp();
+          if (held < 32) return;
+          count(q[lane]);
+          __syncwarp();
+          const uint16_t rest = q[32 + lane];
+          __syncwarp();
+          q[lane] = rest;
+          held -= 32;
+          __syncwarp();
+        };
+        int i0 = 0;
         if ((reinterpret_cast<uintptr_t>(text) & 15u) == 0) {   // four at a time
-#pragma unroll 2
-          for (int k = tid; k < n / 4; k += ADJ_THREADS) {
-            const int4 id = __ldg(reinterpret_cast<const int4*>(text) + k);
-            token(id.x, 4 * k < np);
-            token(id.y, 4 * k + 1 < np);
-            token(id.z, 4 * k + 2 < np);
-            token(id.w, 4 * k + 3 < np);
+          constexpr int N = 2;
+#pragma unroll 1
+          for (; i0 + 4 * ADJ_THREADS * (N - 1) < n; i0 += 4 * ADJ_THREADS * N) {
+            int4 id[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+              const int i = i0 + 4 * (u * ADJ_THREADS + tid);
+              id[u] = i + 3 < n ? __ldg(reinterpret_cast<const int4*>(text + i)) : make_int4(-1, -1, -1, -1);
+              if (i < n && i + 3 >= n) {
+                id[u].x = __ldg(text + i);
+                if (i + 1 < n) id[u].y = __ldg(text + i + 1);
+                if (i + 2 < n) id[u].z = __ldg(text + i + 2);
+              }
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+              const int i = i0 + 4 * (u * ADJ_THREADS + tid);
+              offer(id[u].x, i);
+              offer(id[u].y, i + 1);
+              offer(id[u].z, i + 2);
+              offer(id[u].w, i + 3);
+            }
           }
-          i += n & ~3;
         }
-#pragma unroll 8
-        for (; i < n; i += ADJ_THREADS) token(__ldg(text + i), i < np);
+#pragma unroll 4
+        for (; i0 < n; i0 += ADJ_THREADS) {
+          const int i = i0 + tid;
+          offer(i < n ? __ldg(text + i) : -1, i);
+        }
+        if (lane < held) count(q[lane]);
       }
       if (p.tokens && !p.anc && tid < j0) token(__ldg(p.tokens + s * p.q + tid), false);   // (a chain: row j comes after tokens 0 .. j)
     }
@@ -230,25 +274,29 @@ __global__ void __launch_bounds__(ADJ_THREADS, 4) adjust_kernel(const __grid_con
   if (largest >= p.V) set_error(p.err, ERR_TOKEN);
 }
 
+template <bool BF16>
+static cudaError_t adj_prepare() {
+  cudaError_t e = cudaFuncSetAttribute(adjust_kernel<BF16, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)adj_smem(ADJ_STRETCH));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adjust_kernel<BF16, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)adj_smem(ADJ_STRETCH));
+  if (e == cudaSuccess) e = prefer_shared(adjust_kernel<BF16, 256>);
+  return e == cudaSuccess ? prefer_shared(adjust_kernel<BF16, 512>) : e;
+}
 cudaError_t adjust_prepare() {
-  cudaError_t e = cudaFuncSetAttribute(adjust_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)adj_smem(ADJ_STRETCH));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adjust_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)adj_smem(ADJ_STRETCH));
-  if (e == cudaSuccess) e = prefer_shared(adjust_kernel<false>);
-  if (e == cudaSuccess) e = prefer_shared(adjust_kernel<true>);
-  return e;
+  const cudaError_t e = adj_prepare<false>();
+  return e == cudaSuccess ? adj_prepare<true>() : e;
 }
 
 cudaError_t launch_adjust(const AdjustParams& p, int num_sms, cudaStream_t st, bool pdl) {
-  // Long stretches and all rows of a sequence in one CTA read the history least often; shorter ones and a CTA for each
-  // row where that leaves SMs without one.
+  // Long stretches, of more threads, and all rows of a sequence in one CTA read the history least often; shorter ones and
+  // a CTA for each row where that leaves SMs without one.
   int ch = ADJ_STRETCH, rp = p.q;
   auto ctas = [&](int c, int r) { return (long long)p.b * ((p.q + r - 1) / r) * ((p.V + c - 1) / c); };
   if (ctas(ch, rp) < 2 * num_sms) rp = 1;
   while (ch > 1024 && ctas(ch, rp) < 2 * num_sms) ch /= 2;
-  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch;
+  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch, threads = ch == ADJ_STRETCH ? 512 : 256;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.b * parts * chunks));
-  cfg.blockDim = dim3(ADJ_THREADS);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = adj_smem(ch);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -256,8 +304,11 @@ cudaError_t launch_adjust(const AdjustParams& p, int num_sms, cudaStream_t st, b
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
-  return p.bf16 ? cudaLaunchKernelEx(&cfg, adjust_kernel<true>, p, rp, ch, parts, chunks)
-                : cudaLaunchKernelEx(&cfg, adjust_kernel<false>, p, rp, ch, parts, chunks);
+  if (threads == 512)
+    return p.bf16 ? cudaLaunchKernelEx(&cfg, adjust_kernel<true, 512>, p, rp, ch, parts, chunks)
+                  : cudaLaunchKernelEx(&cfg, adjust_kernel<false, 512>, p, rp, ch, parts, chunks);
+  return p.bf16 ? cudaLaunchKernelEx(&cfg, adjust_kernel<true, 256>, p, rp, ch, parts, chunks)
+                : cudaLaunchKernelEx(&cfg, adjust_kernel<false, 256>, p, rp, ch, parts, chunks);
 }
 
 }  // namespace sdsat
