@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
     const uint32_t* allowed = p.allowed ? p.allowed + (size_t)r * p.allowed_ld + (v0 >> 5) : nullptr;
     const int mask_words = (p.V + 31) / 32 - (v0 >> 5);
     uint4 x[ADJ_U];
-    uint32_t ok[ADJ_U];
+    uint32_t mask[ADJ_U][2];   // the words that a vector's bits begin in and may go on in
     auto load = [&](int k) { return k >= v_first && k <= v_last ? vin[k] : make_uint4(0u, 0u, 0u, 0u); };
     auto ask = [&](int k0) {
 #pragma unroll
@@ -135,8 +135,8 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
         x[u] = load(k);
         if (allowed && k < nvec) {
           const int w = max(e, 0) >> 5;
-          const uint32_t a0 = __ldg(allowed + w), a1 = __ldg(allowed + min(w + 1, mask_words - 1));
-          ok[u] = e < 0 ? a0 << -e : __funnelshift_r(a0, a1, e);
+          mask[u][0] = __ldg(allowed + w);
+          mask[u][1] = __ldg(allowed + min(w + 1, mask_words - 1));
         }
       }
     };
@@ -155,7 +155,10 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
           x[u] = shift < 4 ? adj_shift<0>(x[u], y, half) : shift < 8 ? adj_shift<1>(x[u], y, half) : shift < 12 ? adj_shift<2>(x[u], y, half)
                                                                                                       : adj_shift<3>(x[u], y, half);
         }
-        if (allowed) adj_mask<BF16>(x[u], ok[u]);
+        if (allowed) {
+          const int e = k * VEC - lead;
+          adj_mask<BF16>(x[u], e < 0 ? mask[u][0] << -e : __funnelshift_r(mask[u][0], mask[u][1], e));
+        }
         if (k > 0 && k < nvec - 1) {
           vout[k] = x[u];
         } else if (k < nvec) {   // (perhaps not whole)
@@ -289,11 +292,12 @@ cudaError_t adjust_prepare() {
 cudaError_t launch_adjust(const AdjustParams& p, int num_sms, cudaStream_t st, bool pdl) {
   // Long stretches, of more threads, and all rows of a sequence in one CTA read the history least often; shorter ones and
   // a CTA for each row where that leaves SMs without one.
-  int ch = ADJ_STRETCH, rp = p.q;
+  const int most = 512 * ADJ_U * (p.bf16 ? 8 : 4) - 128;   // (whose vectors, one more than whole ones, the threads ask for at once)
+  int ch = most, rp = p.q;
   auto ctas = [&](int c, int r) { return (long long)p.b * ((p.q + r - 1) / r) * ((p.V + c - 1) / c); };
   if (ctas(ch, rp) < 2 * num_sms) rp = 1;
-  while (ch > 1024 && ctas(ch, rp) < 2 * num_sms) ch /= 2;
-  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch, threads = ch == ADJ_STRETCH ? 512 : 256;
+  while (ch > 1024 && ctas(ch, rp) < 2 * num_sms) ch = (ch / 2 + 127) / 128 * 128;
+  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch, threads = ch == most ? 512 : 256;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.b * parts * chunks));
   cfg.blockDim = dim3(threads);
