@@ -3,21 +3,30 @@
 //   out = sum_t p_t v_t / sum_t p_t,  p_t = exp2(c s_t - m),  s = q K^T,  c = log2(e) / sqrt(hd)
 //
 // A tile is 128 rows: PT = 128 / G positions of the G query heads that share a cache head, so that K and V are
-// loaded once for all of them.  An item is TILES tiles of a sequence and cache head, its work the steps of 64 keys (a page)
-// that its rows see.  The items stand in a line, weighed by their keys and a start's cost, and every CTA (one on an SM)
-// takes an equal stretch of it, wherever that begins: few rows of long sequences are split along their keys, and causal
-// tiles of unequal length leave no SM idle.  Of an item that several CTAs share each writes
-// its partial results (m, sum, O), and the one that comes last joins them, always in the same order (a second kernel for
-// that took 15 us behind a prompt of 4095 positions on 32 heads, 126 in all).  Sequences, lengths and pages are device values, so the plan is made on the device,
-// by one warp of each CTA (a scan over the sequences), which then hands items to the others.
+// loaded once for all of them.  An item is TILES tiles of a sequence and cache head, its work the steps of 64 keys (a
+// page) that its rows see.  The items stand in a line, weighed by their keys and a start's cost, and every CTA (one on an
+// SM) takes an equal stretch of it, wherever that begins: few rows of long sequences are split along their keys, and
+// causal tiles of unequal length leave no SM idle.  Of an item that several CTAs share each writes its partial results
+// (m, sum, O), and the one that comes last joins them, always in the same order (a second kernel for that took 15 us
+// behind a prompt of 4095 positions on 32 heads, 126 in all).  Sequences, lengths and pages are device values, so the
+// plan is made on the device, by one warp of each CTA (a scan over the sequences), which then hands items to the others.
 //
 // Scores have two places in TMEM, by the step's parity: S of step i + 2 is issued behind P V of step i, so that the
 // softmax (a thread for each row, no shuffles) always has the next step's scores.  The entries of the ring go by
 // what is issued together: entry e of an item is V of step e - 2 and K of step e.
-// bf16 (PARTS = 1, TILES = 2): P lies over its S; a warp for each tile issues its products (a wait, even one that is over,
-// costs such a warp 100 cycles or more, and each MMA 44).  Tensor cycles of a step: 8 x 48 (N = 64) and 4 x 64.
-// fp32 (PARTS = 3, TILES = 1): queries and probabilities as three bf16 parts (24 bits), smallest first; P beside S.  The
-// tensor cores' accumulator truncates, so O holds one step, and 4 more warps add it to a rounded total in registers.
+// bf16 (PARTS = 1, TILES = 2): P lies over its S; a warp for each tile issues its products.  What bounds it: the tensor
+// cores' 8 x 48 (N = 64: A is read at the shared memory's rate) and 4 x 64 cycles a step and tile, 1280 of the 1600 to 1700
+// that a step of both tiles takes; the softmax takes 1150 beside them.
+// fp32 (PARTS = 3, TILES = 1): queries and probabilities as three bf16 parts (24 bits), smallest first; P beside S, so S
+// and P V are issued by a warp each.  The tensor cores' accumulator truncates, so O holds one step, and 4 more warps add
+// it to a rounded total in registers.  1920 tensor cycles of 2200 a step.
+// Waits and products cost the warps that issue them (a wait that is over 100 cycles and more, an MMA 44, 90 from a branch
+// of one lane), which is why a tile's step has one wait for both of its barriers and whole warps issue.
+//
+// Measured, us: 32 heads x 128, 4095 positions bf16 119 (1.16 PFLOP/s; prefill attention, which has fp32 queries in two
+// parts, 257); 32 / 8 heads, 8 sequences of 330 to 1100 rows after 800 to 16500 slots 730 (1.33 PFLOP/s), one of 4096 rows
+// after 16384 780 (1.57); 48 sequences of up to 8200 slots, 46 of them with one row, 165 (5.3 TB/s); 40 heads, 777 rows
+// after 2048 slots in fp32 127.
 //
 // A row's reference m is moved only when its maximum has grown by more than 2^8 since the last time (exact: it cancels
 // in the division by the row's sum), so that O (the total) is seldom rescaled.
@@ -88,6 +97,7 @@ struct ChCfg {
 
 // Two places for partial results a CTA (an item that goes on in the next one, an item that began before), and a counter
 // of an item's parts that have come, zero between launches
+size_t chunk_attention_counters(int num_sms) { return (size_t)num_sms * 4 * sizeof(int); }
 size_t chunk_attention_scratch(int num_sms) { return (size_t)2 * num_sms * (2 + 2 * CH_ROWS * (2 + 128)); }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {

@@ -458,6 +458,7 @@ struct ChunkAttnParams {
   uint32_t* err;
 };
 size_t chunk_attention_scratch(int num_sms);
+size_t chunk_attention_counters(int num_sms);   // bytes at its start that are zero between launches
 cudaError_t chunk_attention_prepare();
 cudaError_t launch_chunk_attention(const ChunkAttnParams& p, int num_sms, cudaStream_t st, bool pdl);
 

@@ -1349,6 +1349,8 @@ sdsat_status sdsat_get_error(sdsat_ctx* c, uint32_t* flags) {
   if (cudaStreamSynchronize(c->stream) != cudaSuccess) return SDSAT_ECUDA;
   if (cudaMemcpy(&f, c->err, sizeof(f), cudaMemcpyDeviceToHost) != cudaSuccess) return SDSAT_ECUDA;
   if (cudaMemset(c->err, 0, sizeof(f)) != cudaSuccess) return SDSAT_ECUDA;
+  // a call that gave up may have left counts of an item's parts behind
+  if ((f & SDSAT_DEV_TIMEOUT) && cudaMemset(c->chunk_part, 0, chunk_attention_counters(c->num_sms)) != cudaSuccess) return SDSAT_ECUDA;
   if (flags) *flags = f;
   return f ? SDSAT_EDEVICE : SDSAT_OK;
 }
