@@ -52,15 +52,18 @@ constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
 constexpr int CH_PART = 4;            // steps that a part of an item has at least
 // What work costs, in quarters of a key's with one tile: a key with two tiles, an item's start, and that for which a CTA
 // is worth its while.  One tile's steps are bound by memory, two tiles' by the products and the softmax: 48 sequences of up to
-// 8200 slots, two of them with 100 new rows, take 167 us with these, 189 with equal keys, 179 with a start of 64 keys.
-constexpr int CH_TWO = 5, CH_START = 4 * 320, CH_LEAST = 4 * 512;
+// 8200 slots, two of them with 100 new rows, take 156 us with these, 189 with equal keys, 179 with a start of 128 keys.
+constexpr int CH_TWO = 5, CH_START = 4 * 512, CH_LEAST = 4 * 512;
 constexpr float CH_LAZY = 8.0f;       // log2 of the growth of a row maximum that is left unscaled
 constexpr float CH_UNSET = -1e30f;    // reference of a row that has seen no key
 
-struct ChItem {
+struct ChHead {
   int row0, npos, pos0, hk;           // first row, positions, slot of the first; cache head (-1: no more items)
   int seq, kb0, kb1, part;            // steps; of an item in parts, which one this is, else -1
   int head, parts, unused[2];         // the CTA of its first part, their number
+};
+struct ChItem : ChHead {
+  int pages[32];                      // of its first steps
 };
 
 struct ChSeq {
@@ -345,21 +348,22 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   auto o_of = [&](size_t at, int rr, int x) { return part_o + (at * (HD / 4) + x / 4) * 2 * CH_ROWS + rr; };
 
   // an item's geometry
-  auto item_keys = [&](const ChItem& it, int t) { return (int)min((long long)cap, (long long)it.pos0 + min(it.npos, (t + 1) * pt1)); };
-  auto item_tiles = [&](const ChItem& it) { return C::TILES == 2 && it.npos > pt1 ? 2 : 1; };
+  auto item_keys = [&](const ChHead& it, int t) { return (int)min((long long)cap, (long long)it.pos0 + min(it.npos, (t + 1) * pt1)); };
+  auto item_tiles = [&](const ChHead& it) { return C::TILES == 2 && it.npos > pt1 ? 2 : 1; };
   // the step up to which this part of tile t goes
-  auto item_end = [&](const ChItem& it, int t) { return min(it.kb1, (item_keys(it, t) + CH_STEP - 1) / CH_STEP); };
+  auto item_end = [&](const ChHead& it, int t) { return min(it.kb1, (item_keys(it, t) + CH_STEP - 1) / CH_STEP); };
   // the last tile's step j has values behind its last key in 16 of a product
-  auto item_tail = [&](const ChItem& it, int j) {
+  auto item_tail = [&](const ChHead& it, int j) {
     const int k = item_keys(it, item_tiles(it) - 1);
     return k % 16 != 0 && j == k / CH_STEP;
   };
   uint32_t d_phase = 0;   // items read
-  auto next_item = [&](ChItem& it) {   // by a warp
+  auto next_item = [&](ChHead& it, int* page = nullptr) {   // by a warp (page: of the item's step `lane`)
     const int d = d_phase % CH_DESC;
     const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&d_full[d], (d_phase / CH_DESC) & 1, abort_flag, p.err));
     if (!ok) return false;
     it = items[d];
+    if (page) *page = items[d].pages[lane];
     __syncwarp();
     if (lane == 0) mbar_arrive(&d_empty[d]);
     ++d_phase;
@@ -369,7 +373,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   // Partial results have been written by warps w0 .. w0 + W - 1, all of which call this: the one whose part is the item's
   // last joins the parts.  False: a wait ran out.
   uint32_t part_phase = 0;
-  auto join = [&](const ChItem& it, int w0) {
+  auto join = [&](const ChHead& it, int w0) {
     constexpr int W = 4 * C::TILES, E = HD / 32;   // warps; values of a lane
     auto wait = [&](uint64_t* bar) { return (bool)__all_sync(0xffffffffu, mbar_wait_bounded(bar, part_phase & 1, abort_flag, p.err)); };
     __threadfence();
@@ -530,43 +534,60 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       return a;
     };
     // the c-th of the borders between the CTAs' stretches
-    auto border = [&](int c) {
-      ChPlace a = {p.b, 0, 0, 0, 0};
-      if (c >= ctas || total == 0) return a;
-      const long long x = total / ctas * c + total % ctas * c / ctas;
-      int lo = 0, hi = p.b;   // the last sequence whose cost before it is at most x
+    auto at_cost = [&](long long x) {   // the last sequence whose cost before it is at most x
+      int lo = 0, hi = p.b;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (plan[mid] <= x) lo = mid;
         else hi = mid;
       }
-      a.s = lo;
-      const ChSeq q = plan_seq[lo];
+      return lo;
+    };
+    auto border = [&](int c) {
+      ChPlace a = {p.b, 0, 0, 0, 0};
+      if (c >= ctas || total == 0) return a;
+      const long long x = total / ctas * c + total % ctas * c / ctas;
+      a.s = at_cost(x);
+      const ChSeq q = plan_seq[a.s];
       const long long of_head = ch_cost(q, pt);
-      long long rem = x - plan[lo];
+      long long rem = x - plan[a.s];
       a.hk = (int)(rem / of_head);
       rem -= a.hk * of_head;
-      lo = 0, hi = (q.n + pt - 1) / pt;
+      int lo = 0, hi = (q.n + pt - 1) / pt;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (ch_before(q, pt, mid) <= rem) lo = mid;
         else hi = mid;
       }
       a.t = lo;
-      a.cost = x - rem + ch_before(q, pt, lo);
+      rem -= ch_before(q, pt, lo);
+      a.cost = x - rem;
+      // the nearest step, an item's start spread over all of them; an end where that is less than CH_PART steps away
       const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
-      const long long kb = (rem - ch_before(q, pt, a.t) - CH_START + q.w * CH_STEP / 2) / (q.w * CH_STEP);
-      a.kb = kb < CH_PART ? 0 : (int)kb;
-      if (a.kb > steps - CH_PART && a.kb > 0) a = after(a, q);
+      const long long cost = ch_item(q, pt, a.t);
+      a.kb = (int)((2 * rem * steps + cost) / (2 * cost));
+      if (a.kb < CH_PART) {
+        a.kb = 0;
+      } else if (a.kb > steps - CH_PART) {   // the item that follows
+        a.kb = 0;
+        a.cost += cost;
+        if (++a.t * pt >= q.n) {
+          a.t = 0;
+          if (++a.hk == p.Hk) a.hk = 0, a.s = a.cost < total ? at_cost(a.cost) : p.b;
+        }
+      }
       return a;
     };
-    // the last CTA whose stretch begins at most y behind the start of the line
-    auto cta_at = [&](long long y) { return (int)min((long long)ctas - 1, ((y + 1) * ctas - 1) / total); };
+    // the last CTA whose stretch begins less than y behind the item that begins at `cost`
+    auto cta_at = [&](long long cost, long long y) { return (int)min((long long)ctas - 1, ((cost + y) * ctas - 1) / total); };
     ChPlace a = {p.b, 0, 0, 0, 0}, z = a;
-    if (!bad && cta < ctas) {
-      a = border(cta);
-      z = border(cta + 1);
-    }
+    if (!bad && cta < ctas && lane < 2) a = border(cta + lane);
+    __syncwarp();
+    z.s = __shfl_sync(0xffffffffu, a.s, 1), a.s = __shfl_sync(0xffffffffu, a.s, 0);
+    z.hk = __shfl_sync(0xffffffffu, a.hk, 1), a.hk = __shfl_sync(0xffffffffu, a.hk, 0);
+    z.t = __shfl_sync(0xffffffffu, a.t, 1), a.t = __shfl_sync(0xffffffffu, a.t, 0);
+    z.kb = __shfl_sync(0xffffffffu, a.kb, 1), a.kb = __shfl_sync(0xffffffffu, a.kb, 0);
+    a.cost = __shfl_sync(0xffffffffu, a.cost, 0);
     uint32_t n = 0;
     ChPlace end = z;
     ChSeq q = {0, 0, 0, 4};
@@ -574,7 +595,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     bool ok = true;
     while (ok) {
       const bool more = a.s < p.b && !(a.s == end.s && a.hk == end.hk && a.t == end.t && a.kb >= end.kb);
-      ChItem it = {0, 0, 0, -1, 0, 0, 0, -1, 0, 0, {0, 0}};
+      ChHead it = {0, 0, 0, -1, 0, 0, 0, -1, 0, 0, {0, 0}};
+      int page = -1;
       bool stop = true;
       if (more) {
         if (!out) q = plan_seq[a.s];
@@ -587,12 +609,13 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         it.hk = a.hk;
         it.seq = a.s;
         it.kb0 = a.kb;
+        if (a.kb + lane < p.ld) page = __ldcg(p.table + (size_t)a.s * p.ld + a.kb + lane);
         stop = a.s == end.s && a.hk == end.hk && a.t == end.t;
         it.kb1 = stop ? end.kb : steps;
-        if (it.kb0 > 0 || it.kb1 < steps) {   // (border() takes what is less than CH_PART steps from an end as the end)
-          const long long from = a.cost + CH_START - q.w * CH_STEP / 2 - 1, step = q.w * CH_STEP;
-          it.head = cta_at(from + CH_PART * step);
-          it.parts = cta_at(from + (steps - CH_PART + 1) * step) - it.head + 1;
+        if (it.kb0 > 0 || it.kb1 < steps) {   // (the CTAs whose first border lies in the item as border() sees it)
+          const long long cost = ch_item(q, pt, a.t);
+          it.head = cta_at(a.cost, ((2 * CH_PART - 1) * cost + 2 * steps - 1) / (2 * steps));
+          it.parts = cta_at(a.cost, ((2 * (steps - CH_PART) + 1) * cost + 2 * steps - 1) / (2 * steps)) - it.head + 1;
           it.part = cta - it.head;
         }
       }
@@ -602,10 +625,10 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       if (!out) fence_proxy_async_smem();   // (the plan's place: read before, written by TMA after)
       out = true;
       __syncwarp();
-      if (lane == 0) {
-        items[d] = it;
-        mbar_arrive(&d_full[d]);
-      }
+      items[d].pages[lane] = page;
+      if (lane == 0) static_cast<ChHead&>(items[d]) = it;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&d_full[d]);
       ++n;
       if (!more) break;
       if (stop) a = z = end = ChPlace{p.b, 0, 0, 0, 0};
@@ -634,35 +657,51 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       ++zn;
       z_slot = -1;
     };
-    // (values that a product waits for are made zeros before anything waits for that product)
+    // the queries of an item wait for the last scores of the one before, its keys and values do not
+    uint32_t q_wanted = 0;   // tiles (bits)
+    ChHead it;
+    auto get_queries = [&](bool wait) {
+      for (int t = 0; PARTS == 1 && t < 2; ++t) {
+        if (!((q_wanted >> t) & 1u)) continue;
+        const uint32_t parity = (qn[t] & 1) ^ 1;
+        if (!__all_sync(0xffffffffu, mbar_try_wait(&q_empty[t], parity))) {
+          if (!wait) continue;
+          make_zeros();
+          ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&q_empty[t], parity, abort_flag, p.err));
+          if (!ok) return;
+        }
+        ++qn[t];
+        q_wanted &= ~(1u << t);
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&q_full[t], C::HALVES * 128 * G * pt1);
+          for (int hh = 0; hh < C::HALVES; ++hh)
+            tma_load_3d(smem + (size_t)t * C::TILE + hh * C::HALF, &p.qmap, &q_full[t], hh * 64, it.hk * G, it.row0 + t * pt1);
+        }
+        __syncwarp();
+      }
+    };
+    // (what a product waits for is brought and made zeros before anything waits for that product)
     auto acquire = [&](uint64_t* bar, uint32_t parity) {
       if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
         make_zeros();
+        get_queries(true);
         ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
       }
       return ok;
     };
-    ChItem it;
     while (ok) {
       if (z_slot >= 0 && !__all_sync(0xffffffffu, mbar_try_wait(&d_full[d_phase % CH_DESC], (d_phase / CH_DESC) & 1))) make_zeros();
-      if (!next_item(it)) break;
+      get_queries(true);
+      int now = -1;
+      if (!ok || !next_item(it, &now)) break;
       const int nt = item_tiles(it), keys = item_keys(it, nt - 1);
-      if (PARTS == 1) {
-        for (int t = 0; t < nt && ok; ++t) {
-          if (item_end(it, t) <= it.kb0) continue;
-          if (!acquire(&q_empty[t], (qn[t] & 1) ^ 1)) break;
-          ++qn[t];
-          if (lane == 0) {
-            mbar_arrive_expect_tx(&q_full[t], C::HALVES * 128 * G * pt1);
-            for (int hh = 0; hh < C::HALVES; ++hh)
-              tma_load_3d(smem + (size_t)t * C::TILE + hh * C::HALF, &p.qmap, &q_full[t], hh * 64, it.hk * G, it.row0 + t * pt1);
-          }
-        }
-      }
+      for (int t = 0; t < nt; ++t)
+        if (item_end(it, t) > it.kb0) q_wanted |= 1u << t;
+      get_queries(false);
       // 32 pages at a time, the next ones asked for ahead
       const int* row = p.table + (size_t)it.seq * p.ld;
       auto pages = [&](int j) { return j + lane < p.ld ? __ldcg(row + j + lane) : -1; };
-      int now = pages(it.kb0), next = pages(it.kb0 + 32), base = it.kb0;
+      int next = it.kb1 > it.kb0 + 32 ? pages(it.kb0 + 32) : -1, base = it.kb0;
       int before[2] = {0, 0};   // the pages of the last two steps
       for (int j = it.kb0; j < it.kb1 + 2 && ok; ++j, ++n) {   // K of step j, V of step j - 2
         if (j == base + 32) base = j, now = next, next = pages(j + 32);
@@ -694,6 +733,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
           }
         }
         __syncwarp();
+        get_queries(false);
       }
     }
     make_zeros();
@@ -731,7 +771,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       tc_fence_after();
       return ok;
     };
-    ChItem it;
+    ChHead it;
     while (ok && next_item(it)) {
       const int nt = item_tiles(it), keys = item_keys(it, t) - it.kb0 * CH_STEP, all = it.kb1 - it.kb0 + 2;
       const int steps = t < nt ? max(0, item_end(it, t) - it.kb0) : 0, mine_too = steps ? steps + 2 : 0;
@@ -880,7 +920,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         tmem_st16(to + x, u);
       }
     };
-    ChItem it;
+    ChHead it;
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
@@ -988,7 +1028,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     const int e = warp & 3, rr = e * 32 + lane, gi = rr / G, g = rr % G;
     const uint32_t tl = tmem + ((uint32_t)(e * 32) << 16), to = tl + C::O_COL(0);
     uint32_t pn = 0, in = 0;   // steps, items
-    ChItem it;
+    ChHead it;
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, p.err));
