@@ -933,19 +933,24 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       const int lim = mine ? (int)min((long long)cap, (long long)it.pos0 + i + 1) : 0x7FFFFFFF;   // keys that it sees
       const int least = __reduce_min_sync(0xffffffffu, lim);
       const int end = item_tiles(it) > t ? item_end(it, t) : 0;
-      if (PARTS != 1) {   // the row's query (the last item's S have all been read here)
-        const float* src = static_cast<const float*>(p.q) + (long long)(it.row0 + gi) * p.q_ld + (it.hk * G + g) * HD;
-#pragma unroll 4
-        for (int x = 0; x < HD; x += 8) {
-          float4 f[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-          if (mine) {
-            f[0] = __ldcg(reinterpret_cast<const float4*>(src + x));
-            f[1] = __ldcg(reinterpret_cast<const float4*>(src + x + 4));
+      if (PARTS != 1) {   // the warp's queries, whole rows at a time (the last item's S have all been read here)
+        constexpr int LANES = HD / 4, AT_ONCE = 32 / LANES, N = 16;   // lanes of a row, rows of a load, loads in flight
+        const long long mine_at = mine ? (long long)(it.row0 + gi) * p.q_ld + (it.hk * G + g) * HD : -1;
+        const int dim = lane % LANES * 4;
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += AT_ONCE * N) {
+          float4 f[N];
+#pragma unroll
+          for (int y = 0; y < N; ++y) {
+            const long long at = __shfl_sync(0xffffffffu, mine_at, r0 + y * AT_ONCE + lane / LANES);
+            f[y] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + at + dim)) : make_float4(0.f, 0.f, 0.f, 0.f);
           }
 #pragma unroll
-          for (int q = 0; q < PARTS; ++q) {
-            const uint4 u = make_uint4(take_bf16(f[0].x, f[0].y), take_bf16(f[0].z, f[0].w), take_bf16(f[1].x, f[1].y), take_bf16(f[1].z, f[1].w));
-            *reinterpret_cast<uint4*>(smem + (size_t)q * C::TILE + (x >> 6) * C::HALF + rr * 128 + ((((x >> 3) & 7) ^ (rr & 7)) << 4)) = u;
+          for (int y = 0; y < N; ++y) {
+            const int r = e * 32 + r0 + y * AT_ONCE + lane / LANES;
+            uint8_t* to = smem + (dim >> 6) * C::HALF + r * 128 + ((((dim >> 3) & 7) ^ (r & 7)) << 4) + (dim & 4) * 2;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<uint2*>(to + (size_t)q * C::TILE) = make_uint2(take_bf16(f[y].x, f[y].y), take_bf16(f[y].z, f[y].w));
           }
         }
         fence_proxy_async_smem();
