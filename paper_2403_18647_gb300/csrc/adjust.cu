@@ -24,9 +24,7 @@ constexpr uint32_t ADJ_PROMPT = 1u << 31;
 constexpr int ADJ_BIAS_SHIFT = 20;                            // 11 bits: ADJ_MAX_BIAS - place, 0: none
 constexpr uint32_t ADJ_COUNT = (1u << ADJ_BIAS_SHIFT) - 1;   // a history and a block's tokens stay below it
 static_assert(ADJ_MAX_HISTORY + SDSAT_ATT_MAXQ <= (int)ADJ_COUNT && ADJ_MAX_BIAS < 2048, "fields of a word");
-// words, list and its length; a tree's token may be listed once for each row that brings it
-constexpr int ADJ_AGAIN = SDSAT_ATT_MAXQ * SDSAT_ATT_MAXQ;
-constexpr size_t adj_smem(int ch) { return (size_t)ch * 6 + ADJ_AGAIN * 2 + 16; }
+constexpr size_t adj_smem(int ch) { return (size_t)ch * 6 + 16; }   // words, list, its length (and its length without tokens)
 
 struct AdjRow {
   float rep, freq, pres;
@@ -80,8 +78,8 @@ template <bool BF16, int ADJ_THREADS>
 __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel(const __grid_constant__ AdjustParams p, int rp, int ch, int parts, int chunks) {
   extern __shared__ uint4 adj_mem[];
   uint32_t* words = reinterpret_cast<uint32_t*>(adj_mem);            // [ch]
-  uint16_t* list = reinterpret_cast<uint16_t*>(words + ch);          // [ch + ADJ_AGAIN]
-  int* listed = reinterpret_cast<int*>(list + ch + ADJ_AGAIN);
+  uint16_t* list = reinterpret_cast<uint16_t*>(words + ch);          // [ch], each id once
+  int* listed = reinterpret_cast<int*>(list + ch);
   __shared__ uint16_t queue[ADJ_THREADS / 32][64];           // of a warp: tokens of the stretch, bit 15: of the prompt
   constexpr int VEC = BF16 ? 8 : 4;         // values of 16 bytes
   constexpr int size = BF16 ? 2 : 4;
@@ -108,6 +106,7 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
   a.freq = p.frequency ? __ldg(p.frequency + s) : 0.f;
   a.pres = p.presence ? __ldg(p.presence + s) : 0.f;
   a.bias = p.bias + (size_t)s * p.n_bias;
+  const bool branches = p.tokens && p.anc && j1 - j0 > 1;   // rows with other tokens each
 
   for (int j = j0; j < j1; ++j) {
     const int r = s * p.q + j;
@@ -245,6 +244,11 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
         }
         if (lane < held) count(q[lane]);
       }
+      if (branches) {
+        __syncthreads();
+        if (tid == 0) listed[1] = *listed;   // ids that are listed for all of them
+        __syncwarp();                        // (the tokens are brought by this warp)
+      }
       if (p.tokens && !p.anc && tid < j0) token(__ldg(p.tokens + s * p.q + tid), false);   // (a chain: row j comes after tokens 0 .. j)
     }
     if (p.tokens && tid < p.q && (mine >> tid & 1u)) token(__ldg(p.tokens + s * p.q + tid), false);
@@ -268,9 +272,13 @@ __global__ void __launch_bounds__(ADJ_THREADS, 1024 / ADJ_THREADS) adjust_kernel
     }
     if (j + 1 < j1) {
       __syncthreads();
-      if (p.tokens && p.anc && tid < p.q && (mine >> tid & 1u)) {   // (taken back: another branch follows)
-        const int id = __ldg(p.tokens + s * p.q + tid);
-        if (here(id)) atomicAdd(&words[id - v0], 0xFFFFFFFFu);
+      if (branches && tid < 32) {   // another branch follows: this one's tokens are taken back (all in the warp that brings them)
+        if (tid < p.q && (mine >> tid & 1u)) {
+          const int id = __ldg(p.tokens + s * p.q + tid);
+          if (here(id)) atomicAdd(&words[id - v0], 0xFFFFFFFFu);
+        }
+        if (tid == 0) *listed = listed[1];
+        __syncwarp();
       }
     }
   }

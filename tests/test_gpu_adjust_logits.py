@@ -160,6 +160,16 @@ def test_in_place(ctx, type, b, q, V, pad):
 
 
 @pytest.mark.parametrize("type", [F32, BF16])
+@pytest.mark.parametrize("b,q,V", [(320, 4, 700), (320, 16, 300), (2, 16, 300)])
+def test_trees_in_place(ctx, type, b, q, V):
+    """A token that is on several branches, but not on the one between them, counts once in each row."""
+    a = make(14, b, q, V, type, anc=True)
+    ref = reference(a)
+    run(ctx, a, a["logits"])
+    assert same(a["logits"], ref) and ctx.get_error() == 0
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
 def test_infinities_nan_and_rows_without_a_token(ctx, type):
     a = make(4, 4, 2, 1000, type)
     x = a["logits"]
