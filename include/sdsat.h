@@ -506,6 +506,7 @@ SDSAT_API sdsat_status sdsat_op_prefix_attention(sdsat_ctx* ctx, const void* q_d
  * The queries go to q_out_dev, keys and the values (as they are) as bf16 to the slot's row of the sequence's page.
  *   q_dev, k_dev, v_dev  [rows] of H*hd, Hk*hd and Hk*hd values of `type` (SDSAT_FP32, SDSAT_BF16), q_ld, k_ld and v_ld
  *                        values apart: also parts of one matrix.  q_out_dev: the same type, q_out_ld apart; may be q_dev
+ *                        with its q_ld, else no memory that the call reads
  *   q_gain_dev, k_gain_dev  bf16 [hd], or NULL: no norm of those heads
  *   position_dev         int32 [rows], or NULL: the slots.  A position outside the table counts as its nearest (device
  *                        bit POSITION)
@@ -526,7 +527,8 @@ SDSAT_API sdsat_status sdsat_op_rotary_append(sdsat_ctx* ctx, const sdsat_rope* 
 /* Causal attention of a ragged batch over pages (its new rows' keys and values among them):
  * out[start[s]+i][h*hd+d] = sum_t softmax_t(q . k_t / sqrt(hd)) v_t[d] over slots t <= len[s] + i.
  *   q_dev, out_dev  [rows] of H*hd values of `type` (SDSAT_FP32, SDSAT_BF16), q_ld and out_ld values apart; sums fp32;
- *                   query head h reads cache head h / (H/Hk)
+ *                   query head h reads cache head h / (H/Hk).  out_dev may be q_dev with its q_ld, else no memory
+ *                   that the call reads
  * fp32 queries and probabilities enter the products in three bf16 parts (24 bits), bf16 queries as they are and their
  * probabilities rounded to bf16.  A slot past the table or on a page outside [0, n_pages) is not attended to and sets
  * device bit PAGE (a row that sees no slot is 0); what a page holds in slots that no row of the sequence sees does not
@@ -566,7 +568,7 @@ SDSAT_API sdsat_status sdsat_op_logprobs(sdsat_ctx* ctx, const void* logits_dev,
  *   l <- l + the bias of t
  *   l <- allowed(t) ? l : -inf
  * in fp32, rounded once.  in_dev, out_dev: rows of `vocab` values of `type`, in_ld and out_ld values apart (any
- * alignment of their values); the same rows, or none in common.
+ * alignment of their values); the same rows (in_ld = out_ld), or none in common.
  *   history_dev       int32 [b][history_ld]: the tokens before the block; history_len_dev int32 [b] of them (clamped to
  *                     [0, history_ld]), the first prompt_len_dev int32 [b] the prompt (NULL: none); NULL: no history
  *   tokens_dev        int32 [b*q]: the block's tokens.  Row j comes after tokens 0 .. j of its sequence, or, with anc_dev,

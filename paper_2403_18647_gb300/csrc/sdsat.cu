@@ -1350,7 +1350,7 @@ sdsat_status sdsat_get_error(sdsat_ctx* c, uint32_t* flags) {
   if (cudaMemcpy(&f, c->err, sizeof(f), cudaMemcpyDeviceToHost) != cudaSuccess) return SDSAT_ECUDA;
   if (cudaMemset(c->err, 0, sizeof(f)) != cudaSuccess) return SDSAT_ECUDA;
   // a call that gave up may have left counts of an item's parts behind
-  if ((f & SDSAT_DEV_TIMEOUT) && cudaMemset(c->chunk_part, 0, chunk_attention_counters(c->num_sms)) != cudaSuccess) return SDSAT_ECUDA;
+  if ((f & SDSAT_DEV_TIMEOUT) && cudaMemsetAsync(c->chunk_part, 0, chunk_attention_counters(c->num_sms), c->stream) != cudaSuccess) return SDSAT_ECUDA;
   if (flags) *flags = f;
   return f ? SDSAT_EDEVICE : SDSAT_OK;
 }
@@ -1587,6 +1587,7 @@ sdsat_status sdsat_op_rotary_append(sdsat_ctx* c, const sdsat_rope* rope, const 
   const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
   const long long R = (long long)H * hd, Rk = (long long)Hk * hd;
   if (q_ld < R || q_out_ld < R || k_ld < Rk || v_ld < Rk || (q_ld | q_out_ld | k_ld | v_ld) % per16) return SDSAT_EINVAL;
+  if (q_dev == q_out_dev && q_ld != q_out_ld && rows > 1) return SDSAT_EINVAL;   // (rows over one another's)
   if (R + 2 * Rk > 1 << 24 || (long long)table_ld * KV_PAGE > 0x7FFFFFFFll || (long long)rows * ((R + 2 * Rk) / 64) >= 1ll << 31)
     return SDSAT_EINVAL;   // (heads of rows, and slots, are counted in 32 bits)
   if (rows == 0) return SDSAT_OK;   // (no rows need no memory)
@@ -1635,6 +1636,7 @@ sdsat_status sdsat_op_chunk_attention(sdsat_ctx* c, const void* q_dev, int64_t q
     return SDSAT_EINVAL;
   const int per16 = type == SDSAT_BF16 ? 8 : 4;   // values in 16 bytes
   if (q_ld < (long long)H * hd || out_ld < (long long)H * hd || q_ld % per16 || out_ld % per16) return SDSAT_EINVAL;
+  if (q_dev == out_dev && q_ld != out_ld && rows > 1) return SDSAT_EINVAL;   // (rows over one another's)
   const long long pool = (long long)n_pages * Hk * KV_PAGE;
   if (pool > 0x7FFFFFFFll || (long long)table_ld * KV_PAGE > 0x3FFFFFFFll || (long long)H * hd > 1 << 24 || rows > 1 << 28)
     return SDSAT_EINVAL;   // (pool rows and slots are counted in 32 bits)
@@ -1680,6 +1682,7 @@ sdsat_status sdsat_op_adjust_logits(sdsat_ctx* c, const void* in_dev, int64_t in
       out_ld < vocab || history_ld < 0 || n_bias < 0 || b > ADJ_MAX_ROWS / q)
     return SDSAT_EINVAL;
   if (allowed_dev && allowed_ld < (vocab + 31) / 32) return SDSAT_EINVAL;
+  if (in_dev == out_dev && in_ld != out_ld && (long long)b * q > 1) return SDSAT_EINVAL;   // (rows over one another's)
   if (b == 0) return SDSAT_OK;   // (no rows need no memory)
   const unsigned value = type == SDSAT_BF16 ? 2 : 4;
   if (!in_dev || !out_dev || reinterpret_cast<uintptr_t>(in_dev) % value || reinterpret_cast<uintptr_t>(out_dev) % value)

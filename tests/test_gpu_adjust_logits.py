@@ -293,3 +293,12 @@ def test_offsets_past_32_bits(ctx):
             a[n] = None
     assert same(x[-2:], reference(a)) and (x[:-2] == 0).all()
     assert ctx.get_error() == 0
+
+
+def test_rows_over_one_anothers_are_refused(sd, ctx):
+    hold = torch.zeros(12, 100, device="cuda")
+    with pytest.raises(sd.SdsatError) as e:
+        ctx.op_adjust_logits(hold[::2], hold[:6])
+    assert e.value.status == 1
+    ctx.op_adjust_logits(hold[::2], hold[::2])
+    assert ctx.get_error() == 0

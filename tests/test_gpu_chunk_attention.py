@@ -296,3 +296,11 @@ def test_wrong_sizes_are_refused(sd, ctx):
     none = torch.zeros(0, 256, device="cuda")
     ctx.op_chunk_attention(**{**base(), "q": none, "out": none})   # no rows: nothing to do
     assert ctx.get_error() == 0
+
+
+def test_rows_over_one_anothers_are_refused(sd, ctx):
+    p = Pages(generator(31), 2, 64, [3], [5])
+    hold = torch.ones(6, 256, device="cuda")
+    with pytest.raises(sd.SdsatError) as e:
+        run(ctx, p, hold[::2], 4, 2, 64, hold[:3])
+    assert e.value.status == 1 and ctx.get_error() == 0

@@ -348,3 +348,11 @@ def test_offsets_past_32_bits(ctx):
     assert torch.equal(b.out.contiguous(), want.out)
     assert torch.equal(k[-small:], want.p.k) and torch.equal(v[-small:], want.p.v)
     assert ctx.get_error() == 0
+
+
+def test_rows_over_one_anothers_are_refused(sd, ctx):
+    b = Batch(15, 4, 2, 64, [2, 4], [70, 80], F32)
+    hold = torch.ones(12, 256, device="cuda")
+    with pytest.raises(sd.SdsatError) as e:
+        ctx.op_rotary_append(ctx.rope(64, 128), hold[::2], b.k, b.v, hold[:6], b.p.k, b.p.v, b.p.table, b.p.lens, b.p.starts, 4, 2, 64)
+    assert e.value.status == 1 and (hold == 1).all() and ctx.get_error() == 0
