@@ -202,8 +202,8 @@ def _array(t, dtype, n: int):
 
 def _pages(k, v, Hk: int, hd: int) -> int:
     """The number of pages of two pools of cache heads."""
-    shape = tuple(k.shape)
-    if len(shape) != 4 or shape[1:] != (Hk, PAGE, hd) or tuple(v.shape) != shape:
+    shape = k.shape
+    if shape != v.shape or len(shape) != 4 or shape != (shape[0], Hk, PAGE, hd):
         raise ValueError("expected pages of [Hk][%d][hd]" % PAGE)
     return shape[0]
 

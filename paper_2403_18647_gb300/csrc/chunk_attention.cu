@@ -866,7 +866,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     const float c = rsqrtf((float)HD) * 1.4426950408889634f;
     const uint64_t c2 = f2_pack(c, c);
     uint32_t bn = 0, x = 0, pn = 0, in = 0;   // entries of the ring and of the tile, P's, items
-    float m, l;                        // reference exponent (log2) and the row's sum relative to it
+    float m = CH_UNSET, l = 0.f;       // reference exponent (log2) and the row's sum relative to it
     // largest of 64 scores, as an exponent
     auto top = [&](const float (&s)[64]) {
       float mx[4] = {s[0], s[1], s[2], s[3]};
