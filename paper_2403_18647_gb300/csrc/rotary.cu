@@ -60,7 +60,7 @@ __device__ __forceinline__ int sequence_of(const int* start, int b, int r, int l
 enum RotaryLayout : int {
   ROT_INTERLEAVED = 0,   // the partner of place e is e ^ 1
   ROT_LANES = 1,         // e + half or e - half, whole lanes away
-  ROT_ANY = 2,           // ... some lanes and places away
+  ROT_ANY = 2,           // ... at any place of another lane
 };
 
 // heads: how many of a row a warp takes, a multiple of RT_U times its parts
@@ -69,6 +69,7 @@ __global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __gr
   constexpr int E = BF16 ? 8 : 4;                        // values of a lane
   constexpr int LANES = HD / E, PARTS = 32 / LANES;      // lanes of a head, heads side by side in a warp
   using Raw = uint4;
+  __shared__ __align__(16) float stage[LAYOUT == ROT_ANY ? RT_WARPS : 1][LAYOUT == ROT_ANY ? PARTS * HD : 4];
   const int lane = threadIdx.x & 31, part = lane / LANES, e0 = lane % LANES * E;
   const long long w = (long long)blockIdx.x * RT_WARPS + (threadIdx.x >> 5);
   const int r = (int)(w / groups), h0 = (int)(w % groups) * heads + part;
@@ -194,20 +195,17 @@ __global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < E; ++i) z[i] = __shfl_sync(0xffffffffu, y[i], on);
       } else {
-        // (half / E) lanes and half % E places on, or back
-        const int d = half % E, lanes = half / E;
-        auto one_of = [&](int i) {
-          float v = y[0];
+        // partners stand at any places of other lanes: through shared memory
+        float* head = stage[LAYOUT == ROT_ANY ? threadIdx.x >> 5 : 0] + part * HD;
+        __syncwarp();
 #pragma unroll
-          for (int k = 1; k < E; ++k)
-            if (i == k) v = y[k];
-          return v;
-        };
+        for (int i = 0; i < E; i += 4)
+          if (e0 + i < dims) *reinterpret_cast<float4*>(head + e0 + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const float f = __shfl_sync(0xffffffffu, one_of((i + d) % E), lane + lanes + (i + d) / E);
-          const float b = __shfl_sync(0xffffffffu, one_of((i + E - d) % E), lane - lanes - (i < d ? 1 : 0));
-          z[i] = e0 + i < half ? f : b;
+          const int e = e0 + i;
+          z[i] = e < dims ? head[e < half ? e + half : e - half] : 0.f;
         }
       }
       if (!is_v) {
