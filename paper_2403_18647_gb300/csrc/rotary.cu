@@ -18,10 +18,6 @@ namespace sdsat {
 
 constexpr int RT_WARPS = 4;
 constexpr int RT_U = 2;
-// Warps that an SM should have before a warp takes more heads of its row (us: 8500 rows of 32 / 8 bf16 heads 46 at 32, 55 at 128,
-// 73 at 512; 4095 rows of 40 / 40 fp32 heads 81 at 32, 75 at 128 and 512).
-constexpr int rt_fill(bool bf16) { return bf16 ? 32 : 128; }
-
 __global__ void rope_table_kernel(const RopeBuild f, float2* turn, int n, int pairs) {
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (long long)n * pairs) return;
@@ -231,10 +227,22 @@ __global__ void __launch_bounds__(RT_WARPS * 32) rotary_append_kernel(const __gr
   }
 }
 
+template <bool BF16, int HD, int LAYOUT, bool NORM>
+static int rt_resident = 0;   // warps on an SM
+
+template <bool BF16, int HD, int LAYOUT, bool NORM>
+static cudaError_t rt_prepare() {
+  const auto kernel = rotary_append_kernel<BF16, HD, LAYOUT, NORM>;
+  cudaError_t e = prefer_shared(kernel);
+  int ctas = 0;
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, RT_WARPS * 32, 0);
+  rt_resident<BF16, HD, LAYOUT, NORM> = std::max(1, ctas) * RT_WARPS;
+  return e;
+}
 template <bool BF16, int HD, int LAYOUT>
 static cudaError_t rt_prepare() {
-  const cudaError_t e = prefer_shared(rotary_append_kernel<BF16, HD, LAYOUT, false>);
-  return e == cudaSuccess ? prefer_shared(rotary_append_kernel<BF16, HD, LAYOUT, true>) : e;
+  const cudaError_t e = rt_prepare<BF16, HD, LAYOUT, false>();
+  return e == cudaSuccess ? rt_prepare<BF16, HD, LAYOUT, true>() : e;
 }
 template <bool BF16, int HD>
 static cudaError_t rt_prepare() {
@@ -249,13 +257,29 @@ cudaError_t rotary_prepare() {
   return e == cudaSuccess ? rt_prepare<true, 128>() : e;
 }
 
-template <bool BF16, int HD, int LAYOUT>
+// Among how many warps a row's `steps` are divided.  A warp costs its steps and its start, all that are resident run beside
+// one another, and what is more than those takes its share and a tail; fp32, close to the copy rate, has its tail in one
+// round too, bf16 is bound by what a warp issues.  Within 2 % of the best division that was measured at 27 sizes of each type
+// (us, bf16 / fp32 of 32 and 8 heads: 400 rows 5.9 / 6.3, a step to each warp 7.2 / 8.2; 800 7.5 / 8.4, 8.8 / 13.0;
+// 4095 fp32 rows of 40 and 40 heads 75, a row to each warp 87).
+static int rt_groups(bool bf16, long long rows, int steps, long long resident) {
+  const double start = bf16 ? 2.5 : 1.5, tail = 0.3;
+  const long long first = std::max(1ll, std::min((long long)steps, resident / rows)), last = std::min((long long)steps, 4 * resident / rows + 1);
+  long long groups = first;
+  double least = 1e30;
+  for (long long g = first; g <= std::max(first, last); ++g) {
+    const long long per = (steps + g - 1) / g;
+    const double rounds = (double)(rows * g) / (double)resident;
+    const double cost = (start + per) * (rounds > 1. ? rounds + tail : bf16 ? 1. : 1. + tail);
+    if (cost < least) least = cost, groups = g;
+  }
+  return (int)groups;
+}
+template <bool BF16, int HD, int LAYOUT, bool NORM>
 static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
   constexpr int step = RT_U * (32 * (BF16 ? 8 : 4) / HD);   // heads of a warp at a time
   const int steps = (p.H + 2 * p.Hk + step - 1) / step;
-  // whole rows to a warp once those fill the SMs, fewer heads while they do not
-  int groups = 1;
-  while (groups < steps && (long long)p.rows * groups < (long long)rt_fill(BF16) * num_sms) ++groups;
+  int groups = rt_groups(BF16, p.rows, steps, (long long)rt_resident<BF16, HD, LAYOUT, NORM> * num_sms);
   const int per = (steps + groups - 1) / groups;
   groups = (steps + per - 1) / per;
   cudaLaunchConfig_t cfg = {};
@@ -267,8 +291,11 @@ static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
-  return p.q_gain || p.k_gain ? cudaLaunchKernelEx(&cfg, rotary_append_kernel<BF16, HD, LAYOUT, true>, p, groups, per * step)
-                              : cudaLaunchKernelEx(&cfg, rotary_append_kernel<BF16, HD, LAYOUT, false>, p, groups, per * step);
+  return cudaLaunchKernelEx(&cfg, rotary_append_kernel<BF16, HD, LAYOUT, NORM>, p, groups, per * step);
+}
+template <bool BF16, int HD, int LAYOUT>
+static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
+  return p.q_gain || p.k_gain ? rt_launch<BF16, HD, LAYOUT, true>(p, num_sms, st, pdl) : rt_launch<BF16, HD, LAYOUT, false>(p, num_sms, st, pdl);
 }
 template <bool BF16, int HD>
 static cudaError_t rt_launch(const RotaryParams& p, int num_sms, cudaStream_t st, bool pdl) {
