@@ -304,14 +304,28 @@ cudaError_t adjust_prepare() {
 }
 
 cudaError_t launch_adjust(const AdjustParams& p, int num_sms, cudaStream_t st, bool pdl) {
-  // Long stretches, of more threads, and all rows of a sequence in one CTA read the history least often (8064 ids on 256
-  // threads 83 us for 72); shorter ones and a CTA for each row where that leaves SMs without one.
-  const int most = 2 * 512 * ADJ_U * (p.bf16 ? 8 : 4) - 128;   // (with the vector more that a misaligned row has, whole turns)
-  int ch = most, rp = p.q;
-  auto ctas = [&](int c, int r) { return (long long)p.b * ((p.q + r - 1) / r) * ((p.V + c - 1) / c); };
-  if (ctas(ch, rp) < 2 * num_sms) rp = 1;
-  while (ch > 1024 && ctas(ch, rp) < 2 * num_sms) ch = (ch / 2 + 127) / 128 * 128;
-  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch, threads = ch == most ? 512 : 256;
+  // Threads of a CTA, ids of its stretch and whether it takes one row or all of a sequence: whichever a model of a CTA's time
+  // makes least (us: its start, a row's waits, the ids and the history by thread; what does not fit in a round takes its
+  // share and a tail).  Long histories go to wide CTAs that read them less often, many rows of a sequence to one CTA once
+  // others fill the SMs.  Against the longest stretches that leave no SM empty (us): 3 rows of 5010 after 8665 tokens 6.6
+  // for 11.3, 13 x 16 rows of 20414 7.8 for 9.5, 197 rows of 16646 4.4 for 7.0, 48 rows of 32016 7.3 for 7.3; 256 of 128003
+  // take 72 in stretches of 16000 on 512 threads, 83 in 8064 on 256.
+  int ch = 0, rp = 1, threads = 0;
+  double least = 1e30;
+  for (int n = 256; n <= 512; n *= 2)
+    for (int r = 1;; r = p.q) {
+      const int most = 2 * n * ADJ_U * (p.bf16 ? 8 : 4) - 128;   // (with the vector more that a misaligned row has, whole turns)
+      for (int chunks = (p.V + most - 1) / most;; chunks *= 2) {
+        const int c = std::min(most, (p.V + chunks * 128 - 1) / (chunks * 128) * 128);
+        const double ctas = (double)p.b * ((p.q + r - 1) / r) * ((p.V + c - 1) / c), rounds = ctas * n / (1024. * num_sms);
+        const double one = 1.2 + r * (1.3 + c * (p.bf16 ? 0.128 : 0.2) / n) + (p.history ? 0.28 * p.history_ld / n : 0.);
+        const double cost = one * (rounds > 1. ? rounds + 0.5 : 1.);
+        if (cost < least) least = cost, ch = c, rp = r, threads = n;
+        if (c <= 512) break;
+      }
+      if (r == p.q) break;
+    }
+  const int parts = (p.q + rp - 1) / rp, chunks = (p.V + ch - 1) / ch;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.b * parts * chunks));
   cfg.blockDim = dim3(threads);

@@ -7,9 +7,9 @@
 // bounds it is memory, then instructions: rows are read and written once, 16 bytes a lane.  A warp takes heads of one
 // row, RT_U of them on each of its parts at a time, the next ones asked for before these are worked on; the first are
 // asked for before the row's sequence, slot and page are looked up, so that those dependent loads run beside the wide
-// ones.  Norm and rotation stay in registers (shuffles; pairs that lanes do not hold alike go through shared memory: by shuffles,
-// with selections of the values, 2645 rows of 32 / 8 bf16 heads took 60 us for 14); sums are fp32, the table's angles are reduced in double (an
-// fp32 angle of position 30000 is off by 1e-3).
+// ones.  Norm and rotation stay in registers (shuffles); pairs that lanes do not hold alike go through shared memory (by
+// shuffles and selections of the values 2645 rows of 32 / 8 bf16 heads took 60 us for 14).  Sums are fp32, the table's
+// angles are reduced in double (an fp32 angle of position 30000 is off by 1e-3).
 #include <algorithm>
 
 #include "common.cuh"
@@ -18,7 +18,9 @@
 namespace sdsat {
 
 constexpr int RT_WARPS = 4;
-constexpr int RT_U = 2;   // (12 sequences of up to 1100 rows of 32 / 8 bf16 heads: 45 us, 4.9 TB/s; 62 with one, 60 with four, of more registers)
+// (12 sequences of up to 1100 rows of 32 / 8 bf16 heads: 45 us, 4.9 TB/s; 62 with one, 60 with four, of more registers)
+constexpr int RT_U = 2;
+
 __global__ void rope_table_kernel(const RopeBuild f, float2* turn, int n, int pairs) {
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (long long)n * pairs) return;

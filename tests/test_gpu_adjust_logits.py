@@ -160,7 +160,7 @@ def test_in_place(ctx, type, b, q, V, pad):
 
 
 @pytest.mark.parametrize("type", [F32, BF16])
-@pytest.mark.parametrize("b,q,V", [(320, 4, 700), (320, 16, 300), (2, 16, 300)])
+@pytest.mark.parametrize("b,q,V", [(320, 4, 700), (320, 16, 300), (2, 16, 300), (700, 16, 64)])
 def test_trees_in_place(ctx, type, b, q, V):
     """A token that is on several branches, but not on the one between them, counts once in each row."""
     a = make(14, b, q, V, type, anc=True)
