@@ -141,6 +141,9 @@ def _lib():
         lib.sdsat_kernel_class_name.restype = ctypes.c_char_p
         lib.sdsat_status_string.argtypes = [ctypes.c_int]
         lib.sdsat_status_string.restype = ctypes.c_char_p
+        from . import _native
+        _native.library(*[ctypes.cast(getattr(lib, "sdsat_" + n), ctypes.c_void_p).value
+                          for n in ("set_stream", "op_rotary_append", "op_chunk_attention", "op_adjust_logits")])
         _LIB = lib
     return _LIB
 
@@ -163,6 +166,7 @@ def _ptr(t) -> Optional[int]:
 
 
 _kinds = _f32 = _bf16 = _i32 = None   # tensor types, once torch is there (the first call of _rows)
+_calls = None                         # the calls whose arguments are checked and converted in C (csrc/binding.c)
 
 
 def _rows(t):
@@ -180,9 +184,13 @@ def _rows(t):
 
 
 def _types():
-    global _kinds, _f32, _bf16, _i32
+    global _kinds, _f32, _bf16, _i32, _calls
     import torch
     _kinds, _f32, _bf16, _i32 = {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.bfloat16, torch.int32
+    _lib()
+    from . import _native
+    _native.types(_f32, _bf16, _i32, _stream)
+    _calls = _native
 
 
 def _array(t, dtype, n: int):
@@ -198,14 +206,6 @@ def _array(t, dtype, n: int):
         raise
     raise ValueError("expected %d values of %s in a contiguous CUDA tensor, got %d of %s on %s"
                      % (n, dtype, t.numel(), t.dtype, t.device))
-
-
-def _pages(k, v, Hk: int, hd: int) -> int:
-    """The number of pages of two pools of cache heads."""
-    shape = k.shape
-    if shape != v.shape or len(shape) != 4 or shape != (shape[0], Hk, PAGE, hd):
-        raise ValueError("expected pages of [Hk][%d][hd]" % PAGE)
-    return shape[0]
 
 
 def _check(status: int, what: str):
@@ -632,64 +632,27 @@ class Context:
         """q, q_out [rows][H*hd], k and v [rows][Hk*hd], all fp32 or all bf16 (rows any distance apart); k_pages, v_pages bf16
         [pages][Hk][PAGE][hd]; table int32 [b][columns]; lens int32 [b]; starts int32 [b + 1]; positions int32 [rows];
         gains bf16 [hd]; refs int32 [pages]."""
-        self._bind_stream()
-        (qp, q_ld, kind, rows, cols), (op, o_ld, o_kind, o_rows, o_cols) = _rows(q), _rows(q_out)
-        (kp, k_ld, k_kind, k_rows, k_cols), (vp, v_ld, v_kind, v_rows, v_cols) = _rows(k), _rows(v)
-        if not kind == o_kind == k_kind == v_kind:
-            raise ValueError("q, k, v and q_out are of different types")
-        if k_rows < rows or v_rows < rows or o_rows < rows:
-            raise ValueError("k, v or q_out of fewer rows than q")
-        if cols < H * hd or o_cols < H * hd or k_cols < Hk * hd or v_cols < Hk * hd:
-            raise ValueError("fewer columns than heads * hd")
-        (b, columns), pages = table.shape, _pages(k_pages, v_pages, Hk, hd)
-        _check(_lib().sdsat_op_rotary_append(self.handle, rope.handle, qp, q_ld, kp, k_ld, vp, v_ld, kind, rows,
-                                             _array(starts, _i32, b + 1), _array(lens, _i32, b), b, _array(positions, _i32, rows),
-                                             _array(q_gain, _bf16, hd), _array(k_gain, _bf16, hd), eps, H, Hk, hd, op, o_ld,
-                                             _array(k_pages, _bf16, 0), _array(v_pages, _bf16, 0), pages,
-                                             _array(table, _i32, 0), columns, _array(refs, _i32, pages)), "sdsat_op_rotary_append")
+        if _calls is None:
+            _types()
+        _check(_calls.rotary_append(self.handle, rope.handle, q, k, v, q_out, k_pages, v_pages, table, lens, starts, H, Hk, hd,
+                                     positions, q_gain, k_gain, eps, refs), "sdsat_op_rotary_append")
 
     def op_chunk_attention(self, q, k_pages, v_pages, table, lens, starts, H: int, Hk: int, hd: int, out):
         """q, out [rows][H*hd], both fp32 or bf16 (rows any distance apart); k_pages, v_pages bf16 [pages][Hk][PAGE][hd];
         table int32 [b][columns]; lens int32 [b]; starts int32 [b + 1]."""
-        self._bind_stream()
-        (qp, q_ld, kind, rows, cols), (op, o_ld, o_kind, o_rows, o_cols) = _rows(q), _rows(out)
-        if kind != o_kind:
-            raise ValueError("q and out are of different types")
-        if o_rows < rows:
-            raise ValueError("out of fewer rows than q")
-        if cols < H * hd or o_cols < H * hd:
-            raise ValueError("fewer columns than H * hd")
-        (b, columns), pages = table.shape, _pages(k_pages, v_pages, Hk, hd)
-        _check(_lib().sdsat_op_chunk_attention(self.handle, qp, q_ld, rows, _array(k_pages, _bf16, 0), _array(v_pages, _bf16, 0), pages,
-                                               _array(table, _i32, 0), columns, _array(starts, _i32, b + 1), _array(lens, _i32, b), b,
-                                               H, Hk, hd, op, o_ld, kind), "sdsat_op_chunk_attention")
+        if _calls is None:
+            _types()
+        _check(_calls.chunk_attention(self.handle, q, k_pages, v_pages, table, lens, starts, H, Hk, hd, out), "sdsat_op_chunk_attention")
 
     def op_adjust_logits(self, logits, out, q: int = 1, history=None, history_lens=None, prompt_lens=None, tokens=None, anc=None,
                          repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, allowed=None):
         """logits, out [b*q][vocab], both fp32 or bf16 (rows any distance apart); history int32 [b][n]; history_lens, prompt_lens
         int32 [b]; tokens, anc int32 [b*q]; repetition, frequency, presence fp32 [b]; bias_ids int32 and bias fp32 [b][m];
         allowed int32 [b*q][words of 32 ids]."""
-        self._bind_stream()
-        (ip, i_ld, kind, rows, vocab), (op, o_ld, o_kind, o_rows, o_cols) = _rows(logits), _rows(out)
-        if kind != o_kind:
-            raise ValueError("logits and out are of different types")
-        if q < 1 or rows % q:
-            raise ValueError("rows are no multiple of q")
-        if o_rows < rows or o_cols < vocab:
-            raise ValueError("out is smaller than logits")
-        b = rows // q
-        n = 0 if history is None else history.size(1)
-        m = 0 if bias_ids is None else bias_ids.size(1)
-        if (bias is None) != (bias_ids is None) or m and bias.shape[1] != m:
-            raise ValueError("bias_ids and bias are of different widths")
-        words = 0 if allowed is None else allowed.size(1)
-        if allowed is not None and words < -(-vocab // 32):
-            raise ValueError("allowed is narrower than the vocabulary")
-        _check(_lib().sdsat_op_adjust_logits(self.handle, ip, i_ld, kind, b, q, vocab, _array(history, _i32, b * n), n,
-                                             _array(history_lens, _i32, b), _array(prompt_lens, _i32, b), _array(tokens, _i32, rows),
-                                             _array(anc, _i32, rows), _array(repetition, _f32, b), _array(frequency, _f32, b),
-                                             _array(presence, _f32, b), _array(bias_ids, _i32, b * m), _array(bias, _f32, b * m), m,
-                                             _array(allowed, _i32, rows * words), words, op, o_ld), "sdsat_op_adjust_logits")
+        if _calls is None:
+            _types()
+        _check(_calls.adjust_logits(self.handle, logits, out, q, history, history_lens, prompt_lens, tokens, anc, repetition,
+                                     frequency, presence, bias_ids, bias, allowed), "sdsat_op_adjust_logits")
 
     def debug_workspace(self, which: int, rows: int):
         """Last-layer workspace of the last forward: 0 h, 1 q, 2 attention out, 3 SwiGLU act."""

@@ -1,7 +1,7 @@
 """Build libsdsat.so in-tree with nvcc for sm_103a (GB300).
 
 Each .cu translation unit is compiled in parallel, then linked into one shared
-library next to this file.  Used by __graft_entry__.build() and by the Python
+library next to this file, beside the C part of the binding.  Used by __graft_entry__.build() and by the Python
 binding's first import when the library is missing or stale.
 """
 from __future__ import annotations
@@ -10,12 +10,14 @@ import concurrent.futures as cf
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsdsat.so")
+NATIVE = os.path.join(PKG, "_native.so")   # the part of the Python binding that is in C
 SOURCES = ["gemm.cu", "attention.cu", "accept.cu", "prefill.cu", "prefill_attention.cu", "pages.cu", "prefix_attention.cu",
            "logprobs.cu", "rotary.cu", "chunk_attention.cu", "adjust.cu", "sdsat.cu", "noalloc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -36,9 +38,9 @@ def _deps():
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(NATIVE):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(NATIVE))
     return any(os.path.getmtime(f) > t for f in _deps())
 
 
@@ -55,8 +57,10 @@ def build(verbose: bool = False, extra=()) -> str:
             print(r.stderr, file=sys.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        native = ex.submit(build_native)
         objs = list(ex.map(one, SOURCES))
+        native.result()
     tmp = LIB + ".tmp"
     cmd = [nvcc(), *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -64,6 +68,17 @@ def build(verbose: bool = False, extra=()) -> str:
         raise RuntimeError("link failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
     os.replace(tmp, LIB)
     return LIB
+
+
+def build_native() -> str:
+    tmp = NATIVE + ".tmp"
+    cmd = ["gcc", "-O2", "-shared", "-fPIC", "-fvisibility=hidden", "-I" + sysconfig.get_paths()["include"],
+           "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "binding.c"), "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("gcc failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
+    os.replace(tmp, NATIVE)
+    return NATIVE
 
 
 if __name__ == "__main__":
