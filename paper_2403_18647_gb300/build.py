@@ -7,6 +7,7 @@ binding's first import when the library is missing or stale.
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib
 import os
 import subprocess
 import sys
@@ -78,6 +79,7 @@ def build_native() -> str:
     if r.returncode != 0:
         raise RuntimeError("gcc failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
     os.replace(tmp, NATIVE)
+    importlib.invalidate_caches()   # (it is imported by the process that built it)
     return NATIVE
 
 
