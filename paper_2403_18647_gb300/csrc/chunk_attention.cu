@@ -28,7 +28,7 @@
 // Measured, us: 32 heads x 128, 4095 positions bf16 118 (1.16 PFLOP/s; prefill attention, which has fp32 queries in two
 // parts, 257); 32 / 8 heads, 8 sequences of 330 to 1100 rows after 800 to 16500 slots 730 (1.33 PFLOP/s; 804 in a long run
 // at the power cap), one of 4096 rows after 16384 780 (1.57); 48 sequences of up to 8200 slots, 46 of them with one row,
-// 156 to 161 (5.5 TB/s); 40 heads, 777 rows after 2048 slots in fp32 112.
+// 154 to 161 (5.5 TB/s); 40 heads, 777 rows after 2048 slots in fp32 111.
 //
 // A row's reference m is moved only when its maximum has grown by more than 2^8 since the last time (exact: it cancels
 // in the division by the row's sum), so that O (the total) is seldom rescaled.
@@ -936,24 +936,21 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       const int least = __reduce_min_sync(0xffffffffu, lim);
       const int end = item_tiles(it) > t ? item_end(it, t) : 0;
       if (PARTS != 1) {   // the warp's queries, whole rows at a time (the last item's S have all been read here)
-        constexpr int LANES = HD / 4, AT_ONCE = 32 / LANES, N = 16;   // lanes of a row, rows of a load, loads in flight
+        constexpr int LANES = HD / 4, AT_ONCE = 32 / LANES, N = 32 / AT_ONCE;   // lanes of a row, rows of a load, loads (all in flight)
         const long long mine_at = mine ? (long long)(it.row0 + gi) * p.q_ld + (it.hk * G + g) * HD : -1;
         const int dim = lane % LANES * 4;
-#pragma unroll 1
-        for (int r0 = 0; r0 < 32; r0 += AT_ONCE * N) {
-          float4 f[N];
+        float4 f[N];
 #pragma unroll
-          for (int y = 0; y < N; ++y) {
-            const long long at = __shfl_sync(0xffffffffu, mine_at, r0 + y * AT_ONCE + lane / LANES);
-            f[y] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + at + dim)) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
+        for (int y = 0; y < N; ++y) {
+          const long long at = __shfl_sync(0xffffffffu, mine_at, y * AT_ONCE + lane / LANES);
+          f[y] = at >= 0 ? __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + at + dim)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
 #pragma unroll
-          for (int y = 0; y < N; ++y) {
-            const int r = e * 32 + r0 + y * AT_ONCE + lane / LANES;
-            uint8_t* to = smem + (dim >> 6) * C::HALF + r * 128 + ((((dim >> 3) & 7) ^ (r & 7)) << 4) + (dim & 4) * 2;
+        for (int y = 0; y < N; ++y) {
+          const int r = e * 32 + y * AT_ONCE + lane / LANES;
+          uint8_t* to = smem + (dim >> 6) * C::HALF + r * 128 + ((((dim >> 3) & 7) ^ (r & 7)) << 4) + (dim & 4) * 2;
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<uint2*>(to + (size_t)q * C::TILE) = make_uint2(take_bf16(f[y].x, f[y].y), take_bf16(f[y].z, f[y].w));
-          }
+          for (int q = 0; q < PARTS; ++q) *reinterpret_cast<uint2*>(to + (size_t)q * C::TILE) = make_uint2(take_bf16(f[y].x, f[y].y), take_bf16(f[y].z, f[y].w));
         }
         fence_proxy_async_smem();
         mbar_arrive(q_full);
