@@ -52,6 +52,11 @@ constexpr int CH_THREADS = 384;
 constexpr int CH_DESC = 4;            // items handed out ahead
 constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
 constexpr int CH_PART = 4;            // steps that a part of an item has at least
+// Barriers of a tile's scores, taken in turn by its entries.  An item's first two entries wait for no P, so they may be
+// complete while the softmax has yet to look at the last two of the item before: four entries that it has not seen.  With two
+// barriers one of these would be two phases behind, where its parity reads as incomplete.
+constexpr int CH_SBARS = 4;
+static_assert((CH_SBARS & (CH_SBARS - 1)) == 0, "an entry's barrier and parity are bits of its number");
 // What work costs, in quarters of a key's with one tile: a key with two tiles, an item's start, and that for which a CTA
 // is worth its while.  One tile's steps are bound by memory, two tiles' by the products and the softmax: 48 sequences of up to
 // 8200 slots, two of them with 100 new rows, take 156 us with these, 189 with equal keys, 179 with a start of 128 keys.
@@ -84,7 +89,7 @@ struct ChCfg {
   static_assert(CH_FLAGS >= SLOTS + 2, "flags outlast the loads ahead");
   static constexpr size_t OFF_RING = (size_t)TILES * PARTS * TILE;
   static constexpr size_t OFF_BAR = OFF_RING + (size_t)SLOTS * 2 * SLOT;
-  static constexpr int NBAR = 2 * SLOTS + 24 + 2 * CH_DESC;
+  static constexpr int NBAR = 2 * SLOTS + 20 + 2 * CH_SBARS + 2 * CH_DESC;
   static constexpr size_t OFF_ITEMS = OFF_BAR + (NBAR + 1) / 2 * 16;
   static constexpr size_t SMEM = 1024 + OFF_ITEMS + CH_DESC * sizeof(ChItem) + CH_FLAGS * 4 + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
@@ -279,8 +284,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
   uint64_t* z_full = empty + SLOTS;       // an entry landed in which values have to be made zeros
   uint64_t* q_full = z_full + 1;          // [2] per tile: Q is there
   uint64_t* q_empty = q_full + 2;         // [2] two tiles: the item's last S is complete
-  uint64_t* s_full = q_empty + 2;         // [2][2] per tile and entry's parity: S of its step, and P V of the one before the last, are complete
-  uint64_t* p_full = s_full + 4;          // [2][2] P is in TMEM, O is rescaled (128 threads)
+  uint64_t* s_full = q_empty + 2;         // [2][CH_SBARS] per tile and entry: S of its step, and P V of the one before the last, are complete
+  uint64_t* p_full = s_full + 2 * CH_SBARS;   // [2][2] P is in TMEM, O is rescaled (128 threads)
   uint64_t* pv_done = p_full + 4;         // [2] one tile, by step's parity: its P V is complete
   uint64_t* o_free = pv_done + 2;         // one tile: O of a step has been read (128 threads)
   uint64_t* part_full = o_free + 1;       // partial results are written (by all who write)
@@ -309,10 +314,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     for (int t = 0; t < 2; ++t) {
       mbar_init(&q_full[t], PARTS == 1 ? 1 : 128);
       mbar_init(&q_empty[t], 1);
-      for (int b = 0; b < 2; ++b) {
-        mbar_init(&s_full[2 * t + b], 1);
-        mbar_init(&p_full[2 * t + b], 128);
-      }
+      for (int b = 0; b < CH_SBARS; ++b) mbar_init(&s_full[CH_SBARS * t + b], 1);
+      for (int b = 0; b < 2; ++b) mbar_init(&p_full[2 * t + b], 128);
       mbar_init(&l_full[t], 128);
       mbar_init(&l_free[t], 128);
     }
@@ -762,7 +765,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
     const uint32_t ts = tmem + C::S_COL(t), tp = tmem + C::P_COL(t), to = tmem + C::O_COL(t);
     bool ok = true;
     uint32_t n = 0, x = 0, qn = 0, pn = 0;   // entries of the ring and of the tile, Q tiles, P's
-    const uint32_t full_at = smem_u32(full), empty_at = smem_u32(empty), s_at = smem_u32(s_full + 2 * t), p_at = smem_u32(p_full + 2 * t),
+    const uint32_t full_at = smem_u32(full), empty_at = smem_u32(empty), s_at = smem_u32(s_full + CH_SBARS * t), p_at = smem_u32(p_full + 2 * t),
                    qe_at = smem_u32(q_empty + t), pv_at = smem_u32(pv_done);
     const bool does_s = PARTS == 1 || warp == 1, does_pv = PARTS == 1 || warp == 3;
     auto wait = [&](uint64_t* bar, uint32_t parity) {   // (the lanes agree before the products)
@@ -837,7 +840,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
               ch_mma(ts + CH_STEP * b, q_desc + part * (C::TILE >> 4) + (kk >> 2) * (C::HALF >> 4) + (kk & 3) * 2,
                      k + (kk >> 2) * (C::BOX >> 4) + (kk & 3) * 2, idesc_s, part < PARTS - 1 || kk ? 1u : 0u, mine);
         }
-        if (PARTS == 1 || (has_s && does_s)) ch_commit(s_at + 8 * b, mine);
+        if (PARTS == 1 || (has_s && does_s)) ch_commit(s_at + 8 * (x % CH_SBARS), mine);
         ch_commit(empty_at + 8 * s, mine);
         if (PARTS == 1 && e == steps - 1) ch_commit(qe_at, mine);
       }
@@ -929,6 +932,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       tc_fence_after();
       return ok;
     };
+    auto wait_s = [&](uint32_t x) { return wait(&s_full[CH_SBARS * t + x % CH_SBARS], (x / CH_SBARS) & 1); };   // the tile's entry x
     while (ok && next_item(it)) {
       const int i = t * pt1 + gi;                              // this row's position in the item
       const bool mine = gi < pt1 && i < it.npos;
@@ -958,7 +962,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       m = CH_UNSET, l = 0.f;
 #pragma unroll 1
       for (int j = it.kb0; j < end; ++j, ++x, ++pn) {
-        if (!wait(&s_full[2 * t + (x & 1)], (x >> 1) & 1)) break;
+        if (!wait_s(x)) break;
         const bool there = flags[(bn + (j - it.kb0)) % CH_FLAGS];   // (keys without a page are not attended to)
         float s[CH_STEP];
         tmem_ld32(ts + CH_STEP * (x & 1), s);
@@ -972,7 +976,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
           if (grow) f = ex2(m - mb), m = mb;
           l *= f;
           if (PARTS == 1 && j > it.kb0) {   // O of the steps before: the last P V came with the next entry
-            if (!wait(&s_full[2 * t + ((x + 1) & 1)], ((x + 1) >> 1) & 1)) break;
+            if (!wait_s(x + 1)) break;
             rescale(f);
           }
         }
@@ -984,7 +988,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         mbar_arrive(&p_full[2 * t + (pn & 1)]);
       }
       if (PARTS == 1 && end > it.kb0) {   // the last two P V's
-        for (int y = 0; y < 2; ++y, ++x) wait(&s_full[2 * t + (x & 1)], (x >> 1) & 1);
+        for (int y = 0; y < 2; ++y, ++x) wait_s(x);
       }
       bn += it.kb1 - it.kb0 + 2;
       if (!ok) break;
