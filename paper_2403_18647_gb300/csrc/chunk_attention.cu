@@ -407,8 +407,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
 #pragma unroll 2
       for (int k = 0; k < it.parts; ++k) {   // (a part that saw no key of the row has a sum of 0, and maybe nothing was written)
         const float2 ml = __ldcg(ml_of(part_at(it.head, k), rr));
-        const float now = ml.y > 0.f ? fmaxf(m, ml.x) : m;
-        l = l * ex2(m - now) + (ml.y > 0.f ? ml.y * ex2(ml.x - now) : 0.f);
+        const bool seen = ml.y != 0.f;       // (a sum that is NaN counts, too: the row's result is NaN)
+        const float now = seen ? fmaxf(m, ml.x) : m;
+        l = l * ex2(m - now) + (seen ? ml.y * ex2(ml.x - now) : 0.f);
         m = now;
       }
       const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
 #pragma unroll
           for (int y = 0; y < 8; ++y) v[y] = __ldcg(o_of(at, rr, x + 4 * y));
           const float w = ex2(ml.x - m);
-          if (ml.y > 0.f)
+          if (ml.y != 0.f)
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
               acc[4 * y] = fmaf(v[y].x, w, acc[4 * y]);
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         float u[E];
 #pragma unroll
         for (int y = 0; y < E; ++y) u[y] = __ldcg(v + y);
-        const bool seen = ml.y > 0.f;
+        const bool seen = ml.y != 0.f;
         const float now = seen ? fmaxf(m, ml.x) : m, f = ex2(m - now), w = seen ? ex2(ml.x - now) : 0.f;
         m = now;
         l = fmaf(l, f, ml.y * w);
