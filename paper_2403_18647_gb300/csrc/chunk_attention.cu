@@ -40,27 +40,21 @@
 // tile 1; with one tile 4-7 bring the queries, too, and 8-11 keep the total and write the output.
 #include <algorithm>
 
+#include "chunk_plan.h"
 #include "common.cuh"
 #include "internal.h"
 
 namespace sdsat {
 
-static_assert(KV_PAGE == 64, "a page is one box of keys");
-constexpr int CH_ROWS = 128;          // rows of a tile
-constexpr int CH_STEP = KV_PAGE;      // keys of a step: a page
+static_assert(KV_PAGE == CH_STEP, "a page is one box of keys");
 constexpr int CH_THREADS = 384;
 constexpr int CH_DESC = 4;            // items handed out ahead
 constexpr int CH_FLAGS = 16;          // entries whose pages' presence is kept
-constexpr int CH_PART = 4;            // steps that a part of an item has at least
 // Barriers of a tile's scores, taken in turn by its entries.  An item's first two entries wait for no P, so they may be
 // complete while the softmax has yet to look at the last two of the item before: four entries that it has not seen.  With two
 // barriers one of these would be two phases behind, where its parity reads as incomplete.
 constexpr int CH_SBARS = 4;
 static_assert((CH_SBARS & (CH_SBARS - 1)) == 0, "an entry's barrier and parity are bits of its number");
-// What work costs, in quarters of a key's with one tile: a key with two tiles, an item's start, and that for which a CTA
-// is worth its while.  One tile's steps are bound by memory, two tiles' by the products and the softmax: 48 sequences of up to
-// 8200 slots, two of them with 100 new rows, take 156 us with these, 189 with equal keys, 179 with a start of 128 keys.
-constexpr int CH_TWO = 5, CH_START = 4 * 512, CH_LEAST = 4 * 512;
 constexpr float CH_LAZY = 8.0f;       // log2 of the growth of a row maximum that is left unscaled
 constexpr float CH_UNSET = -1e30f;    // reference of a row that has seen no key
 
@@ -71,10 +65,6 @@ struct ChHead {
 };
 struct ChItem : ChHead {
   int pages[32];                      // of its first steps
-};
-
-struct ChSeq {
-  int first, n, len, w;               // w: what a key costs
 };
 
 template <int HD, int PARTS>
@@ -243,34 +233,6 @@ __device__ __forceinline__ uint32_t take_bf16(float& a, float& b) {
   b -= __uint_as_float(r & 0xFFFF0000u);
   return r;
 }
-
-// ---- the plan: sequences of n new positions after `len` slots, items of pt positions -----------
-__device__ __forceinline__ ChSeq ch_sequence(const ChunkAttnParams& p, int s, int pt1, int tiles) {
-  ChSeq q;
-  q.first = __ldcg(p.start + s);
-  q.n = __ldcg(p.start + s + 1) - q.first;
-  q.len = min(max(__ldcg(p.len + s), 0), p.ld * KV_PAGE);
-  q.w = tiles == 2 && q.n > pt1 ? CH_TWO : 4;
-  return q;
-}
-// cost of a head's items before item t, and of item t
-__device__ __forceinline__ long long ch_before(const ChSeq& q, int pt, int t) {
-  return (long long)t * ((long long)q.w * q.len + CH_START) + (long long)q.w * pt * ((long long)t * (t + 1) / 2);
-}
-__device__ __forceinline__ long long ch_item(const ChSeq& q, int pt, int t) {
-  return (long long)q.w * (q.len + min((long long)q.n, (long long)(t + 1) * pt)) + CH_START;
-}
-__device__ __forceinline__ long long ch_cost(const ChSeq& q, int pt) {
-  if (q.n <= 0) return 0;
-  const int t = (q.n + pt - 1) / pt;
-  return ch_before(q, pt, t - 1) + ch_item(q, pt, t - 1);
-}
-__device__ __forceinline__ int ch_keys(const ChSeq& q, int pt, int cap, int t) { return min((long long)cap, (long long)q.len + min((long long)q.n, (long long)(t + 1) * pt)); }
-
-struct ChPlace {
-  int s, hk, t, kb;   // s = b: behind the last item
-  long long cost;     // before the item
-};
 
 template <int HD, int PARTS>
 __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __grid_constant__ ChunkAttnParams p) {
@@ -496,8 +458,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         const int a = __ldcg(p.start + s), z = __ldcg(p.start + s + 1), len = __ldcg(p.len + s);
         bad |= a < 0 || z < a || z > p.rows;
         past |= z > a && (long long)max(len, 0) + (z - a) > cap;
-        const ChSeq q = {a, z - a, min(max(len, 0), cap), C::TILES == 2 && z - a > pt1 ? CH_TWO : 4};
-        if (z >= a) cost = ch_cost(q, pt) * p.Hk, items_here = (int)min(1ll << 15, ((long long)q.n + pt - 1) / pt * p.Hk);
+        const ChSeq q = ch_sequence(a, z, len, pt1, C::TILES, cap);
+        if (z >= a) cost = ch_cost(q, pt, cap) * p.Hk, items_here = ch_items(q, pt, p.Hk);
         plan_seq[s] = q;
       }
       long long sum = cost;
@@ -518,8 +480,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       else if (past) set_error(p.err, ERR_PAGE);
     }
     __syncwarp();
-    // (of two for each item none takes two of them)
-    const int ctas = (int)max(1ll, min((long long)gridDim.x, max(2ll * n_items, total / CH_LEAST))), cta = blockIdx.x;
+    const int ctas = ch_ctas(gridDim.x, n_items, total), cta = blockIdx.x;
+    const ChPlan line = {plan, plan_seq, p.b, p.Hk, pt, cap, ctas, total};
     // the first sequence from s on that has rows (b: none); the plan is gone once items are handed out (out)
     bool out = false;
     auto with_rows = [&](int s) {
@@ -530,64 +492,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       }
       return p.b;
     };
-    auto after = [&](ChPlace a, const ChSeq& q) {   // the item that follows
-      a.kb = 0;
-      a.cost += ch_item(q, pt, a.t);
-      if (++a.t * pt >= q.n) {
-        a.t = 0;
-        if (++a.hk == p.Hk) a.hk = 0, a.s = with_rows(a.s + 1);
-      }
-      return a;
-    };
-    // the c-th of the borders between the CTAs' stretches
-    auto at_cost = [&](long long x) {   // the last sequence whose cost before it is at most x
-      int lo = 0, hi = p.b;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (plan[mid] <= x) lo = mid;
-        else hi = mid;
-      }
-      return lo;
-    };
-    auto border = [&](int c) {
-      ChPlace a = {p.b, 0, 0, 0, 0};
-      if (c >= ctas || total == 0) return a;
-      const long long x = total / ctas * c + total % ctas * c / ctas;
-      a.s = at_cost(x);
-      const ChSeq q = plan_seq[a.s];
-      const long long of_head = ch_cost(q, pt);
-      long long rem = x - plan[a.s];
-      a.hk = (int)(rem / of_head);
-      rem -= a.hk * of_head;
-      int lo = 0, hi = (q.n + pt - 1) / pt;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (ch_before(q, pt, mid) <= rem) lo = mid;
-        else hi = mid;
-      }
-      a.t = lo;
-      rem -= ch_before(q, pt, lo);
-      a.cost = x - rem;
-      // the nearest step, an item's start spread over all of them; an end where that is less than CH_PART steps away
-      const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
-      const long long cost = ch_item(q, pt, a.t);
-      a.kb = (int)((2 * rem * steps + cost) / (2 * cost));
-      if (a.kb < CH_PART) {
-        a.kb = 0;
-      } else if (a.kb > steps - CH_PART) {   // the item that follows
-        a.kb = 0;
-        a.cost += cost;
-        if (++a.t * pt >= q.n) {
-          a.t = 0;
-          if (++a.hk == p.Hk) a.hk = 0, a.s = a.cost < total ? at_cost(a.cost) : p.b;
-        }
-      }
-      return a;
-    };
-    // the last CTA whose stretch begins less than y behind the item that begins at `cost`
-    auto cta_at = [&](long long cost, long long y) { return (int)min((long long)ctas - 1, ((cost + y) * ctas - 1) / total); };
     ChPlace a = {p.b, 0, 0, 0, 0}, z = a;
-    if (!bad && cta < ctas && lane < 2) a = border(cta + lane);
+    if (!bad && cta < ctas && lane < 2) a = line.border(cta + lane);
     __syncwarp();
     z.s = __shfl_sync(0xffffffffu, a.s, 1), a.s = __shfl_sync(0xffffffffu, a.s, 0);
     z.hk = __shfl_sync(0xffffffffu, a.hk, 1), a.hk = __shfl_sync(0xffffffffu, a.hk, 0);
@@ -606,9 +512,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       bool stop = true;
       if (more) {
         if (!out) q = plan_seq[a.s];
-        else if (a.s != it_seq) q = ch_sequence(p, a.s, pt1, C::TILES);
+        else if (a.s != it_seq) q = ch_sequence(__ldcg(p.start + a.s), __ldcg(p.start + a.s + 1), __ldcg(p.len + a.s), pt1, C::TILES, cap);
         it_seq = a.s;
-        const int steps = (ch_keys(q, pt, cap, a.t) + CH_STEP - 1) / CH_STEP;
+        const int steps = ch_steps(q, pt, cap, a.t);
         it.row0 = q.first + a.t * pt;
         it.npos = min(pt, q.n - a.t * pt);
         it.pos0 = q.len + a.t * pt;
@@ -618,10 +524,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
         if (a.kb + lane < p.ld) page = __ldcg(p.table + (size_t)a.s * p.ld + a.kb + lane);
         stop = a.s == end.s && a.hk == end.hk && a.t == end.t;
         it.kb1 = stop ? end.kb : steps;
-        if (it.kb0 > 0 || it.kb1 < steps) {   // (the CTAs whose first border lies in the item as border() sees it)
-          const long long cost = ch_item(q, pt, a.t);
-          it.head = cta_at(a.cost, ((2 * CH_PART - 1) * cost + 2 * steps - 1) / (2 * steps));
-          it.parts = cta_at(a.cost, ((2 * (steps - CH_PART) + 1) * cost + 2 * steps - 1) / (2 * steps)) - it.head + 1;
+        if (it.kb0 > 0 || it.kb1 < steps) {
+          line.parts(a, q, it.head, it.parts);
           it.part = cta - it.head;
         }
       }
@@ -638,7 +542,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_attention_kernel(const __
       ++n;
       if (!more) break;
       if (stop) a = z = end = ChPlace{p.b, 0, 0, 0, 0};
-      else a = after(a, q);
+      else a = line.after(a, q, with_rows);
     }
   } else if (warp == 0) {
     // ---- loads
