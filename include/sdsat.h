@@ -209,7 +209,7 @@ typedef struct {
   int32_t max_position;    /* positions 0 .. max_position - 1, at most 2^24 */
   int32_t scaling;         /* SDSAT_ROPE_* */
   int32_t original;        /* PARTS: positions of the context that the model was trained on */
-  int32_t reserved;        /* 0 */
+  int32_t reserved;        /* 0, else EINVAL */
   double theta;            /* f_i = theta^(-2 i / dims) radians a position */
   double factor;           /* LINEAR, PARTS */
   double low, high;        /* PARTS: turns up to which a pair is interpolated, and from which on it stays */

@@ -1529,7 +1529,7 @@ sdsat_status sdsat_rope_create(sdsat_ctx* c, const sdsat_rope_config* f, sdsat_r
   if (!c || !f || !out) return SDSAT_EINVAL;
   *out = nullptr;
   auto positive = [](double x) { return x > 0. && std::isfinite(x); };
-  if (f->dims < 2 || f->dims > 128 || f->dims % 2 || f->max_position < 1 || f->max_position > ROPE_MAX_POSITION ||
+  if (f->reserved != 0 || f->dims < 2 || f->dims > 128 || f->dims % 2 || f->max_position < 1 || f->max_position > ROPE_MAX_POSITION ||
       (f->interleaved != 0 && f->interleaved != 1) || f->scaling < SDSAT_ROPE_PLAIN || f->scaling > SDSAT_ROPE_PARTS ||
       !positive(f->theta) || !positive(f->magnitude))
     return SDSAT_EINVAL;
