@@ -79,7 +79,7 @@ def _lib():
     global _LIB
     if _LIB is None:
         if _build.is_stale():
-            _build.build()
+            _build.build_library()
         lib = ctypes.CDLL(_build.LIB)
         P, I, F, U64, I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint64, ctypes.c_int64
         sig = {
@@ -141,9 +141,6 @@ def _lib():
         lib.sdsat_kernel_class_name.restype = ctypes.c_char_p
         lib.sdsat_status_string.argtypes = [ctypes.c_int]
         lib.sdsat_status_string.restype = ctypes.c_char_p
-        from . import _native
-        _native.library(*[ctypes.cast(getattr(lib, "sdsat_" + n), ctypes.c_void_p).value
-                          for n in ("set_stream", "op_rotary_append", "op_chunk_attention", "op_adjust_logits")])
         _LIB = lib
     return _LIB
 
@@ -165,7 +162,7 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-_kinds = _f32 = _bf16 = _i32 = None   # tensor types, once torch is there (the first call of _rows)
+_kinds = _f32 = _bf16 = _i32 = None   # tensor types, once torch is there (the first call that asks for them)
 _calls = None                         # the calls whose arguments are checked and converted in C (csrc/binding.c)
 
 
@@ -173,7 +170,7 @@ def _rows(t):
     """(address, values from one row to the next, element type, rows, columns) of a CUDA matrix whose rows are
     contiguous."""
     if _kinds is None:
-        _types()
+        _tensor_types()
     kind = _kinds.get(t.dtype)
     if kind is None or not t.is_cuda or t.dim() != 2:
         raise ValueError("expected a float32 or bfloat16 CUDA matrix")
@@ -183,12 +180,22 @@ def _rows(t):
     return t.data_ptr(), ld if rows > 1 else columns, kind, rows, columns
 
 
-def _types():
-    global _kinds, _f32, _bf16, _i32, _calls
+def _tensor_types():
+    global _kinds, _f32, _bf16, _i32
     import torch
     _kinds, _f32, _bf16, _i32 = {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.bfloat16, torch.int32
-    _lib()
+
+
+def _types():
+    """The tensor types, and the calls that are in C (which alone need a compiler and the interpreter's headers)."""
+    global _calls
+    _tensor_types()
+    lib = _lib()
+    if _build.native_is_stale():
+        _build.build_native()
     from . import _native
+    _native.library(*[ctypes.cast(getattr(lib, "sdsat_" + n), ctypes.c_void_p).value
+                      for n in ("set_stream", "op_rotary_append", "op_chunk_attention", "op_adjust_logits")])
     _native.types(_f32, _bf16, _i32, _stream)
     _calls = _native
 
@@ -407,7 +414,7 @@ class Context:
         """Sequence s takes the pages and the length of sequence src[s] (int32 CUDA tensor [b]; -1: none)."""
         self._bind_stream()
         if _kinds is None:
-            _types()
+            _tensor_types()
         b = src.numel() if b is None else b
         _check(_lib().sdsat_kv_fork(self.handle, kv.handle, _array(src, _i32, min(b, kv.batch)), b), "sdsat_kv_fork")
 
@@ -424,7 +431,7 @@ class Context:
         """Pages in use move to the front of the pool; used: int32 CUDA tensor [1] for their number."""
         self._bind_stream()
         if _kinds is None:
-            _types()
+            _tensor_types()
         _check(_lib().sdsat_kv_compact(self.handle, kv.handle, _array(used, _i32, 1)), "sdsat_kv_compact")
 
     def kv_write(self, kv: KV, layer: int, seq: int, slot0: int, k, v):
