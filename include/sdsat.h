@@ -532,9 +532,10 @@ SDSAT_API sdsat_status sdsat_op_rotary_append(sdsat_ctx* ctx, const sdsat_rope* 
  * fp32 queries and probabilities enter the products in three bf16 parts (24 bits), bf16 queries as they are and their
  * probabilities rounded to bf16.  A slot past the table or on a page outside [0, n_pages) is not attended to and sets
  * device bit PAGE (a row that sees no slot is 0); what a page holds in slots that no row of the sequence sees does not
- * matter; a row's invisible slots that a later row sees count 0 times their value.  A start_dev that does not ascend
- * within [0, rows] leaves out_dev as it is and sets device bit CAPACITY; negative lengths count as 0.  Partial results
- * go through the context's workspace (see the conventions on streams).
+ * matter; a row's invisible slots that a later row sees count 0 times their value.  A NaN that a row sees makes its result NaN, and
+ * so does a score of inf (fp32: any infinite key, whose products with the parts are infinities of both signs); a row whose scores
+ * are all -inf is 0.  A start_dev that does not ascend within [0, rows] leaves out_dev as it is and sets device bit CAPACITY;
+ * negative lengths count as 0.  Partial results go through the context's workspace (see the conventions on streams).
  * hd 64 or 128, H a multiple of Hk, H/Hk <= 128, b <= 1024, n_pages * Hk * SDSAT_PAGE < 2^31; pointers 16-byte
  * aligned, rows a multiple of 16 bytes apart.  Errors: EINVAL, EUNSUPPORTED (H/Hk or b above that). */
 SDSAT_API sdsat_status sdsat_op_chunk_attention(sdsat_ctx* ctx, const void* q_dev, int64_t q_ld, int rows,

@@ -18,7 +18,8 @@
 // cores' 8 x 48 (N = 64: A is read at the shared memory's rate) and 4 x 64 cycles a step and tile, 1280 of the 1600 to 1700
 // that a step of both tiles takes; the softmax takes 1150 beside them.
 // P is one bf16 part, as the values that it weighs are (2^-9 of each probability, at random: 2.2e-3 of the result against 64
-// bits, where the rounding of the result itself is 1.7e-3); two parts would take the cores 1536 cycles a step.
+// bits, where the rounding of the result itself is 1.7e-3); two parts leave only that, but take 16 to 30 % longer (7B prompt
+// 137 us, 64 single tokens after 8200 slots 235 for 201): not kept.
 // fp32 (PARTS = 3, TILES = 1): queries and probabilities as three bf16 parts (24 bits), smallest first; P beside S, so S
 // and P V are issued by a warp each.  The tensor cores' accumulator truncates, so O holds one step, and 4 more warps add
 // it to a rounded total in registers.  1920 tensor cycles of 2200 a step.
@@ -28,7 +29,7 @@
 // Measured, us: 32 heads x 128, 4095 positions bf16 118 (1.16 PFLOP/s; prefill attention, which has fp32 queries in two
 // parts, 257); 32 / 8 heads, 8 sequences of 330 to 1100 rows after 800 to 16500 slots 730 (1.33 PFLOP/s; 804 in a long run
 // at the power cap), one of 4096 rows after 16384 780 (1.57); 48 sequences of up to 8200 slots, 46 of them with one row,
-// 154 to 161 (5.5 TB/s); 40 heads, 777 rows after 2048 slots in fp32 111.
+// 154 to 161 (5.5 TB/s); 40 heads, 777 rows after 2048 slots in fp32 111, 2 x 6 rows after 70 slots 7.2.
 //
 // A row's reference m is moved only when its maximum has grown by more than 2^8 since the last time (exact: it cancels
 // in the division by the row's sum), so that O (the total) is seldom rescaled.
